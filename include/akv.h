@@ -544,6 +544,167 @@ akv_status akv_decode_set_debug(int32_t ctas, int32_t withhold_last);
  */
 akv_status akv_decode_set_events(void* after_scores, void* after_decode);
 
+/*
+ * ---- Paged cache in 4 bits -------------------------------------------------------
+ *
+ * A second way to hold keys and values, for what the compressed arena does not do: tokens
+ * enter as they come, requests share pages, and a query may attend to a part of its pages.
+ * Every row is held in 4 bits per value; a long prompt can be read back (akv_paged_read) as
+ * the dense rows that akv_encode takes.
+ *
+ * Codec.  x in R^128 is one key or value row of one head.  v = x, or with AKV_FLAG_ROTATE
+ * v = H (s o x) / 8, H the Sylvester Hadamard matrix by the radix-2 butterfly (stages 1, 2, 4,
+ * .., 64, fp32) and s the signs of rot_seed (the rotation of Appendix A.1, Eq. 12).  Each
+ * `group` of 64 or 128 consecutive dimensions has, in fp32 rounded to nearest even,
+ *     m = fp16(min v),  a = fp16(max(max v - m, 0) / 15)     (both saturating at 65504),
+ *     c_j = clamp(rne((v_j - m) * (1 / a)), 0, 15),  all 0 where a = 0,
+ * and stands for v^_j = m + c_j a, x^ = v^ or s o (H v^) / 16.  A group with an infinity or a
+ * NaN has a = m = NaN: a query that sees the token has NaN outputs.
+ *
+ * Page.  page_tokens (16, 32, 64 or 128) tokens of all KV heads, akv_paged_page_bytes bytes:
+ * one block per head, each of page_tokens / 16 sub-blocks of 16 tokens and, with
+ * AKV_FLAG_BOUNDS, 512 bytes of bounds.  With NG = 128 / group, a sub-block (2048 + 128 NG
+ * bytes) is
+ *     +0     key codes, 64 bytes per token: 32-bit word 4 t + j holds dimensions
+ *            32 j + 8 t + i in nibble i (t, j in 0..3, i in 0..7)
+ *     +1024  value codes: token 8 p + 2 t + o (p, o in 0..1, t in 0..3), dimension
+ *            64 s + 8 g + 4 u + n (s, u in 0..1, g in 0..7, n in 0..3): byte
+ *            512 p + 16 (4 g + t) + 4 (2 s + u) + 2 o + n / 2, the low half where n is even
+ *     +2048  16 x 2 NG words: a token's NG key groups, then its NG value groups; fp16 a in
+ *            bits 0-15, fp16 m in bits 16-31
+ * (the operand order of the attention's tensor-core products: a lane's codes are one 16-byte
+ * load per 8 tokens, and no two tokens share a byte).  The bounds are the smallest, then the
+ * largest key of the page in each dimension (128 values each, the rows' type, before
+ * rotation), over every token written since the page's first slot was last written.
+ *
+ * Pool.  n_layers layers of n_pages pages each; one table of page numbers serves all layers.
+ * All integer state is on the device, so that a step may be captured in a CUDA graph.
+ */
+#define AKV_FLAG_BOUNDS 8u /* pages carry their keys' bounds (akv_paged_select needs them) */
+#define AKV_DTYPE_BF16 0
+#define AKV_DTYPE_FP16 1
+#define AKV_PAGED_MAX_QUERY 64 /* query tokens per request of one attention or selection call */
+
+typedef struct akv_paged_params {
+  int32_t n_kv_heads;  /* 1 .. 256 */
+  int32_t n_q_heads;   /* G * n_kv_heads, G in 1 .. 64; query head j reads KV head floor(j / G) */
+  int32_t head_dim;    /* must be 128 */
+  int32_t page_tokens; /* 16, 32, 64 or 128 */
+  int32_t group;       /* dimensions per scale: 64 or 128 */
+  int32_t dtype;       /* AKV_DTYPE_* of K, V, q, out and the bounds */
+  uint32_t flags;      /* AKV_FLAG_ROTATE, AKV_FLAG_BOUNDS */
+  int32_t reserved;    /* 0 */
+  uint64_t rot_seed;
+} akv_paged_params;
+
+typedef struct akv_pages {
+  void* pool;           /* device, 16-byte aligned: layer l starts at l * layer_stride bytes */
+  size_t pool_bytes;    /* >= (n_layers - 1) * layer_stride + n_pages * page bytes */
+  size_t layer_stride;  /* a multiple of 16, >= n_pages * page bytes (one layer: not read) */
+  int32_t n_layers;
+  int32_t n_pages;      /* pages per layer */
+  int32_t* table;       /* device [rows][table_stride]: page of tokens [j P, (j + 1) P) of a request, -1 = none */
+  int64_t table_stride; /* elements, >= max_pages */
+  int32_t rows;         /* requests (rows of the table) */
+  int32_t max_pages;    /* table entries per request */
+  int32_t* lens;        /* device [rows]: tokens held; read as clamped to [0, max_pages * P] */
+  int32_t* refs;        /* device [n_pages]: holders of each page, 0 = free (akv_pages_* only; else may be null) */
+} akv_pages;
+
+/* Rows of 128 values: request b, token t, head h at ptr + b stride_b + t stride_t + h stride_h
+ * (strides in elements, 0 allowed for what is read; rows that are written must not overlap). */
+typedef struct akv_rows {
+  void* ptr;
+  int64_t stride_b, stride_t, stride_h;
+} akv_rows;
+
+/* Pages kept for each query token and KV head: [rows][T][n_kv_heads][top] table positions,
+ * ascending, and how many of them there are. */
+typedef struct akv_selection {
+  int32_t* pages;
+  int32_t* count;
+  int32_t top;
+} akv_selection;
+
+/* Bytes of one page of one layer. */
+akv_status akv_paged_page_bytes(const akv_paged_params* p, size_t* bytes);
+
+/* Writes up to T new tokens per request (K, V: [rows][T][n_kv_heads][128]) behind the lens[b]
+ * tokens it holds: n_new[b] of them (device int32, null = T each; clamped to 0 .. T and to the
+ * table).  lens is read, not advanced: the layers of a model share it, and the caller adds
+ * n_new once all have been written.  Tokens whose page number is not one of the pool's are not
+ * written.  A page that is written must have one holder (akv_pages_reserve sees to it). */
+akv_status akv_paged_append(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* K,
+                            const akv_rows* V, int32_t T, const int32_t* n_new, akv_stream_t stream);
+
+/* Reads tokens start[b] .. start[b] + T - 1 (device int32, null = 0) of every request back into
+ * dense rows of the cache's type; rows of tokens that a request does not hold are zeros. */
+akv_status akv_paged_read(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const int32_t* start,
+                          const akv_rows* K, const akv_rows* V, int32_t T, akv_stream_t stream);
+
+/* Attention of the last T tokens of every request (1 .. AKV_PAGED_MAX_QUERY; 1 = a decode step)
+ * over the cache, their own keys and values included: query token t sees tokens
+ * i < lens[b] - T + 1 + t, or with `sel` those of them that are in its kept pages.
+ *     l_i = sm_scale q . k^_i,  out = sum_i softmax(l)_i v^_i,  lse = log sum_i exp(l_i)
+ * (fp32 sums).  A query that sees no token has out = 0 and lse = -infinity; a request with a
+ * page number outside the pool among the pages that it attends has NaN outputs.
+ * q, out: [rows][T][n_q_heads][128]; lse: fp32 [rows][T][n_q_heads] or null.  `top` of the
+ * workspace size is the selection's, 0 without one. */
+akv_status akv_paged_attn_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T, int32_t top,
+                                         size_t* ws_bytes);
+akv_status akv_paged_attn(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
+                          const akv_rows* out, float* lse, int32_t T, float sm_scale, const akv_selection* sel,
+                          void* ws, size_t ws_bytes, akv_stream_t stream);
+
+/* Chooses the pages that each query token attends, from the pages' bounds.  Of the n pages that
+ * it sees, the first `sink` and the last `recent` are kept, and of the others those of the
+ * highest score, `top` in all (top >= sink + recent; ties to the lower page; all n where
+ * n <= top).  Entries of sel->pages beyond the count are -1.  The score bounds q . k over the page from above, in
+ * whole numbers of 7 bits: q^ = rne(q 2^(7 - e)) clamped to +-127, e the exponent (frexp) of the
+ * largest |q| among the G rows of the query group; lo^, hi^ likewise from the page's bounds with
+ * the page's own exponent e_p (clamped to +-100);
+ *     score = 2^e_p max over the G rows of sum_d max(q^_d lo^_d, q^_d hi^_d),
+ * whose sums are exact: the choice does not depend on an order of additions.  A page with an
+ * infinite or NaN bound has the score +infinity; a page number outside the pool -infinity. */
+akv_status akv_paged_select_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
+                                           size_t* ws_bytes);
+akv_status akv_paged_select(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
+                            int32_t T, int32_t sink, int32_t recent, const akv_selection* sel, void* ws,
+                            size_t ws_bytes, akv_stream_t stream);
+
+/* Copies page src[i] to page dst[i] (device int32 [n]) in every layer.  No page may be written
+ * twice or both read and written; pairs with a number outside the pool are left out. */
+akv_status akv_pages_copy(const akv_paged_params* p, const akv_pages* pages, const int32_t* src, const int32_t* dst,
+                          int32_t n, akv_stream_t stream);
+
+/* Row dst[i] of the table becomes a second holder of the pages with tokens of row src[i] (device
+ * int32 [n]), at its length; no page is copied.  dst rows must hold no pages, each once; pairs
+ * with a row outside the table, or with dst = src, are left out. */
+akv_status akv_pages_fork(const akv_paged_params* p, const akv_pages* pages, const int32_t* src, const int32_t* dst,
+                          int32_t n, akv_stream_t stream);
+
+/* Sees to the pages of each request's next n_new[b] tokens (device int32 [rows]; <= 0: none).
+ * Where the first of them falls into a page with other holders, the request gets a copy of that
+ * page in every layer - unless all holders write into it in this call: then the lowest row keeps
+ * the page.  Then table positions up to the last new token that have no page get one.  Pages are
+ * taken in order of row and position, the lowest free number first.  *missing (device) is set to
+ * the number of pages that the pool lacks; where it is not 0, nothing else is changed.  Tokens
+ * past the table get no page. */
+akv_status akv_pages_workspace_size(const akv_paged_params* p, const akv_pages* pages, size_t* ws_bytes);
+akv_status akv_pages_reserve(const akv_paged_params* p, const akv_pages* pages, const int32_t* n_new,
+                             int32_t* missing, void* ws, size_t ws_bytes, akv_stream_t stream);
+
+/* Rows rows[i] (device int32 [n]) give up their pages: one holder less each, table entries -1,
+ * length 0.  A row named twice gives them up once. */
+akv_status akv_pages_free(const akv_paged_params* p, const akv_pages* pages, const int32_t* rows, int32_t n,
+                          akv_stream_t stream);
+
+/* Moves live pages (refs > 0) to the front of the pool: with n_live of them, the i-th live page at
+ * n_live or above goes, in every layer, to the i-th free page below; table entries and refs follow.
+ * *n_live (device) is their number. */
+akv_status akv_pages_compact(const akv_paged_params* p, const akv_pages* pages, int32_t* n_live, void* ws,
+                             size_t ws_bytes, akv_stream_t stream);
+
 #ifdef __cplusplus
 } /* extern "C" */
 #endif

@@ -14,6 +14,13 @@ from dataclasses import dataclass
 
 import numpy as np
 
+from . import paged as _paged
+from .paged import (  # noqa: F401 - the paged 4-bit cache
+    AKV_DTYPE_BF16, AKV_DTYPE_FP16, AKV_FLAG_BOUNDS, AKV_PAGED_MAX_QUERY, PagedParams, Pages, PageSelection,
+    akv_paged_append, akv_paged_attn, akv_paged_attn_workspace_size, akv_paged_page_bytes, akv_paged_read,
+    akv_paged_select, akv_paged_select_workspace_size, akv_pages_compact, akv_pages_copy, akv_pages_fork,
+    akv_pages_free, akv_pages_reserve, akv_pages_workspace_size)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libakv.so")
 
@@ -29,7 +36,7 @@ EXPORTED = (
     "akv_decode_set_debug", "akv_decode_set_events", "akv_cache_size_select", "akv_encode_select",
     "akv_decode_workspace_size_suffix", "akv_decode_attn_suffix", "akv_suffix_append", "akv_table1_bytes",
     "akv_pack_table1_host",
-)
+) + _paged.EXPORTED
 AKV_MAX_SUFFIX = 1 << 20
 NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -162,6 +169,7 @@ def lib():
         L.akv_table1_bytes.argtypes = [P, i32p, ctypes.POINTER(ctypes.c_size_t)]
         L.akv_pack_table1_host.restype = st
         L.akv_pack_table1_host.argtypes = [P, i32p, ctypes.POINTER(_UnitHost), vp, ctypes.c_size_t]
+        _paged.declare(L)
         _lib = L
     return _lib
 

@@ -25,6 +25,11 @@ SOURCES = {
     "akv_decode_g2w.cu": [],
     "akv_decode_g4w.cu": [],
     "akv_decode_g8w.cu": [],
+    "akv_paged_api.cpp": [],
+    "akv_paged_append.cu": [],
+    "akv_paged_attn.cu": [],
+    "akv_paged_select.cu": [],
+    "akv_pages.cu": [],
     "akv_encode.cu": ["--fmad=false"],  # fp64 decisions: no contraction
 }
 
@@ -40,7 +45,7 @@ def _compile(src: str, extra: list, verbose: bool) -> str:
     obj = os.path.join(BUILD, src + ".o")
     path = os.path.join(CSRC, src)
     deps = [path, os.path.join(ROOT, "include", "akv.h")]
-    deps += [os.path.join(CSRC, h) for h in ("akv_internal.h", "akv_device.cuh", "akv_decode.cuh")]
+    deps += [os.path.join(CSRC, h) for h in ("akv_internal.h", "akv_device.cuh", "akv_decode.cuh", "akv_paged.cuh")]
     if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
         return obj
     cmd = [_nvcc(), *ARCH, *COMMON, *extra, "-c", path, "-o", obj]

@@ -164,6 +164,59 @@ extern std::atomic<int> g_debug_cluster, g_debug_withhold;
 // its two launches; both null = off.
 void set_decode_events(void* after_scores, void* after_decode);
 void get_decode_events(void** after_scores, void** after_decode);
+// ---- paged cache in 4 bits (akv_paged_*.cu, akv_pages.cu) ----
+constexpr int kSubTokens = 16;  // tokens of a sub-block
+AKV_HD constexpr uint32_t sub_bytes(int ng) { return 2048u + 128u * (uint32_t)ng; }
+
+// One layer of a paged cache as the kernels see it (validated on the host).
+struct PagedView {
+  uint8_t* base;           // the layer's first page
+  const int32_t* table;
+  const int32_t* lens;
+  int64_t table_stride;
+  uint64_t page_bytes;
+  uint64_t sign_bits[2];   // rotation signs
+  int32_t n_pages, rows, max_pages;
+  int32_t H, G;
+  int32_t page_log;        // log2 of page_tokens
+  int32_t ng;              // groups per row: 128 / group
+  uint32_t block_bytes;    // one head's part of a page
+  int32_t half, rotate, bounds;
+};
+
+// What the page operations change.
+struct PagesState {
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  int64_t table_stride;
+  uint8_t* pool;
+  uint64_t layer_stride, page_bytes;
+  int32_t n_layers, n_pages, rows, max_pages, page_log;
+};
+
+constexpr int kPagedMaxGrid = 512;  // CTAs of the attention launch at most
+// CTA slots of partial results: two per CTA (the unit it begins in, the unit it ends in) of `rows` query rows, each
+// 128 values, a normaliser and a maximum.
+AKV_HD constexpr size_t paged_slot_floats(int rows) { return (size_t)rows * 130; }
+// query rows of one attention unit: one, two or four 8-column operand tiles
+constexpr int paged_unit_rows(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+
+int launch_paged_append(const PagedView& v, const akv_rows& K, const akv_rows& V, int32_t T, const int32_t* n_new, void* stream);
+int launch_paged_read(const PagedView& v, const int32_t* start, const akv_rows& K, const akv_rows& V, int32_t T, void* stream);
+int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
+                      const akv_selection* sel, void* ws, void* stream);
+size_t paged_attn_ws_bytes(const PagedView& v, int32_t T, int32_t top);
+int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_t sink, int32_t recent, const akv_selection& sel,
+                        void* ws, void* stream);
+size_t paged_select_ws_bytes(const PagedView& v, int32_t T);
+size_t pages_ws_bytes(const PagesState& s);
+int launch_pages_copy(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+int launch_pages_fork(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+int launch_pages_reserve(const PagesState& s, const int32_t* n_new, int32_t* missing, void* ws, void* stream);
+int launch_pages_free(const PagesState& s, const int32_t* rows, int32_t n, void* stream);
+int launch_pages_compact(const PagesState& s, int32_t* n_live, void* ws, void* stream);
+
 // Device address of the library's static encode scratch on the current device
 // and context (looked up on every call); returns a cudaError_t as int.
 int noalloc_scratch(void** ptr, size_t* bytes);

@@ -1,0 +1,329 @@
+// Page operations of the paged cache: copy, fork, reserve (with copy on write), free, compact.
+//
+// Their integer work is small (a table, a count per page); what costs is the pages' bytes, 2 x page bytes x layers for
+// each copied page.  The state is on the device, so a plan kernel of one CTA decides (its order is the documented
+// one: rows ascending, lowest free page first) and a copy kernel over all SMs moves what the plan lists.
+#include "akv_paged.cuh"
+
+namespace akv {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// Workspace: counters, then lists of the pool's and the table's size.
+struct PagesWs {
+  int32_t* n_copies;  // [0]: pairs in src / dst
+  int32_t* src;       // [max(n_pages, rows)]
+  int32_t* dst;
+  int32_t* free;      // [n_pages] free pages taken, ascending; compaction: where a live page goes
+  int32_t* writers;   // [n_pages] requests that write into a shared page
+  int32_t* lowest;    // [n_pages] the lowest of them
+  int32_t* base;      // [rows] pages taken by the rows before
+  int32_t* cbase;     // [rows] copies by the rows before
+};
+
+size_t pages_ws_ints(const PagesState& s) {
+  const size_t list = (size_t)(s.n_pages > s.rows ? s.n_pages : s.rows);
+  return 64 + 2 * list + 3 * (size_t)s.n_pages + 2 * (size_t)s.rows;
+}
+PagesWs pages_ws(const PagesState& s, void* ws) {
+  const size_t list = (size_t)(s.n_pages > s.rows ? s.n_pages : s.rows);
+  int32_t* p = (int32_t*)ws;
+  PagesWs w;
+  w.n_copies = p;
+  w.src = p + 64;
+  w.dst = w.src + list;
+  w.free = w.dst + list;
+  w.writers = w.free + s.n_pages;
+  w.lowest = w.writers + s.n_pages;
+  w.base = w.lowest + s.n_pages;
+  w.cbase = w.base + s.rows;
+  return w;
+}
+
+__device__ __forceinline__ bool in_pool(const PagesState& s, int page) { return (uint32_t)page < (uint32_t)s.n_pages; }
+
+// Exclusive prefix sum over the CTA's threads of x; *total: the sum.  All threads call it.
+__device__ __forceinline__ int block_scan(int x, int* total) {
+  __shared__ int part[33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  int inc = x;
+#pragma unroll
+  for (int h = 1; h < 32; h *= 2) {
+    const int o = __shfl_up_sync(0xffffffffu, inc, h);
+    if (lane >= h) inc += o;
+  }
+  __syncthreads();  // part of the call before has been read
+  if (lane == 31) part[warp] = inc;
+  __syncthreads();
+  if (warp == 0) {
+    const int mine = lane < warps ? part[lane] : 0;
+    int p = mine;
+#pragma unroll
+    for (int h = 1; h < 32; h *= 2) {
+      const int o = __shfl_up_sync(0xffffffffu, p, h);
+      if (lane >= h) p += o;
+    }
+    part[lane] = p - mine;
+    if (lane == 31) part[32] = p;
+  }
+  __syncthreads();
+  *total = part[32];
+  return part[warp] + inc - x;
+}
+
+// Pair i of the lists, page copied in every layer: a unit of work is 16 KiB of one page in one layer.
+constexpr int kCopyThreads = 256, kCopyChunk = kCopyThreads * 4 * 16;
+__global__ void __launch_bounds__(kCopyThreads) akv_pages_copy_kernel(PagesState s, const int32_t* src, const int32_t* dst, int n,
+                                                                      const int32_t* n_dev) {
+  if (n_dev) n = *n_dev;
+  const int chunks = (int)((s.page_bytes + kCopyChunk - 1) / kCopyChunk);
+  const int64_t work = (int64_t)n * s.n_layers * chunks;
+  for (int64_t k = blockIdx.x; k < work; k += gridDim.x) {
+    const int c = (int)(k % chunks);
+    const int64_t pl = k / chunks;
+    const int layer = (int)(pl % s.n_layers);
+    const int i = (int)(pl / s.n_layers);
+    const int a = src[i], b = dst[i];
+    if (!in_pool(s, a) || !in_pool(s, b) || a == b) continue;
+    uint8_t* base = s.pool + (uint64_t)layer * s.layer_stride;
+    const uint4* from = (const uint4*)(base + (uint64_t)a * s.page_bytes);
+    uint4* to = (uint4*)(base + (uint64_t)b * s.page_bytes);
+    const int64_t units = (int64_t)(s.page_bytes / 16), at = (int64_t)c * (kCopyChunk / 16) + threadIdx.x;
+    uint4 x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + j * kCopyThreads < units) x[j] = from[at + j * kCopyThreads];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (at + j * kCopyThreads < units) to[at + j * kCopyThreads] = x[j];
+  }
+}
+
+__global__ void __launch_bounds__(256) akv_pages_fork_kernel(PagesState s, const int32_t* src, const int32_t* dst) {
+  const int a = src[blockIdx.x], b = dst[blockIdx.x];
+  if ((uint32_t)a >= (uint32_t)s.rows || (uint32_t)b >= (uint32_t)s.rows || a == b) return;
+  const int len = min(max(s.lens[a], 0), s.max_pages << s.page_log);
+  const int held = (len + (1 << s.page_log) - 1) >> s.page_log;
+  for (int j = threadIdx.x; j < s.max_pages; j += blockDim.x) {
+    int page = -1;
+    if (j < held) {
+      page = s.table[(int64_t)a * s.table_stride + j];
+      if (in_pool(s, page)) atomicAdd(s.refs + page, 1);
+    }
+    s.table[(int64_t)b * s.table_stride + j] = page;
+  }
+  if (threadIdx.x == 0) s.lens[b] = s.lens[a];
+}
+
+// A page of the row is given up by the one thread that takes it out of the table.
+__global__ void __launch_bounds__(256) akv_pages_free_kernel(PagesState s, const int32_t* rows) {
+  const int r = rows[blockIdx.x];
+  if ((uint32_t)r >= (uint32_t)s.rows) return;
+  for (int j = threadIdx.x; j < s.max_pages; j += blockDim.x) {
+    const int page = atomicExch(s.table + (int64_t)r * s.table_stride + j, -1);
+    if (in_pool(s, page)) atomicSub(s.refs + page, 1);
+  }
+  if (threadIdx.x == 0) s.lens[r] = 0;
+}
+
+struct RowPlan {
+  int first, need;  // table positions that get a page where they have none
+  int tail;         // page that the first new token falls into, -1: none
+};
+__device__ __forceinline__ RowPlan row_plan(const PagesState& s, const int32_t* n_new, int r) {
+  const int most = s.max_pages << s.page_log, P = 1 << s.page_log;
+  const int len = min(max(s.lens[r], 0), most);
+  const int n = min(max(n_new[r], 0), most - len);
+  RowPlan p;
+  p.first = (len + P - 1) >> s.page_log;
+  p.need = n > 0 ? (len + n + P - 1) >> s.page_log : p.first;
+  p.tail = -1;
+  if (n > 0 && (len & P - 1)) {
+    const int page = s.table[(int64_t)r * s.table_stride + (len >> s.page_log)];
+    if (in_pool(s, page)) p.tail = page;
+  }
+  return p;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesState s, const int32_t* n_new, int32_t* missing, PagesWs w) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  // who writes into a page that others may hold too
+  for (int r = tid; r < s.rows; r += blockDim.x) {
+    const RowPlan p = row_plan(s, n_new, r);
+    if (p.tail >= 0) w.writers[p.tail] = 0, w.lowest[p.tail] = INT32_MAX;
+  }
+  __syncthreads();
+  for (int r = tid; r < s.rows; r += blockDim.x) {
+    const RowPlan p = row_plan(s, n_new, r);
+    if (p.tail >= 0) atomicAdd(w.writers + p.tail, 1), atomicMin(w.lowest + p.tail, r);
+  }
+  __syncthreads();
+  auto copies = [&](const RowPlan& p, int r) {
+    if (p.tail < 0) return false;
+    const int refs = s.refs[p.tail];
+    return refs > 1 && !(w.writers[p.tail] == refs && w.lowest[p.tail] == r);
+  };
+  // pages per row (a warp each)
+  for (int r = warp; r < s.rows; r += warps) {
+    const RowPlan p = row_plan(s, n_new, r);
+    int n = 0;
+    for (int j = p.first + lane; j < p.need; j += 32) n += s.table[(int64_t)r * s.table_stride + j] < 0;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) {
+      const bool c = copies(p, r);
+      w.base[r] = n + c;
+      w.cbase[r] = c;
+    }
+  }
+  __syncthreads();
+  int total = 0, n_copies = 0;
+  for (int r0 = 0; r0 < s.rows; r0 += blockDim.x) {
+    const int r = r0 + tid;
+    int sum;
+    const int a = block_scan(r < s.rows ? w.base[r] : 0, &sum);
+    if (r < s.rows) w.base[r] = total + a;
+    total += sum;
+    const int b = block_scan(r < s.rows ? w.cbase[r] : 0, &sum);
+    // copies by the rows before, and whether this row copies in the sign bit
+    if (r < s.rows) w.cbase[r] = (n_copies + b) | (w.cbase[r] ? (int)0x80000000 : 0);
+    n_copies += sum;
+  }
+  // the lowest free pages
+  int found = 0;
+  for (int p0 = 0; p0 < s.n_pages && found < total; p0 += blockDim.x) {
+    const int page = p0 + tid;
+    const bool is_free = page < s.n_pages && s.refs[page] == 0;
+    int sum;
+    const int at = found + block_scan(is_free, &sum);
+    if (is_free) w.free[at] = page;
+    found += sum;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    *missing = max(0, total - found);
+    *w.n_copies = found < total ? 0 : n_copies;
+  }
+  if (found < total) return;
+  for (int r = warp; r < s.rows; r += warps) {
+    const RowPlan p = row_plan(s, n_new, r);
+    int at = w.base[r];
+    const int cb = w.cbase[r];
+    __syncwarp();
+    if (cb < 0) {
+      if (lane == 0) {
+        const int page = w.free[at];
+        s.table[(int64_t)r * s.table_stride + p.first - 1] = page;
+        s.refs[page] = 1;
+        w.src[cb & 0x7fffffff] = p.tail;
+        w.dst[cb & 0x7fffffff] = page;
+      }
+      ++at;
+    }
+    for (int j0 = p.first; j0 < p.need; j0 += 32) {
+      const int j = j0 + lane;
+      int32_t* cell = s.table + (int64_t)r * s.table_stride + j;
+      const bool want = j < p.need && *cell < 0;
+      const uint32_t m = __ballot_sync(0xffffffffu, want);
+      if (want) {
+        const int page = w.free[at + __popc(m & ((1u << lane) - 1))];
+        *cell = page;
+        s.refs[page] = 1;
+      }
+      at += __popc(m);
+    }
+  }
+  __syncthreads();
+  // a copy's page has one holder less (after every row has read the counts)
+  for (int i = tid; i < n_copies; i += blockDim.x) atomicSub(s.refs + w.src[i], 1);
+}
+
+__global__ void __launch_bounds__(kPlanThreads) akv_pages_compact_plan(PagesState s, int32_t* n_live, PagesWs w) {
+  const int tid = threadIdx.x;
+  int live = 0;
+  for (int p = tid; p < s.n_pages; p += blockDim.x) live += s.refs[p] > 0;
+  int n;
+  block_scan(live, &n);
+  // free pages below n, then live ones at n and above: as many of each
+  int found = 0;
+  for (int p0 = 0; p0 < n; p0 += blockDim.x) {
+    const int page = p0 + tid;
+    const bool hole = page < n && s.refs[page] <= 0;
+    int sum;
+    const int at = found + block_scan(hole, &sum);
+    if (hole) w.dst[at] = page;
+    found += sum;
+  }
+  const int holes = found;
+  __syncthreads();
+  found = 0;
+  for (int p0 = n; p0 < s.n_pages && found < holes; p0 += blockDim.x) {
+    const int page = p0 + tid;
+    const bool moves = page < s.n_pages && s.refs[page] > 0;
+    int sum;
+    const int at = found + block_scan(moves, &sum);
+    if (moves) w.src[at] = page, w.free[page] = w.dst[at];
+    found += sum;
+  }
+  if (tid == 0) *n_live = n, *w.n_copies = holes;
+}
+
+// Table entries and counts follow the pages (n_live and the moves are the plan's).
+__global__ void __launch_bounds__(256) akv_pages_compact_table(PagesState s, const int32_t* n_live, PagesWs w) {
+  const int n = *n_live;
+  const int64_t cells = (int64_t)s.rows * s.max_pages, step = (int64_t)gridDim.x * blockDim.x;
+  const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  for (int64_t k = at; k < cells; k += step) {
+    int32_t* cell = s.table + k / s.max_pages * s.table_stride + k % s.max_pages;
+    const int page = *cell;
+    if (page >= n && page < s.n_pages && s.refs[page] > 0) *cell = w.free[page];
+  }
+}
+__global__ void __launch_bounds__(256) akv_pages_compact_refs(PagesState s, PagesWs w) {
+  const int n = *w.n_copies;
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
+    s.refs[w.dst[i]] = s.refs[w.src[i]];
+    s.refs[w.src[i]] = 0;
+  }
+}
+
+constexpr int kCopyGrid = 152 * 8;
+
+}  // namespace
+
+size_t pages_ws_bytes(const PagesState& s) { return (pages_ws_ints(s) * 4 + 255) & ~(size_t)255; }
+
+int launch_pages_copy(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
+  akv_pages_copy_kernel<<<kCopyGrid, kCopyThreads, 0, (cudaStream_t)stream>>>(s, src, dst, n, nullptr);
+  return (int)cudaGetLastError();
+}
+
+int launch_pages_fork(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
+  akv_pages_fork_kernel<<<n, 256, 0, (cudaStream_t)stream>>>(s, src, dst);
+  return (int)cudaGetLastError();
+}
+
+int launch_pages_free(const PagesState& s, const int32_t* rows, int32_t n, void* stream) {
+  akv_pages_free_kernel<<<n, 256, 0, (cudaStream_t)stream>>>(s, rows);
+  return (int)cudaGetLastError();
+}
+
+int launch_pages_reserve(const PagesState& s, const int32_t* n_new, int32_t* missing, void* ws, void* stream) {
+  const PagesWs w = pages_ws(s, ws);
+  cudaStream_t st = (cudaStream_t)stream;
+  akv_pages_reserve_kernel<<<1, kPlanThreads, 0, st>>>(s, n_new, missing, w);
+  akv_pages_copy_kernel<<<kCopyGrid, kCopyThreads, 0, st>>>(s, w.src, w.dst, 0, w.n_copies);
+  return (int)cudaGetLastError();
+}
+
+int launch_pages_compact(const PagesState& s, int32_t* n_live, void* ws, void* stream) {
+  const PagesWs w = pages_ws(s, ws);
+  cudaStream_t st = (cudaStream_t)stream;
+  akv_pages_compact_plan<<<1, kPlanThreads, 0, st>>>(s, n_live, w);
+  akv_pages_copy_kernel<<<kCopyGrid, kCopyThreads, 0, st>>>(s, w.src, w.dst, 0, w.n_copies);
+  akv_pages_compact_table<<<152, 256, 0, st>>>(s, n_live, w);
+  akv_pages_compact_refs<<<152, 256, 0, st>>>(s, w);
+  return (int)cudaGetLastError();
+}
+
+}  // namespace akv
