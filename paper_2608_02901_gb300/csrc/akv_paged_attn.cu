@@ -1,113 +1,834 @@
-// Attention over the paged 4-bit cache.
+// Attention over the paged 4-bit cache: a persistent launch that reads each attended page once, and a launch that joins
+// the shares of units that several CTAs worked on.
+//
+// A unit is one KV head of one request (or of one query token, where each has its own pages) with up to 8 NT query
+// rows.  Units are cut into tiles of 128 tokens, and the tiles of all units into equal contiguous ranges, one per CTA,
+// so that one long request and many short ones fill the GPU alike.  In a CTA one warp copies (bulk copies of whole
+// sub-blocks into a ring of stages) and the others take the sub-blocks of 16 tokens in turn, without a barrier between
+// them: each has its own running maximum, sum and output, joined at the unit's end.
+//
+// The codes go into the tensor cores as they are.  A nibble, masked in place, is the fp16 subnormal c 2^-24 (or
+// 16 c 2^-24 for the odd ones, whose partner is scaled by 1/16), so eight values cost five integer operations and no
+// conversion; the products are exact in fp32, and a row's scale and minimum are applied to the sums:
+//     l_i = a_i (c_i . q) + m_i sum(q),     y = sum_i (p_i a_i) c_i + sum_i p_i m_i .
+// Queries are exact in fp16 (a power of two times what was given); rotated ones are fp32 and enter as a high and a
+// low half.  The weights p_i a_i are rounded to fp16 (relative 2^-12, below the 2^-9 of a bf16 result), scaled by the
+// largest a so far so that a weight only underflows 2^-31 below the largest.  Sums, maxima and logits are fp32.
+#include <cuda_runtime.h>
+
+#include "akv_device.cuh"
 #include "akv_paged.cuh"
 
 namespace akv {
 namespace {
 
+constexpr int kTileTokens = 128, kTileSubs = kTileTokens / kSubTokens;
+// Computing warps of a CTA, next to one that copies: the registers a warp needs grow with the query rows, and an SM
+// has room for 16 warps of 128, 12 of 168 or 8 of 255 (a 17th of 96 spills).  Two CTAs per SM of the smallest.
+AKV_HD constexpr int warps_of(int nt) { return nt == 2 ? 11 : 7; }
+AKV_HD constexpr int ctas_of(int nt) { return nt == 1 ? 2 : 1; }
+constexpr int kStages = 4;
 constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLow = -1e30f;                  // running maximum before any token
+constexpr float kSlack = 8.f;                   // a weight may pass its reference by 2^8 before the reference moves
+constexpr int kWeightLog = 7;                   // p a / (largest a) is held times 2^7: at most 2^15 with the slack
+constexpr int kRowPad = kD + 4;                 // floats between rows of the joined outputs
 
-// One CTA of 128 threads: one query row.  Chunks of 128 tokens: a thread scores one token, then holds one dimension
-// of the output.  fp32 throughout.
-__global__ void __launch_bounds__(kD) akv_paged_attn_kernel(PagedView v, const uint16_t* q, int64_t qb, int64_t qt, int64_t qh,
-                                                            uint16_t* out, int64_t ob, int64_t ot, int64_t oh, float* lse, int T,
-                                                            float sm_scale, const int32_t* sel, const int32_t* count, int top) {
-  const int Hq = v.H * v.G;
-  const int hq = blockIdx.x % Hq, t = blockIdx.x / Hq % T, b = blockIdx.x / Hq / T;
-  const int h = hq / v.G, d = threadIdx.x, lane = d & 31, warp = d >> 5;
-  const int P = 1 << v.page_log;
-  const int sees = max(0, held_tokens(v, b) - T + 1 + t);
-  __shared__ float qs[kD], p[kD], red[4], ys[kD];
-  __shared__ const uint8_t* sub_of[kD];
-  const float x0 = row_to_float(q[b * qb + t * qt + hq * qh + d], v.half);
-  if (v.rotate) {
-    ys[d] = __uint_as_float(__float_as_uint(x0) ^ sign_flip(v, d));
-    __syncthreads();
-    if (warp == 0) {
-      float x[4];
-      for (int e = 0; e < 4; ++e) x[e] = ys[4 * lane + e];
-      wht_32x4(x, lane);
-      for (int e = 0; e < 4; ++e) qs[4 * lane + e] = x[e] * 0.0625f;
-    }
+struct AttnArgs {
+  PagedView v;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  int64_t qb, qt, qh, ob, ot, oh;
+  const int32_t* sel;
+  const int32_t* count;
+  int4* desc;     // [grid]: unit that starts in a CTA and goes on: group, index in it, last CTA
+  float* slots;   // [grid][2] partial results of 8 NT rows
+  float scale;    // sm_scale log2(e)
+  int T, top;
+  int rows;       // query rows of a unit in all (T G, or G)
+  int n_blocks;   // units that share them
+  int groups;     // requests, or (request, query token, head) with a selection
+  int per_group;  // units of a group
+};
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float word_scale(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
+__device__ __forceinline__ float word_min(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+__device__ __forceinline__ uint32_t comp(const uint4& x, int j) { return j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w; }
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // -126 .. 127
+
+// Tokens that a group's units go through, in the order of its tiles.
+struct Group {
+  int b, t, h;   // (t, h: with a selection)
+  int tokens;    // positions its tiles cover: the request's, or the kept pages'
+  int sees;      // tokens that may be attended at all
+};
+template <bool SEL>
+__device__ __forceinline__ Group group_of(const AttnArgs& a, int gi) {
+  Group g;
+  if (SEL) {
+    g.h = gi % a.v.H;
+    g.t = gi / a.v.H % a.T;
+    g.b = gi / a.v.H / a.T;
+    g.sees = max(0, held_tokens(a.v, g.b) - a.T + 1 + g.t);
+    g.tokens = min(max(a.count[gi], 0), a.top) << a.v.page_log;
   } else {
-    qs[d] = x0;
+    g.b = gi;
+    g.t = g.h = 0;
+    g.sees = g.tokens = held_tokens(a.v, gi);
   }
-  const int64_t unit = ((int64_t)b * T + t) * v.H + h;
-  const int n_sel = sel ? min(max(count[unit], 0), top) : 0;
-  const int n = sel ? n_sel << v.page_log : sees;
-  float m = kNegInf, l = 0.f, y = 0.f;
-  bool bad = false;
-  for (int i0 = 0; i0 < n; i0 += kD) {
-    __syncthreads();
-    const int i = i0 + d;
-    int pos = i, j = i >> v.page_log;
-    bool there = i < n;
-    if (there && sel) {
-      j = sel[unit * top + j];
-      there = (uint32_t)j < (uint32_t)v.max_pages;
-      pos = there ? (j << v.page_log) + (i & P - 1) : 0;
+  return g;
+}
+__device__ __forceinline__ int tiles_of(const Group& g) { return max(1, (g.tokens + kTileTokens - 1) / kTileTokens); }
+
+// Where a CTA's range of tiles begins and how long it is.
+struct Range {
+  int64_t lo, hi, total;
+  int ctas;
+};
+// The place of a tile: unit `index` of group `gi`, tile `ti` of the unit.
+template <bool SEL>
+struct Cursor {
+  int gi, index, ti, tiles;
+  Group g;
+  __device__ __forceinline__ void open(const AttnArgs& a) {
+    g = group_of<SEL>(a, gi);
+    tiles = tiles_of(g);
+  }
+  // the first tile of the next unit
+  __device__ __forceinline__ void next_unit(const AttnArgs& a) {
+    ti = 0;
+    if (++index == a.per_group) {
+      index = 0;
+      ++gi;
+      if (gi < a.groups) open(a);
     }
-    there = there && pos < sees;
-    const int page = there ? page_of(v, b, j) : -1;
-    bad = bad || (there && page < 0);
-    const uint8_t* sub = page < 0 ? nullptr : block_of(v, page, h) + (uint32_t)((pos & P - 1) >> 4) * sub_bytes(v.ng);
-    sub_of[d] = sub;
-    float s = kNegInf;
-    if (sub) {
-      s = 0.f;
-      for (int g = 0; g < v.ng; ++g) {
-        const uint32_t w = *(const uint32_t*)(sub + 2048 + 4 * (2 * v.ng * (pos & 15) + g));
-        const float a = row_to_float((uint16_t)w, 1), mn = row_to_float((uint16_t)(w >> 16), 1);
-        for (int e = g * kD / v.ng; e < (g + 1) * kD / v.ng; ++e) s += qs[e] * fmaf((float)key_code(sub, pos & 15, e), a, mn);
+  }
+};
+
+// Every thread: this CTA's range and its first tile.  `strip` [blockDim]: tiles of the groups before each thread's strip.
+template <int kThreads, bool SEL>
+__device__ __forceinline__ Range plan(const AttnArgs& a, int64_t* strip, Cursor<SEL>& c) {
+  const int tid = threadIdx.x, n = blockDim.x;
+  const int per = (a.groups + n - 1) / n;
+  int64_t mine = 0;
+  for (int gi = tid * per; gi < min(a.groups, (tid + 1) * per); ++gi) mine += tiles_of(group_of<SEL>(a, gi));
+  strip[tid] = mine * a.per_group;
+  __syncthreads();
+  if (tid < 32) {
+    constexpr int kEach = (kThreads + 31) / 32;
+    int64_t x[kEach], sum = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = tid * kEach + k;
+      const int64_t y = i < kThreads ? strip[i] : 0;
+      x[k] = sum;
+      sum += y;
+    }
+    int64_t inc = sum;
+#pragma unroll
+    for (int h = 1; h < 32; h *= 2) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, inc, h);
+      if (tid >= h) inc += o;
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int i = tid * kEach + k;
+      if (i < kThreads) strip[i] = inc - sum + x[k];
+    }
+    if (tid == 31) strip[kThreads] = inc;
+  }
+  __syncthreads();
+  Range r;
+  r.total = strip[kThreads];
+  r.ctas = (int)min((int64_t)gridDim.x, r.total);
+  r.lo = r.hi = 0;
+  if ((int)blockIdx.x >= r.ctas) return r;
+  r.lo = blockIdx.x * r.total / r.ctas;
+  r.hi = (blockIdx.x + 1) * r.total / r.ctas;
+  int s = 0;  // the last strip that begins at or before lo and is not empty
+  for (int step = 512; step; step /= 2)
+    if (s + step < kThreads && strip[s + step] <= r.lo) s += step;
+  int64_t at = strip[s];
+  c.gi = s * per;
+  for (;;) {
+    c.open(a);
+    const int64_t all = (int64_t)c.tiles * a.per_group;
+    if (r.lo < at + all) break;
+    at += all;
+    ++c.gi;
+  }
+  c.index = (int)((r.lo - at) / c.tiles);
+  c.ti = (int)((r.lo - at) % c.tiles);
+  return r;
+}
+
+template <int NT>
+struct Smem {
+  static constexpr int kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1);
+  alignas(128) uint8_t stage[kStages][kTileSubs * 2304];
+  alignas(16) uint4 frag[2][NT][4][32];     // query operand: high, low halves
+  float red[kWarps][8 * NT][kRowPad];       // the warps' outputs at a unit's end
+  float red_m[kWarps][8 * NT], red_l[kWarps][8 * NT];
+  float qsum[8 * NT][2];                    // sums of a query row over each group of dimensions
+  float qmax[kWarps];
+  int pos[kStages][kTileSubs];              // first token of each sub-block; -1: none, -2: a page outside the pool
+  int64_t strip[kThreads + 1];
+  uint64_t full[kStages], empty[kStages];
+  int failed;
+};
+
+constexpr int kConsumerBar = 1;
+
+template <int NG, int NT, bool HILO, bool SEL>
+__global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_paged_attn_kernel(const __grid_constant__ AttnArgs a) {
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  Smem<NT>& S = *reinterpret_cast<Smem<NT>*>(smem_raw);
+  constexpr uint32_t kSub = 2048 + 128 * NG;
+  constexpr int kRows = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const PagedView& v = a.v;
+
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(smem_u32(&S.full[s]), 1);
+      mbar_init(smem_u32(&S.empty[s]), kTileSubs);
+    }
+    S.failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  Cursor<SEL> c;
+  const Range r = plan<kThreads, SEL>(a, S.strip, c);  // (its barriers order the initialisation too)
+  if (tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if (r.lo >= r.hi) return;
+  volatile int* failed = &S.failed;
+
+  if (warp == kWarps) {
+    // ---- the copying warp: lane k < 8 sees to sub-block k of a tile, the first lane of a page copies its sub-blocks
+    const int per_page = min(kTileSubs, 1 << (v.page_log - 4));
+    int stage = 0;
+    uint32_t phase = 1;  // the first pass over the ring waits for nobody
+    auto look = [&](int& pos, int& page) {
+      pos = -1;
+      page = -1;
+      if (lane >= kTileSubs) return;
+      const int i = c.ti * kTileTokens + lane * kSubTokens;
+      if (i >= c.g.tokens) return;
+      int j = i >> v.page_log;
+      if (SEL) {
+        j = a.sel[(int64_t)c.gi * a.top + j];
+        if ((uint32_t)j >= (uint32_t)v.max_pages) return;
       }
-      s *= sm_scale;
+      const int at = (j << v.page_log) + (i & ((1 << v.page_log) - 1));
+      if (at >= c.g.sees) return;
+      page = page_of(v, c.g.b, j);
+      pos = page < 0 ? -2 : at;
+    };
+    auto head = [&]() { return SEL ? c.g.h : c.index / a.n_blocks; };
+    int pos, page, h = head();
+    look(pos, page);
+    for (int64_t k = r.lo; k < r.hi; ++k) {
+      const int pos0 = pos, page0 = page, h0 = h;
+      if (k + 1 < r.hi) {  // the next tile's pages are looked up while this one waits for its stage
+        if (++c.ti == c.tiles) c.next_unit(a);
+        h = head();
+        look(pos, page);
+      }
+      if (!mbar_wait_w(smem_u32(&S.empty[stage]), phase)) {
+        if (lane == 0) *failed = 1;
+        return;
+      }
+      const uint32_t there = __ballot_sync(0xffffffffu, pos0 >= 0);
+      if (lane < kTileSubs) S.pos[stage][lane] = pos0;
+      __syncwarp();
+      const uint32_t bar = smem_u32(&S.full[stage]);
+      if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(there) * kSub);
+      __syncwarp();
+      if (pos0 >= 0 && lane % per_page == 0) {
+        const uint32_t n = (uint32_t)__popc(there >> lane & ((1u << per_page) - 1));
+        bulk_g2s(smem_u32(&S.stage[stage][lane * kSub]), block_of(v, page0, h0) + (uint64_t)((pos0 & ((1 << v.page_log) - 1)) >> 4) * kSub,
+                 n * kSub, bar);
+      }
+      if (++stage == kStages) stage = 0, phase ^= 1;
     }
-    float top_s = s;
-    for (int k = 16; k; k >>= 1) top_s = max_nan(top_s, __shfl_xor_sync(0xffffffffu, top_s, k));
-    if (lane == 0) red[warp] = top_s;
-    __syncthreads();
-    const float mn = max_nan(m, max_nan(max_nan(red[0], red[1]), max_nan(red[2], red[3])));
-    const float f = m == kNegInf ? 0.f : expf(m - mn);
-    p[d] = s == kNegInf ? 0.f : expf(s - mn);
+    return;
+  }
+
+  // ---- the computing warps
+  const int g8 = lane >> 2, t4 = lane & 3;
+  int64_t k = r.lo;
+  while (k < r.hi) {
+    const int b = c.g.b;
+    const int h = SEL ? c.g.h : c.index / a.n_blocks;
+    const int row0 = (SEL ? c.index : c.index % a.n_blocks) * kRows;
+    const int n_rows = min(kRows, a.rows - row0);
+    const int n_tiles = (int)min((int64_t)(c.tiles - c.ti), r.hi - k);
+    const bool from_start = c.ti == 0, to_end = c.ti + n_tiles == c.tiles;
+
+    // queries: a warp per row, four dimensions a lane
+    constexpr int kTurns = (kRows + kWarps - 1) / kWarps;
+    float qx[kTurns][4];
+    float big = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int rr = warp + kWarps * i;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qx[i][e] = 0.f;
+      if (rr < n_rows) {
+        const int t = SEL ? c.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
+        const uint16_t* row = a.q + b * a.qb + t * a.qt + (int64_t)(h * v.G + g) * a.qh + 4 * lane;
+        if (((uintptr_t)row & 7) == 0) {
+          const uint2 w = *(const uint2*)row;
+          qx[i][0] = row_to_float((uint16_t)w.x, v.half);
+          qx[i][1] = row_to_float((uint16_t)(w.x >> 16), v.half);
+          qx[i][2] = row_to_float((uint16_t)w.y, v.half);
+          qx[i][3] = row_to_float((uint16_t)(w.y >> 16), v.half);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qx[i][e] = row_to_float(row[e], v.half);
+        }
+      }
+      if (HILO) {  // q' = H (s o q) / 16
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qx[i][e] = __uint_as_float(__float_as_uint(qx[i][e]) ^ sign_flip(v, 4 * lane + e));
+        wht_32x4(qx[i], lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qx[i][e] *= 0.0625f;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = fabsf(qx[i][e]);
+        if (x <= 3.402823466e38f) big = fmaxf(big, x);  // an infinite or NaN row spoils itself alone
+      }
+    }
+    big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
+    if (lane == 0) S.qmax[warp] = big;
+    named_sync(kConsumerBar, 32 * kWarps);  // (also: every warp is through with the unit before)
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) big = fmaxf(big, S.qmax[w]);
+    // the rows times 2^(14 - e): below 2^14, exact in fp16 down to 2^-23 of the largest
+    const int e_q = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 100);
+    const float up = pow2(14 - e_q);
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int rr = warp + kWarps * i;
+      if (rr >= kRows) break;
+      float sum = (qx[i][0] + qx[i][1]) + (qx[i][2] + qx[i][3]);
+#pragma unroll
+      for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+      if (lane % (32 / NG) == 0) S.qsum[rr][lane / (32 / NG)] = sum * a.scale;
+      uint4 f[HILO ? 2 : 1];
+#pragma unroll
+      for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // nibble e: odd ones stand for 16 times their value
+          const float x = qx[i][e] * (e & 1 ? up * 0.0625f : up);
+          const float hi = __half2float(__float2half_rn(x));
+          const float mine = lo ? x - hi : x;
+          const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
+          w[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
+        }
+        f[lo] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      // lanes 2 x and 2 x + 1 hold dimensions 8 x ..: word j = x / 4, operand lane 4 row + x % 4
+      const int at = 4 * (rr & 7) + (lane >> 1 & 3);
+      if (!(lane & 1)) S.frag[0][rr >> 3][lane >> 3][at] = f[0];
+      if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][at] = f[HILO ? 1 : 0];
+    }
+    named_sync(kConsumerBar, 32 * kWarps);
+    const float dot_scale = a.scale * pow2(10 + e_q);  // codes count 2^-24, queries 2^(14 - e)
+    uint4 qf[HILO ? 2 : 1][NT == 1 ? 4 : 1];
+    if (NT == 1) {
+#pragma unroll
+      for (int lo = 0; lo < (HILO ? 2 : 1); ++lo)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qf[lo][NT == 1 ? j : 0] = S.frag[lo][0][j][lane];
+    }
+    float qs[NT][2][NG];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) qs[nt][x][g] = S.qsum[8 * nt + 2 * t4 + x][g];
+
+    float acc[NT][8][4], sum[NT][2], mins[NT][2][NG], ref[NT][2];
+    int e_s = 103;  // the values' scales so far are at most 2^(e_s - 127)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc[nt][mt][x] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        sum[nt][x] = 0.f;
+        ref[nt][x] = kLow;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) mins[nt][x][g] = 0.f;
+      }
+    }
+    // every row of the unit sees the tokens before this one
+    const int all_see = SEL ? c.g.sees : c.g.sees - a.T + 1;
+
+    auto spoil = [&]() {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = __int_as_float(0x7fffffff);
+    };
+
+    for (int item = warp; item < n_tiles * kTileSubs; item += kWarps) {
+      const int sub = item % kTileSubs;
+      const uint32_t tile = (uint32_t)(k - r.lo) + item / kTileSubs;  // of the CTA's
+      const int stage = tile % kStages;
+      if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.full[stage]), tile / kStages & 1)) {
+        *failed = 1;
+        spoil();
+        break;
+      }
+      const int pos = S.pos[stage][sub];
+      uint4 kc[2], vc[2];
+      uint32_t kw[2][NG], vw[2][NG];
+      if (pos >= 0) {
+        const uint32_t sb = smem_u32(&S.stage[stage][sub * kSub]) + 16 * lane;
+        kc[0] = lds128(sb);
+        kc[1] = lds128(sb + 512);
+        vc[0] = lds128(sb + 1024);
+        vc[1] = lds128(sb + 1536);
+        const uint8_t* meta = &S.stage[stage][sub * kSub + 2048];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (NG == 2) {
+            const uint4 w = *(const uint4*)(meta + 16 * (g8 + 8 * x));
+            kw[x][0] = w.x, kw[x][NG - 1] = w.y, vw[x][0] = w.z, vw[x][NG - 1] = w.w;
+          } else {
+            const uint2 w = *(const uint2*)(meta + 8 * (g8 + 8 * x));
+            kw[x][0] = w.x, vw[x][0] = w.y;
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&S.empty[stage]));  // what is needed is in registers
+      if (pos < 0) {
+        if (pos == -2) spoil();
+        continue;
+      }
+
+      // logits of tokens g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1 (log2 units)
+      float l[NT][4];
+      {
+        float s[NT][NG][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[nt][g][x] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t x0 = comp(kc[0], j), x1 = comp(kc[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
+              const uint4 q = NT == 1 ? qf[lo][NT == 1 ? j : 0] : S.frag[lo][nt][j][lane];
+              float(&d)[4] = s[nt][NG == 2 ? j >> 1 : 0];
+              mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+              mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
+            }
+        }
+        float ks[2][NG], km[2][NG];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            ks[x][g] = word_scale(kw[x][g]) * dot_scale;
+            km[x][g] = word_min(kw[x][g]);
+          }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float y = km[x >> 1][0] * qs[nt][x & 1][0];
+            if (NG == 2) y = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], y);
+            y = fmaf(ks[x >> 1][0], s[nt][0][x], y);
+            if (NG == 2) y = fmaf(ks[x >> 1][NG - 1], s[nt][NG - 1][x], y);
+            l[nt][x] = y;
+          }
+      }
+      float vs[2][NG], vm[2][NG];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          vs[x][g] = word_scale(vw[x][g]);
+          vm[x][g] = word_min(vw[x][g]);
+        }
+      const bool edge = pos + kSubTokens > all_see;
+      if (edge) {  // tokens past the request, and those that a draft's earlier rows do not see
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const bool held = pos + g8 + 8 * x < c.g.sees;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            vs[x][g] = held ? vs[x][g] : 0.f;
+            vm[x][g] = held ? vm[x][g] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int row = row0 + 8 * nt + 2 * t4 + (x & 1);
+            const int sees = SEL ? c.g.sees : min(c.g.sees, all_see + row / v.G);
+            if (pos + g8 + 8 * (x >> 1) >= sees) l[nt][x] = kNegInf;
+          }
+      }
+
+      // references move only where a weight would pass its room
+      bool move = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) move = move || l[nt][x] > ref[nt][x & 1] + kSlack;
+      const float s_most = __int_as_float(e_s << 23);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) move = move || vs[x][g] > s_most;
+      if (__any_sync(0xffffffffu, move)) {
+        float top = fmaxf(vs[0][0], vs[1][0]);  // (a NaN is left out)
+        if (NG == 2) top = fmaxf(top, fmaxf(vs[0][NG - 1], vs[1][NG - 1]));
+        const int e_new = max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top, 0.f))) >> 23) + 1);
+        const float shrink = e_new == e_s ? 1.f : __int_as_float(max(127 + e_s - e_new, 0) << 23);
+        e_s = min(e_new, 255);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float m = fmaxf(l[nt][x], l[nt][x + 2]);
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            m = fmaxf(m, ref[nt][x]);
+            const float f = exp2_fast(ref[nt][x] - m);
+            ref[nt][x] = m;
+            sum[nt][x] *= f;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) mins[nt][x][g] *= f;
+#pragma unroll
+            for (int mt = 0; mt < 8; ++mt) {
+              acc[nt][mt][x] *= f * shrink;
+              acc[nt][mt][x + 2] *= f * shrink;
+            }
+          }
+      }
+      const float wf = __int_as_float((254 + kWeightLog - e_s) << 23);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) vs[x][g] *= wf;
+
+      uint32_t w0[NT][NG], w1[NT][NG];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          p[x] = exp2_fast(l[nt][x] - ref[nt][x & 1]);
+          sum[nt][x & 1] += p[x];
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          float u[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            u[x] = p[x] * vs[x >> 1][g];
+            float m = vm[x >> 1][g];
+            if (edge && l[nt][x] == kNegInf) u[x] = m = 0.f;  // a NaN that this row does not see
+            mins[nt][x & 1][g] = fmaf(p[x], m, mins[nt][x & 1][g]);
+          }
+          w0[nt][g] = transpose_8x8(half2_bits(u[0], u[1]));
+          w1[nt][g] = transpose_8x8(half2_bits(u[2], u[3]));
+        }
+      }
+      // outputs: rows of the product are dimensions 64 s + 8 g8 + 4 u + n of word 2 s + u
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x0 = comp(vc[0], j), x1 = comp(vc[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+        constexpr int kShift = NG == 2 ? 1 : 2;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_16816(acc[nt][2 * j], x0 & 0x000f000fu, y0 & 0x000f000fu, x1 & 0x000f000fu, y1 & 0x000f000fu, w0[nt][j >> kShift],
+                    w1[nt][j >> kShift]);
+          mma_16816(acc[nt][2 * j + 1], x0 & 0x00f000f0u, y0 & 0x00f000f0u, x1 & 0x00f000f0u, y1 & 0x00f000f0u, w0[nt][j >> kShift],
+                    w1[nt][j >> kShift]);
+        }
+      }
+    }
+
+    // ---- the unit's end, or the range's: the warps' outputs are joined
+    {
+      const int e_out = 24 - kWeightLog + e_s - 127;
+      const float down = pow2(max(e_out, -126)), down16 = down * 0.0625f;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float s = sum[nt][x], m[NG];
+#pragma unroll
+          for (int sh = 4; sh < 32; sh *= 2) s += __shfl_xor_sync(0xffffffffu, s, sh);
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            m[g] = mins[nt][x][g];
+#pragma unroll
+            for (int sh = 4; sh < 32; sh *= 2) m[g] += __shfl_xor_sync(0xffffffffu, m[g], sh);
+          }
+          const int row = 8 * nt + 2 * t4 + x;
+          if (g8 == 0) S.red_m[warp][row] = ref[nt][x], S.red_l[warp][row] = s;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float add = m[NG == 2 ? j >> 1 : 0];
+            const float4 y = make_float4(fmaf(acc[nt][2 * j][x], down, add), fmaf(acc[nt][2 * j + 1][x], down16, add),
+                                         fmaf(acc[nt][2 * j][x + 2], down, add), fmaf(acc[nt][2 * j + 1][x + 2], down16, add));
+            *(float4*)&S.red[warp][row][64 * (j >> 1) + 8 * g8 + 4 * (j & 1)] = y;
+          }
+        }
+    }
+    named_sync(kConsumerBar, 32 * kWarps);
+    const bool whole = from_start && to_end;
+    float* slot = a.slots + (2 * (size_t)blockIdx.x + (from_start ? 1 : 0)) * paged_slot_floats(kRows);
+#pragma unroll 1
+    for (int rr = warp; rr < n_rows; rr += kWarps) {
+      float m = kLow, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, S.red_m[w][rr]);
+      float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2_fast(S.red_m[w][rr] - m);
+        const float4 x = *(const float4*)&S.red[w][rr][4 * lane];
+        l = fmaf(f, S.red_l[w][rr], l);
+        y[0] = fmaf(f, x.x, y[0]);
+        y[1] = fmaf(f, x.y, y[1]);
+        y[2] = fmaf(f, x.z, y[2]);
+        y[3] = fmaf(f, x.w, y[3]);
+      }
+      if (!whole) {
+        *(float4*)(slot + rr * kD + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
+        if (lane == 0) slot[kRows * kD + 2 * rr] = m, slot[kRows * kD + 2 * rr + 1] = l;
+        continue;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= inv;
+      if (HILO) {
+        wht_32x4(y, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(y[e] * 0.0625f) ^ sign_flip(v, 4 * lane + e));
+      }
+      const int t = SEL ? c.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
+      uint16_t* row = a.out + b * a.ob + t * a.ot + (int64_t)(h * v.G + g) * a.oh + 4 * lane;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) row[e] = float_to_row(y[e], v.half);
+      if (a.lse && lane == 0)
+        a.lse[((int64_t)b * a.T + t) * (v.H * v.G) + h * v.G + g] = l == 0.f ? kNegInf : (m + log2f(l)) * 0.693147180559945f;
+    }
+    if (from_start && !to_end && tid == 0) {
+      // the CTA of the unit's last tile: (x + 1) ctas - 1 over the tiles of all
+      const int64_t last = k - c.ti + c.tiles - 1;
+      a.desc[blockIdx.x] = make_int4(c.gi, c.index, (int)(((last + 1) * r.ctas - 1) / r.total), 1);
+    }
+    k += n_tiles;
+    c.next_unit(a);
+  }
+}
+
+// Joins the shares of the unit that starts in CTA blockIdx.x and goes on in others: one CTA per query row, its warps
+// take the shares in turn.
+constexpr int kJoinWarps = 8;
+template <bool SEL>
+__global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_join_kernel(const __grid_constant__ AttnArgs a, int kRows) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int4 d = a.desc[blockIdx.x];
+  if (d.w <= 0) return;
+  const PagedView& v = a.v;
+  const int rr = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = (SEL ? d.y : d.y % a.n_blocks) * kRows + rr;
+  if (row >= a.rows) return;
+  const int first = blockIdx.x, n = d.z - first + 1;
+  const size_t floats = paged_slot_floats(kRows);
+  auto slot = [&](int i) { return a.slots + (i == 0 ? 2 * (size_t)first + 1 : 2 * (size_t)(first + i)) * floats; };
+  __shared__ float sm[kJoinWarps], sl[kJoinWarps], sy[kJoinWarps][kD];
+  float m = kLow, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = warp; i0 < n; i0 += 4 * kJoinWarps) {
+    float4 x[4];
+    float mm[4], ll[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * kJoinWarps;
+      mm[u] = kLow, ll[u] = 0.f, x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i < n) {
+        const float* s = slot(i);
+        x[u] = *(const float4*)(s + rr * kD + 4 * lane);
+        const float2 ml = *(const float2*)(s + kRows * kD + 2 * rr);
+        mm[u] = ml.x, ll[u] = ml.y;
+      }
+    }
+    const float mn = fmaxf(m, fmaxf(fmaxf(mm[0], mm[1]), fmaxf(mm[2], mm[3])));
+    const float f = exp2_fast(m - mn);
     m = mn;
     l *= f;
-    y *= f;
-    __syncthreads();
-    for (int k = 0; k < min(kD, n - i0); ++k) {
-      const uint8_t* sb = sub_of[k];
-      if (!sb) continue;
-      const int i16 = i0 + k & 15;  // (a page's tokens keep their place in the list)
-      const uint32_t w = *(const uint32_t*)(sb + 2048 + 4 * (2 * v.ng * i16 + v.ng + d / (kD / v.ng)));
-      y += p[k] * fmaf((float)value_code(sb, i16, d), row_to_float((uint16_t)w, 1), row_to_float((uint16_t)(w >> 16), 1));
-      l += p[k];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] *= f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float w = exp2_fast(mm[u] - m);
+      l = fmaf(w, ll[u], l);
+      y[0] = fmaf(w, x[u].x, y[0]);
+      y[1] = fmaf(w, x[u].y, y[1]);
+      y[2] = fmaf(w, x[u].z, y[2]);
+      y[3] = fmaf(w, x[u].w, y[3]);
     }
   }
-  bad = __syncthreads_or(bad);
-  ys[d] = l != 0.f ? y / l : 0.f;
+  *(float4*)&sy[warp][4 * lane] = make_float4(y[0], y[1], y[2], y[3]);
+  if (lane == 0) sm[warp] = m, sl[warp] = l;
   __syncthreads();
-  if (v.rotate && warp == 0) {
-    float x[4];
-    for (int e = 0; e < 4; ++e) x[e] = ys[4 * lane + e];
-    wht_32x4(x, lane);
-    for (int e = 0; e < 4; ++e) ys[4 * lane + e] = __uint_as_float(__float_as_uint(x[e] * 0.0625f) ^ sign_flip(v, 4 * lane + e));
+  if (warp) return;
+  for (int w = 1; w < kJoinWarps; ++w) m = fmaxf(m, sm[w]);
+  l = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = 0.f;
+  for (int w = 0; w < kJoinWarps; ++w) {
+    const float f = exp2_fast(sm[w] - m);
+    l = fmaf(f, sl[w], l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(f, sy[w][4 * lane + e], y[e]);
   }
-  __syncthreads();
-  const float nan = __int_as_float(0x7fffffff);
-  out[b * ob + t * ot + hq * oh + d] = float_to_row(bad ? nan : ys[d], v.half);
-  if (lse && d == 0) lse[((int64_t)b * T + t) * Hq + hq] = bad ? nan : l == 0.f ? kNegInf : m + logf(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] *= inv;
+  if (v.rotate) {
+    wht_32x4(y, lane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(y[e] * 0.0625f) ^ sign_flip(v, 4 * lane + e));
+  }
+  const Group grp = group_of<SEL>(a, d.x);
+  const int h = SEL ? grp.h : d.y / a.n_blocks, t = SEL ? grp.t : row / v.G, g = SEL ? row : row % v.G;
+  uint16_t* o = a.out + grp.b * a.ob + t * a.ot + (int64_t)(h * v.G + g) * a.oh + 4 * lane;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = float_to_row(y[e], v.half);
+  if (a.lse && lane == 0)
+    a.lse[((int64_t)grp.b * a.T + t) * (v.H * v.G) + h * v.G + g] = l == 0.f ? kNegInf : (m + log2f(l)) * 0.693147180559945f;
+}
+
+// Workspace: descriptors, then slots.
+constexpr size_t kShareDescBytes = (kPagedMaxGrid * sizeof(int4) + 255) & ~(size_t)255;
+
+static_assert(sizeof(Smem<1>) <= 115712, "two CTAs of an SM share 228 KiB, 1 KiB each of it taken");
+static_assert(sizeof(Smem<2>) <= 232448 && sizeof(Smem<4>) <= 232448, "shared memory of a CTA");
+
+template <int NG, int NT, bool HILO, bool SEL>
+int launch(const AttnArgs& a, int sms, cudaStream_t stream) {
+  auto* kernel = akv_paged_attn_kernel<NG, NT, HILO, SEL>;
+  const size_t smem = sizeof(Smem<NT>);
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return (int)e;
+  int grid = sms * ctas_of(NT);
+  if (grid > kPagedMaxGrid) grid = kPagedMaxGrid;
+  kernel<<<grid, Smem<NT>::kThreads, smem, stream>>>(a);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return (int)e;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute pdl{};
+  pdl.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT);
+  cfg.blockDim = dim3(32 * kJoinWarps);
+  cfg.stream = stream;
+  cfg.attrs = &pdl;
+  cfg.numAttrs = 1;
+  return (int)cudaLaunchKernelEx(&cfg, akv_paged_join_kernel<SEL>, a, 8 * NT);
+}
+
+template <int NT, bool HILO, bool SEL>
+int launch_ng(const AttnArgs& a, int sms, cudaStream_t s) {
+  return a.v.ng == 2 ? launch<2, NT, HILO, SEL>(a, sms, s) : launch<1, NT, HILO, SEL>(a, sms, s);
+}
+template <bool HILO, bool SEL>
+int launch_nt(const AttnArgs& a, int unit_rows, int sms, cudaStream_t s) {
+  switch (unit_rows) {
+    case 8: return launch_ng<1, HILO, SEL>(a, sms, s);
+    case 16: return launch_ng<2, HILO, SEL>(a, sms, s);
+    default: return launch_ng<4, HILO, SEL>(a, sms, s);
+  }
 }
 
 }  // namespace
 
-size_t paged_attn_ws_bytes(const PagedView&, int32_t, int32_t) { return 256; }
+size_t paged_attn_ws_bytes(const PagedView& v, int32_t T, int32_t top) {
+  const int rows = paged_unit_rows(top > 0 ? v.G : T * v.G);
+  return kShareDescBytes + kPagedMaxGrid * 2 * paged_slot_floats(rows) * sizeof(float);
+}
 
 int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
-                      const akv_selection* sel, void*, void* stream) {
-  const int64_t grid = (int64_t)v.rows * T * v.H * v.G;
-  if (grid > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
-  akv_paged_attn_kernel<<<(unsigned)grid, kD, 0, (cudaStream_t)stream>>>(
-      v, (const uint16_t*)q.ptr, q.stride_b, q.stride_t, q.stride_h, (uint16_t*)out.ptr, out.stride_b, out.stride_t, out.stride_h,
-      lse, T, sm_scale, sel ? sel->pages : nullptr, sel ? sel->count : nullptr, sel ? sel->top : 0);
-  return (int)cudaGetLastError();
+                      const akv_selection* sel, void* ws, void* stream) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return (int)e;
+  AttnArgs a{};
+  a.v = v;
+  a.q = (const uint16_t*)q.ptr;
+  a.qb = q.stride_b, a.qt = q.stride_t, a.qh = q.stride_h;
+  a.out = (uint16_t*)out.ptr;
+  a.ob = out.stride_b, a.ot = out.stride_t, a.oh = out.stride_h;
+  a.lse = lse;
+  a.scale = (float)((double)sm_scale * 1.4426950408889634);
+  a.T = T;
+  a.rows = sel ? v.G : T * v.G;
+  const int unit_rows = paged_unit_rows(a.rows);
+  a.n_blocks = (a.rows + unit_rows - 1) / unit_rows;
+  if (sel) {
+    a.sel = sel->pages;
+    a.count = sel->count;
+    a.top = sel->top;
+    a.groups = v.rows * T * v.H;
+    a.per_group = a.n_blocks;
+  } else {
+    a.groups = v.rows;
+    a.per_group = v.H * a.n_blocks;
+  }
+  a.desc = (int4*)ws;
+  a.slots = (float*)((uint8_t*)ws + kShareDescBytes);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (v.rotate) return sel ? launch_nt<true, true>(a, unit_rows, sms, s) : launch_nt<true, false>(a, unit_rows, sms, s);
+  return sel ? launch_nt<false, true>(a, unit_rows, sms, s) : launch_nt<false, false>(a, unit_rows, sms, s);
 }
 
 }  // namespace akv
