@@ -553,8 +553,8 @@ akv_status akv_decode_set_events(void* after_scores, void* after_decode);
  * the dense rows that akv_encode takes.
  *
  * Codec.  x in R^128 is one key or value row of one head.  v = x, or with AKV_FLAG_ROTATE
- * v = H (s o x) / 8, H the Sylvester Hadamard matrix by the radix-2 butterfly (stages 1, 2, 4,
- * .., 64, fp32) and s the signs of rot_seed (the rotation of Appendix A.1, Eq. 12).  Each
+ * v = H (s o x) / 8 in fp32 sums, H the Sylvester Hadamard matrix and s the signs of rot_seed
+ * (the rotation of Appendix A.1, Eq. 12).  Each
  * `group` of 64 or 128 consecutive dimensions has, in fp32 rounded to nearest even,
  *     m = fp16(min v),  a = fp16(max(max v - m, 0) / 15)     (both saturating at 65504),
  *     c_j = clamp(rne((v_j - m) * (1 / a)), 0, 15),  all 0 where a = 0,

@@ -33,30 +33,10 @@ __device__ __forceinline__ uint8_t* block_of(const PagedView& v, int page, int h
 }
 // +0 or -0 pattern that flips the sign of dimension d where the rotation does.
 __device__ __forceinline__ uint32_t sign_flip(const PagedView& v, int d) {
-  return (uint32_t)(v.sign_bits[d >> 6] >> (d & 63) & 1ull) << 31;
+  return (uint32_t)((d < 64 ? v.sign_bits[0] : v.sign_bits[1]) >> (d & 63) & 1ull) << 31;
 }
 
-// Butterfly of a row spread over 8 neighbouring lanes, 16 dimensions each (d = 16 u + e): stages 1, 2, 4, 8 in a
-// lane, 16, 32, 64 between lanes.  fp32, the stages' order is the codec's.
-__device__ __forceinline__ void wht_8x16(float (&x)[16], int u) {
-#pragma unroll
-  for (int h = 1; h < 16; h *= 2)
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (!(e & h)) {
-        const float a = x[e], b = x[e | h];
-        x[e] = __fadd_rn(a, b);
-        x[e | h] = __fsub_rn(a, b);
-      }
-#pragma unroll
-  for (int h = 1; h < 8; h *= 2)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float o = __shfl_xor_sync(0xffffffffu, x[e], h);
-      x[e] = u & h ? __fsub_rn(o, x[e]) : __fadd_rn(x[e], o);
-    }
-}
-// The same for a row spread over a warp, four dimensions a lane (d = 4 lane + e).
+// Butterfly (stages 1, 2, 4, .., 64) of a row spread over a warp, four dimensions a lane (d = 4 lane + e).
 __device__ __forceinline__ void wht_32x4(float (&x)[4], int lane) {
   float a = x[0] + x[1], b = x[0] - x[1], c = x[2] + x[3], d = x[2] - x[3];
   x[0] = a + c;
@@ -81,21 +61,6 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
-}
-
-// Place of token i (0 .. 15) and value dimensions 64 s + 8 g + 4 u .. + 3 in a sub-block's value codes: two bytes.
-__device__ __forceinline__ int value_place(int i, int s, int g, int u) {
-  return 512 * (i >> 3) + 16 * (4 * g + ((i & 7) >> 1)) + 4 * (2 * s + u) + 2 * (i & 1);
-}
-
-// Code of dimension d of token i in a sub-block (any lane, byte reads).
-__device__ __forceinline__ int key_code(const uint8_t* sub, int i, int d) {
-  const int byte = 64 * i + 4 * (4 * (d >> 3 & 3) + (d >> 5)) + (d >> 1 & 3);
-  return sub[byte] >> 4 * (d & 1) & 15;
-}
-__device__ __forceinline__ int value_code(const uint8_t* sub, int i, int d) {
-  const int byte = 1024 + value_place(i, d >> 6, d >> 3 & 7, d >> 2 & 1) + (d >> 1 & 1);
-  return sub[byte] >> 4 * (d & 1) & 15;
 }
 
 }  // namespace

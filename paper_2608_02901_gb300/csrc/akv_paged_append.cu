@@ -5,7 +5,9 @@
 //   - the dense side is four 16-byte accesses a lane, 64 contiguous bytes a row each time;
 //   - the key codes of a lane are the 16 contiguous bytes of its row's words 4 u .. 4 u + 3, the value codes (after an
 //     exchange with the neighbouring token's lanes, whose halves share the words) one 16-byte unit;
-//   - the rotation needs shuffles for two of its seven stages only (8 and 16), the minimum and maximum of a group two.
+//   - a warp's 8 rows are operands of the tensor cores as they were loaded, and its products come back in the same
+//     places: four of the rotation's seven stages are products with the signs of a 16 x 16 Hadamard matrix (exact
+//     products, fp32 sums), the other three additions within a lane, and no value is shuffled.
 #include "akv_paged.cuh"
 
 namespace akv {
@@ -43,136 +45,222 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-// The codec's butterfly of a row over four lanes: x[8 c + n] is dimension 32 c + 8 u + n.
-__device__ __forceinline__ void wht_4x32(float (&x)[32], int u) {
+template <bool HALF>
+__device__ __forceinline__ void mma_rows(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  const float z = 0.f;
+  if (HALF)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(z));
+}
+
+// The second operand of the rotation's products: signs (-1)^(bits that input and output share) of four dimension bits.
+// Inputs: lane t has bits 3 and 4, register r bit 1, the pair's halves bit `first` (0 or 2); outputs: column g has bits
+// 3 and 4 in g / 2, column parity bit 0 (first 0) or bit 1 (first 2), tile n bit 1 or bit 2.
+template <bool HALF>
+__device__ __forceinline__ void hadamard_operand(int lane, int first, uint32_t (&b)[2][2]) {
+  const int g = lane >> 2, t = lane & 3;
+  const uint32_t one = HALF ? 0x3c00u : 0x3f80u, far = (uint32_t)__popc(t & (g >> 1)) & 1u;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (uint32_t r = 0; r < 2; ++r) {
+      const uint32_t tile = (uint32_t)n, parity = (uint32_t)g & 1u;
+      const uint32_t low = far ^ (r & (first ? parity : tile));        // the pair's half 0
+      const uint32_t high = low ^ (first ? tile : parity);             // and half 1
+      b[n][r] = (one | low << 15) | (one | high << 15) << 16;
+    }
+}
+
+// H (s o x) of the warp's 8 rows, x as loaded with its signs flipped: word 4 c + m is dimensions 32 c + 8 u + 2 m and
+// the next, y[8 c + n] dimension 32 c + 8 u + n.  fp32 sums.
+template <bool HALF>
+__device__ __forceinline__ void rotate_rows(const uint32_t (&w)[16], const uint32_t (&b)[2][2], float (&y)[32]) {
+  uint64_t p[16];  // p[4 c + 2 d2 + d1]: a pair of neighbouring dimensions
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {  // bits 0, 1, 3, 4; the tile's lower rows are the dimensions with bit 2
+      float d[4];
+      mma_rows<HALF>(d, w[4 * c], w[4 * c + 2], w[4 * c + 1], w[4 * c + 3], b[n][0], b[n][1]);
+      p[4 * c + n] = pair(d[0], d[1]);
+      p[4 * c + 2 + n] = pair(d[2], d[3]);
+    }
   const uint64_t minus = pair(-1.f, -1.f);
 #pragma unroll
-  for (int i = 0; i < 32; i += 2) {  // stage 1
-    const float a = x[i], b = x[i + 1];
-    x[i] = __fadd_rn(a, b);
-    x[i + 1] = __fsub_rn(a, b);
-  }
-  uint64_t p[16];  // pairs of neighbouring dimensions
-#pragma unroll
-  for (int i = 0; i < 16; ++i) p[i] = pair(x[2 * i], x[2 * i + 1]);
-  auto stage = [&](int h) {  // h: distance in pairs
+  for (int h = 2; h < 16; h *= 2)  // bits 2, 5, 6
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (!(i & h)) {
-        const uint64_t a = p[i], b = p[i | h];
-        p[i] = add2(a, b);
-        p[i | h] = fma2(b, minus, a);
+        const uint64_t a = p[i], q = p[i | h];
+        p[i] = add2(a, q);
+        p[i | h] = fma2(q, minus, a);
       }
-  };
-  stage(1);  // 2
-  stage(2);  // 4
 #pragma unroll
-  for (int h = 1; h < 4; h *= 2) {  // 8, 16: the lane with the bit holds b of a + b, a - b
-    const uint64_t sign = u & h ? minus : pair(1.f, 1.f);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float a, b;
-      unpair(p[i], a, b);
-      const uint64_t o = pair(__shfl_xor_sync(0xffffffffu, a, h), __shfl_xor_sync(0xffffffffu, b, h));
-      p[i] = fma2(p[i], sign, o);
-    }
-  }
-  stage(4);  // 32
-  stage(8);  // 64
-#pragma unroll
-  for (int i = 0; i < 16; ++i) unpair(p[i], x[2 * i], x[2 * i + 1]);
+  for (int i = 0; i < 16; ++i) unpair(p[i], y[2 * i], y[2 * i + 1]);
 }
 
-__device__ __forceinline__ float lo_half(uint32_t w, int half) {
-  return half ? __half2float(__ushort_as_half((unsigned short)w)) : __uint_as_float(w << 16);
+template <bool HALF>
+__device__ __forceinline__ float lo_half(uint32_t w) {
+  return HALF ? __half2float(__ushort_as_half((unsigned short)w)) : __uint_as_float(w << 16);
 }
-__device__ __forceinline__ float hi_half(uint32_t w, int half) {
-  return half ? __half2float(__ushort_as_half((unsigned short)(w >> 16))) : __uint_as_float(w & 0xffff0000u);
+template <bool HALF>
+__device__ __forceinline__ float hi_half(uint32_t w) {
+  return HALF ? __half2float(__ushort_as_half((unsigned short)(w >> 16))) : __uint_as_float(w & 0xffff0000u);
 }
-__device__ __forceinline__ uint32_t pack_rows(float a, float b, int half) {
-  if (half) {
+template <bool HALF>
+__device__ __forceinline__ uint32_t pack_rows(float a, float b) {
+  if (HALF) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// Smaller and larger of two pairs of rows' values (a NaN is left out).
-__device__ __forceinline__ uint32_t min_rows(uint32_t a, uint32_t b, int half) {
+// Smaller and larger of two pairs of rows' values: a NaN is left out, or (NAN) passed on.
+template <bool HALF, bool NAN_ = false>
+__device__ __forceinline__ uint32_t min_rows(uint32_t a, uint32_t b) {
   uint32_t r;
-  if (half) asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  if (HALF && NAN_) asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else if (HALF) asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else if (NAN_) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   else asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint32_t max_rows(uint32_t a, uint32_t b, int half) {
+template <bool HALF, bool NAN_ = false>
+__device__ __forceinline__ uint32_t max_rows(uint32_t a, uint32_t b) {
   uint32_t r;
-  if (half) asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  if (HALF && NAN_) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else if (HALF) asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else if (NAN_) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   else asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-
-// Signs of the rotation as pairs of rows' sign bits: word 4 c + m of lane u is dimensions 32 c + 8 u + 2 m, + 1.
-__device__ __forceinline__ void sign_words(const PagedView& v, int u, uint32_t (&w)[16]) {
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const uint32_t bits = (uint32_t)(v.sign_bits[c >> 1] >> (32 * (c & 1) + 8 * u));
-#pragma unroll
-    for (int m = 0; m < 4; ++m) w[4 * c + m] = (bits >> (2 * m) & 1u) << 15 | (bits >> (2 * m + 1) & 1u) << 31;
-  }
+__device__ __forceinline__ float min3_nan(float a, float b, float c) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
-// A row's values (packed as stored, signs flipped) -> this lane's codes, word c: dimensions 32 c + 8 u + n in nibble n,
-// and the words (scale | minimum << 16) of the row's groups.
-template <int NG, bool ROT>
-__device__ __forceinline__ void quantise(const uint32_t (&w)[16], int half, int u, uint32_t (&codes)[4], uint32_t (&word)[NG]) {
-  float x[32];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[2 * i] = lo_half(w[i], half), x[2 * i + 1] = hi_half(w[i], half);
-  if (ROT) {
-    wht_4x32(x, u);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] *= 0.125f;
+// Signs of the rotation as pairs of rows' sign bits, in shared memory: word 16 u + 4 c + m is dimensions
+// 32 c + 8 u + 2 m and the next.  Called by every thread of the CTA.
+__device__ __forceinline__ void fill_signs(const PagedView& v, uint32_t* sign) {
+  for (int i = threadIdx.x; i < 64; i += blockDim.x) {
+    const int d = 32 * (i >> 2 & 3) + 8 * (i >> 4) + 2 * (i & 3);
+    const uint32_t bits = (uint32_t)((d < 64 ? v.sign_bits[0] : v.sign_bits[1]) >> (d & 63)) & 3u;
+    sign[i] = (bits & 1u) << 15 | (bits & 2u) << 30;
   }
+  __syncthreads();
+}
+
+// A row's values (as given, packed; signs flipped where rotated) -> this lane's codes, word c: dimensions 32 c + 8 u + n
+// in nibble n, and the words (scale | minimum << 16) of the row's groups.
+template <int NG, bool ROT, bool HALF>
+__device__ __forceinline__ void quantise(const uint32_t (&w)[16], const uint32_t (&b)[2][2], int u, uint32_t (&codes)[4], uint32_t (&word)[NG]) {
+  float x[32];
+  if (ROT) {
+    rotate_rows<HALF>(w, b, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[2 * i] = lo_half<HALF>(w[i]), x[2 * i + 1] = hi_half<HALF>(w[i]);
+  }
+  constexpr float kUnit = ROT ? 0.125f : 1.f;  // v = x times this (exact: a power of two)
   constexpr int kEach = 32 / NG;
+  float lo[NG], hi[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    float lo = x[g * kEach], hi = lo;
+    if (ROT) {
+      lo[g] = hi[g] = x[g * kEach];
 #pragma unroll
-    for (int i = 1; i < kEach; ++i) {
-      lo = min_nan(lo, x[g * kEach + i]);
-      hi = max_nan(hi, x[g * kEach + i]);
-    }
+      for (int i = 1; i + 1 < kEach; i += 2) {
+        lo[g] = min3_nan(lo[g], x[g * kEach + i], x[g * kEach + i + 1]);
+        hi[g] = max3_nan(hi[g], x[g * kEach + i], x[g * kEach + i + 1]);
+      }
+      lo[g] = min_nan(lo[g], x[g * kEach + kEach - 1]);
+      hi[g] = max_nan(hi[g], x[g * kEach + kEach - 1]);
+    } else {
+      uint32_t a = w[g * kEach / 2], c = a;
 #pragma unroll
-    for (int h = 1; h < kRowLanes; h *= 2) {
-      lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, h));
-      hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, h));
+      for (int i = 1; i < kEach / 2; ++i) {
+        a = min_rows<HALF, true>(a, w[g * kEach / 2 + i]);
+        c = max_rows<HALF, true>(c, w[g * kEach / 2 + i]);
+      }
+      lo[g] = min_nan(lo_half<HALF>(a), hi_half<HALF>(a));
+      hi[g] = max_nan(lo_half<HALF>(c), hi_half<HALF>(c));
     }
-    const bool fine = fabsf(lo) <= 3.402823466e38f && fabsf(hi) <= 3.402823466e38f;  // no infinity, no NaN
-    const __half mh = __float2half_rn(fminf(fmaxf(lo, -65504.f), 65504.f));
-    const float m = __half2float(mh);
-    const __half ah = __float2half_rn(fminf(__fdiv_rn(fmaxf(__fsub_rn(hi, m), 0.f), 15.f), 65504.f));
-    const float a = __half2float(ah);
-    word[g] = fine ? (uint32_t)__half_as_ushort(ah) | (uint32_t)__half_as_ushort(mh) << 16 : 0x7e007e00u;
-    const float inv = a > 0.f ? __frcp_rn(a) : 0.f;
-    const uint64_t inv2 = pair(inv, inv), minus_m = pair(-m, -m), magic = pair(12582912.f, 12582912.f);
+  }
+  // over the row's lanes; of two groups, lanes with an odd u are left with the second
+  float my_lo = lo[0], my_hi = hi[0];
+  if (NG == 2) {
+    my_lo = u & 1 ? lo[NG - 1] : lo[0];
+    my_hi = u & 1 ? hi[NG - 1] : hi[0];
+  }
+  my_lo = min_nan(my_lo, __shfl_xor_sync(0xffffffffu, NG == 2 && !(u & 1) ? lo[NG - 1] : lo[0], 1));
+  my_hi = max_nan(my_hi, __shfl_xor_sync(0xffffffffu, NG == 2 && !(u & 1) ? hi[NG - 1] : hi[0], 1));
+  my_lo = min_nan(my_lo, __shfl_xor_sync(0xffffffffu, my_lo, 2)) * kUnit;
+  my_hi = max_nan(my_hi, __shfl_xor_sync(0xffffffffu, my_hi, 2)) * kUnit;
+  const bool my_fine = fabsf(my_lo) <= 3.402823466e38f && fabsf(my_hi) <= 3.402823466e38f;  // no infinity, no NaN
+  const __half mh = __float2half_rn(fminf(fmaxf(my_lo, -65504.f), 65504.f));
+  const float my_m = __half2float(mh);
+  const __half ah = __float2half_rn(fminf(__fdiv_rn(fmaxf(__fsub_rn(my_hi, my_m), 0.f), 15.f), 65504.f));
+  const float my_a = __half2float(ah);
+  const uint32_t my_word = my_fine ? (uint32_t)__half_as_ushort(ah) | (uint32_t)__half_as_ushort(mh) << 16 : 0x7e007e00u;
+  const float my_inv = my_a > 0.f && my_fine ? __frcp_rn(my_a) : 0.f;
+  // the ends of the range: between them (every step of t is monotone) no code needs clamping
+  const bool inside = my_fine && __fmul_rn(__fsub_rn(my_lo, my_m), my_inv) >= -0.5f && __fmul_rn(__fsub_rn(my_hi, my_m), my_inv) < 15.5f;
+  float inv[NG], m[NG];
+  if (NG == 2) {
+    const float o_inv = __shfl_xor_sync(0xffffffffu, my_inv, 1);
+    const uint32_t o_word = __shfl_xor_sync(0xffffffffu, my_word, 1);
+    inv[0] = u & 1 ? o_inv : my_inv;
+    inv[NG - 1] = u & 1 ? my_inv : o_inv;
+    word[0] = u & 1 ? o_word : my_word;
+    word[NG - 1] = u & 1 ? my_word : o_word;
+  } else {
+    inv[0] = my_inv;
+    word[0] = my_word;
+  }
+#pragma unroll
+  for (int g = 0; g < NG; ++g) m[g] = __half2float(__ushort_as_half((unsigned short)(word[g] >> 16)));
+  const bool clamp = !__all_sync(0xffffffffu, inside);
+  const uint64_t magic = pair(12582912.f, 12582912.f), unit = pair(kUnit, kUnit);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    const uint64_t inv2 = pair(inv[g], inv[g]), minus_m = pair(-m[g], -m[g]);
 #pragma unroll
     for (int c = g * 4 / NG; c < (g + 1) * 4 / NG; ++c) {
-      // c + 1.5 2^23 has the rounded code in its low bits; the exponents' sum over the eight nibbles is a constant
-      uint32_t sum = 0;
+      // t + 1.5 2^23 has the rounded code in its low bits; the rest sums up to a constant over the eight nibbles
+      uint64_t t[4];
 #pragma unroll
-      for (int n = 6; n >= 0; n -= 2) {
+      for (int n = 0; n < 4; ++n) t[n] = mul2(fma2(pair(x[8 * c + 2 * n], x[8 * c + 2 * n + 1]), unit, minus_m), inv2);
+      if (clamp) {  // (a NaN becomes 0)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          float t0, t1;
+          unpair(t[n], t0, t1);
+          t[n] = pair(fminf(fmaxf(t0, 0.f), 15.f), fminf(fmaxf(t1, 0.f), 15.f));
+        }
+      }
+      uint32_t sum = 0, bias = 0;
+#pragma unroll
+      for (int n = 3; n >= 0; --n) {
         float t0, t1;
-        unpair(mul2(add2(pair(x[8 * c + n], x[8 * c + n + 1]), minus_m), inv2), t0, t1);
-        t0 = fminf(fmaxf(t0, 0.f), 15.f);
-        t1 = fminf(fmaxf(t1, 0.f), 15.f);
-        unpair(add2(pair(t0, t1), magic), t0, t1);
+        unpair(add2(t[n], magic), t0, t1);
         sum = (sum << 4) + __float_as_uint(t1);
         sum = (sum << 4) + __float_as_uint(t0);
+        bias = (bias << 4) + 0x4B400000u;
+        bias = (bias << 4) + 0x4B400000u;
       }
-      uint32_t bias = 0;
-#pragma unroll
-      for (int n = 0; n < 8; ++n) bias = (bias << 4) + 0x4B400000u;
-      codes[c] = fine ? sum - bias : 0u;
+      codes[c] = sum - bias;
     }
   }
 }
@@ -191,28 +279,13 @@ __device__ __forceinline__ void load_row(const RowsIO& R, int64_t at, int u, uin
   }
 }
 
-// One step over the rows of a warp (lanes 2 kWords apart): a lane gives away one half of its 2 kWords words and joins the
-// other half with its partner's.
-template <int kWords>
-__device__ __forceinline__ void join_rows(uint32_t (&lo)[16], uint32_t (&hi)[16], int& first, int lane, int half) {
-  const bool up = lane & 2 * kWords;
-#pragma unroll
-  for (int k = 0; k < kWords; ++k) {
-    const uint32_t ol = __shfl_xor_sync(0xffffffffu, up ? lo[k] : lo[k + kWords], 2 * kWords);
-    const uint32_t oh = __shfl_xor_sync(0xffffffffu, up ? hi[k] : hi[k + kWords], 2 * kWords);
-    lo[k] = min_rows(up ? lo[k + kWords] : lo[k], ol, half);
-    hi[k] = max_rows(up ? hi[k + kWords] : hi[k], oh, half);
-  }
-  first += up ? kWords : 0;
-}
-
-// One CTA: the keys or the values of one page of one request that gets new tokens, one head.
-template <int NG, bool ROT>
+// One CTA: one page of one request that gets new tokens, one head; its keys, then its values, or (sides 1) one of them.
+// The row after the present one is loaded while that is worked on.
+template <int NG, bool ROT, bool HALF>
 __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedView v, RowsIO K, RowsIO V, int T, const int32_t* n_new,
-                                                                          int pages_each) {
-  const int side = blockIdx.x & 1;
-  const int slot = (blockIdx.x >> 1) % pages_each;
-  const int bh = (blockIdx.x >> 1) / pages_each;
+                                                                          int pages_each, int sides) {
+  const int part = sides == 1 ? blockIdx.x & 1 : 0, cta = sides == 1 ? blockIdx.x >> 1 : blockIdx.x;
+  const int slot = cta % pages_each, bh = cta / pages_each;
   const int h = bh % v.H, b = bh / v.H;
   const int P = 1 << v.page_log;
   const int held = held_tokens(v, b);
@@ -224,37 +297,42 @@ __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedV
   if (page < 0) return;
   uint8_t* block = block_of(v, page, h);
   constexpr uint32_t kSub = 2048 + 128 * NG;
-  const RowsIO& R = side ? V : K;
-  const int lane = threadIdx.x & 31, u = lane & 3;
-  const int rows_at_once = blockDim.x / kRowLanes;
-  const int64_t base = b * R.sb + h * R.sh + ((int64_t)(j << v.page_log) - held) * R.st;
-  const bool bounds = v.bounds && side == 0;
-  const uint32_t none_lo = v.half ? 0x7c007c00u : 0x7f807f80u, none_hi = none_lo | 0x80008000u;  // + and - infinity
-  uint32_t lo[16], hi[16], sign[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) lo[i] = none_lo, hi[i] = none_hi;
-  if (ROT) sign_words(v, u, sign);
+  const int u = threadIdx.x & 3, row = threadIdx.x / kRowLanes;
+  const int at_once = blockDim.x / kRowLanes;  // rows: the page's, or 32
+  const int turns_log = max(0, v.page_log - 5), turns = sides << turns_log;
+  const int64_t to = (int64_t)(j << v.page_log) - held;  // token of the page's first place, among the new ones
+  const int64_t base_k = b * K.sb + h * K.sh + to * K.st, base_v = b * V.sb + h * V.sh + to * V.st;
+  __shared__ __align__(16) uint32_t sign[64];
+  if (ROT) fill_signs(v, sign);
 
-  for (int i_at = 0; i_at < P; i_at += rows_at_once) {
-    const int i = i_at + threadIdx.x / kRowLanes;
-    const bool there = i >= i0 && i < i1;
-    if (!__any_sync(0xffffffffu, there)) continue;
-    uint32_t w[16];
+  auto load = [&](int turn, uint32_t (&w)[16]) {
+    const int side = part + (turn >> turns_log), i = (turn & ((1 << turns_log) - 1)) * at_once + row;
 #pragma unroll
     for (int k = 0; k < 16; ++k) w[k] = 0;
-    if (there) {
-      load_row(R, base + i * R.st, u, w);
-      if (bounds) {
-#pragma unroll
-        for (int k = 0; k < 16; ++k) lo[k] = min_rows(lo[k], w[k], v.half), hi[k] = max_rows(hi[k], w[k], v.half);
-      }
+    if (turn < turns && i >= i0 && i < i1) {
+      if (side) load_row(V, base_v + i * V.st, u, w);
+      else load_row(K, base_k + i * K.st, u, w);
     }
+  };
+  uint32_t signs[2][2];
+  if (ROT) hadamard_operand<HALF>(threadIdx.x & 31, 0, signs);
+  uint32_t next[16];
+  load(0, next);
+#pragma unroll 1
+  for (int turn = 0; turn < turns; ++turn) {
+    uint32_t w[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) w[k] = next[k];
+    load(turn + 1, next);
+    const int side = part + (turn >> turns_log), i = (turn & ((1 << turns_log) - 1)) * at_once + row;
+    const bool there = i >= i0 && i < i1;
+    if (!__any_sync(0xffffffffu, there)) continue;
     if (ROT) {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) w[k] ^= sign[k];
+      for (int k = 0; k < 16; ++k) w[k] ^= sign[16 * u + k];
     }
     uint32_t c[4], word[NG];
-    quantise<NG, ROT>(w, v.half, u, c, word);
+    quantise<NG, ROT, HALF>(w, signs, u, c, word);
     uint8_t* s = block + (uint32_t)(i >> 4) * kSub;
     const int i16 = i & 15;
     if (side == 0) {
@@ -283,110 +361,197 @@ __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedV
       for (int g = 0; g < NG; ++g) at[g] = word[g];
     }
   }
-  if (!bounds) return;
-  // over the 8 rows of a warp, after which a lane has two words (of the smallest, and of the largest) left; then over
-  // the warps
-  int first = 0;
-  join_rows<8>(lo, hi, first, lane, v.half);
-  join_rows<4>(lo, hi, first, lane, v.half);
-  join_rows<2>(lo, hi, first, lane, v.half);
-  __shared__ uint32_t red[kMaxThreads / 32][2][64];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int i = first + k, at = 16 * (i >> 2) + 4 * u + (i & 3);  // dimensions 32 c + 8 u + 2 m as pair 16 c + 4 u + m
-    red[threadIdx.x >> 5][0][at] = lo[k];
-    red[threadIdx.x >> 5][1][at] = hi[k];
+  if (!v.bounds || part != 0) return;
+  // The page's bounds: the keys once more, which the caches hold; a thread takes two dimensions of every other row.
+  __shared__ uint32_t red[2][64];
+  const int at = threadIdx.x & 63, rows = blockDim.x >> 6;
+  uint32_t lo = HALF ? 0x7c007c00u : 0x7f807f80u, hi = lo | 0x80008000u;  // + and - infinity
+#pragma unroll 8
+  for (int i = i0 + (threadIdx.x >> 6); i < i1; i += rows) {
+    const uint16_t* x = K.ptr + base_k + i * K.st + 2 * at;
+    const uint32_t w = K.vec ? *(const uint32_t*)x : x[0] | (uint32_t)x[1] << 16;
+    lo = min_rows<HALF>(lo, w);
+    hi = max_rows<HALF>(hi, w);
   }
-  __syncthreads();
-  for (int k = threadIdx.x; k < 128; k += blockDim.x) {
-    const int most = k >> 6, at = k & 63;
-    uint32_t x = red[0][most][at];
-    for (unsigned w = 1; w < blockDim.x / 32; ++w) x = most ? max_rows(x, red[w][1][at], v.half) : min_rows(x, red[w][0][at], v.half);
-    uint32_t* to = (uint32_t*)(block + (uint32_t)(P >> 4) * kSub) + k;
-    if (i0 != 0) x = most ? max_rows(x, *to, v.half) : min_rows(x, *to, v.half);  // what the page held before
-    *to = x;
+  if (rows == 2) {
+    if (threadIdx.x >= 64) red[0][at] = lo, red[1][at] = hi;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    lo = min_rows<HALF>(lo, red[0][at]);
+    hi = max_rows<HALF>(hi, red[1][at]);
+  }
+  uint32_t* to_b = (uint32_t*)(block + (uint32_t)(P >> 4) * kSub) + at;
+  if (i0 != 0) lo = min_rows<HALF>(lo, to_b[0]), hi = max_rows<HALF>(hi, to_b[64]);  // what the page held before
+  to_b[0] = lo;
+  to_b[64] = hi;
+}
+
+// H v^ / 16 of the warp's 8 rows from their codes: over the six bits of a group H v^ = a (H c) + 64 m at dimension 0, and
+// the codes' sums are whole numbers, exact; bit 6 joins the groups.  Nibbles are taken in place as fp16 subnormals,
+// c 2^-24 or (odd dimensions) c 2^-20.
+template <int NG>
+__device__ __forceinline__ void unrotate_codes(const uint32_t (&c)[4], const uint32_t (&b)[2][2], const float (&scale)[NG],
+                                               const float (&low)[NG], int u, float (&y)[32]) {
+  uint64_t p[16];  // p[4 c + 2 d2 + d0]: the pair of bit 1
+  const uint64_t up = pair(0.0625f, 0.0625f), down = pair(-0.0625f, -0.0625f), minus = pair(-1.f, -1.f);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {  // bits 1, 2, 3, 4; the tile's lower rows are the odd dimensions; then bit 0
+      const uint32_t x = c[k], z = c[k] >> 8;
+      float d[4];
+      mma_rows<true>(d, x & 0x000f000fu, x & 0x00f000f0u, z & 0x000f000fu, z & 0x00f000f0u, b[n][0], b[n][1]);
+      const uint64_t even = pair(d[0], d[1]), odd = pair(d[2], d[3]);
+      p[4 * k + 2 * n] = fma2(odd, up, even);
+      p[4 * k + 2 * n + 1] = fma2(odd, down, even);
+    }
+#pragma unroll
+  for (int i = 0; i < 16; ++i)  // bit 5
+    if (!(i & 4)) {
+      const uint64_t a = p[i], q = p[i | 4];
+      p[i] = add2(a, q);
+      p[i | 4] = fma2(q, minus, a);
+    }
+  const float a0 = scale[0] * 1048576.f, a1 = scale[NG - 1] * 1048576.f;  // 2^24 / 16
+  const uint64_t s0 = pair(a0, a0), s1 = pair(a1, a1);
+  const float m0 = u == 0 ? low[0] * 4.f : 0.f, m1 = u == 0 ? low[NG - 1] * 4.f : 0.f;  // 64 / 16
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {  // bit 6
+    uint64_t q = mul2(p[i + 8], s1), r = q;
+    if (i == 0) {  // dimension 0 of each group
+      q = fma2(p[8], s1, pair(m0 + m1, 0.f));
+      r = fma2(p[8], s1, pair(m1 - m0, 0.f));
+    }
+    const uint64_t a = fma2(p[i], s0, q), d = fma2(r, minus, mul2(p[i], s0));
+    const int c0 = i >> 2, d2 = i >> 1 & 1, d0 = i & 1, at = 8 * c0 + 4 * d2 + d0;
+    unpair(a, y[at], y[at + 2]);
+    unpair(d, y[at + 16], y[at + 18]);
   }
 }
 
-template <int NG, bool ROT>
-__global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_read_kernel(PagedView v, const int32_t* start, RowsIO K, RowsIO V, int T,
-                                                                        int chunks) {
+constexpr int kReadTurns = 4;  // rows a thread reads back at most
+
+template <int NG, bool ROT, bool HALF>
+__global__ void __launch_bounds__(kMaxThreads, 5) akv_paged_read_kernel(PagedView v, const int32_t* start, RowsIO K, RowsIO V, int T,
+                                                                        int chunks, int turns) {
   constexpr int kRowsAtOnce = kMaxThreads / kRowLanes;
   const int side = blockIdx.x & 1;
   const int chunk = (blockIdx.x >> 1) % chunks;
   const int bh = (blockIdx.x >> 1) / chunks;
   const int h = bh % v.H, b = bh / v.H;
-  const int u = threadIdx.x & 3, t = chunk * kRowsAtOnce + threadIdx.x / kRowLanes;
-  const int64_t pos = (start ? (int64_t)start[b] : 0) + t;
-  const int P = 1 << v.page_log;
-  int page = -1;
-  if (t < T && pos >= 0 && pos < held_tokens(v, b)) page = page_of(v, b, (int)(pos >> v.page_log));
-  const int i = (int)(pos & (P - 1)), i16 = i & 15;
-  float x[32];
+  const int u = threadIdx.x & 3;
+  const int64_t first = start ? (int64_t)start[b] : 0;
+  const int held = held_tokens(v, b), P = 1 << v.page_log;
+  const RowsIO& R = side ? V : K;
+  __shared__ __align__(16) uint32_t sign[64];
+  if (ROT) fill_signs(v, sign);
+  auto token = [&](int turn) { return (chunk * turns + turn) * kRowsAtOnce + (int)threadIdx.x / kRowLanes; };
+  auto find = [&](int turn) {
+    const int t = token(turn);
+    const int64_t pos = first + t;
+    return turn < turns && t < T && pos >= 0 && pos < held ? page_of(v, b, (int)(pos >> v.page_log)) : -1;
+  };
+  struct Held {
+    uint4 y, z;  // a key's codes; the two units that hold a value's
+    uint32_t words[NG];
+  };
+  auto fetch = [&](int turn, int page) {
+    Held r;
+    r.y = r.z = make_uint4(0, 0, 0, 0);
 #pragma unroll
-  for (int e = 0; e < 32; ++e) x[e] = 0.f;
-  if (page >= 0) {
+    for (int g = 0; g < NG; ++g) r.words[g] = 0;
+    if (page < 0) return r;
+    const int i = (int)((first + token(turn)) & (P - 1)), i16 = i & 15;
     const uint8_t* s = block_of(v, page, h) + (uint32_t)(i >> 4) * (2048 + 128 * NG);
-    uint32_t c[4];
+    const uint32_t* at = (const uint32_t*)(s + 2048) + 2 * NG * i16 + NG * side;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) r.words[g] = at[g];
     if (side == 0) {
-      const uint4 k = *(const uint4*)(s + 64 * i16 + 16 * u);
-      c[0] = k.x, c[1] = k.y, c[2] = k.z, c[3] = k.w;
+      r.y = *(const uint4*)(s + 64 * i16 + 16 * u);
     } else {
       const uint8_t* unit = s + 1024 + 512 * (i16 >> 3) + 16 * (4 * u + ((i16 & 7) >> 1));
-      const uint4 y = *(const uint4*)unit, z = *(const uint4*)(unit + 256);
-      const uint32_t pick = i & 1 ? 0x7632 : 0x5410;
-      c[0] = __byte_perm(y.x, y.y, pick);
-      c[1] = __byte_perm(z.x, z.y, pick);
-      c[2] = __byte_perm(y.z, y.w, pick);
-      c[3] = __byte_perm(z.z, z.w, pick);
+      r.y = *(const uint4*)unit;
+      r.z = *(const uint4*)(unit + 256);
     }
-    const uint32_t* words = (const uint32_t*)(s + 2048) + 2 * NG * i16 + NG * side;
+    return r;
+  };
+  uint32_t signs[2][2];
+  if (ROT) hadamard_operand<true>(threadIdx.x & 31, 2, signs);
+  // the page of the row after the next and the codes of the next are under way while a row is worked on
+  int page = find(0), page1 = find(1);
+  Held ahead = fetch(0, page);
+#pragma unroll 1
+  for (int turn = 0; turn < turns; ++turn) {
+    const Held r = ahead;
+    const int t = token(turn);
+    const bool there = page >= 0, odd = (first + t) & 1;
+    ahead = fetch(turn + 1, page1);
+    page = page1;
+    page1 = find(turn + 2);
+    float x[32];
+    {
+      uint32_t c[4] = {r.y.x, r.y.y, r.y.z, r.y.w};
+      const uint32_t* words = r.words;
+      float scale[NG], low[NG];
+      if (side) {
+        const uint32_t pick = odd ? 0x7632 : 0x5410;
+        c[0] = __byte_perm(r.y.x, r.y.y, pick);
+        c[1] = __byte_perm(r.z.x, r.z.y, pick);
+        c[2] = __byte_perm(r.y.z, r.y.w, pick);
+        c[3] = __byte_perm(r.z.z, r.z.w, pick);
+      }
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const uint32_t w = words[g];
-      const float a = __half2float(__ushort_as_half((unsigned short)w)), m = __half2float(__ushort_as_half((unsigned short)(w >> 16)));
-      const float a24 = a * 16777216.f, a20 = a * 1048576.f;
+      for (int g = 0; g < NG; ++g) {
+        scale[g] = __half2float(__ushort_as_half((unsigned short)words[g]));
+        low[g] = __half2float(__ushort_as_half((unsigned short)(words[g] >> 16)));
+      }
+      if (ROT) {
+        unrotate_codes<NG>(c, signs, scale, low, u, x);
+      } else {
 #pragma unroll
-      for (int k = g * 4 / NG; k < (g + 1) * 4 / NG; ++k)
+        for (int k = 0; k < 4; ++k) {
+          const float a24 = scale[k * NG / 4] * 16777216.f, a20 = scale[k * NG / 4] * 1048576.f, m = low[k * NG / 4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {  // nibbles q and q + 4, in place, as fp16 subnormals: c 2^-24, odd ones c 2^-20
-          const uint32_t y = (q & 2 ? c[k] >> 8 : c[k]) & (q & 1 ? 0x00f000f0u : 0x000f000fu);
-          const __half2 hh = *reinterpret_cast<const __half2*>(&y);
-          x[8 * k + q] = fmaf(__low2float(hh), q & 1 ? a20 : a24, m);
-          x[8 * k + q + 4] = fmaf(__high2float(hh), q & 1 ? a20 : a24, m);
+          for (int q = 0; q < 4; ++q) {  // nibbles q and q + 4, in place, as fp16 subnormals: c 2^-24, odd ones c 2^-20
+            const uint32_t y = (q & 2 ? c[k] >> 8 : c[k]) & (q & 1 ? 0x00f000f0u : 0x000f000fu);
+            const __half2 hh = *reinterpret_cast<const __half2*>(&y);
+            x[8 * k + q] = fmaf(__low2float(hh), q & 1 ? a20 : a24, m);
+            x[8 * k + q + 4] = fmaf(__high2float(hh), q & 1 ? a20 : a24, m);
+          }
         }
+      }
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) w[k] = pack_rows<HALF>(x[2 * k], x[2 * k + 1]);
+    if (ROT && there) {  // (a row that is not there is +0)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) w[k] ^= sign[16 * u + k];
+    }
+    if (t >= T) continue;
+    uint16_t* row = R.ptr + b * R.sb + t * R.st + h * R.sh + 8 * u;
+    if (R.vec) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *(uint4*)(row + 32 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        row[32 * (k >> 2) + 2 * (k & 3)] = (uint16_t)w[k];
+        row[32 * (k >> 2) + 2 * (k & 3) + 1] = (uint16_t)(w[k] >> 16);
+      }
     }
   }
-  uint32_t w[16];
-  if (ROT) {
-    wht_4x32(x, u);
-#pragma unroll
-    for (int e = 0; e < 32; ++e) x[e] *= 0.0625f;
-  }
-#pragma unroll
-  for (int k = 0; k < 16; ++k) w[k] = pack_rows(x[2 * k], x[2 * k + 1], v.half);
-  if (ROT) {
-    uint32_t sign[16];
-    sign_words(v, u, sign);
-#pragma unroll
-    for (int k = 0; k < 16; ++k) w[k] ^= sign[k];
-    if (page < 0)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) w[k] = 0;  // (no negative zeros)
-  }
-  if (t >= T) return;
-  const RowsIO& R = side ? V : K;
-  uint16_t* row = R.ptr + b * R.sb + t * R.st + h * R.sh + 8 * u;
-  if (R.vec) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) *(uint4*)(row + 32 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      row[32 * (k >> 2) + 2 * (k & 3)] = (uint16_t)w[k];
-      row[32 * (k >> 2) + 2 * (k & 3) + 1] = (uint16_t)(w[k] >> 16);
-    }
-  }
+}
+
+template <bool HALF>
+auto append_kernel(const PagedView& v) {
+  return v.rotate ? (v.ng == 2 ? akv_paged_append_kernel<2, true, HALF> : akv_paged_append_kernel<1, true, HALF>)
+                  : (v.ng == 2 ? akv_paged_append_kernel<2, false, HALF> : akv_paged_append_kernel<1, false, HALF>);
+}
+template <bool HALF>
+auto read_kernel(const PagedView& v) {
+  return v.rotate ? (v.ng == 2 ? akv_paged_read_kernel<2, true, HALF> : akv_paged_read_kernel<1, true, HALF>)
+                  : (v.ng == 2 ? akv_paged_read_kernel<2, false, HALF> : akv_paged_read_kernel<1, false, HALF>);
 }
 
 RowsIO rows_io(const akv_rows& r) {
@@ -401,22 +566,25 @@ int launch_paged_append(const PagedView& v, const akv_rows& K, const akv_rows& V
   const int P = 1 << v.page_log;
   int64_t each = ((int64_t)T + P - 2) / P + 1;  // pages that T tokens can touch
   if (each > v.max_pages) each = v.max_pages;
-  const int64_t grid = 2 * each * v.H * v.rows;
+  // keys and values by one CTA where there are CTAs enough for the GPU (four an SM) all the same
+  const int sides = each * v.H * v.rows >= 4 * 152 ? 2 : 1;
+  const int64_t grid = (sides == 1 ? 2 : 1) * each * v.H * v.rows;
   if (grid > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
   const int threads = P * kRowLanes < kMaxThreads ? P * kRowLanes : kMaxThreads;
-  auto* kernel = v.rotate ? (v.ng == 2 ? akv_paged_append_kernel<2, true> : akv_paged_append_kernel<1, true>)
-                          : (v.ng == 2 ? akv_paged_append_kernel<2, false> : akv_paged_append_kernel<1, false>);
-  kernel<<<(unsigned)grid, threads, 0, (cudaStream_t)stream>>>(v, rows_io(K), rows_io(V), T, n_new, (int)each);
+  auto kernel = v.half ? append_kernel<true>(v) : append_kernel<false>(v);
+  kernel<<<(unsigned)grid, threads, 0, (cudaStream_t)stream>>>(v, rows_io(K), rows_io(V), T, n_new, (int)each, sides);
   return (int)cudaGetLastError();
 }
 
 int launch_paged_read(const PagedView& v, const int32_t* start, const akv_rows& K, const akv_rows& V, int32_t T, void* stream) {
-  const int64_t each = ((int64_t)T + kMaxThreads / kRowLanes - 1) / (kMaxThreads / kRowLanes);
+  const int64_t chunks = ((int64_t)T + kMaxThreads / kRowLanes - 1) / (kMaxThreads / kRowLanes);
+  // more rows a thread only where the grid stays above a few waves (the signs' set-up is shared by them)
+  const int turns = chunks * v.H * v.rows >= 8192 ? kReadTurns : 1;
+  const int64_t each = (chunks + turns - 1) / turns;
   const int64_t grid = 2 * each * v.H * v.rows;
   if (grid > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
-  auto* kernel = v.rotate ? (v.ng == 2 ? akv_paged_read_kernel<2, true> : akv_paged_read_kernel<1, true>)
-                          : (v.ng == 2 ? akv_paged_read_kernel<2, false> : akv_paged_read_kernel<1, false>);
-  kernel<<<(unsigned)grid, kMaxThreads, 0, (cudaStream_t)stream>>>(v, start, rows_io(K), rows_io(V), T, (int)each);
+  auto kernel = v.half ? read_kernel<true>(v) : read_kernel<false>(v);
+  kernel<<<(unsigned)grid, kMaxThreads, 0, (cudaStream_t)stream>>>(v, start, rows_io(K), rows_io(V), T, (int)each, turns);
   return (int)cudaGetLastError();
 }
 
