@@ -284,6 +284,8 @@ __device__ __forceinline__ void load_row(const RowsIO& R, int64_t at, int u, uin
 template <int NG, bool ROT, bool HALF>
 __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedView v, RowsIO K, RowsIO V, int T, const int32_t* n_new,
                                                                           int pages_each, int sides) {
+  __shared__ __align__(16) uint32_t sign[64];
+  if (ROT) fill_signs(v, sign);
   const int part = sides == 1 ? blockIdx.x & 1 : 0, cta = sides == 1 ? blockIdx.x >> 1 : blockIdx.x;
   const int slot = cta % pages_each, bh = cta / pages_each;
   const int h = bh % v.H, b = bh / v.H;
@@ -293,17 +295,13 @@ __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedV
   const int j = (held >> v.page_log) + slot;  // table position
   const int i0 = max(0, held - (j << v.page_log)), i1 = min(P, held + n - (j << v.page_log));  // places in the page
   if (i0 >= i1) return;
-  const int page = page_of(v, b, j);
-  if (page < 0) return;
-  uint8_t* block = block_of(v, page, h);
+  const int page = page_of(v, b, j);  // (looked at once the first rows are under way)
   constexpr uint32_t kSub = 2048 + 128 * NG;
   const int u = threadIdx.x & 3, row = threadIdx.x / kRowLanes;
   const int at_once = blockDim.x / kRowLanes;  // rows: the page's, or 32
   const int turns_log = max(0, v.page_log - 5), turns = sides << turns_log;
   const int64_t to = (int64_t)(j << v.page_log) - held;  // token of the page's first place, among the new ones
   const int64_t base_k = b * K.sb + h * K.sh + to * K.st, base_v = b * V.sb + h * V.sh + to * V.st;
-  __shared__ __align__(16) uint32_t sign[64];
-  if (ROT) fill_signs(v, sign);
 
   auto load = [&](int turn, uint32_t (&w)[16]) {
     const int side = part + (turn >> turns_log), i = (turn & ((1 << turns_log) - 1)) * at_once + row;
@@ -318,6 +316,8 @@ __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedV
   if (ROT) hadamard_operand<HALF>(threadIdx.x & 31, 0, signs);
   uint32_t next[16];
   load(0, next);
+  if (page < 0) return;
+  uint8_t* block = block_of(v, page, h);
 #pragma unroll 1
   for (int turn = 0; turn < turns; ++turn) {
     uint32_t w[16];
@@ -429,7 +429,7 @@ __device__ __forceinline__ void unrotate_codes(const uint32_t (&c)[4], const uin
   }
 }
 
-constexpr int kReadTurns = 4;  // rows a thread reads back at most
+constexpr int kReadTurns = 8;  // rows a thread reads back at most
 
 template <int NG, bool ROT, bool HALF>
 __global__ void __launch_bounds__(kMaxThreads, 5) akv_paged_read_kernel(PagedView v, const int32_t* start, RowsIO K, RowsIO V, int T,

@@ -16,6 +16,8 @@
 // largest a so far so that a weight only underflows 2^-31 below the largest.  Sums, maxima and logits are fp32.
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "akv_device.cuh"
 #include "akv_paged.cuh"
 
@@ -754,11 +756,17 @@ static_assert(sizeof(Smem<1>) <= 115712, "two CTAs of an SM share 228 KiB, 1 KiB
 static_assert(sizeof(Smem<2>) <= 232448 && sizeof(Smem<4>) <= 232448, "shared memory of a CTA");
 
 template <int NG, int NT, bool HILO, bool SEL>
-int launch(const AttnArgs& a, int sms, cudaStream_t stream) {
+int launch(const AttnArgs& a, int dev, int sms, cudaStream_t stream) {
   auto* kernel = akv_paged_attn_kernel<NG, NT, HILO, SEL>;
   const size_t smem = sizeof(Smem<NT>);
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return (int)e;
+  cudaError_t e;
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel's shared memory has been set
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return (int)e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
   int grid = sms * ctas_of(NT);
   if (grid > kPagedMaxGrid) grid = kPagedMaxGrid;
   kernel<<<grid, Smem<NT>::kThreads, smem, stream>>>(a);
@@ -777,15 +785,15 @@ int launch(const AttnArgs& a, int sms, cudaStream_t stream) {
 }
 
 template <int NT, bool HILO, bool SEL>
-int launch_ng(const AttnArgs& a, int sms, cudaStream_t s) {
-  return a.v.ng == 2 ? launch<2, NT, HILO, SEL>(a, sms, s) : launch<1, NT, HILO, SEL>(a, sms, s);
+int launch_ng(const AttnArgs& a, int dev, int sms, cudaStream_t s) {
+  return a.v.ng == 2 ? launch<2, NT, HILO, SEL>(a, dev, sms, s) : launch<1, NT, HILO, SEL>(a, dev, sms, s);
 }
 template <bool HILO, bool SEL>
-int launch_nt(const AttnArgs& a, int unit_rows, int sms, cudaStream_t s) {
+int launch_nt(const AttnArgs& a, int unit_rows, int dev, int sms, cudaStream_t s) {
   switch (unit_rows) {
-    case 8: return launch_ng<1, HILO, SEL>(a, sms, s);
-    case 16: return launch_ng<2, HILO, SEL>(a, sms, s);
-    default: return launch_ng<4, HILO, SEL>(a, sms, s);
+    case 8: return launch_ng<1, HILO, SEL>(a, dev, sms, s);
+    case 16: return launch_ng<2, HILO, SEL>(a, dev, sms, s);
+    default: return launch_ng<4, HILO, SEL>(a, dev, sms, s);
   }
 }
 
@@ -827,8 +835,8 @@ int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out
   a.desc = (int4*)ws;
   a.slots = (float*)((uint8_t*)ws + kShareDescBytes);
   cudaStream_t s = (cudaStream_t)stream;
-  if (v.rotate) return sel ? launch_nt<true, true>(a, unit_rows, sms, s) : launch_nt<true, false>(a, unit_rows, sms, s);
-  return sel ? launch_nt<false, true>(a, unit_rows, sms, s) : launch_nt<false, false>(a, unit_rows, sms, s);
+  if (v.rotate) return sel ? launch_nt<true, true>(a, unit_rows, dev, sms, s) : launch_nt<true, false>(a, unit_rows, dev, sms, s);
+  return sel ? launch_nt<false, true>(a, unit_rows, dev, sms, s) : launch_nt<false, false>(a, unit_rows, dev, sms, s);
 }
 
 }  // namespace akv

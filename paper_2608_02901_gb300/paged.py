@@ -94,27 +94,31 @@ def akv_paged_page_bytes(p: PagedParams) -> int:
     return n.value
 
 
+_loaded = None
+_torch = None
+
+
+def _lib():
+    """The library; torch is loaded with it."""
+    global _loaded, _torch
+    if _loaded is None:
+        import torch
+
+        from . import lib
+        _torch, _loaded = torch, lib()
+    return _loaded
+
+
 def _check(status, where):
     if status:
         from . import _check as check
         check(status, where)
 
 
-_loaded = None
-
-
-def _lib():
-    global _loaded
-    if _loaded is None:
-        from . import lib
-        _loaded = lib()
-    return _loaded
-
-
-def _stream(stream):
+def _stream(stream, pages):
+    """Address of a stream: the current one of the pool's device for None."""
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _torch._C._cuda_getCurrentRawStream(pages.index)
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -122,7 +126,7 @@ def _ints(t, what, n=None, device=None):
     """Address of a contiguous CUDA int32 tensor (with n elements), or None for None."""
     if t is None:
         return None
-    if not t.is_cuda or str(t.dtype) != "torch.int32" or not t.is_contiguous():
+    if t.dtype is not _torch.int32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous CUDA int32 tensor")
     if n is not None and t.numel() != n:
         raise ValueError(f"{what} must hold {n} numbers")
@@ -142,19 +146,20 @@ class Pages:
     """
 
     def __init__(self, p: PagedParams, pool, table, lens, refs=None):
-        page = akv_paged_page_bytes(p)
+        page = akv_paged_page_bytes(p)  # (loads the library)
         if not pool.is_cuda or pool.dim() < 2:
             raise ValueError("pool must be a CUDA tensor [n_layers][n_pages][...]")
         n_layers, n_pages = int(pool.shape[0]), int(pool.shape[1])
         if pool[0].numel() * pool.element_size() != n_pages * page or not pool[0].is_contiguous():
             raise ValueError(f"pool must hold pages of {page} contiguous bytes")
-        if not table.is_cuda or str(table.dtype) != "torch.int32" or table.dim() != 2 or table.stride(1) != 1:
+        if not table.is_cuda or table.dtype is not _torch.int32 or table.dim() != 2 or table.stride(1) != 1:
             raise ValueError("table must be a CUDA int32 tensor [rows][max_pages] with adjacent columns")
         if table.device != pool.device:
             raise ValueError("table must be on the pool's device")
         rows, most = table.shape
         self.p, self.pool, self.table, self.lens, self.refs = p, pool, table, lens, refs
         self.rows, self.max_pages, self.n_layers, self.n_pages, self.device = rows, most, n_layers, n_pages, pool.device
+        self.index = pool.device.index
         stride = pool.stride(0) * pool.element_size() if n_layers > 1 else n_pages * page
         self._params = p.c()
         self._c = _Pages(pool.data_ptr(), (n_layers - 1) * stride + n_pages * page, stride, n_layers, n_pages,
@@ -184,44 +189,52 @@ def _params(p: PagedParams, pages: Pages):
     return ctypes.byref(p.c())
 
 
-def _rows(t, what, p: PagedParams, rows, heads, T=None):
+def _rows(t, what, p: PagedParams, pages: Pages, T, heads):
     """The C view of a [rows][T][heads][128] tensor of the cache's type, any strides but adjacent values."""
-    if not t.is_cuda or str(t.dtype) != ("torch.float16" if p.half else "torch.bfloat16"):
+    if t.dtype is not (_torch.float16 if p.half else _torch.bfloat16) or not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor of {'fp16' if p.half else 'bf16'}")
-    if t.dim() != 4 or t.shape[0] != rows or t.shape[2] != heads or t.shape[3] != p.head_dim or (T is not None and t.shape[1] != T):
-        raise ValueError(f"{what} must be [{rows}][{'T' if T is None else T}][{heads}][{p.head_dim}], got {list(t.shape)}")
+    if t.shape != (pages.rows, T, heads, 128):
+        raise ValueError(f"{what} must be [{pages.rows}][{T}][{heads}][128], got {list(t.shape)}")
+    if t.device != pages.device:
+        raise ValueError(f"{what} must be on the pool's device")
     sb, st, sh, sd = t.stride()
     if sd != 1:
         raise ValueError(f"{what} must have adjacent values in its last axis")
-    return ctypes.byref(_Rows(t.data_ptr(), sb, st, sh))
+    return _Rows(t.data_ptr(), sb, st, sh)
 
 
-def _workspace(ws, need, device, stream):
+def _tokens(t, what):
+    if t.dim() != 4:
+        raise ValueError(f"{what} must be [rows][T][heads][128], got {list(t.shape)}")
+    return t.shape[1]
+
+
+def _workspace(ws, need, pages, stream):
     if ws is None:
-        import torch
-        ws = torch.empty(need(), dtype=torch.uint8, device=device)
+        ws = _torch.empty(need(), dtype=_torch.uint8, device=pages.device)
         if stream is not None:  # the allocator must not hand it out again before that stream is done with it
-            ws.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device))
+            ws.record_stream(stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(stream, pages.device))
     elif not ws.is_cuda or not ws.is_contiguous():
         raise ValueError("ws must be a contiguous CUDA tensor")
-    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws, ws.data_ptr(), ws.nbytes
 
 
 def akv_paged_append(p: PagedParams, pages: Pages, K, V, n_new=None, layer: int = 0, stream=None):
     """K, V: [rows][T][n_kv_heads][128]; n_new: CUDA int32 [rows] (None: T each).  lens is not advanced."""
-    T = int(K.shape[1])
-    _check(_lib().akv_paged_append(_params(p, pages), pages.ref, layer, _rows(K, "K", p, pages.rows, p.n_kv_heads),
-                                   _rows(V, "V", p, pages.rows, p.n_kv_heads, T), T,
-                                   _ints(n_new, "n_new", pages.rows, pages.device), _stream(stream)), "akv_paged_append")
+    T = _tokens(K, "K")
+    _check(_lib().akv_paged_append(_params(p, pages), pages.ref, layer, _rows(K, "K", p, pages, T, p.n_kv_heads),
+                                   _rows(V, "V", p, pages, T, p.n_kv_heads), T,
+                                   _ints(n_new, "n_new", pages.rows, pages.device), _stream(stream, pages)),
+           "akv_paged_append")
 
 
 def akv_paged_read(p: PagedParams, pages: Pages, K, V, start=None, layer: int = 0, stream=None):
     """Fills K, V [rows][T][n_kv_heads][128] (any strides, e.g. a transposed [rows][n_kv_heads][T][128]) with the
     tokens from start (CUDA int32 [rows], None: 0) on; tokens that a request does not hold are zeros."""
-    T = int(K.shape[1])
+    T = _tokens(K, "K")
     _check(_lib().akv_paged_read(_params(p, pages), pages.ref, layer, _ints(start, "start", pages.rows, pages.device),
-                                 _rows(K, "K", p, pages.rows, p.n_kv_heads),
-                                 _rows(V, "V", p, pages.rows, p.n_kv_heads, T), T, _stream(stream)), "akv_paged_read")
+                                 _rows(K, "K", p, pages, T, p.n_kv_heads), _rows(V, "V", p, pages, T, p.n_kv_heads), T,
+                                 _stream(stream, pages)), "akv_paged_read")
 
 
 def akv_paged_attn_workspace_size(p: PagedParams, pages: Pages, T: int = 1, top: int = 0) -> int:
@@ -232,7 +245,7 @@ def akv_paged_attn_workspace_size(p: PagedParams, pages: Pages, T: int = 1, top:
 
 
 def _match(sel: PageSelection, pages: Pages, T, heads):
-    if tuple(sel.count.shape) != (pages.rows, T, heads) or sel.pages.device != pages.device:
+    if sel.count.shape != (pages.rows, T, heads) or sel.pages.device != pages.device:
         raise ValueError(f"the selection must be for [{pages.rows}][{T}][{heads}], on the pool's device")
 
 
@@ -240,18 +253,18 @@ def akv_paged_attn(p: PagedParams, pages: Pages, q, out, lse=None, sel: PageSele
                    sm_scale: float = 1.0, layer: int = 0, ws=None, stream=None):
     """q, out: [rows][T][n_q_heads][128]; lse: optional contiguous fp32 [rows][T][n_q_heads].
     ws: CUDA workspace of akv_paged_attn_workspace_size bytes; when None, one is taken from torch's allocator."""
-    T = int(q.shape[1])
+    T = _tokens(q, "q")
+    L = _lib()
     if sel is not None:
         _match(sel, pages, T, p.n_kv_heads)
-    if lse is not None and (not lse.is_cuda or str(lse.dtype) != "torch.float32" or not lse.is_contiguous()
-                            or tuple(lse.shape) != (pages.rows, T, p.n_q_heads)):
+    if lse is not None and (lse.dtype is not _torch.float32 or not lse.is_cuda or not lse.is_contiguous()
+                            or lse.shape != (pages.rows, T, p.n_q_heads)):
         raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{pages.rows}][{T}][{p.n_q_heads}]")
     ws, at, n = _workspace(ws, lambda: akv_paged_attn_workspace_size(p, pages, T, sel.top if sel is not None else 0),
-                           pages.device, stream)
-    _check(_lib().akv_paged_attn(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages.rows, p.n_q_heads),
-                                 _rows(out, "out", p, pages.rows, p.n_q_heads, T),
-                                 None if lse is None else lse.data_ptr(), T, sm_scale,
-                                 None if sel is None else sel.ref, at, n, _stream(stream)), "akv_paged_attn")
+                           pages, stream)
+    _check(L.akv_paged_attn(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads),
+                            _rows(out, "out", p, pages, T, p.n_q_heads), None if lse is None else lse.data_ptr(), T,
+                            sm_scale, None if sel is None else sel.ref, at, n, _stream(stream, pages)), "akv_paged_attn")
 
 
 def akv_paged_select_workspace_size(p: PagedParams, pages: Pages, T: int = 1) -> int:
@@ -264,11 +277,12 @@ def akv_paged_select_workspace_size(p: PagedParams, pages: Pages, T: int = 1) ->
 def akv_paged_select(p: PagedParams, pages: Pages, q, sel: PageSelection, sink: int = 1, recent: int = 1,
                      layer: int = 0, ws=None, stream=None):
     """q: [rows][T][n_q_heads][128]; fills sel.  ws as in akv_paged_attn, of akv_paged_select_workspace_size bytes."""
-    T = int(q.shape[1])
+    T = _tokens(q, "q")
+    L = _lib()
     _match(sel, pages, T, p.n_kv_heads)
-    ws, at, n = _workspace(ws, lambda: akv_paged_select_workspace_size(p, pages, T), pages.device, stream)
-    _check(_lib().akv_paged_select(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages.rows, p.n_q_heads), T,
-                                   sink, recent, sel.ref, at, n, _stream(stream)), "akv_paged_select")
+    ws, at, n = _workspace(ws, lambda: akv_paged_select_workspace_size(p, pages, T), pages, stream)
+    _check(L.akv_paged_select(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads), T, sink, recent,
+                              sel.ref, at, n, _stream(stream, pages)), "akv_paged_select")
 
 
 def _pair(src, dst, device):
@@ -279,13 +293,13 @@ def _pair(src, dst, device):
 def akv_pages_copy(p: PagedParams, pages: Pages, src, dst, stream=None):
     """Copies page src[i] to page dst[i] in every layer (CUDA int32)."""
     a, b, n = _pair(src, dst, pages.device)
-    _check(_lib().akv_pages_copy(_params(p, pages), pages.ref, a, b, n, _stream(stream)), "akv_pages_copy")
+    _check(_lib().akv_pages_copy(_params(p, pages), pages.ref, a, b, n, _stream(stream, pages)), "akv_pages_copy")
 
 
 def akv_pages_fork(p: PagedParams, pages: Pages, src, dst, stream=None):
     """Row dst[i] becomes a second holder of row src[i]'s pages (CUDA int32)."""
     a, b, n = _pair(src, dst, pages.device)
-    _check(_lib().akv_pages_fork(_params(p, pages), pages.ref, a, b, n, _stream(stream)), "akv_pages_fork")
+    _check(_lib().akv_pages_fork(_params(p, pages), pages.ref, a, b, n, _stream(stream, pages)), "akv_pages_fork")
 
 
 def akv_pages_workspace_size(pages: Pages) -> int:
@@ -296,19 +310,19 @@ def akv_pages_workspace_size(pages: Pages) -> int:
 
 def akv_pages_reserve(p: PagedParams, pages: Pages, n_new, missing, ws=None, stream=None):
     """Pages for each row's next n_new tokens (CUDA int32 [rows]); missing: CUDA int32 [1]."""
-    ws, at, n = _workspace(ws, lambda: akv_pages_workspace_size(pages), pages.device, stream)
+    ws, at, n = _workspace(ws, lambda: akv_pages_workspace_size(pages), pages, stream)
     _check(_lib().akv_pages_reserve(_params(p, pages), pages.ref, _ints(n_new, "n_new", pages.rows, pages.device),
-                                    _ints(missing, "missing", 1, pages.device), at, n, _stream(stream)), "akv_pages_reserve")
+                                    _ints(missing, "missing", 1, pages.device), at, n, _stream(stream, pages)), "akv_pages_reserve")
 
 
 def akv_pages_free(p: PagedParams, pages: Pages, rows, stream=None):
     """Rows (CUDA int32) give up their pages."""
     _check(_lib().akv_pages_free(_params(p, pages), pages.ref, _ints(rows, "rows", None, pages.device), rows.numel(),
-                                 _stream(stream)), "akv_pages_free")
+                                 _stream(stream, pages)), "akv_pages_free")
 
 
 def akv_pages_compact(p: PagedParams, pages: Pages, n_live, ws=None, stream=None):
     """Moves live pages to the front of the pool; n_live: CUDA int32 [1]."""
-    ws, at, n = _workspace(ws, lambda: akv_pages_workspace_size(pages), pages.device, stream)
+    ws, at, n = _workspace(ws, lambda: akv_pages_workspace_size(pages), pages, stream)
     _check(_lib().akv_pages_compact(_params(p, pages), pages.ref, _ints(n_live, "n_live", 1, pages.device), at, n,
-                                    _stream(stream)), "akv_pages_compact")
+                                    _stream(stream, pages)), "akv_pages_compact")
