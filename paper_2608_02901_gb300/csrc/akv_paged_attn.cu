@@ -12,11 +12,13 @@
 // conversion; the products are exact in fp32, and a row's scale and minimum are applied to the sums:
 //     l_i = a_i (c_i . q) + m_i sum(q),     y = sum_i (p_i a_i) c_i + sum_i p_i m_i .
 // Queries are exact in fp16 (a power of two times what was given); rotated ones are fp32 and enter as a high and a
-// low half.  The weights p_i a_i are rounded to fp16 (relative 2^-12, below the 2^-9 of a bf16 result), scaled by the
-// largest a so far so that a weight only underflows 2^-31 below the largest.  Sums, maxima and logits are fp32.
+// low half.  The weights p_i a_i are rounded to fp16 (relative 2^-12, below the 2^-9 of a bf16 result); the reference that
+// the exponents p = 2^(l - reference) are taken from follows the largest logit and the largest a so far, so that a weight
+// is at most 2^15 and only underflows 2^-31 below the largest.  Sums, maxima and logits are fp32.
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "akv_device.cuh"
 #include "akv_paged.cuh"
@@ -31,9 +33,9 @@ AKV_HD constexpr int warps_of(int nt) { return nt == 2 ? 11 : 7; }
 AKV_HD constexpr int ctas_of(int nt) { return nt == 1 ? 2 : 1; }
 constexpr int kStages = 4;
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kLow = -1e30f;                  // running maximum before any token
-constexpr float kSlack = 8.f;                   // a weight may pass its reference by 2^8 before the reference moves
-constexpr int kWeightLog = 7;                   // p a / (largest a) is held times 2^7: at most 2^15 with the slack
+constexpr float kLow = -1e30f;                  // reference of a share that saw no token
+constexpr float kSlack = 8.f;                   // a weight may pass its place by 2^8 before the reference moves
+constexpr float kWeightLog = 7.f;               // the largest weight's place: 2^7 (at most 2^15 with the slack)
 constexpr int kRowPad = kD + 4;                 // floats between rows of the joined outputs
 
 struct AttnArgs {
@@ -59,6 +61,11 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -68,6 +75,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// The larger of three (a NaN is left out).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 v;
@@ -382,6 +395,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 
     float acc[NT][8][4], sum[NT][2], mins[NT][2][NG], ref[NT][2];
     int e_s = 103;  // the values' scales so far are at most 2^(e_s - 127)
+    float most = kNegInf;  // what l - reference may be, 15 - (e_s - 127); no reference yet
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -391,7 +405,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         sum[nt][x] = 0.f;
-        ref[nt][x] = kLow;
+        ref[nt][x] = 0.f;
 #pragma unroll
         for (int g = 0; g < NG; ++g) mins[nt][x][g] = 0.f;
       }
@@ -408,7 +422,8 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       const int sub = item % kTileSubs;
       const uint32_t tile = (uint32_t)(k - r.lo) + item / kTileSubs;  // of the CTA's
       const int stage = tile % kStages;
-      if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.full[stage]), tile / kStages & 1)) {
+      const uint32_t bar = smem_u32(&S.full[stage]), parity = tile / kStages & 1;
+      if (!__all_sync(0xffffffffu, mbar_try(bar, parity)) && (warp_failed(failed) || !mbar_wait_w(bar, parity))) {
         *failed = 1;
         spoil();
         break;
@@ -441,16 +456,10 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         continue;
       }
 
-      // logits of tokens g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1 (log2 units)
+      // logits of tokens g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1 (log2 units), less the rows' references
       float l[NT][4];
       {
         float s[NT][NG][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) s[nt][g][x] = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t x0 = comp(kc[0], j), x1 = comp(kc[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
@@ -460,7 +469,10 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
             for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
               const uint4 q = NT == 1 ? qf[lo][NT == 1 ? j : 0] : S.frag[lo][nt][j][lane];
               float(&d)[4] = s[nt][NG == 2 ? j >> 1 : 0];
-              mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+              if (lo == 0 && (j == 0 || (NG == 2 && j == 2)))
+                mma_16816_first(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+              else
+                mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
               mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
             }
         }
@@ -476,7 +488,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            float y = km[x >> 1][0] * qs[nt][x & 1][0];
+            float y = fmaf(km[x >> 1][0], qs[nt][x & 1][0], -ref[nt][x & 1]);
             if (NG == 2) y = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], y);
             y = fmaf(ks[x >> 1][0], s[nt][0][x], y);
             if (NG == 2) y = fmaf(ks[x >> 1][NG - 1], s[nt][NG - 1][x], y);
@@ -513,22 +525,18 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       }
 
       // references move only where a weight would pass its room
-      bool move = false;
+      float top_s = fmaxf(vs[0][0], vs[1][0]);  // (a NaN is left out)
+      if (NG == 2) top_s = max3(top_s, vs[0][NG - 1], vs[1][NG - 1]);
+      float top_l = kNegInf;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) move = move || l[nt][x] > ref[nt][x & 1] + kSlack;
-      const float s_most = __int_as_float(e_s << 23);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) move = move || vs[x][g] > s_most;
-      if (__any_sync(0xffffffffu, move)) {
-        float top = fmaxf(vs[0][0], vs[1][0]);  // (a NaN is left out)
-        if (NG == 2) top = fmaxf(top, fmaxf(vs[0][NG - 1], vs[1][NG - 1]));
-        const int e_new = max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top, 0.f))) >> 23) + 1);
-        const float shrink = e_new == e_s ? 1.f : __int_as_float(max(127 + e_s - e_new, 0) << 23);
-        e_s = min(e_new, 255);
+      for (int nt = 0; nt < NT; ++nt) top_l = max3(max3(l[nt][0], l[nt][1], l[nt][2]), l[nt][3], top_l);
+      if (__any_sync(0xffffffffu, top_l > most || top_s > __int_as_float(e_s << 23))) {
+        const int e_new = min(max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top_s, 0.f))) >> 23) + 1), 254);
+        // (a row that sees none of its warp's first tokens sees none of the later ones: it keeps its reference)
+        const bool first = most == kNegInf;
+        const float place_was = first ? kNegInf : kWeightLog - (float)(e_s - 127), place = kWeightLog - (float)(e_new - 127);
+        e_s = e_new;
+        most = kSlack + place;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -537,48 +545,52 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-            m = fmaxf(m, ref[nt][x]);
-            const float f = exp2_fast(ref[nt][x] - m);
-            ref[nt][x] = m;
+            // the largest logit so far goes to the new place
+            float up = fmaxf(m, place_was) - place;
+            if (up == kNegInf) up = 0.f;
+            ref[nt][x] += up;
+            l[nt][x] -= up;
+            l[nt][x + 2] -= up;
+            const float f = first ? 0.f : exp2_fast(-up);
             sum[nt][x] *= f;
 #pragma unroll
             for (int g = 0; g < NG; ++g) mins[nt][x][g] *= f;
 #pragma unroll
             for (int mt = 0; mt < 8; ++mt) {
-              acc[nt][mt][x] *= f * shrink;
-              acc[nt][mt][x + 2] *= f * shrink;
+              acc[nt][mt][x] *= f;
+              acc[nt][mt][x + 2] *= f;
             }
           }
       }
-      const float wf = __int_as_float((254 + kWeightLog - e_s) << 23);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) vs[x][g] *= wf;
 
       uint32_t w0[NT][NG], w1[NT][NG];
+      auto weigh = [&](auto edge_) {
+        constexpr bool kEdge = decltype(edge_)::value;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          p[x] = exp2_fast(l[nt][x] - ref[nt][x & 1]);
-          sum[nt][x & 1] += p[x];
-        }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          float u[4];
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            u[x] = p[x] * vs[x >> 1][g];
-            float m = vm[x >> 1][g];
-            if (edge && l[nt][x] == kNegInf) u[x] = m = 0.f;  // a NaN that this row does not see
-            mins[nt][x & 1][g] = fmaf(p[x], m, mins[nt][x & 1][g]);
+            p[x] = exp2_fast(l[nt][x]);
+            sum[nt][x & 1] += p[x];
           }
-          w0[nt][g] = transpose_8x8(half2_bits(u[0], u[1]));
-          w1[nt][g] = transpose_8x8(half2_bits(u[2], u[3]));
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            float u[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              u[x] = p[x] * vs[x >> 1][g];
+              float m = vm[x >> 1][g];
+              if (kEdge && l[nt][x] == kNegInf) u[x] = m = 0.f;  // a NaN that this row does not see
+              mins[nt][x & 1][g] = fmaf(p[x], m, mins[nt][x & 1][g]);
+            }
+            w0[nt][g] = transpose_8x8(half2_bits(u[0], u[1]));
+            w1[nt][g] = transpose_8x8(half2_bits(u[2], u[3]));
+          }
         }
-      }
+      };
+      if (edge) weigh(std::true_type{});
+      else weigh(std::false_type{});
       // outputs: rows of the product are dimensions 64 s + 8 g8 + 4 u + n of word 2 s + u
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -596,8 +608,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 
     // ---- the unit's end, or the range's: the warps' outputs are joined
     {
-      const int e_out = 24 - kWeightLog + e_s - 127;
-      const float down = pow2(max(e_out, -126)), down16 = down * 0.0625f;
+      const float down = 16777216.f, down16 = 1048576.f;  // codes count 2^-24, odd ones 2^-20
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -612,7 +623,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
             for (int sh = 4; sh < 32; sh *= 2) m[g] += __shfl_xor_sync(0xffffffffu, m[g], sh);
           }
           const int row = 8 * nt + 2 * t4 + x;
-          if (g8 == 0) S.red_m[warp][row] = ref[nt][x], S.red_l[warp][row] = s;
+          if (g8 == 0) S.red_m[warp][row] = s == 0.f ? kLow : ref[nt][x], S.red_l[warp][row] = s;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float add = m[NG == 2 ? j >> 1 : 0];
