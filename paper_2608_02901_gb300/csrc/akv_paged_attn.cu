@@ -31,6 +31,8 @@ constexpr int kTileTokens = 128, kTileSubs = kTileTokens / kSubTokens;
 // has room for 16 warps of 128, 12 of 168 or 8 of 255 (a 17th of 96 spills).  Two CTAs per SM of the smallest.
 AKV_HD constexpr int warps_of(int nt) { return nt == 2 ? 11 : 7; }
 AKV_HD constexpr int ctas_of(int nt) { return nt == 1 ? 2 : 1; }
+// Sub-blocks that a warp takes at a time: two where the registers allow it, whose products then overlap.
+AKV_HD constexpr int subs_of(int nt) { return nt == 1 ? 2 : 1; }
 constexpr int kStages = 4;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -1e30f;                  // reference of a share that saw no token
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   extern __shared__ __align__(128) uint8_t smem_raw[];
   Smem<NT>& S = *reinterpret_cast<Smem<NT>*>(smem_raw);
   constexpr uint32_t kSub = 2048 + 128 * NG;
-  constexpr int kRows = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1);
+  constexpr int kRows = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1), NS = subs_of(NT);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedView& v = a.v;
 
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&S.full[s]), 1);
-      mbar_init(smem_u32(&S.empty[s]), kTileSubs);
+      mbar_init(smem_u32(&S.empty[s]), kTileSubs / NS);
     }
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -378,13 +380,6 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     }
     named_sync(kConsumerBar, 32 * kWarps);
     const float dot_scale = a.scale * pow2(10 + e_q);  // codes count 2^-24, queries 2^(14 - e)
-    uint4 qf[HILO ? 2 : 1][NT == 1 ? 4 : 1];
-    if (NT == 1) {
-#pragma unroll
-      for (int lo = 0; lo < (HILO ? 2 : 1); ++lo)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) qf[lo][NT == 1 ? j : 0] = S.frag[lo][0][j][lane];
-    }
     float qs[NT][2][NG];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -418,9 +413,9 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = __int_as_float(0x7fffffff);
     };
 
-    for (int item = warp; item < n_tiles * kTileSubs; item += kWarps) {
-      const int sub = item % kTileSubs;
-      const uint32_t tile = (uint32_t)(k - r.lo) + item / kTileSubs;  // of the CTA's
+    for (int item = warp; item < n_tiles * (kTileSubs / NS); item += kWarps) {
+      const int sub = item % (kTileSubs / NS) * NS;
+      const uint32_t tile = (uint32_t)(k - r.lo) + item / (kTileSubs / NS);  // of the CTA's
       const int stage = tile % kStages;
       const uint32_t bar = smem_u32(&S.full[stage]), parity = tile / kStages & 1;
       if (!__all_sync(0xffffffffu, mbar_try(bar, parity)) && (warp_failed(failed) || !mbar_wait_w(bar, parity))) {
@@ -428,110 +423,130 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         spoil();
         break;
       }
-      const int pos = S.pos[stage][sub];
-      uint4 kc[2], vc[2];
-      uint32_t kw[2][NG], vw[2][NG];
-      if (pos >= 0) {
-        const uint32_t sb = smem_u32(&S.stage[stage][sub * kSub]) + 16 * lane;
-        kc[0] = lds128(sb);
-        kc[1] = lds128(sb + 512);
-        vc[0] = lds128(sb + 1024);
-        vc[1] = lds128(sb + 1536);
-        const uint8_t* meta = &S.stage[stage][sub * kSub + 2048];
+      int pos[NS];
+      bool none = true, edge = false, outside = false;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (NG == 2) {
-            const uint4 w = *(const uint4*)(meta + 16 * (g8 + 8 * x));
-            kw[x][0] = w.x, kw[x][NG - 1] = w.y, vw[x][0] = w.z, vw[x][NG - 1] = w.w;
-          } else {
-            const uint2 w = *(const uint2*)(meta + 8 * (g8 + 8 * x));
-            kw[x][0] = w.x, vw[x][0] = w.y;
-          }
-        }
+      for (int i = 0; i < NS; ++i) {
+        pos[i] = S.pos[stage][sub + i];
+        outside = outside || pos[i] == -2;
+        none = none && pos[i] < 0;
+        if (pos[i] < 0) pos[i] = 1 << 30;  // (nobody sees its tokens)
+        edge = edge || pos[i] + kSubTokens > all_see;
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&S.empty[stage]));  // what is needed is in registers
-      if (pos < 0) {
-        if (pos == -2) spoil();
+      if (outside) spoil();
+      if (none) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.empty[stage]));
         continue;
       }
+      const uint32_t sb = smem_u32(&S.stage[stage][sub * kSub]);
 
       // logits of tokens g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1 (log2 units), less the rows' references
-      float l[NT][4];
+      float l[NS][NT][4];
+      float vs[NS][2][NG], vm[NS][2][NG];
       {
-        float s[NT][NG][4];
+        uint4 kc[NS][2];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          kc[i][0] = lds128(sb + i * kSub + 16 * lane);
+          kc[i][1] = lds128(sb + i * kSub + 512 + 16 * lane);
+        }
+        float s[NS][NT][NG][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t x0 = comp(kc[0], j), x1 = comp(kc[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
-              const uint4 q = NT == 1 ? qf[lo][NT == 1 ? j : 0] : S.frag[lo][nt][j][lane];
-              float(&d)[4] = s[nt][NG == 2 ? j >> 1 : 0];
-              if (lo == 0 && (j == 0 || (NG == 2 && j == 2)))
-                mma_16816_first(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
-              else
-                mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
-              mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
+              const uint4 q = S.frag[lo][nt][j][lane];
+#pragma unroll
+              for (int i = 0; i < NS; ++i) {
+                const uint32_t x0 = comp(kc[i][0], j), x1 = comp(kc[i][1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+                float(&d)[4] = s[i][nt][NG == 2 ? j >> 1 : 0];
+                if (lo == 0 && (j == 0 || (NG == 2 && j == 2)))
+                  mma_16816_first(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+                else
+                  mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+                mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
+              }
             }
         }
-        float ks[2][NG], km[2][NG];
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int i = 0; i < NS; ++i) {
+          float ks[2][NG], km[2][NG];
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            ks[x][g] = word_scale(kw[x][g]) * dot_scale;
-            km[x][g] = word_min(kw[x][g]);
+          for (int x = 0; x < 2; ++x) {
+            uint32_t kw[NG], vw[NG];
+            const uint8_t* meta = &S.stage[stage][(sub + i) * kSub + 2048];
+            if (NG == 2) {
+              const uint4 w = *(const uint4*)(meta + 16 * (g8 + 8 * x));
+              kw[0] = w.x, kw[NG - 1] = w.y, vw[0] = w.z, vw[NG - 1] = w.w;
+            } else {
+              const uint2 w = *(const uint2*)(meta + 8 * (g8 + 8 * x));
+              kw[0] = w.x, vw[0] = w.y;
+            }
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              ks[x][g] = word_scale(kw[g]) * dot_scale;
+              km[x][g] = word_min(kw[g]);
+              vs[i][x][g] = word_scale(vw[g]);
+              vm[i][x][g] = word_min(vw[g]);
+            }
           }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float y = fmaf(km[x >> 1][0], qs[nt][x & 1][0], -ref[nt][x & 1]);
-            if (NG == 2) y = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], y);
-            y = fmaf(ks[x >> 1][0], s[nt][0][x], y);
-            if (NG == 2) y = fmaf(ks[x >> 1][NG - 1], s[nt][NG - 1][x], y);
-            l[nt][x] = y;
-          }
-      }
-      float vs[2][NG], vm[2][NG];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          vs[x][g] = word_scale(vw[x][g]);
-          vm[x][g] = word_min(vw[x][g]);
+            for (int x = 0; x < 4; ++x) {
+              float y = fmaf(km[x >> 1][0], qs[nt][x & 1][0], -ref[nt][x & 1]);
+              if (NG == 2) y = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], y);
+              y = fmaf(ks[x >> 1][0], s[i][nt][0][x], y);
+              if (NG == 2) y = fmaf(ks[x >> 1][NG - 1], s[i][nt][NG - 1][x], y);
+              l[i][nt][x] = y;
+            }
         }
-      const bool edge = pos + kSubTokens > all_see;
+      }
+      uint4 vc[NS][2];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        vc[i][0] = lds128(sb + i * kSub + 1024 + 16 * lane);
+        vc[i][1] = lds128(sb + i * kSub + 1536 + 16 * lane);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&S.empty[stage]));  // what is needed is in registers
       if (edge) {  // tokens past the request, and those that a draft's earlier rows do not see
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const bool held = pos + g8 + 8 * x < c.g.sees;
+        for (int i = 0; i < NS; ++i) {
 #pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            vs[x][g] = held ? vs[x][g] : 0.f;
-            vm[x][g] = held ? vm[x][g] : 0.f;
+          for (int x = 0; x < 2; ++x) {
+            const bool held = pos[i] + g8 + 8 * x < c.g.sees;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              vs[i][x][g] = held ? vs[i][x][g] : 0.f;
+              vm[i][x][g] = held ? vm[i][x][g] : 0.f;
+            }
           }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int row = row0 + 8 * nt + 2 * t4 + (x & 1);
+              const int sees = SEL ? c.g.sees : min(c.g.sees, all_see + row / v.G);
+              if (pos[i] + g8 + 8 * (x >> 1) >= sees) l[i][nt][x] = kNegInf;
+            }
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int row = row0 + 8 * nt + 2 * t4 + (x & 1);
-            const int sees = SEL ? c.g.sees : min(c.g.sees, all_see + row / v.G);
-            if (pos + g8 + 8 * (x >> 1) >= sees) l[nt][x] = kNegInf;
-          }
       }
 
       // references move only where a weight would pass its room
-      float top_s = fmaxf(vs[0][0], vs[1][0]);  // (a NaN is left out)
-      if (NG == 2) top_s = max3(top_s, vs[0][NG - 1], vs[1][NG - 1]);
-      float top_l = kNegInf;
+      float top_s = 0.f, top_l = kNegInf;  // (a NaN is left out)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) top_l = max3(max3(l[nt][0], l[nt][1], l[nt][2]), l[nt][3], top_l);
+      for (int i = 0; i < NS; ++i) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) top_s = max3(top_s, vs[i][0][g], vs[i][1][g]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) top_l = max3(max3(l[i][nt][0], l[i][nt][1], l[i][nt][2]), l[i][nt][3], top_l);
+      }
       if (__any_sync(0xffffffffu, top_l > most || top_s > __int_as_float(e_s << 23))) {
-        const int e_new = min(max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(fmaxf(top_s, 0.f))) >> 23) + 1), 254);
+        const int e_new = min(max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top_s)) >> 23) + 1), 254);
         // (a row that sees none of its warp's first tokens sees none of the later ones: it keeps its reference)
         const bool first = most == kNegInf;
         const float place_was = first ? kNegInf : kWeightLog - (float)(e_s - 127), place = kWeightLog - (float)(e_new - 127);
@@ -541,7 +556,8 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            float m = fmaxf(l[nt][x], l[nt][x + 2]);
+            float m = fmaxf(l[0][nt][x], l[0][nt][x + 2]);
+            if (NS == 2) m = max3(m, l[NS - 1][nt][x], l[NS - 1][nt][x + 2]);
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -549,8 +565,11 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
             float up = fmaxf(m, place_was) - place;
             if (up == kNegInf) up = 0.f;
             ref[nt][x] += up;
-            l[nt][x] -= up;
-            l[nt][x + 2] -= up;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+              l[i][nt][x] -= up;
+              l[i][nt][x + 2] -= up;
+            }
             const float f = first ? 0.f : exp2_fast(-up);
             sum[nt][x] *= f;
 #pragma unroll
@@ -563,45 +582,48 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
           }
       }
 
-      uint32_t w0[NT][NG], w1[NT][NG];
-      auto weigh = [&](auto edge_) {
-        constexpr bool kEdge = decltype(edge_)::value;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float p[4];
+      for (int i = 0; i < NS; ++i) {
+        uint32_t w0[NT][NG], w1[NT][NG];
+        auto weigh = [&](auto edge_) {
+          constexpr bool kEdge = decltype(edge_)::value;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            p[x] = exp2_fast(l[nt][x]);
-            sum[nt][x & 1] += p[x];
-          }
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            float u[4];
+          for (int nt = 0; nt < NT; ++nt) {
+            float p[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              u[x] = p[x] * vs[x >> 1][g];
-              float m = vm[x >> 1][g];
-              if (kEdge && l[nt][x] == kNegInf) u[x] = m = 0.f;  // a NaN that this row does not see
-              mins[nt][x & 1][g] = fmaf(p[x], m, mins[nt][x & 1][g]);
+              p[x] = exp2_fast(l[i][nt][x]);
+              sum[nt][x & 1] += p[x];
             }
-            w0[nt][g] = transpose_8x8(half2_bits(u[0], u[1]));
-            w1[nt][g] = transpose_8x8(half2_bits(u[2], u[3]));
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              float u[4];
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                u[x] = p[x] * vs[i][x >> 1][g];
+                float m = vm[i][x >> 1][g];
+                if (kEdge && l[i][nt][x] == kNegInf) u[x] = m = 0.f;  // a NaN that this row does not see
+                mins[nt][x & 1][g] = fmaf(p[x], m, mins[nt][x & 1][g]);
+              }
+              w0[nt][g] = transpose_8x8(half2_bits(u[0], u[1]));
+              w1[nt][g] = transpose_8x8(half2_bits(u[2], u[3]));
+            }
           }
-        }
-      };
-      if (edge) weigh(std::true_type{});
-      else weigh(std::false_type{});
-      // outputs: rows of the product are dimensions 64 s + 8 g8 + 4 u + n of word 2 s + u
+        };
+        if (edge) weigh(std::true_type{});
+        else weigh(std::false_type{});
+        // outputs: rows of the product are dimensions 64 s + 8 g8 + 4 u + n of word 2 s + u
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t x0 = comp(vc[0], j), x1 = comp(vc[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
-        constexpr int kShift = NG == 2 ? 1 : 2;
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t x0 = comp(vc[i][0], j), x1 = comp(vc[i][1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+          constexpr int kShift = NG == 2 ? 1 : 2;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          mma_16816(acc[nt][2 * j], x0 & 0x000f000fu, y0 & 0x000f000fu, x1 & 0x000f000fu, y1 & 0x000f000fu, w0[nt][j >> kShift],
-                    w1[nt][j >> kShift]);
-          mma_16816(acc[nt][2 * j + 1], x0 & 0x00f000f0u, y0 & 0x00f000f0u, x1 & 0x00f000f0u, y1 & 0x00f000f0u, w0[nt][j >> kShift],
-                    w1[nt][j >> kShift]);
+          for (int nt = 0; nt < NT; ++nt) {
+            mma_16816(acc[nt][2 * j], x0 & 0x000f000fu, y0 & 0x000f000fu, x1 & 0x000f000fu, y1 & 0x000f000fu, w0[nt][j >> kShift],
+                      w1[nt][j >> kShift]);
+            mma_16816(acc[nt][2 * j + 1], x0 & 0x00f000f0u, y0 & 0x00f000f0u, x1 & 0x00f000f0u, y1 & 0x00f000f0u, w0[nt][j >> kShift],
+                      w1[nt][j >> kShift]);
+          }
         }
       }
     }
