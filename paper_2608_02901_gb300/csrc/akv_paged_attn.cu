@@ -250,32 +250,43 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     const int per_page = min(kTileSubs, 1 << (v.page_log - 4));
     int stage = 0;
     uint32_t phase = 1;  // the first pass over the ring waits for nobody
-    auto look = [&](int& pos, int& page) {
-      pos = -1;
-      page = -1;
-      if (lane >= kTileSubs) return;
+    // The page numbers of the next kAhead tiles are under way while a tile waits for its stage (nothing looks at them
+    // before their turn).
+    constexpr int kAhead = 3;
+    struct Look {
+      int at, page, h;  // first token of the lane's sub-block, -1: none; its page as the table says; the tile's head
+    };
+    auto look = [&]() {
+      Look r{-1, -1, SEL ? c.g.h : c.index / a.n_blocks};
       const int i = c.ti * kTileTokens + lane * kSubTokens;
-      if (i >= c.g.tokens) return;
+      if (lane >= kTileSubs || i >= c.g.tokens) return r;
       int j = i >> v.page_log;
       if (SEL) {
         j = a.sel[(int64_t)c.gi * a.top + j];
-        if ((uint32_t)j >= (uint32_t)v.max_pages) return;
+        if ((uint32_t)j >= (uint32_t)v.max_pages) return r;
       }
       const int at = (j << v.page_log) + (i & ((1 << v.page_log) - 1));
-      if (at >= c.g.sees) return;
-      page = page_of(v, c.g.b, j);
-      pos = page < 0 ? -2 : at;
+      if (at >= c.g.sees) return r;
+      r.at = at;
+      r.page = v.table[(int64_t)c.g.b * v.table_stride + j];
+      return r;
     };
-    auto head = [&]() { return SEL ? c.g.h : c.index / a.n_blocks; };
-    int pos, page, h = head();
-    look(pos, page);
+    Look ahead[kAhead];
+    int64_t looked = r.lo;
+    auto look_next = [&]() {
+      if (looked >= r.hi) return Look{-1, -1, 0};
+      if (looked++ > r.lo && ++c.ti == c.tiles) c.next_unit(a);
+      return look();
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ahead[i] = look_next();
     for (int64_t k = r.lo; k < r.hi; ++k) {
-      const int pos0 = pos, page0 = page, h0 = h;
-      if (k + 1 < r.hi) {  // the next tile's pages are looked up while this one waits for its stage
-        if (++c.ti == c.tiles) c.next_unit(a);
-        h = head();
-        look(pos, page);
-      }
+      const Look now = ahead[0];
+#pragma unroll
+      for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+      ahead[kAhead - 1] = look_next();
+      const int page0 = now.page, h0 = now.h;
+      const int pos0 = now.at < 0 ? -1 : (uint32_t)page0 < (uint32_t)v.n_pages ? now.at : -2;
       if (!mbar_wait_w(smem_u32(&S.empty[stage]), phase)) {
         if (lane == 0) *failed = 1;
         return;
