@@ -250,41 +250,57 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     const int per_page = min(kTileSubs, 1 << (v.page_log - 4));
     int stage = 0;
     uint32_t phase = 1;  // the first pass over the ring waits for nobody
-    // The page numbers of the next kAhead tiles are under way while a tile waits for its stage (nothing looks at them
-    // before their turn).
+    // What the next tiles need is under way while a tile waits for its stage, and nothing looks at it before its turn:
+    // the table's page numbers kAhead tiles before, with a selection its entries as much earlier.
     constexpr int kAhead = 3;
+    struct Place {
+      int j, off, b, h, sees;  // the lane's sub-block: table position (-1: none), first token in its page; request, head
+    };
     struct Look {
-      int at, page, h;  // first token of the lane's sub-block, -1: none; its page as the table says; the tile's head
+      int at, page, h;  // first token, -1: none; its page as the table says; head
     };
-    auto look = [&]() {
-      Look r{-1, -1, SEL ? c.g.h : c.index / a.n_blocks};
-      const int i = c.ti * kTileTokens + lane * kSubTokens;
-      if (lane >= kTileSubs || i >= c.g.tokens) return r;
-      int j = i >> v.page_log;
-      if (SEL) {
-        j = a.sel[(int64_t)c.gi * a.top + j];
-        if ((uint32_t)j >= (uint32_t)v.max_pages) return r;
-      }
-      const int at = (j << v.page_log) + (i & ((1 << v.page_log) - 1));
-      if (at >= c.g.sees) return r;
-      r.at = at;
-      r.page = v.table[(int64_t)c.g.b * v.table_stride + j];
-      return r;
-    };
-    Look ahead[kAhead];
     int64_t looked = r.lo;
-    auto look_next = [&]() {
-      if (looked >= r.hi) return Look{-1, -1, 0};
+    auto next_place = [&]() {
+      Place p{-1, 0, 0, 0, 0};
+      if (looked >= r.hi) return p;
       if (looked++ > r.lo && ++c.ti == c.tiles) c.next_unit(a);
-      return look();
+      const int i = c.ti * kTileTokens + lane * kSubTokens;
+      p.b = c.g.b, p.h = SEL ? c.g.h : c.index / a.n_blocks, p.sees = c.g.sees;
+      if (lane >= kTileSubs || i >= c.g.tokens) return p;
+      p.off = i & ((1 << v.page_log) - 1);
+      p.j = SEL ? a.sel[(int64_t)c.gi * a.top + (i >> v.page_log)] : i >> v.page_log;
+      return p;
+    };
+    auto look = [&](const Place& p) {
+      Look l{-1, -1, p.h};
+      if ((uint32_t)p.j >= (uint32_t)v.max_pages) return l;
+      const int at = (p.j << v.page_log) + p.off;
+      if (at >= p.sees) return l;
+      l.at = at;
+      l.page = v.table[(int64_t)p.b * v.table_stride + p.j];
+      return l;
+    };
+    Place places[kAhead];
+    Look looks[kAhead];
+    if (SEL) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) places[i] = next_place();
+    }
+    auto look_next = [&]() {
+      if (!SEL) return look(next_place());
+      const Look l = look(places[0]);
+#pragma unroll
+      for (int i = 0; i + 1 < kAhead; ++i) places[i] = places[i + 1];
+      places[kAhead - 1] = next_place();
+      return l;
     };
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) ahead[i] = look_next();
+    for (int i = 0; i < kAhead; ++i) looks[i] = look_next();
     for (int64_t k = r.lo; k < r.hi; ++k) {
-      const Look now = ahead[0];
+      const Look now = looks[0];
 #pragma unroll
-      for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
-      ahead[kAhead - 1] = look_next();
+      for (int i = 0; i + 1 < kAhead; ++i) looks[i] = looks[i + 1];
+      looks[kAhead - 1] = look_next();
       const int page0 = now.page, h0 = now.h;
       const int pos0 = now.at < 0 ? -1 : (uint32_t)page0 < (uint32_t)v.n_pages ? now.at : -2;
       if (!mbar_wait_w(smem_u32(&S.empty[stage]), phase)) {

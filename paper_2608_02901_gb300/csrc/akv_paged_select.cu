@@ -1,9 +1,11 @@
 // Choice of the pages that a query attends: a score per page in whole numbers, then the best of them.
 //
-// The score reads the pages' bounds once (512 bytes a page and head) and does 2 G x 128 multiply-adds on them, in bytes:
-// with a query row split into its positive and its negative part, the larger of q lo and q hi in each dimension is
-// q+ hi + q- lo, two four-way byte products.  Whole numbers make the sums exact in any order, so that the choice is the
-// same on every machine.  The choice itself finds the key of the last page kept bit by bit.
+// The score reads the pages' bounds once (512 bytes a page and head) and does 2 G x 128 multiply-adds on them: with a
+// query row split into its positive and its negative part, the larger of q lo and q hi in each dimension is
+// q+ hi + q- lo, two products.  The numbers are at most 127, exact in bf16, and the sums at most 2^22, exact in fp32: the
+// tensor cores add them up without rounding, in any order, so that the choice is the same on every machine.  What costs
+// is turning the bounds into whole numbers (2 x 128 a page and head, two or three operations each); a warp does it once
+// for up to 8 query rows.  The choice itself finds the key of the last page kept, 8 bits of its range a pass.
 #include "akv_paged.cuh"
 
 namespace akv {
@@ -19,149 +21,146 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kScoreThreads = 128;
-constexpr int kPageLanes = 8;                               // lanes of a page: dimensions 8 u .. and 64 + 8 u ..
-constexpr int kAtOnce = kScoreThreads / kPageLanes;         // pages of a CTA at a time
-constexpr int kRowsAtOnce = 8;                              // query rows whose sums are reduced together
+constexpr int kScoreThreads = 128, kScoreWarps = kScoreThreads / 32;
+constexpr int kWarpPages = 16;                          // pages of a warp at a time: the rows of its products
+constexpr int kAtOnce = kWarpPages * kScoreWarps;
+constexpr int kSteps = 16;                              // products over 16 dimensions: 8 of the largest, 8 of the smallest
 
 template <bool HALF>
 __device__ __forceinline__ float value(uint32_t w, int hi) {
   if (HALF) return __half2float(__ushort_as_half((unsigned short)(hi ? w >> 16 : w)));
   return __uint_as_float(hi ? w & 0xffff0000u : w << 16);
 }
-
-// Four values of two words times `unit` -> whole numbers in bytes (clamped to +-127 where `clamp`).
+// The pair of larger magnitudes (a NaN is passed on; the signs mean nothing).
 template <bool HALF>
-__device__ __forceinline__ uint32_t whole4(uint32_t w0, uint32_t w1, float unit, bool clamp) {
-  float t[4] = {value<HALF>(w0, 0) * unit, value<HALF>(w0, 1) * unit, value<HALF>(w1, 0) * unit, value<HALF>(w1, 1) * unit};
-  uint32_t b[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (clamp) t[i] = fminf(fmaxf(t[i], -127.f), 127.f);
-    b[i] = __float_as_uint(t[i] + 12582912.f);  // 1.5 2^23: the rounded number in the low bits
-  }
-  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (HALF) asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Two values times `unit` as whole numbers (clamped to +-127 where `clamp`), in bf16.
+template <bool HALF>
+__device__ __forceinline__ uint32_t whole2(uint32_t w, float unit, bool clamp) {
+  float a = value<HALF>(w, 0), b = value<HALF>(w, 1);
+  asm("{ .reg .b64 p, u, m, n;\n"
+      "  mov.b64 p, {%0, %1}; mov.b64 u, {%2, %2}; mov.b64 m, {%3, %3}; mov.b64 n, {%4, %4};\n"
+      "  fma.rn.f32x2 p, p, u, m; add.rn.f32x2 p, p, n; mov.b64 {%0, %1}, p; }"
+      : "+f"(a), "+f"(b)
+      : "f"(unit), "f"(12582912.f), "f"(-12582912.f));  // 1.5 2^23: rounds to nearest even
+  if (clamp) a = fminf(fmaxf(a, -127.f), 127.f), b = fminf(fmaxf(b, -127.f), 127.f);
+  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
 }
 
 template <bool HALF>
-__global__ void __launch_bounds__(kScoreThreads) akv_paged_score_kernel(PagedView v, const uint16_t* q, int64_t qb, int64_t qt,
-                                                                        int64_t qh, int T, int chunks, int per_cta, uint32_t* keys) {
+__global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(PagedView v, const uint16_t* q, int64_t qb, int64_t qt,
+                                                                           int64_t qh, int T, int chunks, int per_cta, uint32_t* keys) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  extern __shared__ __align__(16) uint32_t q_words[];  // [rows to a multiple of 8][8 lanes][4 positive, 4 negative]
-  __shared__ float q_max[kScoreThreads / 32];
+  extern __shared__ __align__(16) uint2 q_frag[];  // [blocks of 8 rows][kSteps][32 lanes]
+  __shared__ float q_max[kScoreWarps];
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
   const int h = unit % v.H, t = unit / v.H % T, b = unit / v.H / T;
-  const int P = 1 << v.page_log, tid = threadIdx.x, lane = tid & 31, u = tid & 7;
+  const int P = 1 << v.page_log, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g8 = lane >> 2, t4 = lane & 3;
   const int sees = max(0, held_tokens(v, b) - T + 1 + t), n = (sees + P - 1) >> v.page_log;
   const int j0 = chunk * per_cta, j1 = min(n, j0 + per_cta);
   if (j0 >= j1) return;
   const uint32_t bounds_at = (uint32_t)(P >> 4) * sub_bytes(v.ng);
-  struct Bounds {
-    uint4 lo0, lo1, hi0, hi1;
-    bool there;
-  };
-  auto load = [&](int j) {
-    Bounds x;
-    x.lo0 = x.lo1 = x.hi0 = x.hi1 = make_uint4(0, 0, 0, 0);
-    const int page = j < j1 ? page_of(v, b, j) : -1;
-    x.there = page >= 0;
-    if (x.there) {
-      const uint4* at = (const uint4*)(block_of(v, page, h) + bounds_at) + u;
-      x.lo0 = at[0], x.lo1 = at[8], x.hi0 = at[16], x.hi1 = at[24];
-    }
-    return x;
-  };
-  Bounds next = load(j0 + tid / kPageLanes);
+  // this lane's pages: g8 and g8 + 8 of the warp's sixteen
+  auto find = [&](int j) { return j < j1 ? v.table[(int64_t)b * v.table_stride + j] : -1; };
+  int j = j0 + kWarpPages * warp + g8;
+  int page[2] = {find(j), find(j + 8)};
 
-  // the query rows as bytes
+  // the query rows as whole numbers
   const uint16_t* rows = q + b * qb + t * qt + (int64_t)h * v.G * qh;
   float top = 0.f;
   for (int i = tid; i < v.G * kD; i += kScoreThreads) top = max_nan(top, fabsf(row_to_float(rows[(int64_t)(i >> 7) * qh + (i & 127)], HALF)));
   for (int k = 16; k; k >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, k));
-  if (lane == 0) q_max[tid >> 5] = top;
+  if (lane == 0) q_max[warp] = top;
   __syncthreads();
   top = max_nan(max_nan(q_max[0], q_max[1]), max_nan(q_max[2], q_max[3]));
   const bool fine = top <= 3.402823466e38f;
   const float unit_q = power(7 - exponent_of(fine ? top : 0.f));
-  const int padded = (v.G + kRowsAtOnce - 1) / kRowsAtOnce * kRowsAtOnce;
-  for (int i = tid; i < padded * 32; i += kScoreThreads) {  // word: dimensions 4 k .. of a row
-    const int g = i >> 5, k = i & 31;
-    uint32_t pos = 0, neg = 0;
-    if (g < v.G && fine) {
+  const int blocks = (v.G + 7) / 8;
+  for (int i = tid; i < blocks * 8 * 32; i += kScoreThreads) {
+    // steps s (the largest) and s + 8 (the smallest): chunk t4 + 4 (s / 2) of 8 dimensions, its half s % 2
+    const int l = i & 31, s = i >> 5 & 7, row = i / 256 * 8 + (l >> 2);
+    uint32_t pos[2] = {0, 0}, neg[2] = {0, 0};
+    if (row < v.G && fine) {
+      const uint16_t* x = rows + row * qh + 8 * ((l & 3) + 4 * (s >> 1)) + 4 * (s & 1);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int x = min(max(__float2int_rn(row_to_float(rows[g * qh + 4 * k + e], HALF) * unit_q), -127), 127);
-        pos |= (uint32_t)(max(x, 0) & 255) << 8 * e;
-        neg |= (uint32_t)(min(x, 0) & 255) << 8 * e;
+        const float y = fminf(fmaxf(rintf(row_to_float(x[e], HALF) * unit_q), -127.f), 127.f);
+        pos[e >> 1] |= (__float_as_uint(fmaxf(y, 0.f)) >> 16) << 16 * (e & 1);
+        neg[e >> 1] |= (__float_as_uint(fminf(y, 0.f)) >> 16) << 16 * (e & 1);
       }
     }
-    uint32_t* to = q_words + (g * 8 + (k & 15) / 2) * 8 + 2 * (k >> 4) + (k & 1);
-    to[0] = pos;
-    to[4] = neg;
+    uint2* to = q_frag + (i / 256 * kSteps + s) * 32 + l;
+    to[0] = make_uint2(pos[0], pos[1]);
+    to[8 * 32] = make_uint2(neg[0], neg[1]);
   }
   __syncthreads();
 
-  for (int j = j0 + tid / kPageLanes; j - tid / kPageLanes < j1; j += kAtOnce) {
-    const Bounds x = next;
-    next = load(j + kAtOnce);
-    const uint32_t w[16] = {x.lo0.x, x.lo0.y, x.lo0.z, x.lo0.w, x.lo1.x, x.lo1.y, x.lo1.z, x.lo1.w,
-                            x.hi0.x, x.hi0.y, x.hi0.z, x.hi0.w, x.hi1.x, x.hi1.y, x.hi1.z, x.hi1.w};
-    uint32_t big = 0;  // largest magnitudes of the even and of the odd values, as their bits
+  for (; j - g8 < j1; j += kAtOnce) {
+    uint32_t w[2][2][16];  // the lane's two pages; their largest, their smallest keys; four chunks of four words
+    bool there[2], number[2];
+    float most[2];
+    int ep[2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) big = __vmaxu2(big, w[i] & 0x7fff7fffu);
+    for (int x = 0; x < 2; ++x) {
+      there[x] = (uint32_t)page[x] < (uint32_t)v.n_pages;
+      const uint4* at = (const uint4*)(block_of(v, there[x] ? page[x] : 0, h) + bounds_at) + t4;
 #pragma unroll
-    for (int k = 1; k < kPageLanes; k *= 2) big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, k));
-    big = max(big & 0xffffu, big >> 16);
-    const bool number = big < (HALF ? 0x7c00u : 0x7f80u);
-    const float most = value<HALF>(number ? big : 0u, 0);
-    const int ep = exponent_of(most);
-    const float unit_p = power(7 - ep);
-    const bool clamp = __any_sync(0xffffffffu, most * unit_p >= 127.5f);
-    uint32_t lo[4], hi[4];
+      for (int side = 0; side < 2; ++side)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      lo[k] = whole4<HALF>(w[2 * k], w[2 * k + 1], unit_p, clamp);
-      hi[k] = whole4<HALF>(w[8 + 2 * k], w[8 + 2 * k + 1], unit_p, clamp);
-    }
-    int best = INT32_MIN;
-    for (int g0 = 0; g0 < v.G; g0 += kRowsAtOnce) {
-      int sum[kRowsAtOnce];
-#pragma unroll
-      for (int g = 0; g < kRowsAtOnce; ++g) {
-        sum[g] = 0;
-        if (g0 + g < v.G) {
-          const uint4 qp = *(const uint4*)(q_words + ((g0 + g) * 8 + u) * 8), qn = *(const uint4*)(q_words + ((g0 + g) * 8 + u) * 8 + 4);
-          sum[g] = __dp4a((int)hi[0], (int)qp.x, sum[g]);
-          sum[g] = __dp4a((int)hi[1], (int)qp.y, sum[g]);
-          sum[g] = __dp4a((int)hi[2], (int)qp.z, sum[g]);
-          sum[g] = __dp4a((int)hi[3], (int)qp.w, sum[g]);
-          sum[g] = __dp4a((int)lo[0], (int)qn.x, sum[g]);
-          sum[g] = __dp4a((int)lo[1], (int)qn.y, sum[g]);
-          sum[g] = __dp4a((int)lo[2], (int)qn.z, sum[g]);
-          sum[g] = __dp4a((int)lo[3], (int)qn.w, sum[g]);
+        for (int c = 0; c < 4; ++c) {
+          const uint4 y = there[x] ? at[16 * (1 - side) + 4 * c] : make_uint4(0, 0, 0, 0);
+          w[x][side][4 * c] = y.x, w[x][side][4 * c + 1] = y.y, w[x][side][4 * c + 2] = y.z, w[x][side][4 * c + 3] = y.w;
         }
-      }
-      // over the page's lanes: at each step a lane keeps half of its rows, in the end one, lane u row bits of u reversed
+    }
+    page[0] = find(j + kAtOnce), page[1] = find(j + kAtOnce + 8);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int give = u & 1 ? sum[k] : sum[k + 4], keep = u & 1 ? sum[k + 4] : sum[k];
-        sum[k] = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+    for (int x = 0; x < 2; ++x) {
+      uint32_t big = larger<HALF>(w[x][0][0], w[x][1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) big = larger<HALF>(big, larger<HALF>(w[x][0][i], w[x][1][i]));
+      big = larger<HALF>(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = larger<HALF>(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      big = max(big & 0x7fffu, big >> 16 & 0x7fffu);
+      number[x] = big < (HALF ? 0x7c00u : 0x7f80u);
+      most[x] = value<HALF>(number[x] ? big : 0u, 0);
+      ep[x] = exponent_of(most[x]);
+    }
+    const float unit_p[2] = {power(7 - ep[0]), power(7 - ep[1])};
+    const bool clamp = __any_sync(0xffffffffu, most[0] * unit_p[0] >= 127.5f || most[1] * unit_p[1] >= 127.5f);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[x][side][i] = whole2<HALF>(w[x][side][i], unit_p[x], clamp);
+    float best[2] = {__int_as_float(0xff800000), __int_as_float(0xff800000)};
+    for (int r = 0; r < blocks; ++r) {
+      float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const uint2 y = q_frag[(r * kSteps + s) * 32 + lane];
+        const int side = s >> 3, i = 2 * (s & 7);
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(w[0][side][i]), "r"(w[1][side][i]), "r"(w[0][side][i + 1]), "r"(w[1][side][i + 1]), "r"(y.x), "r"(y.y));
       }
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int give = u & 2 ? sum[k] : sum[k + 2], keep = u & 2 ? sum[k + 2] : sum[k];
-        sum[k] = keep + __shfl_xor_sync(0xffffffffu, give, 2);
-      }
-      const int give = u & 4 ? sum[0] : sum[1], keep = u & 4 ? sum[1] : sum[0];
-      const int s = keep + __shfl_xor_sync(0xffffffffu, give, 4);
-      const int row = g0 + 4 * (u & 1) + (u & 2) + (u >> 2);
-      if (row < v.G) best = max(best, s);
+      for (int e = 0; e < 4; ++e)
+        if (8 * r + 2 * t4 + (e & 1) < v.G) best[e >> 1] = fmaxf(best[e >> 1], d[e]);
     }
 #pragma unroll
-    for (int k = 1; k < kPageLanes; k *= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, k));
-    if (u == 0 && j < j1) {
+    for (int x = 0; x < 2; ++x) {
+      best[x] = fmaxf(best[x], __shfl_xor_sync(0xffffffffu, best[x], 1));
+      best[x] = fmaxf(best[x], __shfl_xor_sync(0xffffffffu, best[x], 2));
       const float inf = __int_as_float(0x7f800000);
-      keys[(int64_t)unit * v.max_pages + j] = order_key(!x.there ? -inf : number ? (float)best * power(ep) : inf);
+      if (t4 == 0 && j + 8 * x < j1)
+        keys[(int64_t)unit * v.max_pages + j + 8 * x] = order_key(!there[x] ? -inf : number[x] ? best[x] * power(ep[x]) : inf);
     }
   }
 }
@@ -203,6 +202,7 @@ __global__ void __launch_bounds__(kPickThreads) akv_paged_pick_kernel(PagedView 
                                                                       int32_t* sel, int32_t* count, int top) {
   __shared__ int part[2][kPickWarps];
   __shared__ uint32_t ends[2][kPickWarps];
+  __shared__ int hist[256], found[3];
   const int64_t unit = blockIdx.x;
   const int t = (int)(unit / v.H % T), b = (int)(unit / v.H / T);
   const int P = 1 << v.page_log, tid = threadIdx.x;
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kPickThreads) akv_paged_pick_kernel(PagedView 
       for (int i = i0; i < i1; ++i) f(i, at(i));
     }
   };
-  // the range of the keys that are not forced
+  // the range of the keys that are not forced (n > top >= sink + recent, so there is one)
   uint32_t low = kForced, high = 0;
   each_key([&](int, uint32_t k) {
     if (k != kForced) low = min(low, k), high = max(high, k);
@@ -242,26 +242,36 @@ __global__ void __launch_bounds__(kPickThreads) akv_paged_pick_kernel(PagedView 
   low = __reduce_min_sync(0xffffffffu, low);
   high = __reduce_max_sync(0xffffffffu, high);
   if ((tid & 31) == 0) ends[0][tid >> 5] = low, ends[1][tid >> 5] = high;
+  if (tid < 256) hist[tid] = 0;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kPickWarps; ++w) low = min(low, ends[0][w]), high = max(high, ends[1][w]);
-  // the largest key `last` of which at least `top` pages have it or more; its bits above the first that differs are known
-  // (n > top >= sink + recent, so there is a page that is not forced)
-  uint32_t last = low;
-  int turn = 0;
-  bool exact = false;  // exactly `top` pages have `last` or more
-  if (low != high) {
-    const int bit0 = 31 - __clz(low ^ high);
-    last = low >> bit0 >> 1 << bit0 << 1;
-    for (int bit = bit0; bit >= 0 && !exact; --bit) {
-      const uint32_t probe = last | 1u << bit;
-      int c = 0;
-      each_key([&](int, uint32_t k) { c += k >= probe; });
-      c = block_sum(c, part[turn ^= 1]);
-      if (c >= top) last = probe;
-      exact = c == top;
+  // The range is narrowed to a 256th a pass: the part that holds the last page kept.  In the end either all pages with
+  // `last` or more are kept (exact), or `last` is the one key of its part and the lowest pages that have it are.
+  int want = top - sink - recent;
+  uint32_t last = kForced;
+  bool exact = want == 0;
+  while (!exact) {
+    const int bits = 32 - __clz(high - low), shift = max(0, bits - 8);
+    each_key([&](int, uint32_t k) {
+      if (k >= low && k <= high) atomicAdd(hist + (k - low >> shift), 1);
+    });
+    __syncthreads();
+    const int mine_h = tid < 256 ? hist[255 - tid] : 0;  // from the highest part down
+    const int before = block_before(mine_h, part[0]);
+    if (tid < 256) {
+      hist[255 - tid] = 0;
+      if (before < want && before + mine_h >= want) found[0] = 255 - tid, found[1] = before, found[2] = mine_h;
     }
+    __syncthreads();
+    low += (uint32_t)found[0] << shift;
+    high = min(high, low + ((1u << shift) - 1));
+    want -= found[1];
+    last = low;
+    exact = found[2] == want;
+    if (shift == 0) break;
   }
+  int turn = 0;
   int above = 0, ties = 0;
   each_key([&](int, uint32_t k) {
     above += exact ? k >= last : k > last;
@@ -288,13 +298,13 @@ int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_
                         void* ws, void* stream) {
   const int64_t units = (int64_t)v.rows * T * v.H;
   cudaStream_t s = (cudaStream_t)stream;
-  // A CTA prepares the query rows (its price) for as many pages as leave 8 CTAs for each SM, at least 16 and at most 256.
-  int64_t per_cta = (units * v.max_pages + 8 * 152 - 1) / (8 * 152);
+  // A CTA prepares the query rows (its price) for as many pages as leave three CTAs for each SM, 64 to 1024.
+  int64_t per_cta = (units * v.max_pages + 3 * 152 - 1) / (3 * 152);
   per_cta = (per_cta + kAtOnce - 1) / kAtOnce * kAtOnce;
-  if (per_cta > 256) per_cta = 256;
+  if (per_cta > 1024) per_cta = 1024;
   const int64_t chunks = ((int64_t)v.max_pages + per_cta - 1) / per_cta;
   if (units * chunks > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
-  const size_t smem = (size_t)((v.G + kRowsAtOnce - 1) / kRowsAtOnce) * kRowsAtOnce * 64 * 4;
+  const size_t smem = (size_t)((v.G + 7) / 8) * kSteps * 32 * sizeof(uint2);
   auto score = v.half ? akv_paged_score_kernel<true> : akv_paged_score_kernel<false>;
   score<<<(unsigned)(units * chunks), kScoreThreads, smem, s>>>(v, (const uint16_t*)q.ptr, q.stride_b, q.stride_t, q.stride_h, T,
                                                                 (int)chunks, (int)per_cta, (uint32_t*)ws);
@@ -310,6 +320,7 @@ int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_
   cfg.attrs = &pdl;
   cfg.numAttrs = 1;
   auto pick = v.max_pages <= 4 * kPickThreads    ? akv_paged_pick_kernel<4>
+              : v.max_pages <= 8 * kPickThreads ? akv_paged_pick_kernel<8>
               : v.max_pages <= 16 * kPickThreads ? akv_paged_pick_kernel<16>
                                                  : akv_paged_pick_kernel<0>;
   return (int)cudaLaunchKernelEx(&cfg, pick, v, T, sink, recent, (const uint32_t*)ws, sel.pages, sel.count, sel.top);
