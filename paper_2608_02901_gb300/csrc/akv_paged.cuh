@@ -12,6 +12,27 @@
 namespace akv {
 namespace {
 
+// Every launch of these files is a programmatic dependent of what runs before it in its stream: its CTAs may be set up
+// beside that, and wait for its end (and for its writes) before they touch memory.  Every CTA waits, so that whoever
+// depends on the launch has waited for all before it as well.
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <class... Params, class... Args>
+int launch_after(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, void* stream, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute pdl{};
+  pdl.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = &pdl;
+  cfg.numAttrs = 1;
+  return (int)cudaLaunchKernelEx(&cfg, kernel, (Params)args...);
+}
+
 __device__ __forceinline__ float row_to_float(uint16_t x, int half) {
   return half ? __half2float(__ushort_as_half(x)) : __uint_as_float((uint32_t)x << 16);
 }

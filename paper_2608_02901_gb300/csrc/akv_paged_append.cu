@@ -285,7 +285,9 @@ template <int NG, bool ROT, bool HALF>
 __global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedView v, RowsIO K, RowsIO V, int T, const int32_t* n_new,
                                                                           int pages_each, int sides) {
   __shared__ __align__(16) uint32_t sign[64];
+  launch_dependents();
   if (ROT) fill_signs(v, sign);
+  wait_for_stream();
   const int part = sides == 1 ? blockIdx.x & 1 : 0, cta = sides == 1 ? blockIdx.x >> 1 : blockIdx.x;
   const int slot = cta % pages_each, bh = cta / pages_each;
   const int h = bh % v.H, b = bh / v.H;
@@ -440,11 +442,13 @@ __global__ void __launch_bounds__(kMaxThreads, 5) akv_paged_read_kernel(PagedVie
   const int bh = (blockIdx.x >> 1) / chunks;
   const int h = bh % v.H, b = bh / v.H;
   const int u = threadIdx.x & 3;
+  __shared__ __align__(16) uint32_t sign[64];
+  launch_dependents();
+  if (ROT) fill_signs(v, sign);
+  wait_for_stream();
   const int64_t first = start ? (int64_t)start[b] : 0;
   const int held = held_tokens(v, b), P = 1 << v.page_log;
   const RowsIO& R = side ? V : K;
-  __shared__ __align__(16) uint32_t sign[64];
-  if (ROT) fill_signs(v, sign);
   auto token = [&](int turn) { return (chunk * turns + turn) * kRowsAtOnce + (int)threadIdx.x / kRowLanes; };
   auto find = [&](int turn) {
     const int t = token(turn);
@@ -572,8 +576,7 @@ int launch_paged_append(const PagedView& v, const akv_rows& K, const akv_rows& V
   if (grid > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
   const int threads = P * kRowLanes < kMaxThreads ? P * kRowLanes : kMaxThreads;
   auto kernel = v.half ? append_kernel<true>(v) : append_kernel<false>(v);
-  kernel<<<(unsigned)grid, threads, 0, (cudaStream_t)stream>>>(v, rows_io(K), rows_io(V), T, n_new, (int)each, sides);
-  return (int)cudaGetLastError();
+  return launch_after(kernel, dim3((unsigned)grid), threads, 0, stream, v, rows_io(K), rows_io(V), T, n_new, (int)each, sides);
 }
 
 int launch_paged_read(const PagedView& v, const int32_t* start, const akv_rows& K, const akv_rows& V, int32_t T, void* stream) {
@@ -584,8 +587,7 @@ int launch_paged_read(const PagedView& v, const int32_t* start, const akv_rows& 
   const int64_t grid = 2 * each * v.H * v.rows;
   if (grid > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
   auto kernel = v.half ? read_kernel<true>(v) : read_kernel<false>(v);
-  kernel<<<(unsigned)grid, kMaxThreads, 0, (cudaStream_t)stream>>>(v, start, rows_io(K), rows_io(V), T, (int)each, turns);
-  return (int)cudaGetLastError();
+  return launch_after(kernel, dim3((unsigned)grid), kMaxThreads, 0, stream, v, start, rows_io(K), rows_io(V), T, (int)each, turns);
 }
 
 }  // namespace akv

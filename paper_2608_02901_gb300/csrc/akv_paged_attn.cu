@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedView& v = a.v;
 
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  launch_dependents();
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&S.full[s]), 1);
@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  wait_for_stream();
   Cursor<SEL> c;
   const Range r = plan<kThreads, SEL>(a, S.strip, c);  // (its barriers order the initialisation too)
   if (tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
@@ -248,6 +249,8 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   if (warp == kWarps) {
     // ---- the copying warp: lane k < 8 sees to sub-block k of a tile, the first lane of a page copies its sub-blocks
     const int per_page = min(kTileSubs, 1 << (v.page_log - 4));
+    // the bulk copies read what launches before this one wrote with ordinary stores
+    asm volatile("fence.proxy.async.global;" ::: "memory");
     int stage = 0;
     uint32_t phase = 1;  // the first pass over the ring waits for nobody
     // What the next tiles need is under way while a tile waits for its stage, and nothing looks at it before its turn:
@@ -736,7 +739,8 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 constexpr int kJoinWarps = 8;
 template <bool SEL>
 __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_join_kernel(const __grid_constant__ AttnArgs a, int kRows) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  launch_dependents();
+  wait_for_stream();
   const int4 d = a.desc[blockIdx.x];
   if (d.w <= 0) return;
   const PagedView& v = a.v;
@@ -829,19 +833,9 @@ int launch(const AttnArgs& a, int dev, int sms, cudaStream_t stream) {
   }
   int grid = sms * ctas_of(NT);
   if (grid > kPagedMaxGrid) grid = kPagedMaxGrid;
-  kernel<<<grid, Smem<NT>::kThreads, smem, stream>>>(a);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return (int)e;
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute pdl{};
-  pdl.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  pdl.val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT);
-  cfg.blockDim = dim3(32 * kJoinWarps);
-  cfg.stream = stream;
-  cfg.attrs = &pdl;
-  cfg.numAttrs = 1;
-  return (int)cudaLaunchKernelEx(&cfg, akv_paged_join_kernel<SEL>, a, 8 * NT);
+  const int err = launch_after(kernel, dim3(grid), Smem<NT>::kThreads, smem, stream, a);
+  if (err) return err;
+  return launch_after(akv_paged_join_kernel<SEL>, dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT), 32 * kJoinWarps, 0, stream, a, 8 * NT);
 }
 
 template <int NT, bool HILO, bool SEL>

@@ -2,10 +2,9 @@
 //
 // The score reads the pages' bounds once (512 bytes a page and head) and does 2 G x 128 multiply-adds on them: with a
 // query row split into its positive and its negative part, the larger of q lo and q hi in each dimension is
-// q+ hi + q- lo, two products.  The numbers are at most 127, exact in bf16, and the sums at most 2^22, exact in fp32: the
-// tensor cores add them up without rounding, in any order, so that the choice is the same on every machine.  What costs
-// is turning the bounds into whole numbers (2 x 128 a page and head, two or three operations each); a warp does it once
-// for up to 8 query rows.  The choice itself finds the key of the last page kept, 8 bits of its range a pass.
+// q+ hi + q- lo, two products.  The numbers are at most 127, exact in bf16 and fp16, and the sums at most 2^22, exact in
+// fp32: the tensor cores add them up without rounding, in any order, so that the choice is the same on every machine.
+// What costs is turning the bounds into whole numbers (three operations a pair); a warp does it once for all query rows.  The choice itself finds the key of the last page kept, 8 bits of its range a pass.
 #include "akv_paged.cuh"
 
 namespace akv {
@@ -39,23 +38,36 @@ __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
   else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-// Two values times `unit` as whole numbers (clamped to +-127 where `clamp`), in bf16.
+// Two values times a power of two (the product of both factors), at most 128 in magnitude, as whole numbers of the same
+// type: at 128 and above (fp16: 1024) its numbers are 1 apart, so adding 128 away from zero rounds to nearest even.
 template <bool HALF>
-__device__ __forceinline__ uint32_t whole2(uint32_t w, float unit, bool clamp) {
-  float a = value<HALF>(w, 0), b = value<HALF>(w, 1);
-  asm("{ .reg .b64 p, u, m, n;\n"
-      "  mov.b64 p, {%0, %1}; mov.b64 u, {%2, %2}; mov.b64 m, {%3, %3}; mov.b64 n, {%4, %4};\n"
-      "  fma.rn.f32x2 p, p, u, m; add.rn.f32x2 p, p, n; mov.b64 {%0, %1}, p; }"
-      : "+f"(a), "+f"(b)
-      : "f"(unit), "f"(12582912.f), "f"(-12582912.f));  // 1.5 2^23: rounds to nearest even
-  if (clamp) a = fminf(fmaxf(a, -127.f), 127.f), b = fminf(fmaxf(b, -127.f), 127.f);
-  return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+__device__ __forceinline__ uint32_t whole2(uint32_t w, uint32_t unit, uint32_t unit_first) {
+  uint32_t far = w & 0x80008000u, r;
+  if (HALF) {
+    far |= 0x64006400u;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(unit_first));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(r), "r"(unit), "r"(far));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(far));
+  } else {
+    far |= 0x43004300u;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w), "r"(unit), "r"(far));
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(r), "r"(far));
+  }
+  return r;
+}
+template <bool HALF>
+__device__ __forceinline__ uint32_t clamp2(uint32_t w) {  // to +-127
+  uint32_t r;
+  if (HALF) asm("min.f16x2 %0, %1, %2;\n max.f16x2 %0, %0, %3;" : "=&r"(r) : "r"(w), "r"(0x57f057f0u), "r"(0xd7f0d7f0u));
+  else asm("min.bf16x2 %0, %1, %2;\n max.bf16x2 %0, %0, %3;" : "=&r"(r) : "r"(w), "r"(0x42fe42feu), "r"(0xc2fec2feu));
+  return r;
 }
 
 template <bool HALF>
 __global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(PagedView v, const uint16_t* q, int64_t qb, int64_t qt,
                                                                            int64_t qh, int T, int chunks, int per_cta, uint32_t* keys) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  launch_dependents();
+  wait_for_stream();
   extern __shared__ __align__(16) uint2 q_frag[];  // [blocks of 8 rows][kSteps][32 lanes]
   __shared__ float q_max[kScoreWarps];
   const int unit = blockIdx.x / chunks, chunk = blockIdx.x % chunks;
@@ -70,6 +82,24 @@ __global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(Paged
   auto find = [&](int j) { return j < j1 ? v.table[(int64_t)b * v.table_stride + j] : -1; };
   int j = j0 + kWarpPages * warp + g8;
   int page[2] = {find(j), find(j + 8)};
+  uint32_t w[2][2][16];  // the lane's two pages; their largest, their smallest keys; four chunks of four words
+  bool there[2];
+  auto load = [&]() {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      there[x] = (uint32_t)page[x] < (uint32_t)v.n_pages;
+      const uint4* at = (const uint4*)(block_of(v, there[x] ? page[x] : 0, h) + bounds_at) + t4;
+#pragma unroll
+      for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint4 y = there[x] ? at[16 * (1 - side) + 4 * c] : make_uint4(0, 0, 0, 0);
+          w[x][side][4 * c] = y.x, w[x][side][4 * c + 1] = y.y, w[x][side][4 * c + 2] = y.z, w[x][side][4 * c + 3] = y.w;
+        }
+    }
+  };
+  load();  // (under way while the queries are prepared)
+  page[0] = find(j + kAtOnce), page[1] = find(j + kAtOnce + 8);
 
   // the query rows as whole numbers
   const uint16_t* rows = q + b * qb + t * qt + (int64_t)h * v.G * qh;
@@ -91,8 +121,8 @@ __global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(Paged
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float y = fminf(fmaxf(rintf(row_to_float(x[e], HALF) * unit_q), -127.f), 127.f);
-        pos[e >> 1] |= (__float_as_uint(fmaxf(y, 0.f)) >> 16) << 16 * (e & 1);
-        neg[e >> 1] |= (__float_as_uint(fminf(y, 0.f)) >> 16) << 16 * (e & 1);
+        pos[e >> 1] |= (uint32_t)float_to_row(fmaxf(y, 0.f), HALF) << 16 * (e & 1);
+        neg[e >> 1] |= (uint32_t)float_to_row(fminf(y, 0.f), HALF) << 16 * (e & 1);
       }
     }
     uint2* to = q_frag + (i / 256 * kSteps + s) * 32 + l;
@@ -102,23 +132,9 @@ __global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(Paged
   __syncthreads();
 
   for (; j - g8 < j1; j += kAtOnce) {
-    uint32_t w[2][2][16];  // the lane's two pages; their largest, their smallest keys; four chunks of four words
-    bool there[2], number[2];
+    bool number[2];
     float most[2];
     int ep[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      there[x] = (uint32_t)page[x] < (uint32_t)v.n_pages;
-      const uint4* at = (const uint4*)(block_of(v, there[x] ? page[x] : 0, h) + bounds_at) + t4;
-#pragma unroll
-      for (int side = 0; side < 2; ++side)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint4 y = there[x] ? at[16 * (1 - side) + 4 * c] : make_uint4(0, 0, 0, 0);
-          w[x][side][4 * c] = y.x, w[x][side][4 * c + 1] = y.y, w[x][side][4 * c + 2] = y.z, w[x][side][4 * c + 3] = y.w;
-        }
-    }
-    page[0] = find(j + kAtOnce), page[1] = find(j + kAtOnce + 8);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       uint32_t big = larger<HALF>(w[x][0][0], w[x][1][0]);
@@ -131,28 +147,46 @@ __global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(Paged
       most[x] = value<HALF>(number[x] ? big : 0u, 0);
       ep[x] = exponent_of(most[x]);
     }
-    const float unit_p[2] = {power(7 - ep[0]), power(7 - ep[1])};
-    const bool clamp = __any_sync(0xffffffffu, most[0] * unit_p[0] >= 127.5f || most[1] * unit_p[1] >= 127.5f);
+    bool clamp = false;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < 2; ++x) {
+      // 2^(7 - e) as a pair; in fp16, whose numbers go from 2^-24 to 2^15, in two factors
+      const int up = 7 - ep[x], first = HALF ? max(up - 15, 0) : 0;
+      const uint32_t unit = HALF ? (uint32_t)(up - first + 15) << 10 : (uint32_t)(up + 127) << 7;
+      const uint32_t unit_first = (uint32_t)(first + 15) << 10;
+      clamp = clamp || most[x] * power(up) >= 127.5f;
 #pragma unroll
       for (int side = 0; side < 2; ++side)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[x][side][i] = whole2<HALF>(w[x][side][i], unit_p[x], clamp);
+        for (int i = 0; i < 16; ++i) w[x][side][i] = whole2<HALF>(w[x][side][i], unit * 0x10001u, unit_first * 0x10001u);
+    }
+    if (__any_sync(0xffffffffu, clamp)) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[x][side][i] = clamp2<HALF>(w[x][side][i]);
+    }
     float best[2] = {__int_as_float(0xff800000), __int_as_float(0xff800000)};
     for (int r = 0; r < blocks; ++r) {
-      float d[4] = {0.f, 0.f, 0.f, 0.f};
+      float d[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};  // two chains of products
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         const uint2 y = q_frag[(r * kSteps + s) * 32 + lane];
         const int side = s >> 3, i = 2 * (s & 7);
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(w[0][side][i]), "r"(w[1][side][i]), "r"(w[0][side][i + 1]), "r"(w[1][side][i + 1]), "r"(y.x), "r"(y.y));
+        if (HALF)
+          asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                       : "+f"(d[side][0]), "+f"(d[side][1]), "+f"(d[side][2]), "+f"(d[side][3])
+                       : "r"(w[0][side][i]), "r"(w[1][side][i]), "r"(w[0][side][i + 1]), "r"(w[1][side][i + 1]), "r"(y.x), "r"(y.y));
+        else
+          asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                       : "+f"(d[side][0]), "+f"(d[side][1]), "+f"(d[side][2]), "+f"(d[side][3])
+                       : "r"(w[0][side][i]), "r"(w[1][side][i]), "r"(w[0][side][i + 1]), "r"(w[1][side][i + 1]), "r"(y.x), "r"(y.y));
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (8 * r + 2 * t4 + (e & 1) < v.G) best[e >> 1] = fmaxf(best[e >> 1], d[e]);
+        if (8 * r + 2 * t4 + (e & 1) < v.G) best[e >> 1] = fmaxf(best[e >> 1], d[0][e] + d[1][e]);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -162,6 +196,8 @@ __global__ void __launch_bounds__(kScoreThreads, 3) akv_paged_score_kernel(Paged
       if (t4 == 0 && j + 8 * x < j1)
         keys[(int64_t)unit * v.max_pages + j + 8 * x] = order_key(!there[x] ? -inf : number[x] ? best[x] * power(ep[x]) : inf);
     }
+    load();
+    page[0] = find(j + 2 * kAtOnce), page[1] = find(j + 2 * kAtOnce + 8);
   }
 }
 
@@ -203,6 +239,8 @@ __global__ void __launch_bounds__(kPickThreads) akv_paged_pick_kernel(PagedView 
   __shared__ int part[2][kPickWarps];
   __shared__ uint32_t ends[2][kPickWarps];
   __shared__ int hist[256], found[3];
+  launch_dependents();
+  wait_for_stream();
   const int64_t unit = blockIdx.x;
   const int t = (int)(unit / v.H % T), b = (int)(unit / v.H / T);
   const int P = 1 << v.page_log, tid = threadIdx.x;
@@ -213,10 +251,8 @@ __global__ void __launch_bounds__(kPickThreads) akv_paged_pick_kernel(PagedView 
   for (int i = kept + tid; i < top; i += kPickThreads) out[i] = -1;
   if (n <= top) {
     for (int i = tid; i < n; i += kPickThreads) out[i] = i;
+    return;
   }
-  // waited for in any case: what follows in the stream may write where the scores are still being written
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (n <= top) return;
   const uint32_t* key = keys + unit * v.max_pages;
   const int each = (n + kPickThreads - 1) / kPickThreads, i0 = tid * each, i1 = min(n, i0 + each);
   uint32_t mine[KEPT > 0 ? KEPT : 1];
@@ -297,7 +333,6 @@ size_t paged_select_ws_bytes(const PagedView& v, int32_t T) {
 int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_t sink, int32_t recent, const akv_selection& sel,
                         void* ws, void* stream) {
   const int64_t units = (int64_t)v.rows * T * v.H;
-  cudaStream_t s = (cudaStream_t)stream;
   // A CTA prepares the query rows (its price) for as many pages as leave three CTAs for each SM, 64 to 1024.
   int64_t per_cta = (units * v.max_pages + 3 * 152 - 1) / (3 * 152);
   per_cta = (per_cta + kAtOnce - 1) / kAtOnce * kAtOnce;
@@ -306,24 +341,15 @@ int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_
   if (units * chunks > INT32_MAX) return (int)cudaErrorInvalidConfiguration;
   const size_t smem = (size_t)((v.G + 7) / 8) * kSteps * 32 * sizeof(uint2);
   auto score = v.half ? akv_paged_score_kernel<true> : akv_paged_score_kernel<false>;
-  score<<<(unsigned)(units * chunks), kScoreThreads, smem, s>>>(v, (const uint16_t*)q.ptr, q.stride_b, q.stride_t, q.stride_h, T,
-                                                                (int)chunks, (int)per_cta, (uint32_t*)ws);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return (int)e;
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute pdl{};
-  pdl.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  pdl.val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)units);
-  cfg.blockDim = dim3(kPickThreads);
-  cfg.stream = s;
-  cfg.attrs = &pdl;
-  cfg.numAttrs = 1;
+  const int err = launch_after(score, dim3((unsigned)(units * chunks)), kScoreThreads, smem, stream, v, (const uint16_t*)q.ptr, q.stride_b,
+                               q.stride_t, q.stride_h, T, (int)chunks, (int)per_cta, (uint32_t*)ws);
+  if (err) return err;
   auto pick = v.max_pages <= 4 * kPickThreads    ? akv_paged_pick_kernel<4>
               : v.max_pages <= 8 * kPickThreads ? akv_paged_pick_kernel<8>
               : v.max_pages <= 16 * kPickThreads ? akv_paged_pick_kernel<16>
                                                  : akv_paged_pick_kernel<0>;
-  return (int)cudaLaunchKernelEx(&cfg, pick, v, T, sink, recent, (const uint32_t*)ws, sel.pages, sel.count, sel.top);
+  return launch_after(pick, dim3((unsigned)units), kPickThreads, 0, stream, v, T, sink, recent, (const uint32_t*)ws, sel.pages, sel.count,
+                      sel.top);
 }
 
 }  // namespace akv

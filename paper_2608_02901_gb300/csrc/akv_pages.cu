@@ -76,6 +76,8 @@ __device__ __forceinline__ int block_scan(int x, int* total) {
 constexpr int kCopyThreads = 256, kCopyChunk = kCopyThreads * 4 * 16;
 __global__ void __launch_bounds__(kCopyThreads) akv_pages_copy_kernel(PagesState s, const int32_t* src, const int32_t* dst, int n,
                                                                       const int32_t* n_dev) {
+  launch_dependents();
+  wait_for_stream();
   if (n_dev) n = *n_dev;
   const int chunks = (int)((s.page_bytes + kCopyChunk - 1) / kCopyChunk);
   const int64_t work = (int64_t)n * s.n_layers * chunks;
@@ -101,6 +103,8 @@ __global__ void __launch_bounds__(kCopyThreads) akv_pages_copy_kernel(PagesState
 }
 
 __global__ void __launch_bounds__(256) akv_pages_fork_kernel(PagesState s, const int32_t* src, const int32_t* dst) {
+  launch_dependents();
+  wait_for_stream();
   const int a = src[blockIdx.x], b = dst[blockIdx.x];
   if ((uint32_t)a >= (uint32_t)s.rows || (uint32_t)b >= (uint32_t)s.rows || a == b) return;
   const int len = min(max(s.lens[a], 0), s.max_pages << s.page_log);
@@ -118,6 +122,8 @@ __global__ void __launch_bounds__(256) akv_pages_fork_kernel(PagesState s, const
 
 // A page of the row is given up by the one thread that takes it out of the table.
 __global__ void __launch_bounds__(256) akv_pages_free_kernel(PagesState s, const int32_t* rows) {
+  launch_dependents();
+  wait_for_stream();
   const int r = rows[blockIdx.x];
   if ((uint32_t)r >= (uint32_t)s.rows) return;
   for (int j = threadIdx.x; j < s.max_pages; j += blockDim.x) {
@@ -147,6 +153,8 @@ __device__ __forceinline__ RowPlan row_plan(const PagesState& s, const int32_t* 
 }
 
 __global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesState s, const int32_t* n_new, int32_t* missing, PagesWs w) {
+  launch_dependents();
+  wait_for_stream();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   // who writes into a page that others may hold too
   for (int r = tid; r < s.rows; r += blockDim.x) {
@@ -239,6 +247,8 @@ __global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesSt
 }
 
 __global__ void __launch_bounds__(kPlanThreads) akv_pages_compact_plan(PagesState s, int32_t* n_live, PagesWs w) {
+  launch_dependents();
+  wait_for_stream();
   const int tid = threadIdx.x;
   int live = 0;
   for (int p = tid; p < s.n_pages; p += blockDim.x) live += s.refs[p] > 0;
@@ -270,6 +280,8 @@ __global__ void __launch_bounds__(kPlanThreads) akv_pages_compact_plan(PagesStat
 
 // Table entries and counts follow the pages (n_live and the moves are the plan's).
 __global__ void __launch_bounds__(256) akv_pages_compact_table(PagesState s, const int32_t* n_live, PagesWs w) {
+  launch_dependents();
+  wait_for_stream();
   const int n = *n_live;
   const int64_t cells = (int64_t)s.rows * s.max_pages, step = (int64_t)gridDim.x * blockDim.x;
   const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
@@ -280,6 +292,8 @@ __global__ void __launch_bounds__(256) akv_pages_compact_table(PagesState s, con
   }
 }
 __global__ void __launch_bounds__(256) akv_pages_compact_refs(PagesState s, PagesWs w) {
+  launch_dependents();
+  wait_for_stream();
   const int n = *w.n_copies;
   for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
     s.refs[w.dst[i]] = s.refs[w.src[i]];
@@ -294,36 +308,31 @@ constexpr int kCopyGrid = 152 * 8;
 size_t pages_ws_bytes(const PagesState& s) { return (pages_ws_ints(s) * 4 + 255) & ~(size_t)255; }
 
 int launch_pages_copy(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
-  akv_pages_copy_kernel<<<kCopyGrid, kCopyThreads, 0, (cudaStream_t)stream>>>(s, src, dst, n, nullptr);
-  return (int)cudaGetLastError();
+  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, src, dst, n, nullptr);
 }
 
 int launch_pages_fork(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
-  akv_pages_fork_kernel<<<n, 256, 0, (cudaStream_t)stream>>>(s, src, dst);
-  return (int)cudaGetLastError();
+  return launch_after(akv_pages_fork_kernel, dim3(n), 256, 0, stream, s, src, dst);
 }
 
 int launch_pages_free(const PagesState& s, const int32_t* rows, int32_t n, void* stream) {
-  akv_pages_free_kernel<<<n, 256, 0, (cudaStream_t)stream>>>(s, rows);
-  return (int)cudaGetLastError();
+  return launch_after(akv_pages_free_kernel, dim3(n), 256, 0, stream, s, rows);
 }
 
 int launch_pages_reserve(const PagesState& s, const int32_t* n_new, int32_t* missing, void* ws, void* stream) {
   const PagesWs w = pages_ws(s, ws);
-  cudaStream_t st = (cudaStream_t)stream;
-  akv_pages_reserve_kernel<<<1, kPlanThreads, 0, st>>>(s, n_new, missing, w);
-  akv_pages_copy_kernel<<<kCopyGrid, kCopyThreads, 0, st>>>(s, w.src, w.dst, 0, w.n_copies);
-  return (int)cudaGetLastError();
+  const int e = launch_after(akv_pages_reserve_kernel, dim3(1), kPlanThreads, 0, stream, s, n_new, missing, w);
+  if (e) return e;
+  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, w.src, w.dst, 0, w.n_copies);
 }
 
 int launch_pages_compact(const PagesState& s, int32_t* n_live, void* ws, void* stream) {
   const PagesWs w = pages_ws(s, ws);
-  cudaStream_t st = (cudaStream_t)stream;
-  akv_pages_compact_plan<<<1, kPlanThreads, 0, st>>>(s, n_live, w);
-  akv_pages_copy_kernel<<<kCopyGrid, kCopyThreads, 0, st>>>(s, w.src, w.dst, 0, w.n_copies);
-  akv_pages_compact_table<<<152, 256, 0, st>>>(s, n_live, w);
-  akv_pages_compact_refs<<<152, 256, 0, st>>>(s, w);
-  return (int)cudaGetLastError();
+  int e = launch_after(akv_pages_compact_plan, dim3(1), kPlanThreads, 0, stream, s, n_live, w);
+  if (!e) e = launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, w.src, w.dst, 0, w.n_copies);
+  if (!e) e = launch_after(akv_pages_compact_table, dim3(152), 256, 0, stream, s, n_live, w);
+  if (!e) e = launch_after(akv_pages_compact_refs, dim3(152), 256, 0, stream, s, w);
+  return e;
 }
 
 }  // namespace akv
