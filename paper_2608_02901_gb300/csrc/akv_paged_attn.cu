@@ -31,9 +31,10 @@ constexpr int kTileTokens = 128, kTileSubs = kTileTokens / kSubTokens;
 // has room for 16 warps of 128, 12 of 168 or 8 of 255 (a 17th of 96 spills).  Two CTAs per SM of the smallest.
 AKV_HD constexpr int warps_of(int nt) { return nt == 2 ? 11 : 7; }
 AKV_HD constexpr int ctas_of(int nt) { return nt == 1 ? 2 : 1; }
+// Stages of the ring: what the warps are working on, and as much again on its way.
+AKV_HD constexpr int stages_of(int nt) { return nt == 2 ? 6 : 4; }
 // Sub-blocks that a warp takes at a time: two where the registers allow it, whose products then overlap.
-AKV_HD constexpr int subs_of(int nt) { return nt == 1 ? 2 : 1; }
-constexpr int kStages = 4;
+AKV_HD constexpr int subs_of(int nt) { return nt <= 2 ? 2 : 1; }
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -1e30f;                  // reference of a share that saw no token
 constexpr float kSlack = 8.f;                   // a weight may pass its place by 2^8 before the reference moves
@@ -206,7 +207,7 @@ __device__ __forceinline__ Range plan(const AttnArgs& a, int64_t* strip, Cursor<
 
 template <int NT>
 struct Smem {
-  static constexpr int kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1);
+  static constexpr int kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1), kStages = stages_of(NT);
   alignas(128) uint8_t stage[kStages][kTileSubs * 2304];
   alignas(16) uint4 frag[2][NT][4][32];     // query operand: high, low halves
   float red[kWarps][8 * NT][kRowPad];       // the warps' outputs at a unit's end
@@ -214,6 +215,7 @@ struct Smem {
   float qsum[8 * NT][2];                    // sums of a query row over each group of dimensions
   float qmax[kWarps];
   int pos[kStages][kTileSubs];              // first token of each sub-block; -1: none, -2: a page outside the pool
+  uint32_t tile[kStages];                   // the CTA's tile that the stage holds or waits for
   int64_t strip[kThreads + 1];
   uint64_t full[kStages], empty[kStages];
   int failed;
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   extern __shared__ __align__(128) uint8_t smem_raw[];
   Smem<NT>& S = *reinterpret_cast<Smem<NT>*>(smem_raw);
   constexpr uint32_t kSub = 2048 + 128 * NG;
-  constexpr int kRows = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1), NS = subs_of(NT);
+  constexpr int kRows = 8 * NT, kWarps = warps_of(NT), kThreads = 32 * (kWarps + 1), NS = subs_of(NT), kStages = stages_of(NT);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedView& v = a.v;
 
@@ -235,6 +237,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&S.full[s]), 1);
       mbar_init(smem_u32(&S.empty[s]), kTileSubs / NS);
+      S.tile[s] = ~0u;
     }
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -312,6 +315,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       }
       const uint32_t there = __ballot_sync(0xffffffffu, pos0 >= 0);
       if (lane < kTileSubs) S.pos[stage][lane] = pos0;
+      if (lane == kTileSubs) *(volatile uint32_t*)&S.tile[stage] = (uint32_t)(k - r.lo);
       __syncwarp();
       const uint32_t bar = smem_u32(&S.full[stage]);
       if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(there) * kSub);
@@ -448,10 +452,24 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       const uint32_t tile = (uint32_t)(k - r.lo) + item / (kTileSubs / NS);  // of the CTA's
       const int stage = tile % kStages;
       const uint32_t bar = smem_u32(&S.full[stage]), parity = tile / kStages & 1;
-      if (!__all_sync(0xffffffffu, mbar_try(bar, parity)) && (warp_failed(failed) || !mbar_wait_w(bar, parity))) {
-        *failed = 1;
-        spoil();
-        break;
+      // A warp passes over tiles that it has no part of, so the parity alone could be that of a phase long ago: the stage
+      // is this tile's once its number is (read first), and then the phase is the right one.
+      auto ready = [&]() {
+        const bool mine = *(volatile uint32_t*)&S.tile[stage] == tile;
+        return __all_sync(0xffffffffu, mbar_try(bar, parity) && mine);
+      };
+      if (!ready()) {
+        bool there = false;
+        const unsigned long long t0 = global_ns();
+        for (unsigned i = 1; !there && !warp_failed(failed); ++i) {
+          there = ready();
+          if ((i & 63u) == 0 && __shfl_sync(0xffffffffu, global_ns() - t0 >= kWaitNs ? 1 : 0, 0)) break;
+        }
+        if (!there) {
+          *failed = 1;
+          spoil();
+          break;
+        }
       }
       int pos[NS];
       bool none = true, edge = false, outside = false;
