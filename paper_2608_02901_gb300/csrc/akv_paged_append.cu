@@ -282,7 +282,7 @@ __device__ __forceinline__ void load_row(const RowsIO& R, int64_t at, int u, uin
 // One CTA: one page of one request that gets new tokens, one head; its keys, then its values, or (sides 1) one of them.
 // The row after the present one is loaded while that is worked on.
 template <int NG, bool ROT, bool HALF>
-__global__ void __launch_bounds__(kMaxThreads, 4) akv_paged_append_kernel(PagedView v, RowsIO K, RowsIO V, int T, const int32_t* n_new,
+__global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedView v, RowsIO K, RowsIO V, int T, const int32_t* n_new,
                                                                           int pages_each, int sides) {
   __shared__ __align__(16) uint32_t sign[64];
   launch_dependents();
@@ -434,7 +434,7 @@ __device__ __forceinline__ void unrotate_codes(const uint32_t (&c)[4], const uin
 constexpr int kReadTurns = 8;  // rows a thread reads back at most
 
 template <int NG, bool ROT, bool HALF>
-__global__ void __launch_bounds__(kMaxThreads, 5) akv_paged_read_kernel(PagedView v, const int32_t* start, RowsIO K, RowsIO V, int T,
+__global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_read_kernel(PagedView v, const int32_t* start, RowsIO K, RowsIO V, int T,
                                                                         int chunks, int turns) {
   constexpr int kRowsAtOnce = kMaxThreads / kRowLanes;
   const int side = blockIdx.x & 1;
