@@ -199,8 +199,8 @@ constexpr int kPagedMaxGrid = 512;  // CTAs of the attention launch at most
 // CTA slots of partial results: two per CTA (the unit it begins in, the unit it ends in) of `rows` query rows, each
 // 128 values, a normaliser and a maximum.
 AKV_HD constexpr size_t paged_slot_floats(int rows) { return (size_t)rows * 130; }
-// query rows of one attention unit: one, two or four 8-column operand tiles
-constexpr int paged_unit_rows(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+// query rows of one attention unit: one or two 8-column operand tiles
+constexpr int paged_unit_rows(int rows) { return rows <= 8 ? 8 : 16; }
 
 int launch_paged_append(const PagedView& v, const akv_rows& K, const akv_rows& V, int32_t T, const int32_t* n_new, void* stream);
 int launch_paged_read(const PagedView& v, const int32_t* start, const akv_rows& K, const akv_rows& V, int32_t T, void* stream);

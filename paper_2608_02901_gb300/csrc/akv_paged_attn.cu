@@ -27,14 +27,17 @@ namespace akv {
 namespace {
 
 constexpr int kTileTokens = 128, kTileSubs = kTileTokens / kSubTokens;
-// Computing warps of a CTA, next to one that copies: the registers a warp needs grow with the query rows, and an SM
-// has room for 16 warps of 128, 12 of 168 or 8 of 255 (a 17th of 96 spills).  Two CTAs per SM of the smallest.
-AKV_HD constexpr int warps_of(int nt) { return nt == 2 ? 11 : 7; }
+// A unit has 8 NT query rows, NT 1 or 2.  (Four were slower than two units of 16 rows that read the cache twice: 375 and
+// 357 us for 32 rows a head over 4 x 131072 tokens, 53 and 42 us over 4 x 8192: 255 registers leave an SM seven warps.)
+// Computing warps of a CTA, next to one that copies: an SM has room for 16 warps of 128 registers or 12 of 168 (a 17th
+// and a 13th would take them down to 96 and 128, which spill).  Two CTAs per SM of 8 rows, one of 16.
+AKV_HD constexpr int warps_of(int nt) { return nt == 1 ? 7 : 11; }
 AKV_HD constexpr int ctas_of(int nt) { return nt == 1 ? 2 : 1; }
 // Stages of the ring: what the warps are working on, and as much again on its way.
-AKV_HD constexpr int stages_of(int nt) { return nt == 2 ? 6 : 4; }
-// Sub-blocks that a warp takes at a time: two where the registers allow it, whose products then overlap.
-AKV_HD constexpr int subs_of(int nt) { return nt <= 2 ? 2 : 1; }
+AKV_HD constexpr int stages_of(int nt) { return nt == 1 ? 4 : 6; }
+// Sub-blocks that a warp takes at a time: two where the registers allow it, whose products then overlap (8 x 128K tokens:
+// 284 us with one, 234 with two; with 16 rows two spill, 179 and 181 us for 4 x 131072 tokens, rotated 217 and 276).
+AKV_HD constexpr int subs_of(int nt) { return nt == 1 ? 2 : 1; }
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -1e30f;                  // reference of a share that saw no token
 constexpr float kSlack = 8.f;                   // a weight may pass its place by 2^8 before the reference moves
@@ -490,69 +493,79 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       const uint32_t sb = smem_u32(&S.stage[stage][sub * kSub]);
 
       // logits of tokens g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1 (log2 units), less the rows' references
+      auto words_at = [&](int i, int x, int side, uint32_t (&w)[NG]) {  // a token's scales and minima
+        const uint8_t* at = &S.stage[stage][(sub + i) * kSub + 2048 + 8 * NG * (g8 + 8 * x) + 4 * NG * side];
+        if (NG == 2) {
+          const uint2 y = *(const uint2*)at;
+          w[0] = y.x, w[NG - 1] = y.y;
+        } else {
+          w[0] = *(const uint32_t*)at;
+        }
+      };
       float l[NS][NT][4];
-      float vs[NS][2][NG], vm[NS][2][NG];
       {
         uint4 kc[NS][2];
+        float ks[NS][2][NG];
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
           kc[i][0] = lds128(sb + i * kSub + 16 * lane);
           kc[i][1] = lds128(sb + i * kSub + 512 + 16 * lane);
-        }
-        float s[NS][NT][NG][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
-              const uint4 q = S.frag[lo][nt][j][lane];
-#pragma unroll
-              for (int i = 0; i < NS; ++i) {
-                const uint32_t x0 = comp(kc[i][0], j), x1 = comp(kc[i][1], j), y0 = x0 >> 8, y1 = x1 >> 8;
-                float(&d)[4] = s[i][nt][NG == 2 ? j >> 1 : 0];
-                if (lo == 0 && (j == 0 || (NG == 2 && j == 2)))
-                  mma_16816_first(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
-                else
-                  mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
-                mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
-              }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          float ks[2][NG], km[2][NG];
+          float km[2][NG];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            uint32_t kw[NG], vw[NG];
-            const uint8_t* meta = &S.stage[stage][(sub + i) * kSub + 2048];
-            if (NG == 2) {
-              const uint4 w = *(const uint4*)(meta + 16 * (g8 + 8 * x));
-              kw[0] = w.x, kw[NG - 1] = w.y, vw[0] = w.z, vw[NG - 1] = w.w;
-            } else {
-              const uint2 w = *(const uint2*)(meta + 8 * (g8 + 8 * x));
-              kw[0] = w.x, vw[0] = w.y;
-            }
+            uint32_t w[NG];
+            words_at(i, x, 0, w);
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              ks[x][g] = word_scale(kw[g]) * dot_scale;
-              km[x][g] = word_min(kw[g]);
-              vs[i][x][g] = word_scale(vw[g]);
-              vm[i][x][g] = word_min(vw[g]);
-            }
+            for (int g = 0; g < NG; ++g) ks[i][x][g] = word_scale(w[g]) * dot_scale, km[x][g] = word_min(w[g]);
           }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              float y = fmaf(km[x >> 1][0], qs[nt][x & 1][0], -ref[nt][x & 1]);
-              if (NG == 2) y = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], y);
-              y = fmaf(ks[x >> 1][0], s[i][nt][0][x], y);
-              if (NG == 2) y = fmaf(ks[x >> 1][NG - 1], s[i][nt][NG - 1][x], y);
-              l[i][nt][x] = y;
+              l[i][nt][x] = fmaf(km[x >> 1][0], qs[nt][x & 1][0], -ref[nt][x & 1]);
+              if (NG == 2) l[i][nt][x] = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], l[i][nt][x]);
             }
         }
+        // (sums of 64 dimensions each, the low halves first: the tensor cores cut what they add off at the sum's size)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float s[NS][NT][4];
+#pragma unroll
+          for (int lo = HILO ? 1 : 0; lo >= 0; --lo)
+#pragma unroll
+            for (int j = 2 * half; j < 2 * half + 2; ++j)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const uint4 q = S.frag[lo][nt][j][lane];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                  const uint32_t x0 = comp(kc[i][0], j), x1 = comp(kc[i][1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+                  float(&d)[4] = s[i][nt];
+                  if (lo == (HILO ? 1 : 0) && j == 2 * half)
+                    mma_16816_first(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+                  else
+                    mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+                  mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
+                }
+              }
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) l[i][nt][x] = fmaf(ks[i][x >> 1][half * (NG - 1)], s[i][nt][x], l[i][nt][x]);
+        }
       }
+      float vs[NS][2][NG], vm[NS][2][NG];
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint32_t w[NG];
+          words_at(i, x, 1, w);
+#pragma unroll
+          for (int g = 0; g < NG; ++g) vs[i][x][g] = word_scale(w[g]), vm[i][x][g] = word_min(w[g]);
+        }
       uint4 vc[NS][2];
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
@@ -653,8 +666,15 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
                 if (kEdge && l[i][nt][x] == kNegInf) u[x] = m = 0.f;  // a NaN that this row does not see
                 mins[nt][x & 1][g] = fmaf(p[x], m, mins[nt][x & 1][g]);
               }
-              w0[nt][g] = transpose_8x8(half2_bits(u[0], u[1]));
-              w1[nt][g] = transpose_8x8(half2_bits(u[2], u[3]));
+              const uint32_t h0 = half2_bits(u[0], u[1]), h1 = half2_bits(u[2], u[3]);
+              if (v.half) {
+                // An fp16 result is as fine as the weights: what their rounding takes from a code of 7.5, the middle, goes to
+                // the sums of the minima, so that only a code's distance from the middle feels it.
+                mins[nt][0][g] = fmaf(7.5f, (u[0] - word_scale(h0)) + (u[2] - word_scale(h1)), mins[nt][0][g]);
+                mins[nt][1][g] = fmaf(7.5f, (u[1] - word_min(h0)) + (u[3] - word_min(h1)), mins[nt][1][g]);
+              }
+              w0[nt][g] = transpose_8x8(h0);
+              w1[nt][g] = transpose_8x8(h1);
             }
           }
         };
@@ -835,7 +855,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_join_kernel(const _
 constexpr size_t kShareDescBytes = (kPagedMaxGrid * sizeof(int4) + 255) & ~(size_t)255;
 
 static_assert(sizeof(Smem<1>) <= 115712, "two CTAs of an SM share 228 KiB, 1 KiB each of it taken");
-static_assert(sizeof(Smem<2>) <= 232448 && sizeof(Smem<4>) <= 232448, "shared memory of a CTA");
+static_assert(sizeof(Smem<2>) <= 232448, "shared memory of a CTA");
 
 template <int NG, int NT, bool HILO, bool SEL>
 int launch(const AttnArgs& a, int dev, int sms, cudaStream_t stream) {
@@ -862,11 +882,7 @@ int launch_ng(const AttnArgs& a, int dev, int sms, cudaStream_t s) {
 }
 template <bool HILO, bool SEL>
 int launch_nt(const AttnArgs& a, int unit_rows, int dev, int sms, cudaStream_t s) {
-  switch (unit_rows) {
-    case 8: return launch_ng<1, HILO, SEL>(a, dev, sms, s);
-    case 16: return launch_ng<2, HILO, SEL>(a, dev, sms, s);
-    default: return launch_ng<4, HILO, SEL>(a, dev, sms, s);
-  }
+  return unit_rows == 8 ? launch_ng<1, HILO, SEL>(a, dev, sms, s) : launch_ng<2, HILO, SEL>(a, dev, sms, s);
 }
 
 }  // namespace
