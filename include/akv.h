@@ -665,7 +665,8 @@ akv_status akv_paged_attn(const akv_paged_params* p, const akv_pages* pages, int
  * the page's own exponent e_p (clamped to +-100);
  *     score = 2^e_p max over the G rows of sum_d max(q^_d lo^_d, q^_d hi^_d),
  * whose sums are exact: the choice does not depend on an order of additions.  A page with an
- * infinite or NaN bound has the score +infinity; a page number outside the pool -infinity. */
+ * infinite or NaN bound has the score +infinity; a page number outside the pool -infinity; with an
+ * infinite or NaN query in the group all pages have the score 0. */
 akv_status akv_paged_select_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
                                            size_t* ws_bytes);
 akv_status akv_paged_select(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
@@ -678,8 +679,8 @@ akv_status akv_pages_copy(const akv_paged_params* p, const akv_pages* pages, con
                           int32_t n, akv_stream_t stream);
 
 /* Row dst[i] of the table becomes a second holder of the pages with tokens of row src[i] (device
- * int32 [n]), at its length; no page is copied.  dst rows must hold no pages, each once; pairs
- * with a row outside the table, or with dst = src, are left out. */
+ * int32 [n]), at its length; no page is copied.  dst rows must hold no pages, each is named once
+ * and none is a src as well; pairs with a row outside the table, or with dst = src, are left out. */
 akv_status akv_pages_fork(const akv_paged_params* p, const akv_pages* pages, const int32_t* src, const int32_t* dst,
                           int32_t n, akv_stream_t stream);
 

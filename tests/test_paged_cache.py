@@ -535,3 +535,68 @@ def test_calls_repeat_bit_for_bit():
     for _ in range(5):
         again = attend(c, q)
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+# ---- rows that are not aligned -----------------------------------------------------------
+
+
+@pytest.mark.parametrize("half,rotate", [(False, True), (True, False)])
+def test_rows_at_odd_addresses(half, rotate):
+    """Keys, values, queries and outputs two bytes off every alignment give what aligned ones give, bit for bit."""
+    p = params(2, 4, 32, 64, half, rotate, bounds=True)
+    c, d = Cache(p, [100, 45], seed=16), Cache(p, [100, 45], seed=16)
+
+    def odd(t):
+        wide = torch.zeros((*t.shape[:-1], D + 3), dtype=t.dtype, device="cuda")
+        view = wide[..., 1 : D + 1]
+        view.copy_(t)
+        assert view.data_ptr() % 4 == 2
+        return view
+
+    k, v = c.rows(100)
+    n = torch.tensor([100, 45], dtype=torch.int32, device="cuda")
+    akv.akv_paged_append(p, c.pages, k, v, n_new=n)
+    akv.akv_paged_append(p, d.pages, odd(k), odd(v), n_new=n)
+    c.lens.copy_(n), d.lens.copy_(n)
+    assert torch.equal(c.pool, d.pool)
+    k2, v2, k3, v3 = torch.empty_like(k), torch.empty_like(v), odd(k), odd(v)
+    akv.akv_paged_read(p, c.pages, k2, v2)
+    akv.akv_paged_read(p, d.pages, k3, v3)
+    assert torch.equal(k2, k3) and torch.equal(v2, v3)
+    q = queries(c, 2)
+    sel, sel2 = selection(c, 2, 2), selection(c, 2, 2)
+    akv.akv_paged_select(p, c.pages, q, sel)
+    akv.akv_paged_select(p, d.pages, odd(q), sel2)
+    assert torch.equal(sel.pages, sel2.pages)
+    out, out2 = torch.empty_like(q), odd(q)
+    akv.akv_paged_attn(p, c.pages, q, out, sm_scale=0.1)
+    akv.akv_paged_attn(p, d.pages, odd(q), out2, sm_scale=0.1)
+    assert torch.equal(out, out2)
+
+
+def test_many_tiles_per_cta_repeat_bit_for_bit():
+    """Long requests with cold caches, one scale a row: copies that come out of order change nothing."""
+    for group, G, T in ((128, 4, 1), (64, 8, 1), (128, 4, 4)):
+        p = params(8, G, 64, group, False, False)
+        n_pages = 4 * 1024
+        gen = torch.Generator(device="cuda").manual_seed(17)
+        pool = torch.zeros((1, n_pages, 8, 4, 2048 + 128 * (D // group)), dtype=torch.uint8, device="cuda")
+        pool[..., :2048] = torch.randint(0, 256, pool[..., :2048].shape, generator=gen, device="cuda", dtype=torch.uint8)
+        words = torch.rand(pool[..., 2048:].shape[:-1] + (64 * (D // group), ), generator=gen, device="cuda")
+        words[..., 0::2] = 0.1 + 0.1 * words[..., 0::2]  # scales
+        words[..., 1::2] = -1.0 - words[..., 1::2]  # minima
+        pool[..., 2048:] = words.half().view(torch.uint8)
+        table = torch.randperm(n_pages, generator=gen, device="cuda").int().view(4, 1024)
+        lens = torch.tensor([65536, 65000, 40001, 65535], dtype=torch.int32, device="cuda")
+        pages = akv.Pages(p, pool.view(1, n_pages, -1), table, lens)
+        q = torch.randn((4, T, 8 * G, D), generator=gen, device="cuda").to(torch.bfloat16)
+        flush = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")
+        first = None
+        for _ in range(20):
+            flush.zero_()
+            out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+            akv.akv_paged_attn(p, pages, q, out, lse=lse, sm_scale=0.1)
+            assert bool(torch.isfinite(lse).all())
+            if first is None:
+                first = out, lse
+            assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
