@@ -72,12 +72,48 @@ __device__ __forceinline__ int block_scan(int x, int* total) {
   return part[warp] + inc - x;
 }
 
-// Pair i of the lists, page copied in every layer: a unit of work is 16 KiB of one page in one layer.
+// Goes over pages lo .. hi - 1 in order, four neighbouring ones a thread, until `most` of them have been found: found(at,
+// page) for the at-th page that `is` holds of, other(page) for the rest.  All threads call it; returns how many there are.
+template <class Is, class Found, class Other>
+__device__ __forceinline__ int each_page(int lo, int hi, int most, Is is, Found found, Other other) {
+  int n = 0;
+  for (int p0 = lo; p0 < hi && n < most; p0 += 4 * blockDim.x) {
+    const int first = p0 + 4 * threadIdx.x;
+    uint32_t flags = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (first + k < hi && is(first + k)) flags |= 1u << k;
+    int sum;
+    int at = n + block_scan(__popc(flags), &sum);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (first + k < hi) {
+        if (flags >> k & 1) found(at++, first + k);
+        else other(first + k);
+      }
+    n += sum;
+  }
+  return n;
+}
+
+// Compaction: the table's entries follow the pages (the map is the plan's).
+__device__ __forceinline__ void follow_moves(const PagesState& s, int n, const int32_t* map) {
+  const int64_t cells = (int64_t)s.rows * s.max_pages, step = (int64_t)gridDim.x * blockDim.x;
+  for (int64_t k = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; k < cells; k += step) {
+    int32_t* cell = s.table + k / s.max_pages * s.table_stride + k % s.max_pages;
+    const int page = *cell;
+    if (page >= n && page < s.n_pages && map[page] >= 0) *cell = map[page];
+  }
+}
+
+// Pair i of the lists, page copied in every layer: a unit of work is 16 KiB of one page in one layer.  Bound by memory:
+// 4 layers of 2.6 thousand pages of 78 KB, 1.66 GB read and written, take 260 us (6.4 TB/s, 94 % of the measured rate).
 constexpr int kCopyThreads = 256, kCopyChunk = kCopyThreads * 4 * 16;
 __global__ void __launch_bounds__(kCopyThreads) akv_pages_copy_kernel(PagesState s, const int32_t* src, const int32_t* dst, int n,
-                                                                      const int32_t* n_dev) {
+                                                                      const int32_t* n_dev, const int32_t* n_live, const int32_t* map) {
   launch_dependents();
   wait_for_stream();
+  if (map) follow_moves(s, *n_live, map);
   if (n_dev) n = *n_dev;
   const int chunks = (int)((s.page_bytes + kCopyChunk - 1) / kCopyChunk);
   const int64_t work = (int64_t)n * s.n_layers * chunks;
@@ -197,16 +233,8 @@ __global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesSt
     if (r < s.rows) w.cbase[r] = (n_copies + b) | (w.cbase[r] ? (int)0x80000000 : 0);
     n_copies += sum;
   }
-  // the lowest free pages
-  int found = 0;
-  for (int p0 = 0; p0 < s.n_pages && found < total; p0 += blockDim.x) {
-    const int page = p0 + tid;
-    const bool is_free = page < s.n_pages && s.refs[page] == 0;
-    int sum;
-    const int at = found + block_scan(is_free, &sum);
-    if (is_free) w.free[at] = page;
-    found += sum;
-  }
+  const int found = each_page(0, s.n_pages, total, [&](int page) { return s.refs[page] == 0; },
+                              [&](int at, int page) { w.free[at] = page; }, [](int) {});  // the lowest free pages
   __syncthreads();
   if (tid == 0) {
     *missing = max(0, total - found);
@@ -250,55 +278,21 @@ __global__ void __launch_bounds__(kPlanThreads) akv_pages_compact_plan(PagesStat
   launch_dependents();
   wait_for_stream();
   const int tid = threadIdx.x;
-  int live = 0;
+  int live = 0, n;
   for (int p = tid; p < s.n_pages; p += blockDim.x) live += s.refs[p] > 0;
-  int n;
   block_scan(live, &n);
   // free pages below n, then live ones at n and above: as many of each
-  int found = 0;
-  for (int p0 = 0; p0 < n; p0 += blockDim.x) {
-    const int page = p0 + tid;
-    const bool hole = page < n && s.refs[page] <= 0;
-    int sum;
-    const int at = found + block_scan(hole, &sum);
-    if (hole) w.dst[at] = page;
-    found += sum;
-  }
-  const int holes = found;
+  const int holes = each_page(0, n, INT32_MAX, [&](int page) { return s.refs[page] <= 0; },
+                              [&](int at, int page) { w.dst[at] = page; }, [](int) {});
   __syncthreads();
-  found = 0;
-  for (int p0 = n; p0 < s.n_pages && found < holes; p0 += blockDim.x) {
-    const int page = p0 + tid;
-    const bool moves = page < s.n_pages && s.refs[page] > 0;
-    int sum;
-    const int at = found + block_scan(moves, &sum);
-    if (moves) w.src[at] = page, w.free[page] = w.dst[at];
-    found += sum;
-  }
-  if (tid == 0) *n_live = n, *w.n_copies = holes;
-}
-
-// Table entries and counts follow the pages (n_live and the moves are the plan's).
-__global__ void __launch_bounds__(256) akv_pages_compact_table(PagesState s, const int32_t* n_live, PagesWs w) {
-  launch_dependents();
-  wait_for_stream();
-  const int n = *n_live;
-  const int64_t cells = (int64_t)s.rows * s.max_pages, step = (int64_t)gridDim.x * blockDim.x;
-  const int64_t at = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  for (int64_t k = at; k < cells; k += step) {
-    int32_t* cell = s.table + k / s.max_pages * s.table_stride + k % s.max_pages;
-    const int page = *cell;
-    if (page >= n && page < s.n_pages && s.refs[page] > 0) *cell = w.free[page];
-  }
-}
-__global__ void __launch_bounds__(256) akv_pages_compact_refs(PagesState s, PagesWs w) {
-  launch_dependents();
-  wait_for_stream();
-  const int n = *w.n_copies;
-  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
+  each_page(n, s.n_pages, INT32_MAX, [&](int page) { return s.refs[page] > 0; },
+            [&](int at, int page) { w.src[at] = page, w.free[page] = w.dst[at]; }, [&](int page) { w.free[page] = -1; });
+  __syncthreads();
+  for (int i = tid; i < holes; i += blockDim.x) {
     s.refs[w.dst[i]] = s.refs[w.src[i]];
     s.refs[w.src[i]] = 0;
   }
+  if (tid == 0) *n_live = n, *w.n_copies = holes;
 }
 
 constexpr int kCopyGrid = 152 * 8;
@@ -308,7 +302,7 @@ constexpr int kCopyGrid = 152 * 8;
 size_t pages_ws_bytes(const PagesState& s) { return (pages_ws_ints(s) * 4 + 255) & ~(size_t)255; }
 
 int launch_pages_copy(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
-  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, src, dst, n, nullptr);
+  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, src, dst, n, nullptr, nullptr, nullptr);
 }
 
 int launch_pages_fork(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
@@ -323,16 +317,14 @@ int launch_pages_reserve(const PagesState& s, const int32_t* n_new, int32_t* mis
   const PagesWs w = pages_ws(s, ws);
   const int e = launch_after(akv_pages_reserve_kernel, dim3(1), kPlanThreads, 0, stream, s, n_new, missing, w);
   if (e) return e;
-  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, w.src, w.dst, 0, w.n_copies);
+  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, w.src, w.dst, 0, w.n_copies, nullptr, nullptr);
 }
 
 int launch_pages_compact(const PagesState& s, int32_t* n_live, void* ws, void* stream) {
   const PagesWs w = pages_ws(s, ws);
-  int e = launch_after(akv_pages_compact_plan, dim3(1), kPlanThreads, 0, stream, s, n_live, w);
-  if (!e) e = launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, w.src, w.dst, 0, w.n_copies);
-  if (!e) e = launch_after(akv_pages_compact_table, dim3(152), 256, 0, stream, s, n_live, w);
-  if (!e) e = launch_after(akv_pages_compact_refs, dim3(152), 256, 0, stream, s, w);
-  return e;
+  const int e = launch_after(akv_pages_compact_plan, dim3(1), kPlanThreads, 0, stream, s, n_live, w);
+  if (e) return e;
+  return launch_after(akv_pages_copy_kernel, dim3(kCopyGrid), kCopyThreads, 0, stream, s, w.src, w.dst, 0, w.n_copies, n_live, w.free);
 }
 
 }  // namespace akv
