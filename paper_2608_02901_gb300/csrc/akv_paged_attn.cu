@@ -1,6 +1,12 @@
 // Attention over the paged 4-bit cache: a persistent launch that reads each attended page once, and a launch that joins
 // the shares of units that several CTAs worked on.
 //
+// Bound by HBM in principle (144 bytes a token and head at two groups a row, 2 x 16 products of 16 x 16 x 8), by the integer
+// operations and the latency of a warp's chain in practice: 4 x 131072 tokens, 8 KV heads, 4 or 8 query heads each, take
+// 115 to 121 us (5.0 TB/s, 74 % of the measured rate), rotated 135 (half as many products again), with 16 query rows 163;
+// 8 x 131072 rotated tokens 230 us (5.3 TB/s).  A call has about 8 us that do not depend on the length: the plan, the
+// first page numbers and copies, the joins (1021 tokens: 7 us, and 4 of the second launch).
+//
 // A unit is one KV head of one request (or of one query token, where each has its own pages) with up to 8 NT query
 // rows.  Units are cut into tiles of 128 tokens, and the tiles of all units into equal contiguous ranges, one per CTA,
 // so that one long request and many short ones fill the GPU alike.  In a CTA one warp copies (bulk copies of whole
@@ -219,7 +225,8 @@ struct Smem {
   float qmax[kWarps];
   int pos[kStages][kTileSubs];              // first token of each sub-block; -1: none, -2: a page outside the pool
   uint32_t tile[kStages];                   // the CTA's tile that the stage holds or waits for
-  int64_t strip[kThreads + 1];
+  int cursor[kWarps][10];                   // a warp's place, kept here while it works on a unit (registers are short)
+  int64_t strip[kThreads + 1], range_lo, range_total;
   uint64_t full[kStages], empty[kStages];
   int failed;
 };
@@ -335,14 +342,38 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 
   // ---- the computing warps
   const int g8 = lane >> 2, t4 = lane & 3;
-  int64_t k = r.lo;
-  while (k < r.hi) {
-    const int b = c.g.b;
-    const int h = SEL ? c.g.h : c.index / a.n_blocks;
-    const int row0 = (SEL ? c.index : c.index % a.n_blocks) * kRows;
+  const uint32_t range = (uint32_t)(r.hi - r.lo);  // tiles of the CTA
+  auto keep = [&](const Cursor<SEL>& x) {
+    __syncwarp();
+    if (lane == 0) {
+      volatile int* to = S.cursor[warp];
+      to[0] = x.gi, to[1] = x.index, to[2] = x.ti, to[3] = x.tiles, to[4] = x.g.b, to[5] = x.g.t, to[6] = x.g.h;
+      to[7] = x.g.tokens, to[8] = x.g.sees;
+    }
+    __syncwarp();
+  };
+  auto kept = [&]() {
+    const volatile int* from = S.cursor[warp];
+    Cursor<SEL> x;
+    x.gi = from[0], x.index = from[1], x.ti = from[2], x.tiles = from[3], x.g.b = from[4], x.g.t = from[5], x.g.h = from[6];
+    x.g.tokens = from[7], x.g.sees = from[8];
+    return x;
+  };
+  auto tiles_here = [&](const Cursor<SEL>& x, uint32_t at) { return (int)min((uint32_t)(x.tiles - x.ti), range - at); };
+  keep(c);
+  if (tid == 0) S.range_lo = r.lo, S.range_total = r.total;  // (read by the same thread)
+  uint32_t at = 0;  // tiles done
+  while (at < range) {
+    int row0, n_tiles, sees, all_see;
+    float dot_scale;
+    {
+    const Cursor<SEL> cu = kept();
+    const int b = cu.g.b, h = SEL ? cu.g.h : cu.index / a.n_blocks;
+    row0 = (SEL ? cu.index : cu.index % a.n_blocks) * kRows;
     const int n_rows = min(kRows, a.rows - row0);
-    const int n_tiles = (int)min((int64_t)(c.tiles - c.ti), r.hi - k);
-    const bool from_start = c.ti == 0, to_end = c.ti + n_tiles == c.tiles;
+    n_tiles = tiles_here(cu, at);
+    sees = cu.g.sees;
+    all_see = SEL ? sees : sees - a.T + 1;  // every row of the unit sees the tokens before this one
 
     // queries: a warp per row, four dimensions a lane
     constexpr int kTurns = (kRows + kWarps - 1) / kWarps;
@@ -354,7 +385,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 #pragma unroll
       for (int e = 0; e < 4; ++e) qx[i][e] = 0.f;
       if (rr < n_rows) {
-        const int t = SEL ? c.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
+        const int t = SEL ? cu.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
         const uint16_t* row = a.q + b * a.qb + t * a.qt + (int64_t)(h * v.G + g) * a.qh + 4 * lane;
         if (((uintptr_t)row & 7) == 0) {
           const uint2 w = *(const uint2*)row;
@@ -411,12 +442,13 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         f[lo] = make_uint4(w[0], w[1], w[2], w[3]);
       }
       // lanes 2 x and 2 x + 1 hold dimensions 8 x ..: word j = x / 4, operand lane 4 row + x % 4
-      const int at = 4 * (rr & 7) + (lane >> 1 & 3);
-      if (!(lane & 1)) S.frag[0][rr >> 3][lane >> 3][at] = f[0];
-      if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][at] = f[HILO ? 1 : 0];
+      const int to = 4 * (rr & 7) + (lane >> 1 & 3);
+      if (!(lane & 1)) S.frag[0][rr >> 3][lane >> 3][to] = f[0];
+      if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][to] = f[HILO ? 1 : 0];
     }
     named_sync(kConsumerBar, 32 * kWarps);
-    const float dot_scale = a.scale * pow2(10 + e_q);  // codes count 2^-24, queries 2^(14 - e)
+    dot_scale = a.scale * pow2(10 + e_q);  // codes count 2^-24, queries 2^(14 - e)
+    }
     float qs[NT][2][NG];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -442,9 +474,6 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         for (int g = 0; g < NG; ++g) mins[nt][x][g] = 0.f;
       }
     }
-    // every row of the unit sees the tokens before this one
-    const int all_see = SEL ? c.g.sees : c.g.sees - a.T + 1;
-
     auto spoil = [&]() {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = __int_as_float(0x7fffffff);
@@ -452,7 +481,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 
     for (int item = warp; item < n_tiles * (kTileSubs / NS); item += kWarps) {
       const int sub = item % (kTileSubs / NS) * NS;
-      const uint32_t tile = (uint32_t)(k - r.lo) + item / (kTileSubs / NS);  // of the CTA's
+      const uint32_t tile = at + item / (kTileSubs / NS);  // of the CTA's
       const int stage = tile % kStages;
       const uint32_t bar = smem_u32(&S.full[stage]), parity = tile / kStages & 1;
       // A warp passes over tiles that it has no part of, so the parity alone could be that of a phase long ago: the stage
@@ -579,7 +608,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         for (int i = 0; i < NS; ++i) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const bool held = pos[i] + g8 + 8 * x < c.g.sees;
+            const bool held = pos[i] + g8 + 8 * x < sees;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
               vs[i][x][g] = held ? vs[i][x][g] : 0.f;
@@ -591,8 +620,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int row = row0 + 8 * nt + 2 * t4 + (x & 1);
-              const int sees = SEL ? c.g.sees : min(c.g.sees, all_see + row / v.G);
-              if (pos[i] + g8 + 8 * (x >> 1) >= sees) l[i][nt][x] = kNegInf;
+              if (pos[i] + g8 + 8 * (x >> 1) >= (SEL ? sees : min(sees, all_see + row / v.G))) l[i][nt][x] = kNegInf;
             }
         }
       }
@@ -724,7 +752,9 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         }
     }
     named_sync(kConsumerBar, 32 * kWarps);
-    const bool whole = from_start && to_end;
+    Cursor<SEL> cu = kept();
+    const int b = cu.g.b, h = SEL ? cu.g.h : cu.index / a.n_blocks, n_rows = min(kRows, a.rows - row0);
+    const bool from_start = cu.ti == 0, to_end = cu.ti + n_tiles == cu.tiles, whole = from_start && to_end;
     float* slot = a.slots + (2 * (size_t)blockIdx.x + (from_start ? 1 : 0)) * paged_slot_floats(kRows);
 #pragma unroll 1
     for (int rr = warp; rr < n_rows; rr += kWarps) {
@@ -755,7 +785,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(y[e] * 0.0625f) ^ sign_flip(v, 4 * lane + e));
       }
-      const int t = SEL ? c.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
+      const int t = SEL ? cu.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
       uint16_t* row = a.out + b * a.ob + t * a.ot + (int64_t)(h * v.G + g) * a.oh + 4 * lane;
 #pragma unroll
       for (int e = 0; e < 4; ++e) row[e] = float_to_row(y[e], v.half);
@@ -764,16 +794,20 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     }
     if (from_start && !to_end && tid == 0) {
       // the CTA of the unit's last tile: (x + 1) ctas - 1 over the tiles of all
-      const int64_t last = k - c.ti + c.tiles - 1;
-      a.desc[blockIdx.x] = make_int4(c.gi, c.index, (int)(((last + 1) * r.ctas - 1) / r.total), 1);
+      const int64_t total = S.range_total, last = S.range_lo + at + cu.tiles - 1;
+      const int64_t ctas = min((int64_t)gridDim.x, total);
+      a.desc[blockIdx.x] = make_int4(cu.gi, cu.index, (int)(((last + 1) * ctas - 1) / total), 1);
     }
-    k += n_tiles;
-    c.next_unit(a);
+    at += (uint32_t)n_tiles;
+    if (at < range) {
+      cu.next_unit(a);
+      keep(cu);
+    }
   }
 }
 
 // Joins the shares of the unit that starts in CTA blockIdx.x and goes on in others: one CTA per query row, its warps
-// take the shares in turn.
+// take the shares in turn.  Latency alone: 4 to 6 us after the attention's last CTA by itself, about 3 as its dependent.
 constexpr int kJoinWarps = 8;
 template <bool SEL>
 __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_join_kernel(const __grid_constant__ AttnArgs a, int kRows) {
