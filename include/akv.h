@@ -26,7 +26,7 @@
  *    akv_last_error() returns a thread-local text for the last failure.
  *  - bf16 / fp16 values are passed as their 16-bit IEEE encodings.
  *  - head_dim is 128.  The query-group size G = n_q_heads / n_kv_heads must be
- *    1, 2, 4 or 8; query head j reads KV head floor(j / G).
+ *    1, 2, 4 or 8 (the paged cache: 1 to 64); query head j reads KV head floor(j / G).
  *
  * The byte layout of the arena is normative and documented with the
  * akv_arena_header and akv_unit_desc structures below.
