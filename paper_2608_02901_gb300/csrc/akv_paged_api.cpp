@@ -172,10 +172,10 @@ akv_status akv_paged_append(const akv_paged_params* p, const akv_pages* pages, i
   PagedCall c;
   AKV_TRY(check_layer(p, pages, layer, &c));
   if (T < 0) return fail(AKV_ERR_INVALID, "negative T");
+  if (T == 0) return AKV_OK;  // (empty tensors have no address)
   AKV_TRY(check_rows(K, "K"));
   AKV_TRY(check_rows(V, "V"));
   if ((uintptr_t)n_new % 4) return fail(AKV_ERR_INVALID, "n_new must be 4-byte aligned");
-  if (T == 0) return AKV_OK;
   return launched(launch_paged_append(c.v, *K, *V, T, n_new, (void*)stream), "append");
 }
 
@@ -184,10 +184,10 @@ akv_status akv_paged_read(const akv_paged_params* p, const akv_pages* pages, int
   PagedCall c;
   AKV_TRY(check_layer(p, pages, layer, &c));
   if (T < 0) return fail(AKV_ERR_INVALID, "negative T");
+  if (T == 0) return AKV_OK;
   AKV_TRY(check_written(K, "K", pages->rows, T, p->n_kv_heads));
   AKV_TRY(check_written(V, "V", pages->rows, T, p->n_kv_heads));
   if ((uintptr_t)start % 4) return fail(AKV_ERR_INVALID, "start must be 4-byte aligned");
-  if (T == 0) return AKV_OK;
   return launched(launch_paged_read(c.v, start, *K, *V, T, (void*)stream), "read");
 }
 

@@ -7,7 +7,7 @@ converts only what changes.
 from __future__ import annotations
 
 import ctypes
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 
 AKV_FLAG_BOUNDS = 8
 AKV_DTYPE_BF16, AKV_DTYPE_FP16 = 0, 1
@@ -95,17 +95,19 @@ def akv_paged_page_bytes(p: PagedParams) -> int:
 
 
 _loaded = None
-_torch = None
+_torch = _bf16 = _fp16 = _int32 = _raw_stream = None
 
 
 def _lib():
     """The library; torch is loaded with it."""
-    global _loaded, _torch
+    global _loaded, _torch, _bf16, _fp16, _int32, _raw_stream
     if _loaded is None:
         import torch
 
         from . import lib
-        _torch, _loaded = torch, lib()
+        _torch, _bf16, _fp16, _int32 = torch, torch.bfloat16, torch.float16, torch.int32
+        _raw_stream = torch._C._cuda_getCurrentRawStream
+        _loaded = lib()
     return _loaded
 
 
@@ -118,20 +120,17 @@ def _check(status, where):
 def _stream(stream, pages):
     """Address of a stream: the current one of the pool's device for None."""
     if stream is None:
-        return _torch._C._cuda_getCurrentRawStream(pages.index)
+        return _raw_stream(pages.index)
     return getattr(stream, "cuda_stream", stream)
 
 
-def _ints(t, what, n=None, device=None):
-    """Address of a contiguous CUDA int32 tensor (with n elements), or None for None."""
+def _ints(t, what, n, index):
+    """Address of a contiguous CUDA int32 tensor of n elements (None: any number) on device `index`, or None for None."""
     if t is None:
         return None
-    if t.dtype is not _torch.int32 or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor")
-    if n is not None and t.numel() != n:
-        raise ValueError(f"{what} must hold {n} numbers")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what} must be on the pool's device")
+    if t.dtype is not _int32 or t.get_device() != index or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{what} must be a contiguous CUDA int32 tensor on the pool's device"
+                         + ("" if n is None else f" and hold {n} numbers"))
     return t.data_ptr()
 
 
@@ -152,7 +151,7 @@ class Pages:
         n_layers, n_pages = int(pool.shape[0]), int(pool.shape[1])
         if pool[0].numel() * pool.element_size() != n_pages * page or not pool[0].is_contiguous():
             raise ValueError(f"pool must hold pages of {page} contiguous bytes")
-        if not table.is_cuda or table.dtype is not _torch.int32 or table.dim() != 2 or table.stride(1) != 1:
+        if not table.is_cuda or table.dtype is not _int32 or table.dim() != 2 or table.stride(1) != 1:
             raise ValueError("table must be a CUDA int32 tensor [rows][max_pages] with adjacent columns")
         if table.device != pool.device:
             raise ValueError("table must be on the pool's device")
@@ -164,7 +163,7 @@ class Pages:
         self._params = p.c()
         self._c = _Pages(pool.data_ptr(), (n_layers - 1) * stride + n_pages * page, stride, n_layers, n_pages,
                          table.data_ptr(), table.stride(0) if rows > 1 else max(table.stride(0), most), rows, most,
-                         _ints(lens, "lens", rows, pool.device), _ints(refs, "refs", n_pages, pool.device))
+                         _ints(lens, "lens", rows, self.index), _ints(refs, "refs", n_pages, self.index))
         self.pref, self.ref = ctypes.byref(self._params), ctypes.byref(self._c)
 
 
@@ -176,7 +175,9 @@ class PageSelection:
         if pages.dim() != 4 or tuple(count.shape) != tuple(pages.shape[:3]):
             raise ValueError("selection: pages [rows][T][n_kv_heads][top] and count [rows][T][n_kv_heads]")
         self.pages, self.count, self.top = pages, count, int(pages.shape[3])
-        self._c = _Selection(_ints(pages, "selection pages"), _ints(count, "selection count", None, pages.device), self.top)
+        _lib()
+        self._c = _Selection(_ints(pages, "selection pages", None, pages.get_device()),
+                             _ints(count, "selection count", None, pages.get_device()), self.top)
         self.ref = ctypes.byref(self._c)
 
 
@@ -184,19 +185,17 @@ def _params(p: PagedParams, pages: Pages):
     """The C parameters of p, which describes the pool's pages (its query heads may differ)."""
     if p is pages.p:
         return pages.pref
-    if akv_paged_page_bytes(p) != akv_paged_page_bytes(pages.p):
-        raise ValueError("the parameters' pages are not the pool's")
+    if replace(p, n_q_heads=pages.p.n_q_heads) != pages.p:
+        raise ValueError("the parameters are not those of the pool's pages")
     return ctypes.byref(p.c())
 
 
 def _rows(t, what, p: PagedParams, pages: Pages, T, heads):
     """The C view of a [rows][T][heads][128] tensor of the cache's type, any strides but adjacent values."""
-    if t.dtype is not (_torch.float16 if p.half else _torch.bfloat16) or not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA tensor of {'fp16' if p.half else 'bf16'}")
+    if t.dtype is not (_fp16 if p.half else _bf16) or t.get_device() != pages.index:
+        raise ValueError(f"{what} must be a CUDA tensor of {'fp16' if p.half else 'bf16'} on the pool's device")
     if t.shape != (pages.rows, T, heads, 128):
         raise ValueError(f"{what} must be [{pages.rows}][{T}][{heads}][128], got {list(t.shape)}")
-    if t.device != pages.device:
-        raise ValueError(f"{what} must be on the pool's device")
     sb, st, sh, sd = t.stride()
     if sd != 1:
         raise ValueError(f"{what} must have adjacent values in its last axis")
@@ -209,13 +208,14 @@ def _tokens(t, what):
     return t.shape[1]
 
 
-def _workspace(ws, need, pages, stream):
+def _workspace(ws, pages, stream, size, *args):
+    """ws, its address and its bytes; one of size(*args) bytes from torch's allocator for None."""
     if ws is None:
-        ws = _torch.empty(need(), dtype=_torch.uint8, device=pages.device)
+        ws = _torch.empty(size(*args), dtype=_torch.uint8, device=pages.device)
         if stream is not None:  # the allocator must not hand it out again before that stream is done with it
             ws.record_stream(stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(stream, pages.device))
-    elif not ws.is_cuda or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous CUDA tensor")
+    elif ws.get_device() != pages.index or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous CUDA tensor on the pool's device")
     return ws, ws.data_ptr(), ws.nbytes
 
 
@@ -224,7 +224,7 @@ def akv_paged_append(p: PagedParams, pages: Pages, K, V, n_new=None, layer: int 
     T = _tokens(K, "K")
     _check(_lib().akv_paged_append(_params(p, pages), pages.ref, layer, _rows(K, "K", p, pages, T, p.n_kv_heads),
                                    _rows(V, "V", p, pages, T, p.n_kv_heads), T,
-                                   _ints(n_new, "n_new", pages.rows, pages.device), _stream(stream, pages)),
+                                   _ints(n_new, "n_new", pages.rows, pages.index), _stream(stream, pages)),
            "akv_paged_append")
 
 
@@ -232,7 +232,7 @@ def akv_paged_read(p: PagedParams, pages: Pages, K, V, start=None, layer: int = 
     """Fills K, V [rows][T][n_kv_heads][128] (any strides, e.g. a transposed [rows][n_kv_heads][T][128]) with the
     tokens from start (CUDA int32 [rows], None: 0) on; tokens that a request does not hold are zeros."""
     T = _tokens(K, "K")
-    _check(_lib().akv_paged_read(_params(p, pages), pages.ref, layer, _ints(start, "start", pages.rows, pages.device),
+    _check(_lib().akv_paged_read(_params(p, pages), pages.ref, layer, _ints(start, "start", pages.rows, pages.index),
                                  _rows(K, "K", p, pages, T, p.n_kv_heads), _rows(V, "V", p, pages, T, p.n_kv_heads), T,
                                  _stream(stream, pages)), "akv_paged_read")
 
@@ -257,11 +257,10 @@ def akv_paged_attn(p: PagedParams, pages: Pages, q, out, lse=None, sel: PageSele
     L = _lib()
     if sel is not None:
         _match(sel, pages, T, p.n_kv_heads)
-    if lse is not None and (lse.dtype is not _torch.float32 or not lse.is_cuda or not lse.is_contiguous()
+    if lse is not None and (lse.dtype is not _torch.float32 or lse.get_device() != pages.index or not lse.is_contiguous()
                             or lse.shape != (pages.rows, T, p.n_q_heads)):
         raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{pages.rows}][{T}][{p.n_q_heads}]")
-    ws, at, n = _workspace(ws, lambda: akv_paged_attn_workspace_size(p, pages, T, sel.top if sel is not None else 0),
-                           pages, stream)
+    ws, at, n = _workspace(ws, pages, stream, akv_paged_attn_workspace_size, p, pages, T, 0 if sel is None else sel.top)
     _check(L.akv_paged_attn(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads),
                             _rows(out, "out", p, pages, T, p.n_q_heads), None if lse is None else lse.data_ptr(), T,
                             sm_scale, None if sel is None else sel.ref, at, n, _stream(stream, pages)), "akv_paged_attn")
@@ -280,25 +279,25 @@ def akv_paged_select(p: PagedParams, pages: Pages, q, sel: PageSelection, sink: 
     T = _tokens(q, "q")
     L = _lib()
     _match(sel, pages, T, p.n_kv_heads)
-    ws, at, n = _workspace(ws, lambda: akv_paged_select_workspace_size(p, pages, T), pages, stream)
+    ws, at, n = _workspace(ws, pages, stream, akv_paged_select_workspace_size, p, pages, T)
     _check(L.akv_paged_select(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads), T, sink, recent,
                               sel.ref, at, n, _stream(stream, pages)), "akv_paged_select")
 
 
-def _pair(src, dst, device):
+def _pair(src, dst, pages):
     n = src.numel()
-    return _ints(src, "src", None, device), _ints(dst, "dst", n, device), n
+    return _ints(src, "src", None, pages.index), _ints(dst, "dst", n, pages.index), n
 
 
 def akv_pages_copy(p: PagedParams, pages: Pages, src, dst, stream=None):
     """Copies page src[i] to page dst[i] in every layer (CUDA int32)."""
-    a, b, n = _pair(src, dst, pages.device)
+    a, b, n = _pair(src, dst, pages)
     _check(_lib().akv_pages_copy(_params(p, pages), pages.ref, a, b, n, _stream(stream, pages)), "akv_pages_copy")
 
 
 def akv_pages_fork(p: PagedParams, pages: Pages, src, dst, stream=None):
     """Row dst[i] becomes a second holder of row src[i]'s pages (CUDA int32)."""
-    a, b, n = _pair(src, dst, pages.device)
+    a, b, n = _pair(src, dst, pages)
     _check(_lib().akv_pages_fork(_params(p, pages), pages.ref, a, b, n, _stream(stream, pages)), "akv_pages_fork")
 
 
@@ -310,19 +309,19 @@ def akv_pages_workspace_size(pages: Pages) -> int:
 
 def akv_pages_reserve(p: PagedParams, pages: Pages, n_new, missing, ws=None, stream=None):
     """Pages for each row's next n_new tokens (CUDA int32 [rows]); missing: CUDA int32 [1]."""
-    ws, at, n = _workspace(ws, lambda: akv_pages_workspace_size(pages), pages, stream)
-    _check(_lib().akv_pages_reserve(_params(p, pages), pages.ref, _ints(n_new, "n_new", pages.rows, pages.device),
-                                    _ints(missing, "missing", 1, pages.device), at, n, _stream(stream, pages)), "akv_pages_reserve")
+    ws, at, n = _workspace(ws, pages, stream, akv_pages_workspace_size, pages)
+    _check(_lib().akv_pages_reserve(_params(p, pages), pages.ref, _ints(n_new, "n_new", pages.rows, pages.index),
+                                    _ints(missing, "missing", 1, pages.index), at, n, _stream(stream, pages)), "akv_pages_reserve")
 
 
 def akv_pages_free(p: PagedParams, pages: Pages, rows, stream=None):
     """Rows (CUDA int32) give up their pages."""
-    _check(_lib().akv_pages_free(_params(p, pages), pages.ref, _ints(rows, "rows", None, pages.device), rows.numel(),
+    _check(_lib().akv_pages_free(_params(p, pages), pages.ref, _ints(rows, "rows", None, pages.index), rows.numel(),
                                  _stream(stream, pages)), "akv_pages_free")
 
 
 def akv_pages_compact(p: PagedParams, pages: Pages, n_live, ws=None, stream=None):
     """Moves live pages to the front of the pool; n_live: CUDA int32 [1]."""
-    ws, at, n = _workspace(ws, lambda: akv_pages_workspace_size(pages), pages, stream)
-    _check(_lib().akv_pages_compact(_params(p, pages), pages.ref, _ints(n_live, "n_live", 1, pages.device), at, n,
+    ws, at, n = _workspace(ws, pages, stream, akv_pages_workspace_size, pages)
+    _check(_lib().akv_pages_compact(_params(p, pages), pages.ref, _ints(n_live, "n_live", 1, pages.index), at, n,
                                     _stream(stream, pages)), "akv_pages_compact")

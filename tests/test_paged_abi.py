@@ -126,6 +126,8 @@ def test_append_and_read():
     refused(INVALID, "start", "akv_paged_read", params(), pages(), 0, AT + 1, rows(), rows(), 1, None)
     assert call("akv_paged_append", params(), pages(), 0, rows(), rows(), 0, None, None) == OK
     assert call("akv_paged_read", params(), pages(), 1, None, rows(), rows(), 0, None) == OK
+    assert call("akv_paged_append", params(), pages(), 0, rows(ptr=None), rows(ptr=None), 0, None, None) == OK
+    assert call("akv_paged_read", params(), pages(), 0, None, rows(ptr=None), rows(ptr=None), 0, None) == OK
 
 
 def test_attention():

@@ -367,6 +367,38 @@ def test_pages_beyond_four_gigabytes():
     assert float((out[:, 0].double() - want).abs().max()) < 3e-2
 
 
+def test_lengths_outside_the_table_are_clamped():
+    p = params(1, 2, 16, bounds=True)
+    c = Cache(p, [64, 64, 40], seed=18, room=0, extra=0)
+    c.fill()
+    assert c.table.shape[1] == 4
+    q = queries(c, 2)
+    c.lens.copy_(torch.tensor([64, 64, 0], dtype=torch.int32))
+    want, sel = attend(c, q), selection(c, 2, 2)
+    akv.akv_paged_select(p, c.pages, q, sel)
+    c.lens.copy_(torch.tensor([65, 2**31 - 1, -5], dtype=torch.int32))
+    got, sel2 = attend(c, q), selection(c, 2, 2)
+    akv.akv_paged_select(p, c.pages, q, sel2)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(sel.pages, sel2.pages) and torch.equal(sel.count, sel2.count)
+    assert bool((got[0][2] == 0).all()) and bool(torch.isneginf(got[1][2]).all())
+    before = c.pool.clone()
+    k, v = c.rows(3)
+    akv.akv_paged_append(p, c.pages, k[:, :3], v[:, :3], n_new=torch.tensor([3, 3, 0], dtype=torch.int32, device="cuda"))
+    assert torch.equal(c.pool, before)  # no room
+
+
+def test_parameters_must_be_the_pools():
+    p = params(2, 4, 32)
+    c = Cache(p, [10], seed=19)
+    c.fill()
+    q = torch.zeros((1, 1, 2, D), dtype=torch.bfloat16, device="cuda")
+    akv.akv_paged_attn(params(2, 1, 32), c.pages, q, torch.empty_like(q))  # other query heads
+    for other in (params(2, 1, 32, rotate=True), params(2, 1, 32, group=128), params(2, 1, 32, half=True), params(1, 2, 32)):
+        with pytest.raises(ValueError):
+            akv.akv_paged_attn(other, c.pages, q, torch.empty_like(q))
+
+
 # ---- selection ---------------------------------------------------------------------------
 
 
