@@ -280,6 +280,17 @@ def test_attention_over_long_requests(G, page):
     check_attention(p, c, q, *attend(c, q), 1 / math.sqrt(D))
 
 
+@pytest.mark.parametrize("lens,page,G", [([300] * 40, 64, 2), ([1 + 7 * i % 61 for i in range(320)], 32, 1), ([390, 129] * 11, 128, 4),
+                                         ([40] * 300 + [1500], 64, 1)])
+def test_attention_of_batches(lens, page, G):
+    """Units with CTAs of their own and cut ones, as many as CTAs and more, more requests than a CTA has threads."""
+    p = params(1, G, page, 128, False, False)
+    c = Cache(p, lens, seed=len(lens))
+    c.fill()
+    q = queries(c, 1)
+    check_attention(p, c, q, *attend(c, q), 1 / math.sqrt(D))
+
+
 @pytest.mark.parametrize("scale,sm", [(1e-3, 1.0), (30.0, 1.0), (2000.0, 1e-6), (1.0, -0.3), (1.0, 0.0)])
 def test_attention_of_other_magnitudes(scale, sm):
     """Small and large values, peaked and flat softmaxes, a negative and a zero scale."""
