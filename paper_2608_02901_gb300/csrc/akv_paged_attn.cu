@@ -3,8 +3,8 @@
 //
 // Bound by HBM in principle (144 bytes a token and head at two groups a row, 2 x 16 products of 16 x 16 x 8), by the integer
 // operations and the latency of a warp's chain in practice: 4 x 131072 tokens, 8 KV heads, 4 or 8 query heads each, take
-// 115 to 121 us (5.0 TB/s, 74 % of the measured rate), rotated 135 (half as many products again), with 16 query rows 163;
-// 8 x 131072 rotated tokens 230 us (5.3 TB/s).  A call has about 8 us that do not depend on the length: the plan, the
+// 114 to 122 us (5.0 TB/s, 74 % of the measured rate), rotated 130 (half as many products again), with 16 query rows 168;
+// 8 x 131072 rotated tokens 233 us (5.2 TB/s).  A call has about 8 us that do not depend on the length: the plan, the
 // first page numbers and copies, the joins (1021 tokens: 7 us, and 4 of the second launch).
 //
 // A unit is one KV head of one request (or of one query token, where each has its own pages) with up to 8 NT query
