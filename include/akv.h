@@ -612,7 +612,8 @@ typedef struct akv_pages {
 } akv_pages;
 
 /* Rows of 128 values: request b, token t, head h at ptr + b stride_b + t stride_t + h stride_h
- * (strides in elements, 0 allowed for what is read; rows that are written must not overlap). */
+ * (strides in elements, 0 allowed for what is read; of rows that are written each axis steps over
+ * all that the axes of smaller strides cover, else the call is refused). */
 typedef struct akv_rows {
   void* ptr;
   int64_t stride_b, stride_t, stride_h;
@@ -638,7 +639,8 @@ akv_status akv_paged_append(const akv_paged_params* p, const akv_pages* pages, i
                             const akv_rows* V, int32_t T, const int32_t* n_new, akv_stream_t stream);
 
 /* Reads tokens start[b] .. start[b] + T - 1 (device int32, null = 0) of every request back into
- * dense rows of the cache's type; rows of tokens that a request does not hold are zeros. */
+ * dense rows of the cache's type; rows of tokens that a request does not hold are zeros.  T is at
+ * most 2^30. */
 akv_status akv_paged_read(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const int32_t* start,
                           const akv_rows* K, const akv_rows* V, int32_t T, akv_stream_t stream);
 

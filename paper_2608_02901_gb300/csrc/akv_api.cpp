@@ -24,6 +24,15 @@ akv_status fail(akv_status s, const std::string& msg) {
   return s;
 }
 
+akv_status fail(akv_status s, const char* a, const char* b, const char* c) noexcept {
+  try {
+    g_last_error = std::string(a) + b + c;
+  } catch (...) {  // out of memory: the status has to do
+    g_last_error.clear();
+  }
+  return s;
+}
+
 uint64_t splitmix64(uint64_t x) {
   // SplitMix64 finaliser applied to x advanced by the golden-ratio increment.
   uint64_t z = x + 0x9E3779B97F4A7C15ull;

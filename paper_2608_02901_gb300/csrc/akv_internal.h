@@ -89,6 +89,8 @@ struct Layout {
 
 // Records a failure text for akv_last_error() and returns the status.
 akv_status fail(akv_status s, const std::string& msg);
+// The same from a text's parts.  Throws nothing: a C entry that uses only this one lets no exception out.
+akv_status fail(akv_status s, const char* a, const char* b = "", const char* c = "") noexcept;
 
 // Validates parameters and context lengths and fills the layout.  With `sel` (the
 // paper's full selection), each unit's residual capacity per side is the most the pooled

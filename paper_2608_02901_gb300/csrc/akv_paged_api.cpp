@@ -1,6 +1,6 @@
 // Host side of the paged cache's entry points: validation, and the views the kernels get.
 #include <cmath>
-#include <string>
+#include <utility>
 
 #include "akv_internal.h"
 
@@ -81,9 +81,9 @@ akv_status check_layer(const akv_paged_params* p, const akv_pages* g, int32_t la
 }
 
 akv_status check_rows(const akv_rows* r, const char* what) {
-  if (!r || !r->ptr) return fail(AKV_ERR_INVALID, std::string("null ") + what);
-  if ((uintptr_t)r->ptr % 2) return fail(AKV_ERR_INVALID, std::string(what) + " must be 2-byte aligned");
-  if (r->stride_b < 0 || r->stride_t < 0 || r->stride_h < 0) return fail(AKV_ERR_INVALID, std::string(what) + ": negative stride");
+  if (!r || !r->ptr) return fail(AKV_ERR_INVALID, "null ", what);
+  if ((uintptr_t)r->ptr % 2) return fail(AKV_ERR_INVALID, what, " must be 2-byte aligned");
+  if (r->stride_b < 0 || r->stride_t < 0 || r->stride_h < 0) return fail(AKV_ERR_INVALID, what, ": negative stride");
   return AKV_OK;
 }
 
@@ -105,12 +105,24 @@ akv_status check_selection(const akv_selection* s) {
   return AKV_OK;
 }
 
-// Rows to write T tokens of: tokens, or heads, or requests on top of one another are refused.
+// Rows to write T tokens of: rows on top of one another are refused.  Axes are taken from the smallest stride up, each
+// has to step over all that lies within the ones before.
 akv_status check_written(const akv_rows* r, const char* what, int32_t rows, int32_t T, int32_t heads) {
   akv_status st = check_rows(r, what);
   if (st != AKV_OK) return st;
-  if ((rows > 1 && r->stride_b < kD) || (T > 1 && r->stride_t < kD) || (heads > 1 && r->stride_h < kD))
-    return fail(AKV_ERR_INVALID, std::string(what) + ": rows overlap");
+  struct Axis {
+    int64_t stride, n;
+  } axes[3] = {{r->stride_b, rows}, {r->stride_t, T}, {r->stride_h, heads}};
+  if (axes[1].stride < axes[0].stride) std::swap(axes[0], axes[1]);
+  if (axes[2].stride < axes[1].stride) std::swap(axes[1], axes[2]);
+  if (axes[1].stride < axes[0].stride) std::swap(axes[0], axes[1]);
+  int64_t extent = kD;  // values from the first row's start to the last one's end
+  for (const Axis& a : axes) {
+    if (a.n <= 1) continue;
+    if (a.stride < extent) return fail(AKV_ERR_INVALID, what, ": rows overlap");
+    if (a.stride > (INT64_MAX / 2 - extent) / (a.n - 1)) return fail(AKV_ERR_INVALID, what, ": strides out of range");
+    extent += a.stride * (a.n - 1);
+  }
   return AKV_OK;
 }
 
@@ -142,7 +154,7 @@ akv_status check_list(const int32_t* a, const int32_t* b, int32_t n) {
 }
 
 akv_status launched(int err, const char* what) {
-  if (err) return fail(AKV_ERR_CUDA, std::string(what) + " launch failed: " + cuda_error_string(err));
+  if (err) return fail(AKV_ERR_CUDA, what, " launch failed: ", cuda_error_string(err));
   return AKV_OK;
 }
 
@@ -185,6 +197,7 @@ akv_status akv_paged_read(const akv_paged_params* p, const akv_pages* pages, int
   AKV_TRY(check_layer(p, pages, layer, &c));
   if (T < 0) return fail(AKV_ERR_INVALID, "negative T");
   if (T == 0) return AKV_OK;
+  if (T > (1 << 30)) return fail(AKV_ERR_UNSUPPORTED, "more than 2^30 tokens per request");  // (32-bit token numbers)
   AKV_TRY(check_written(K, "K", pages->rows, T, p->n_kv_heads));
   AKV_TRY(check_written(V, "V", pages->rows, T, p->n_kv_heads));
   if ((uintptr_t)start % 4) return fail(AKV_ERR_INVALID, "start must be 4-byte aligned");

@@ -206,3 +206,17 @@ def test_every_entry_point_is_in_the_package():
     for name in paged.EXPORTED:
         assert callable(getattr(akv, name)) and hasattr(akv.lib(), name)
     assert os.path.exists(akv.LIB_PATH)
+
+
+def test_written_rows_may_lie_in_any_order_but_not_on_top_of_one_another():
+    """[rows][T][heads] = 3 x 4 x 2 rows of 128, T = 4."""
+    def read(K, T=4):
+        return "akv_paged_read", params(), pages(), 0, None, K, rows(), T, None
+
+    # two heads 128 apart step over 256 values, four tokens of them over 1024
+    for b, t, h in ((1024, 256, 64), (1024, 192, 128), (960, 256, 128), (128, 128, 128), (512, 256, 128), (256, 700, 128),
+                    (256, 128, 512), (128, 4096, 300), (0, 256, 128), (2**62, 2**62, 2**61)):
+        assert call(*read(rows(stride_b=b, stride_t=t, stride_h=h))) == INVALID, (b, t, h)
+    refused(INVALID, "overlap", *read(rows(stride_b=896, stride_t=256, stride_h=128)))
+    refused(INVALID, "out of range", *read(rows(stride_b=2**62, stride_t=256, stride_h=128)))
+    refused(UNSUPPORTED, "2^30", *read(rows(), T=2**30 + 1))
