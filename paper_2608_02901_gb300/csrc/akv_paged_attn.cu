@@ -352,7 +352,8 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) looks[i] = look_next();
-    for (int64_t k = r.lo; k < r.hi; ++k) {
+    int64_t end = r.hi;
+    for (int64_t k = r.lo; k < end; ++k) {
       const Look now = looks[0];
 #pragma unroll
       for (int i = 0; i + 1 < kAhead; ++i) looks[i] = looks[i + 1];
@@ -361,7 +362,8 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       const int pos0 = now.at < 0 ? -1 : (uint32_t)page0 < (uint32_t)v.n_pages ? now.at : -2;
       if (!mbar_wait_w(smem_u32(&S.empty[stage]), phase)) {
         if (lane == 0) *failed = 1;
-        return;
+        end = k;
+        break;
       }
       const uint32_t there = __ballot_sync(0xffffffffu, pos0 >= 0);
       if (lane < kTileSubs) S.pos[stage][lane] = pos0;
@@ -377,6 +379,9 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       }
       if (++stage == kStages) stage = 0, phase ^= 1;
     }
+    // shared memory is the copies' until the last have landed, also where a warp has given up
+    for (uint32_t n = (uint32_t)(end - r.lo), k = n > kStages ? n - kStages : 0; k < n; ++k)
+      if (!mbar_wait_w(smem_u32(&S.full[k % kStages]), k / kStages & 1)) break;
     return;
   }
 
