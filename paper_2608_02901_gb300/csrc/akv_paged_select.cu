@@ -6,7 +6,9 @@
 // fp32: the tensor cores add them up without rounding, in any order, so that the choice is the same on every machine.
 // What costs is turning the bounds into whole numbers (three operations a pair); a warp does it once for all query rows.
 // 8 x 2048 pages of 8 heads: 21 us, 3.2 TB/s.  The bytes bound it: a plain read of 512-byte pieces 9.7 KB apart reaches 3.35
-// TB/s in any order and at any number of CTAs.  The choice takes 6 us for 512 pages and 8 us for 2048, latency alone.  The choice itself finds the key of the last page kept, 8 bits of its range a pass.
+// TB/s in any order and at any number of CTAs.
+// The choice finds the key of the last page kept, 8 bits of its range a pass: 6 us for 512 pages and 8 us for 2048,
+// latency alone.
 #include "akv_paged.cuh"
 
 namespace akv {
