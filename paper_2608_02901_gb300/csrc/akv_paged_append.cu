@@ -282,7 +282,7 @@ __device__ __forceinline__ void load_row(const RowsIO& R, int64_t at, int u, uin
 
 // One CTA: one page of one request that gets new tokens, one head; its keys, then its values, or (sides 1) one of them.
 // The row after the present one is loaded while that is worked on.  Seven CTAs an SM: 128K rotated tokens of 8 heads take
-// 195 us (3.5 TB/s; with four CTAs 217).
+// 162 us (4.2 TB/s).
 template <int NG, bool ROT, bool HALF>
 __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedView v, RowsIO K, RowsIO V, int T, const int32_t* n_new,
                                                                           int pages_each, int sides) {
@@ -307,10 +307,8 @@ __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedV
   const int64_t to = (int64_t)(j << v.page_log) - held;  // token of the page's first place, among the new ones
   const int64_t base_k = b * K.sb + h * K.sh + to * K.st, base_v = b * V.sb + h * V.sh + to * V.st;
 
-  auto load = [&](int turn, uint32_t (&w)[16]) {
+  auto load = [&](int turn, uint32_t (&w)[16]) {  // (a row that is not there leaves what was: nothing of it is stored)
     const int side = part + (turn >> turns_log), i = (turn & ((1 << turns_log) - 1)) * at_once + row;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) w[k] = 0;
     if (turn < turns && i >= i0 && i < i1) {
       if (side) load_row(V, base_v + i * V.st, u, w);
       else load_row(K, base_k + i * K.st, u, w);
@@ -319,6 +317,8 @@ __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedV
   uint32_t signs[2][2];
   if (ROT) hadamard_operand<HALF>(threadIdx.x & 31, 0, signs);
   uint32_t next[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) next[k] = 0;
   load(0, next);
   if (page < 0) return;
   uint8_t* block = block_of(v, page, h);
@@ -366,28 +366,43 @@ __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedV
     }
   }
   if (!v.bounds || part != 0) return;
-  // The page's bounds: the keys once more, which the caches hold; a thread takes two dimensions of every other row.
-  __shared__ uint32_t red[2][64];
-  const int at = threadIdx.x & 63, rows = blockDim.x >> 6;
-  uint32_t lo = HALF ? 0x7c007c00u : 0x7f807f80u, hi = lo | 0x80008000u;  // + and - infinity
-#pragma unroll 8
-  for (int i = i0 + (threadIdx.x >> 6); i < i1; i += rows) {
-    const uint16_t* x = K.ptr + base_k + i * K.st + 2 * at;
-    const uint32_t w = K.vec ? *(const uint32_t*)x : x[0] | (uint32_t)x[1] << 16;
-    lo = min_rows<HALF>(lo, w);
-    hi = max_rows<HALF>(hi, w);
+  // The page's bounds: the keys once more, which the caches hold; a thread takes 16 bytes of every eighth row (128K tokens:
+  // 162 us in all, 198 with 4 bytes of every other row, 140 without bounds; read first, or between keys and values, 170 to 187).
+  __shared__ __align__(16) uint4 red[kMaxThreads / 32][2][16];
+  const int at = threadIdx.x & 15, warp = threadIdx.x >> 5, rows = blockDim.x >> 4;
+  uint4 lo, hi;
+  lo.x = lo.y = lo.z = lo.w = HALF ? 0x7c007c00u : 0x7f807f80u;  // + and - infinity
+  hi.x = hi.y = hi.z = hi.w = lo.x | 0x80008000u;
+  auto take = [&](const uint4& a, const uint4& b) {
+    lo.x = min_rows<HALF>(lo.x, a.x), lo.y = min_rows<HALF>(lo.y, a.y), lo.z = min_rows<HALF>(lo.z, a.z), lo.w = min_rows<HALF>(lo.w, a.w);
+    hi.x = max_rows<HALF>(hi.x, b.x), hi.y = max_rows<HALF>(hi.y, b.y), hi.z = max_rows<HALF>(hi.z, b.z), hi.w = max_rows<HALF>(hi.w, b.w);
+  };
+  const uint16_t* x = K.ptr + base_k + 8 * at;
+#pragma unroll 4
+  for (int i = i0 + (threadIdx.x >> 4); i < i1; i += rows) {
+    uint4 w;
+    const uint16_t* y = x + i * K.st;
+    if (K.vec) {
+      w = *(const uint4*)y;
+    } else {
+      w.x = y[0] | (uint32_t)y[1] << 16, w.y = y[2] | (uint32_t)y[3] << 16;
+      w.z = y[4] | (uint32_t)y[5] << 16, w.w = y[6] | (uint32_t)y[7] << 16;
+    }
+    take(w, w);
   }
-  if (rows == 2) {
-    if (threadIdx.x >= 64) red[0][at] = lo, red[1][at] = hi;
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    lo = min_rows<HALF>(lo, red[0][at]);
-    hi = max_rows<HALF>(hi, red[1][at]);
-  }
-  uint32_t* to_b = (uint32_t*)(block + (uint32_t)(P >> 4) * kSub) + at;
-  if (i0 != 0) lo = min_rows<HALF>(lo, to_b[0]), hi = max_rows<HALF>(hi, to_b[64]);  // what the page held before
+  auto other = [&](const uint4& w) {
+    return make_uint4(__shfl_xor_sync(0xffffffffu, w.x, 16), __shfl_xor_sync(0xffffffffu, w.y, 16),
+                      __shfl_xor_sync(0xffffffffu, w.z, 16), __shfl_xor_sync(0xffffffffu, w.w, 16));
+  };
+  take(other(lo), other(hi));
+  if (!(threadIdx.x & 16)) red[warp][0][at] = lo, red[warp][1][at] = hi;
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  for (int w = 1; w < (int)blockDim.x >> 5; ++w) take(red[w][0][at], red[w][1][at]);
+  uint4* to_b = (uint4*)(block + (uint32_t)(P >> 4) * kSub) + at;
+  if (i0 != 0) take(to_b[0], to_b[16]);  // what the page held before
   to_b[0] = lo;
-  to_b[64] = hi;
+  to_b[16] = hi;
 }
 
 // H v^ / 16 of the warp's 8 rows from their codes: over the six bits of a group H v^ = a (H c) + 64 m at dimension 0, and
@@ -434,7 +449,7 @@ __device__ __forceinline__ void unrotate_codes(const uint32_t (&c)[4], const uin
 }
 
 constexpr int kReadTurns = 8;  // rows a thread reads back at most (128K rotated tokens of 8 heads: 140 us with four, 132
-                               // with eight; 120 us, 5.6 TB/s, since seven CTAs share an SM)
+                               // with eight; 120 us, 5.7 TB/s, since seven CTAs share an SM)
 
 template <int NG, bool ROT, bool HALF>
 __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_read_kernel(PagedView v, const int32_t* start, RowsIO K, RowsIO V, int T,
