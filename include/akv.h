@@ -687,12 +687,14 @@ akv_status akv_pages_fork(const akv_paged_params* p, const akv_pages* pages, con
                           int32_t n, akv_stream_t stream);
 
 /* Sees to the pages of each request's next n_new[b] tokens (device int32 [rows]; <= 0: none).
- * Where the first of them falls into a page with other holders, the request gets a copy of that
- * page in every layer - unless all holders write into it in this call: then the lowest row keeps
- * the page.  Then table positions up to the last new token that have no page get one.  Pages are
- * taken in order of row and position, the lowest free number first.  *missing (device) is set to
- * the number of pages that the pool lacks; where it is not 0, nothing else is changed.  Tokens
- * past the table get no page. */
+ * Table positions that they fall into and that have no page get one (but for one that should hold
+ * tokens already).  Where a position has a page with other holders (the page of the last token
+ * held, or, after the caller lowered a length to go on from an earlier token, any page behind it),
+ * the request gets a page of its own instead, with a copy of the content in every layer if the page
+ * holds tokens of the request - unless all holders write into it in this call: then the lowest row
+ * keeps the page.  Pages are taken in order of row and position, the lowest free number first.
+ * *missing (device) is set to the number of pages that the pool lacks; where it is not 0, nothing
+ * else is changed.  Tokens past the table get no page. */
 akv_status akv_pages_workspace_size(const akv_paged_params* p, const akv_pages* pages, size_t* ws_bytes);
 akv_status akv_pages_reserve(const akv_paged_params* p, const akv_pages* pages, const int32_t* n_new,
                              int32_t* missing, void* ws, size_t ws_bytes, akv_stream_t stream);

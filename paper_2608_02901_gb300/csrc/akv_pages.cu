@@ -16,15 +16,16 @@ struct PagesWs {
   int32_t* src;       // [max(n_pages, rows)]
   int32_t* dst;
   int32_t* free;      // [n_pages] free pages taken, ascending; compaction: where a live page goes
-  int32_t* writers;   // [n_pages] requests that write into a shared page
+  int32_t* writers;   // [n_pages] requests that write into a page
   int32_t* lowest;    // [n_pages] the lowest of them
   int32_t* base;      // [rows] pages taken by the rows before
   int32_t* cbase;     // [rows] copies by the rows before
+  int32_t* given;     // [n_pages] the page that a free page taken stands in for, -1: none
 };
 
 size_t pages_ws_ints(const PagesState& s) {
   const size_t list = (size_t)(s.n_pages > s.rows ? s.n_pages : s.rows);
-  return 64 + 2 * list + 3 * (size_t)s.n_pages + 2 * (size_t)s.rows;
+  return 64 + 2 * list + 4 * (size_t)s.n_pages + 2 * (size_t)s.rows;
 }
 PagesWs pages_ws(const PagesState& s, void* ws) {
   const size_t list = (size_t)(s.n_pages > s.rows ? s.n_pages : s.rows);
@@ -38,6 +39,7 @@ PagesWs pages_ws(const PagesState& s, void* ws) {
   w.lowest = w.writers + s.n_pages;
   w.base = w.lowest + s.n_pages;
   w.cbase = w.base + s.rows;
+  w.given = w.cbase + s.rows;
   return w;
 }
 
@@ -170,53 +172,67 @@ __global__ void __launch_bounds__(256) akv_pages_free_kernel(PagesState s, const
 }
 
 struct RowPlan {
-  int first, need;  // table positions that get a page where they have none
-  int tail;         // page that the first new token falls into, -1: none
+  int first, need;  // table positions that the new tokens fall into
+  bool cut;         // the first of them holds tokens of the row already
 };
 __device__ __forceinline__ RowPlan row_plan(const PagesState& s, const int32_t* n_new, int r) {
   const int most = s.max_pages << s.page_log, P = 1 << s.page_log;
   const int len = min(max(s.lens[r], 0), most);
   const int n = min(max(n_new[r], 0), most - len);
   RowPlan p;
-  p.first = (len + P - 1) >> s.page_log;
+  p.first = len >> s.page_log;
   p.need = n > 0 ? (len + n + P - 1) >> s.page_log : p.first;
-  p.tail = -1;
-  if (n > 0 && (len & P - 1)) {
-    const int page = s.table[(int64_t)r * s.table_stride + (len >> s.page_log)];
-    if (in_pool(s, page)) p.tail = page;
-  }
+  p.cut = len & P - 1;
   return p;
 }
+// A position without a page gets one, but where it should hold tokens already (they stay missing).
+__device__ __forceinline__ bool lacks(const RowPlan& p, int j, int page) { return page < 0 && !(p.cut && j == p.first); }
 
 __global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesState s, const int32_t* n_new, int32_t* missing, PagesWs w) {
   launch_dependents();
   wait_for_stream();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  // who writes into a page that others may hold too
-  for (int r = tid; r < s.rows; r += blockDim.x) {
-    const RowPlan p = row_plan(s, n_new, r);
-    if (p.tail >= 0) w.writers[p.tail] = 0, w.lowest[p.tail] = INT32_MAX;
-  }
-  __syncthreads();
-  for (int r = tid; r < s.rows; r += blockDim.x) {
-    const RowPlan p = row_plan(s, n_new, r);
-    if (p.tail >= 0) atomicAdd(w.writers + p.tail, 1), atomicMin(w.lowest + p.tail, r);
-  }
-  __syncthreads();
-  auto copies = [&](const RowPlan& p, int r) {
-    if (p.tail < 0) return false;
-    const int refs = s.refs[p.tail];
-    return refs > 1 && !(w.writers[p.tail] == refs && w.lowest[p.tail] == r);
+  // Who writes into a page that others may hold too: each position that new tokens fall into, the first of a row (all there
+  // is in a decode step) by a thread, later ones, which a row has pages at already if its length was lowered, by a warp.
+  auto each_cell = [&](auto f) {
+    bool more = false;
+    for (int r = tid; r < s.rows; r += blockDim.x) {
+      const RowPlan p = row_plan(s, n_new, r);
+      if (p.first < p.need) f(r, s.table[(int64_t)r * s.table_stride + p.first]);
+      more = more || p.need - p.first > 1;
+    }
+    if (__syncthreads_or(more))
+      for (int r = warp; r < s.rows; r += warps) {
+        const RowPlan p = row_plan(s, n_new, r);
+        for (int j = p.first + 1 + lane; j < p.need; j += 32) f(r, s.table[(int64_t)r * s.table_stride + j]);
+      }
+    __syncthreads();
+  };
+  each_cell([&](int, int page) {
+    if (in_pool(s, page)) w.writers[page] = 0, w.lowest[page] = INT32_MAX;
+  });
+  each_cell([&](int r, int page) {
+    if (in_pool(s, page)) atomicAdd(w.writers + page, 1), atomicMin(w.lowest + page, r);
+  });
+  auto gives = [&](int r, int page) {  // the row leaves the page to its other holders
+    if (!in_pool(s, page)) return false;
+    const int refs = s.refs[page];
+    return refs > 1 && !(w.writers[page] == refs && w.lowest[page] == r);
   };
   // pages per row (a warp each)
   for (int r = warp; r < s.rows; r += warps) {
     const RowPlan p = row_plan(s, n_new, r);
     int n = 0;
-    for (int j = p.first + lane; j < p.need; j += 32) n += s.table[(int64_t)r * s.table_stride + j] < 0;
+    bool c = false;
+    for (int j = p.first + lane; j < p.need; j += 32) {
+      const int page = s.table[(int64_t)r * s.table_stride + j];
+      const bool give = gives(r, page);
+      n += lacks(p, j, page) || give;
+      if (j == p.first) c = give && p.cut;
+    }
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) {
-      const bool c = copies(p, r);
-      w.base[r] = n + c;
+      w.base[r] = n;
       w.cbase[r] = c;
     }
   }
@@ -229,8 +245,7 @@ __global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesSt
     if (r < s.rows) w.base[r] = total + a;
     total += sum;
     const int b = block_scan(r < s.rows ? w.cbase[r] : 0, &sum);
-    // copies by the rows before, and whether this row copies in the sign bit
-    if (r < s.rows) w.cbase[r] = (n_copies + b) | (w.cbase[r] ? (int)0x80000000 : 0);
+    if (r < s.rows) w.cbase[r] = n_copies + b;
     n_copies += sum;
   }
   const int found = each_page(0, s.n_pages, total, [&](int page) { return s.refs[page] == 0; },
@@ -244,34 +259,29 @@ __global__ void __launch_bounds__(kPlanThreads) akv_pages_reserve_kernel(PagesSt
   for (int r = warp; r < s.rows; r += warps) {
     const RowPlan p = row_plan(s, n_new, r);
     int at = w.base[r];
-    const int cb = w.cbase[r];
-    __syncwarp();
-    if (cb < 0) {
-      if (lane == 0) {
-        const int page = w.free[at];
-        s.table[(int64_t)r * s.table_stride + p.first - 1] = page;
-        s.refs[page] = 1;
-        w.src[cb & 0x7fffffff] = p.tail;
-        w.dst[cb & 0x7fffffff] = page;
-      }
-      ++at;
-    }
     for (int j0 = p.first; j0 < p.need; j0 += 32) {
       const int j = j0 + lane;
       int32_t* cell = s.table + (int64_t)r * s.table_stride + j;
-      const bool want = j < p.need && *cell < 0;
+      const int was = j < p.need ? *cell : 0;
+      const bool give = j < p.need && gives(r, was), want = j < p.need && (lacks(p, j, was) || give);
       const uint32_t m = __ballot_sync(0xffffffffu, want);
       if (want) {
-        const int page = w.free[at + __popc(m & ((1u << lane) - 1))];
+        const int k = at + __popc(m & ((1u << lane) - 1)), page = w.free[k];
         *cell = page;
         s.refs[page] = 1;
+        w.given[k] = give ? was : -1;
+        if (give && j == p.first && p.cut) {
+          w.src[w.cbase[r]] = was;
+          w.dst[w.cbase[r]] = page;
+        }
       }
       at += __popc(m);
     }
   }
   __syncthreads();
-  // a copy's page has one holder less (after every row has read the counts)
-  for (int i = tid; i < n_copies; i += blockDim.x) atomicSub(s.refs + w.src[i], 1);
+  // a page that was left has one holder less (after every row has read the counts)
+  for (int i = tid; i < total; i += blockDim.x)
+    if (w.given[i] >= 0) atomicSub(s.refs + w.given[i], 1);
 }
 
 __global__ void __launch_bounds__(kPlanThreads) akv_pages_compact_plan(PagesState s, int32_t* n_live, PagesWs w) {
