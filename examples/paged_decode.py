@@ -37,21 +37,21 @@ def clustered(gen, centres, shape, outliers):
     return x.to(torch.bfloat16)
 
 
-def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=3, page=64, seed=0, verbose=True):
+def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=3, page=64, seed=0, verbose=True, pool_pages=None):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     say = print if verbose else (lambda *a: None)
     B = len(prompts)
     rows = B * (1 + answers)  # the prompts, then their answers
     most = max(prompts) + steps + 16
     max_pages = -(-most // page)
-    n_pages = sum(-(-n // page) for n in prompts) + rows * (2 + (steps + 16) // page)
+    n_pages = pool_pages or sum(-(-n // page) for n in prompts) + rows * (2 + (steps + 16) // page)
     p = akv.PagedParams(n_kv_heads=heads, n_q_heads=heads * group, page_tokens=page, rotate=True, bounds=True)
     page_bytes = akv.akv_paged_page_bytes(p)
     int32 = dict(dtype=torch.int32, device="cuda")
     pool = torch.zeros((1, n_pages, page_bytes), dtype=torch.uint8, device="cuda")
     table = torch.full((rows, max_pages), -1, **int32)
     lens, refs = torch.zeros(rows, **int32), torch.zeros(n_pages, **int32)
-    missing = torch.zeros(1, **int32)
+    missing, lacked = torch.zeros(1, **int32), torch.zeros(1, **int32)
     pages = akv.Pages(p, pool, table, lens, refs)
     sel = akv.PageSelection(torch.empty((rows, 1, heads, top), **int32), torch.empty((rows, 1, heads), **int32))
     draft = 4
@@ -65,8 +65,11 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
         return clustered(gen, ck, (rows, T, heads), True), clustered(gen, cv, (rows, T, heads), False)
 
     def put(n_new, T):
-        """Room for the new tokens, then their keys and values; every layer of a model would append before lens moves."""
+        """Room for the new tokens, then their keys and values; every layer of a model would append before lens moves.  Where the
+        pool has no room the step does nothing (a scheduler would look at `lacked` now and then, and free something)."""
         akv.akv_pages_reserve(p, pages, n_new, missing, ws=ws)
+        torch.maximum(lacked, missing, out=lacked)
+        n_new = n_new * (missing == 0)
         K, V = tokens(T)
         akv.akv_paged_append(p, pages, K, V, n_new=n_new)
         lens.add_(n_new)
@@ -101,7 +104,7 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
         live = one.bool()
         share += float((kept_lse - lse)[live].exp().mean()) / steps
         cosine += float(torch.cosine_similarity(out[live].float(), kept[live].float(), dim=-1).mean()) / steps
-    assert int(missing) == 0
+    assert pool_pages or int(lacked) == 0
     say(f"{steps} steps: {int((refs > 0).sum())} pages; the {top} pages kept of up to {max_pages} hold {share:.3f} of the "
         f"softmax, outputs' cosine {cosine:.4f}")
     put(one * draft, draft)
@@ -140,7 +143,7 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
         agree = float(torch.cosine_similarity(near[0, 0].float(), far[0].float(), dim=-1).mean())
         say(f"prompt of {S} tokens: {-(-S // page) * page_bytes / 1e6:.2f} MB in pages, {arena_bytes / 1e6:.2f} MB as anchors and "
             f"residuals; outputs' cosine {agree:.4f}")
-    return dict(share=share, cosine=cosine, unmoved=unmoved, agree=agree, live=int(n_live), table=table, lens=lens, refs=refs)
+    return dict(share=share, cosine=cosine, unmoved=unmoved, agree=agree, live=int(n_live), lacked=int(lacked), table=table, lens=lens, refs=refs)
 
 
 if __name__ == "__main__":

@@ -608,7 +608,8 @@ typedef struct akv_pages {
   int32_t rows;         /* requests (rows of the table) */
   int32_t max_pages;    /* table entries per request */
   int32_t* lens;        /* device [rows]: tokens held; read as clamped to [0, max_pages * P] */
-  int32_t* refs;        /* device [n_pages]: holders of each page, 0 = free (akv_pages_* only; else may be null) */
+  int32_t* refs;        /* device [n_pages]: holders of each page, 0 = free (read by akv_paged_append too; may be
+                           null but for akv_pages_fork, _reserve, _free and _compact) */
 } akv_pages;
 
 /* Rows of 128 values: request b, token t, head h at ptr + b stride_b + t stride_t + h stride_h
@@ -634,7 +635,10 @@ akv_status akv_paged_page_bytes(const akv_paged_params* p, size_t* bytes);
  * tokens it holds: n_new[b] of them (device int32, null = T each; clamped to 0 .. T and to the
  * table).  lens is read, not advanced: the layers of a model share it, and the caller adds
  * n_new once all have been written.  Tokens whose page number is not one of the pool's are not
- * written.  A page that is written must have one holder (akv_pages_reserve sees to it). */
+ * written.  A page that is written must have one holder (akv_pages_reserve sees to it); where
+ * pages->refs is given, tokens whose page has more are not written, so that a step whose
+ * reservation found no room changes nothing of other requests (its lengths must not advance
+ * either: n_new times *missing == 0 keeps such a step on the device). */
 akv_status akv_paged_append(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* K,
                             const akv_rows* V, int32_t T, const int32_t* n_new, akv_stream_t stream);
 

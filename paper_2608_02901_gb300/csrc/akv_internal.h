@@ -175,6 +175,7 @@ struct PagedView {
   uint8_t* base;           // the layer's first page
   const int32_t* table;
   const int32_t* lens;
+  const int32_t* refs;     // holders of each page, or null (read where pages are written)
   int64_t table_stride;
   uint64_t page_bytes;
   uint64_t sign_bits[2];   // rotation signs

@@ -65,6 +65,7 @@ akv_status check_pages(const akv_paged_params* p, const akv_pages* g, PagedCall*
   v.base = (uint8_t*)g->pool;
   v.table = g->table;
   v.lens = g->lens;
+  v.refs = g->refs;
   v.table_stride = g->table_stride;
   v.n_pages = g->n_pages;
   v.rows = g->rows;

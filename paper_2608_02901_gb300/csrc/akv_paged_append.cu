@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedV
 #pragma unroll
   for (int k = 0; k < 16; ++k) next[k] = 0;
   load(0, next);
-  if (page < 0) return;
+  if (page < 0 || (v.refs && v.refs[page] > 1)) return;  // (never over what another request holds)
   uint8_t* block = block_of(v, page, h);
 #pragma unroll 1
   for (int turn = 0; turn < turns; ++turn) {

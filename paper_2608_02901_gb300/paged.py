@@ -141,7 +141,8 @@ class Pages:
            the page before; layers may lie further apart
     table  int32 [rows][max_pages], rows may lie further apart: the page of each page_tokens tokens, -1 = none
     lens   int32 [rows]: tokens held
-    refs   int32 [n_pages]: holders of each page, 0 = free; needed by akv_pages_fork, _reserve, _free and _compact
+    refs   int32 [n_pages]: holders of each page, 0 = free; needed by akv_pages_fork, _reserve, _free and _compact, and
+           where given akv_paged_append writes to no page with more than one
     """
 
     def __init__(self, p: PagedParams, pool, table, lens, refs=None):
@@ -220,7 +221,8 @@ def _workspace(ws, pages, stream, size, *args):
 
 
 def akv_paged_append(p: PagedParams, pages: Pages, K, V, n_new=None, layer: int = 0, stream=None):
-    """K, V: [rows][T][n_kv_heads][128]; n_new: CUDA int32 [rows] (None: T each).  lens is not advanced."""
+    """K, V: [rows][T][n_kv_heads][128]; n_new: CUDA int32 [rows] (None: T each).  lens is not advanced.  Pages with more
+    than one holder are not written."""
     T = _tokens(K, "K")
     _check(_lib().akv_paged_append(_params(p, pages), pages.ref, layer, _rows(K, "K", p, pages, T, p.n_kv_heads),
                                    _rows(V, "V", p, pages, T, p.n_kv_heads), T,
