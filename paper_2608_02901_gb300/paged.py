@@ -7,6 +7,7 @@ converts only what changes.
 from __future__ import annotations
 
 import ctypes
+from contextlib import nullcontext
 from dataclasses import dataclass, replace
 
 AKV_FLAG_BOUNDS = 8
@@ -210,11 +211,14 @@ def _tokens(t, what):
 
 
 def _workspace(ws, pages, stream, size, *args):
-    """ws, its address and its bytes; one of size(*args) bytes from torch's allocator for None."""
+    """ws, its address and its bytes; one of size(*args) bytes from torch's allocator, the stream's own, for None."""
     if ws is None:
-        ws = _torch.empty(size(*args), dtype=_torch.uint8, device=pages.device)
-        if stream is not None:  # the allocator must not hand it out again before that stream is done with it
-            ws.record_stream(stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(stream, pages.device))
+        # asked for on the stream that uses it: the allocator hands a block that was given back to the same stream alone
+        n = size(*args)
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = _torch.cuda.ExternalStream(stream, device=pages.device)
+        with nullcontext() if stream is None else _torch.cuda.stream(stream):
+            ws = _torch.empty(n, dtype=_torch.uint8, device=pages.device)
     elif ws.get_device() != pages.index or not ws.is_contiguous():
         raise ValueError("ws must be a contiguous CUDA tensor on the pool's device")
     return ws, ws.data_ptr(), ws.nbytes
