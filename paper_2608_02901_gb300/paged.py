@@ -96,18 +96,18 @@ def akv_paged_page_bytes(p: PagedParams) -> int:
 
 
 _loaded = None
-_torch = _bf16 = _fp16 = _int32 = _raw_stream = None
+_torch = _bf16 = _fp16 = _int32 = _raw_stream = _device = None
 
 
 def _lib():
     """The library; torch is loaded with it."""
-    global _loaded, _torch, _bf16, _fp16, _int32, _raw_stream
+    global _loaded, _torch, _bf16, _fp16, _int32, _raw_stream, _device
     if _loaded is None:
         import torch
 
         from . import lib
         _torch, _bf16, _fp16, _int32 = torch, torch.bfloat16, torch.float16, torch.int32
-        _raw_stream = torch._C._cuda_getCurrentRawStream
+        _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _loaded = lib()
     return _loaded
 
@@ -122,7 +122,15 @@ def _stream(stream, pages):
     """Address of a stream: the current one of the pool's device for None."""
     if stream is None:
         return _raw_stream(pages.index)
+    if getattr(stream, "device_index", pages.index) != pages.index:
+        raise ValueError("stream must be one of the pool's device")
     return getattr(stream, "cuda_stream", stream)
+
+
+def _there(pages, call, *args):
+    """The call with the pool's device as the current one: entries launch on that."""
+    with _torch.cuda.device(pages.index):
+        return call(*args)
 
 
 def _ints(t, what, n, index):
@@ -227,6 +235,8 @@ def _workspace(ws, pages, stream, size, *args):
 def akv_paged_append(p: PagedParams, pages: Pages, K, V, n_new=None, layer: int = 0, stream=None):
     """K, V: [rows][T][n_kv_heads][128]; n_new: CUDA int32 [rows] (None: T each).  lens is not advanced.  Pages with more
     than one holder are not written."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_append, p, pages, K, V, n_new, layer, stream)
     T = _tokens(K, "K")
     _check(_lib().akv_paged_append(_params(p, pages), pages.ref, layer, _rows(K, "K", p, pages, T, p.n_kv_heads),
                                    _rows(V, "V", p, pages, T, p.n_kv_heads), T,
@@ -237,6 +247,8 @@ def akv_paged_append(p: PagedParams, pages: Pages, K, V, n_new=None, layer: int 
 def akv_paged_read(p: PagedParams, pages: Pages, K, V, start=None, layer: int = 0, stream=None):
     """Fills K, V [rows][T][n_kv_heads][128] (any strides, e.g. a transposed [rows][n_kv_heads][T][128]) with the
     tokens from start (CUDA int32 [rows], None: 0) on; tokens that a request does not hold are zeros."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_read, p, pages, K, V, start, layer, stream)
     T = _tokens(K, "K")
     _check(_lib().akv_paged_read(_params(p, pages), pages.ref, layer, _ints(start, "start", pages.rows, pages.index),
                                  _rows(K, "K", p, pages, T, p.n_kv_heads), _rows(V, "V", p, pages, T, p.n_kv_heads), T,
@@ -259,6 +271,8 @@ def akv_paged_attn(p: PagedParams, pages: Pages, q, out, lse=None, sel: PageSele
                    sm_scale: float = 1.0, layer: int = 0, ws=None, stream=None):
     """q, out: [rows][T][n_q_heads][128]; lse: optional contiguous fp32 [rows][T][n_q_heads].
     ws: CUDA workspace of akv_paged_attn_workspace_size bytes; when None, one is taken from torch's allocator."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_attn, p, pages, q, out, lse, sel, sm_scale, layer, ws, stream)
     T = _tokens(q, "q")
     L = _lib()
     if sel is not None:
@@ -282,6 +296,8 @@ def akv_paged_select_workspace_size(p: PagedParams, pages: Pages, T: int = 1) ->
 def akv_paged_select(p: PagedParams, pages: Pages, q, sel: PageSelection, sink: int = 1, recent: int = 1,
                      layer: int = 0, ws=None, stream=None):
     """q: [rows][T][n_q_heads][128]; fills sel.  ws as in akv_paged_attn, of akv_paged_select_workspace_size bytes."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_select, p, pages, q, sel, sink, recent, layer, ws, stream)
     T = _tokens(q, "q")
     L = _lib()
     _match(sel, pages, T, p.n_kv_heads)
@@ -297,12 +313,16 @@ def _pair(src, dst, pages):
 
 def akv_pages_copy(p: PagedParams, pages: Pages, src, dst, stream=None):
     """Copies page src[i] to page dst[i] in every layer (CUDA int32)."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_copy, p, pages, src, dst, stream)
     a, b, n = _pair(src, dst, pages)
     _check(_lib().akv_pages_copy(_params(p, pages), pages.ref, a, b, n, _stream(stream, pages)), "akv_pages_copy")
 
 
 def akv_pages_fork(p: PagedParams, pages: Pages, src, dst, stream=None):
     """Row dst[i] becomes a second holder of row src[i]'s pages (CUDA int32)."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_fork, p, pages, src, dst, stream)
     a, b, n = _pair(src, dst, pages)
     _check(_lib().akv_pages_fork(_params(p, pages), pages.ref, a, b, n, _stream(stream, pages)), "akv_pages_fork")
 
@@ -315,6 +335,8 @@ def akv_pages_workspace_size(pages: Pages) -> int:
 
 def akv_pages_reserve(p: PagedParams, pages: Pages, n_new, missing, ws=None, stream=None):
     """Pages for each row's next n_new tokens (CUDA int32 [rows]); missing: CUDA int32 [1]."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_reserve, p, pages, n_new, missing, ws, stream)
     ws, at, n = _workspace(ws, pages, stream, akv_pages_workspace_size, pages)
     _check(_lib().akv_pages_reserve(_params(p, pages), pages.ref, _ints(n_new, "n_new", pages.rows, pages.index),
                                     _ints(missing, "missing", 1, pages.index), at, n, _stream(stream, pages)), "akv_pages_reserve")
@@ -322,12 +344,16 @@ def akv_pages_reserve(p: PagedParams, pages: Pages, n_new, missing, ws=None, str
 
 def akv_pages_free(p: PagedParams, pages: Pages, rows, stream=None):
     """Rows (CUDA int32) give up their pages."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_free, p, pages, rows, stream)
     _check(_lib().akv_pages_free(_params(p, pages), pages.ref, _ints(rows, "rows", None, pages.index), rows.numel(),
                                  _stream(stream, pages)), "akv_pages_free")
 
 
 def akv_pages_compact(p: PagedParams, pages: Pages, n_live, ws=None, stream=None):
     """Moves live pages to the front of the pool; n_live: CUDA int32 [1]."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_compact, p, pages, n_live, ws, stream)
     ws, at, n = _workspace(ws, pages, stream, akv_pages_workspace_size, pages)
     _check(_lib().akv_pages_compact(_params(p, pages), pages.ref, _ints(n_live, "n_live", 1, pages.index), at, n,
                                     _stream(stream, pages)), "akv_pages_compact")
