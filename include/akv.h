@@ -575,7 +575,8 @@ akv_status akv_decode_set_events(void* after_scores, void* after_decode);
  * (the operand order of the attention's tensor-core products: a lane's codes are one 16-byte
  * load per 8 tokens, and no two tokens share a byte).  The bounds are the smallest, then the
  * largest key of the page in each dimension (128 values each, the rows' type, before
- * rotation), over every token written since the page's first slot was last written.
+ * rotation), over every token written since the page's first slot was last written; NaN in
+ * a dimension where one of those keys is NaN.
  *
  * Pool.  n_layers layers of n_pages pages each; one table of page numbers serves all layers.
  * All integer state is on the device, so that a step may be captured in a CUDA graph.

@@ -122,23 +122,19 @@ __device__ __forceinline__ uint32_t pack_rows(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// Smaller and larger of two pairs of rows' values: a NaN is left out, or (NAN) passed on.
-template <bool HALF, bool NAN_ = false>
+// Smaller and larger of two pairs of rows' values (a NaN is passed on).
+template <bool HALF>
 __device__ __forceinline__ uint32_t min_rows(uint32_t a, uint32_t b) {
   uint32_t r;
-  if (HALF && NAN_) asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else if (HALF) asm("min.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else if (NAN_) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  if (HALF) asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-template <bool HALF, bool NAN_ = false>
+template <bool HALF>
 __device__ __forceinline__ uint32_t max_rows(uint32_t a, uint32_t b) {
   uint32_t r;
-  if (HALF && NAN_) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else if (HALF) asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else if (NAN_) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  if (HALF) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 __device__ __forceinline__ float min3_nan(float a, float b, float c) {
@@ -192,8 +188,8 @@ __device__ __forceinline__ void quantise(const uint32_t (&w)[16], const uint32_t
       uint32_t a = w[g * kEach / 2], c = a;
 #pragma unroll
       for (int i = 1; i < kEach / 2; ++i) {
-        a = min_rows<HALF, true>(a, w[g * kEach / 2 + i]);
-        c = max_rows<HALF, true>(c, w[g * kEach / 2 + i]);
+        a = min_rows<HALF>(a, w[g * kEach / 2 + i]);
+        c = max_rows<HALF>(c, w[g * kEach / 2 + i]);
       }
       lo[g] = min_nan(lo_half<HALF>(a), hi_half<HALF>(a));
       hi[g] = max_nan(lo_half<HALF>(c), hi_half<HALF>(c));
@@ -373,7 +369,7 @@ __global__ void __launch_bounds__(kMaxThreads, 7) akv_paged_append_kernel(PagedV
   uint4 lo, hi;
   lo.x = lo.y = lo.z = lo.w = HALF ? 0x7c007c00u : 0x7f807f80u;  // + and - infinity
   hi.x = hi.y = hi.z = hi.w = lo.x | 0x80008000u;
-  auto take = [&](const uint4& a, const uint4& b) {
+  auto take = [&](const uint4& a, const uint4& b) {  // (a page with a NaN has the score +infinity)
     lo.x = min_rows<HALF>(lo.x, a.x), lo.y = min_rows<HALF>(lo.y, a.y), lo.z = min_rows<HALF>(lo.z, a.z), lo.w = min_rows<HALF>(lo.w, a.w);
     hi.x = max_rows<HALF>(hi.x, b.x), hi.y = max_rows<HALF>(hi.y, b.y), hi.z = max_rows<HALF>(hi.z, b.z), hi.w = max_rows<HALF>(hi.w, b.w);
   };
