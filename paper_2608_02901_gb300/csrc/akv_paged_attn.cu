@@ -18,9 +18,11 @@
 // conversion; the products are exact in fp32, and a row's scale and minimum are applied to the sums:
 //     l_i = a_i (c_i . q) + m_i sum(q),     y = sum_i (p_i a_i) c_i + sum_i p_i m_i .
 // Queries are exact in fp16 (a power of two times what was given); rotated ones are fp32 and enter as a high and a
-// low half.  The weights p_i a_i are rounded to fp16 (relative 2^-12, below the 2^-9 of a bf16 result); the reference that
-// the exponents p = 2^(l - reference) are taken from follows the largest logit and the largest a so far, so that a weight
-// is at most 2^15 and only underflows 2^-31 below the largest.  Sums, maxima and logits are fp32.
+// low half.  The weights p_i a_i are rounded to fp16: relative 2^-11 for those of 2^-14 and more (a bf16 result is rounded by up
+// to 2^-8).  The reference that a row's exponents p = 2^(l - reference) are taken from follows its largest p a so far, of tokens
+// that it sees and of both groups: that weight is between 2^6 and 2^15, and one down to 2^-20 of it keeps its 2^-11; what
+// smaller ones lose is at most 2^-31 of the largest (tokens whose scale is large but that hardly weigh, or are not seen, cost
+// the others nothing).  Sums, maxima and logits are fp32.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -504,7 +506,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 
     float acc[NT][8][4], sum[NT][2], mins[NT][2][NG], ref[NT][2];
     int e_s = 103;  // the values' scales so far are at most 2^(e_s - 127)
-    float most = kNegInf;  // what l - reference may be, 15 - (e_s - 127); no reference yet
+    float most = kNegInf;  // up to here l - reference has room with any scale so far, 15 - (e_s - 127); no reference yet
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -680,24 +682,30 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         for (int nt = 0; nt < NT; ++nt) top_l = max3(max3(l[i][nt][0], l[i][nt][1], l[i][nt][2]), l[i][nt][3], top_l);
       }
       if (__any_sync(0xffffffffu, top_l > most || top_s > __int_as_float(e_s << 23))) {
-        const int e_new = min(max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top_s)) >> 23) + 1), 254);
+        e_s = min(max(e_s, (int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top_s)) >> 23) + 1), 254);
         // (a row that sees none of its warp's first tokens sees none of the later ones: it keeps its reference)
         const bool first = most == kNegInf;
-        const float place_was = first ? kNegInf : kWeightLog - (float)(e_s - 127), place = kWeightLog - (float)(e_new - 127);
-        e_s = e_new;
-        most = kSlack + place;
+        most = kSlack + kWeightLog - (float)(e_s - 127);
+        float above[NS][2];  // log2 of a power of two above the token's scales, of 2^-24 (the smallest) for scales of 0
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float a = NG == 2 ? fmaxf(vs[i][x][0], vs[i][x][NG - 1]) : vs[i][x][0];
+            above[i][x] = (float)(min(max((int)(__float_as_uint(a) >> 23), 102), 142) - 126);
+          }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            float m = fmaxf(l[0][nt][x], l[0][nt][x + 2]);
-            if (NS == 2) m = max3(m, l[NS - 1][nt][x], l[NS - 1][nt][x + 2]);
+            float m = kNegInf;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) m = max3(m, l[i][nt][x] + above[i][0], l[i][nt][x + 2] + above[i][1]);
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-            // the largest logit so far goes to the new place
-            float up = fmaxf(m, place_was) - place;
-            if (up == kNegInf) up = 0.f;
+            // the row's largest weight goes to its place where it has passed its room
+            const float up = m > (first ? kNegInf : kSlack + kWeightLog) ? m - kWeightLog : 0.f;
             ref[nt][x] += up;
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
