@@ -10,7 +10,7 @@ What a model would give (queries, keys and values of each token) is random here.
   4. frees the answers that are done and compacts the pool,
   5. hands the longest request over to the anchor-residual cache: akv_paged_read gives its rows, akv_encode compresses
      them, akv_decode_attn attends.
-Steps 3's integer state stays on the device: nothing waits for the GPU.
+Step 3's integer state stays on the device: no step waits for the GPU.
 """
 from __future__ import annotations
 
@@ -92,7 +92,8 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
     one = (ids >= B).int()
     out, lse = torch.empty((rows, 1, heads * group, D), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, 1, heads * group), device="cuda")
     kept, kept_lse = torch.empty_like(out), torch.empty_like(lse)
-    share = cosine = 0.0
+    share, cosine = torch.zeros(2, device="cuda")
+    answering = ids[B:]
     for _ in range(steps):
         put(one, 1)
         at = torch.randint(0, 32, (rows,), generator=gen, device="cuda")
@@ -101,9 +102,9 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
         akv.akv_paged_attn(p, pages, q, out, lse=lse, sm_scale=1 / math.sqrt(D), ws=ws)
         akv.akv_paged_select(p, pages, q, sel, sink=1, recent=2, ws=ws)
         akv.akv_paged_attn(p, pages, q, kept, lse=kept_lse, sel=sel, sm_scale=1 / math.sqrt(D), ws=ws)
-        live = one.bool()
-        share += float((kept_lse - lse)[live].exp().mean()) / steps
-        cosine += float(torch.cosine_similarity(out[live].float(), kept[live].float(), dim=-1).mean()) / steps
+        share += (kept_lse - lse)[answering].exp().mean() / steps
+        cosine += torch.cosine_similarity(out[answering].float(), kept[answering].float(), dim=-1).mean() / steps
+    share, cosine = float(share), float(cosine)
     assert pool_pages or int(lacked) == 0
     say(f"{steps} steps: {int((refs > 0).sum())} pages; the {top} pages kept of up to {max_pages} hold {share:.3f} of the "
         f"softmax, outputs' cosine {cosine:.4f}")
