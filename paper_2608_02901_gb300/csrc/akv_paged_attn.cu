@@ -47,7 +47,7 @@ AKV_HD constexpr int stages_of(int nt) { return nt == 1 ? 4 : 6; }
 // 284 us with one, 234 with two; with 16 rows two spill, 179 and 181 us for 4 x 131072 tokens, rotated 217 and 276).
 AKV_HD constexpr int subs_of(int nt) { return nt == 1 ? 2 : 1; }
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kLow = -1e30f;                  // reference of a share that saw no token
+constexpr float kLow = -3.402823466e38f;        // reference of a share that saw no token: below all others
 constexpr float kSlack = 8.f;                   // a weight may pass its place by 2^8 before the reference moves
 constexpr float kWeightLog = 7.f;               // the largest weight's place: 2^7 (at most 2^15 with the slack)
 constexpr int kAlignTiles = 16;                 // tiles a CTA up to which units may get CTAs of their own
