@@ -262,7 +262,7 @@ struct Smem {
   float red[kWarps][8 * NT][kRowPad];       // the warps' outputs at a unit's end
   float red_m[kWarps][8 * NT], red_l[kWarps][8 * NT];
   float qsum[8 * NT][2];                    // sums of a query row over each group of dimensions
-  float qmax[kWarps];
+  float qscale[8 * NT];                     // what its products count
   int pos[kStages][kTileSubs];              // first token of each sub-block; -1: none, -2: a page outside the pool
   uint32_t tile[kStages];                   // the CTA's tile that the stage holds or waits for
   int cursor[kWarps][10];                   // a warp's place, kept here while it works on a unit (registers are short)
@@ -412,7 +412,6 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   uint32_t at = 0;  // tiles done
   while (at < range) {
     int row0, n_tiles, sees, all_see;
-    float dot_scale;
     {
     const Cursor<SEL> cu = kept();
     const int b = cu.g.b, h = SEL ? cu.g.h : cu.index / a.n_blocks;
@@ -424,13 +423,13 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 
     // queries: a warp per row, four dimensions a lane
     constexpr int kTurns = (kRows + kWarps - 1) / kWarps;
-    float qx[kTurns][4];
-    float big = 0.f;
+    float qx[kTurns][4], big[kTurns];
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       const int rr = warp + kWarps * i;
 #pragma unroll
       for (int e = 0; e < 4; ++e) qx[i][e] = 0.f;
+      big[i] = 0.f;
       if (rr < n_rows) {
         const int t = SEL ? cu.g.t : (row0 + rr) / v.G, g = SEL ? row0 + rr : (row0 + rr) % v.G;
         const uint16_t* row = a.q + b * a.qb + t * a.qt + (int64_t)(h * v.G + g) * a.qh + 4 * lane;
@@ -455,21 +454,20 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float x = fabsf(qx[i][e]);
-        if (x <= 3.402823466e38f) big = fmaxf(big, x);  // an infinite or NaN row spoils itself alone
+        if (x <= 3.402823466e38f) big[i] = fmaxf(big[i], x);  // an infinite or NaN row spoils itself alone
       }
+      big[i] = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big[i])));
     }
-    big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-    if (lane == 0) S.qmax[warp] = big;
     named_sync(kConsumerBar, 32 * kWarps);  // (also: every warp is through with the unit before)
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) big = fmaxf(big, S.qmax[w]);
-    // the rows times 2^(14 - e): below 2^14, exact in fp16 down to 2^-23 of the largest
-    const int e_q = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 100);
-    const float up = pow2(14 - e_q);
+    // A row times 2^(14 - e), e its own exponent: below 2^14, and exact in fp16 down to 2^-23 of that.  (With one e for the
+    // rows of a unit, 233.5 us for 235.5 over 8 x 128K tokens, a large row, padding say, took the others' values below fp16's range.)
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       const int rr = warp + kWarps * i;
       if (rr >= kRows) break;
+      const int e = min(max((int)(__float_as_uint(big[i]) >> 23) - 126, -100), 128);
+      const float up = pow2(14 - e);
+      if (lane == 0) S.qscale[rr] = a.scale * pow2(e - 10) * 1048576.f;  // codes count 2^-24, queries 2^(14 - e)
       float sum = (qx[i][0] + qx[i][1]) + (qx[i][2] + qx[i][3]);
 #pragma unroll
       for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
@@ -494,15 +492,16 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][to] = f[HILO ? 1 : 0];
     }
     named_sync(kConsumerBar, 32 * kWarps);
-    dot_scale = a.scale * pow2(10 + e_q);  // codes count 2^-24, queries 2^(14 - e)
     }
-    float qs[NT][2][NG];
+    float qs[NT][2][NG], dot_scale[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int x = 0; x < 2; ++x) {
+        dot_scale[nt][x] = S.qscale[8 * nt + 2 * t4 + x];
 #pragma unroll
         for (int g = 0; g < NG; ++g) qs[nt][x][g] = S.qsum[8 * nt + 2 * t4 + x][g];
+      }
 
     float acc[NT][8][4], sum[NT][2], mins[NT][2][NG], ref[NT][2];
     int e_s = 103;  // the values' scales so far are at most 2^(e_s - 127)
@@ -581,26 +580,13 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       float l[NS][NT][4];
       {
         uint4 kc[NS][2];
-        float ks[NS][2][NG];
+        uint32_t kw[NS][2][NG];
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
           kc[i][0] = lds128(sb + i * kSub + 16 * lane);
           kc[i][1] = lds128(sb + i * kSub + 512 + 16 * lane);
-          float km[2][NG];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            uint32_t w[NG];
-            words_at(i, x, 0, w);
-#pragma unroll
-            for (int g = 0; g < NG; ++g) ks[i][x][g] = word_scale(w[g]) * dot_scale, km[x][g] = word_min(w[g]);
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              l[i][nt][x] = fmaf(km[x >> 1][0], qs[nt][x & 1][0], -ref[nt][x & 1]);
-              if (NG == 2) l[i][nt][x] = fmaf(km[x >> 1][NG - 1], qs[nt][x & 1][NG - 1], l[i][nt][x]);
-            }
+          for (int x = 0; x < 2; ++x) words_at(i, x, 0, kw[i][x]);
         }
         // (sums of 64 dimensions each, the low halves first: the tensor cores cut what they add off at the sum's size)
 #pragma unroll
@@ -629,8 +615,21 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int x = 0; x < 4; ++x) l[i][nt][x] = fmaf(ks[i][x >> 1][half * (NG - 1)], s[i][nt][x], l[i][nt][x]);
+              for (int x = 0; x < 4; ++x) {
+                const float unit = word_scale(kw[i][x >> 1][half * (NG - 1)]);
+                l[i][nt][x] = half ? fmaf(unit, s[i][nt][x], l[i][nt][x]) : unit * s[i][nt][x];
+              }
         }
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              float y = fmaf(word_min(kw[i][x >> 1][0]), qs[nt][x & 1][0], -ref[nt][x & 1]);
+              if (NG == 2) y = fmaf(word_min(kw[i][x >> 1][NG - 1]), qs[nt][x & 1][NG - 1], y);
+              l[i][nt][x] = fmaf(l[i][nt][x], dot_scale[nt][x & 1], y);
+            }
       }
       float vs[NS][2][NG], vm[NS][2][NG];
 #pragma unroll
