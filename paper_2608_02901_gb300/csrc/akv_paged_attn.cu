@@ -493,15 +493,17 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     }
     named_sync(kConsumerBar, 32 * kWarps);
     }
-    float qs[NT][2][NG], dot_scale[NT][2];
+    // What goes with a lane's rows, 2 t4 and 2 t4 + 1 of each eight: with 16 rows it stays in shared memory, registers are short
+    // (4 x 128K tokens, 4 query tokens each: 168 us for 183).
+    float own_sum[2][NG], own_scale[2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int x = 0; x < 2; ++x) {
+      own_scale[x] = S.qscale[2 * t4 + x];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        dot_scale[nt][x] = S.qscale[8 * nt + 2 * t4 + x];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) qs[nt][x][g] = S.qsum[8 * nt + 2 * t4 + x][g];
-      }
+      for (int g = 0; g < NG; ++g) own_sum[x][g] = S.qsum[2 * t4 + x][g];
+    }
+    auto row_sum = [&](int nt, int x, int g) { return NT == 1 ? own_sum[x][g] : S.qsum[8 * nt + 2 * t4 + x][g]; };
+    auto row_scale = [&](int nt, int x) { return NT == 1 ? own_scale[x] : S.qscale[8 * nt + 2 * t4 + x]; };
 
     float acc[NT][8][4], sum[NT][2], mins[NT][2][NG], ref[NT][2];
     int e_s = 103;  // the values' scales so far are at most 2^(e_s - 127)
@@ -626,9 +628,9 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              float y = fmaf(word_min(kw[i][x >> 1][0]), qs[nt][x & 1][0], -ref[nt][x & 1]);
-              if (NG == 2) y = fmaf(word_min(kw[i][x >> 1][NG - 1]), qs[nt][x & 1][NG - 1], y);
-              l[i][nt][x] = fmaf(l[i][nt][x], dot_scale[nt][x & 1], y);
+              float y = fmaf(word_min(kw[i][x >> 1][0]), row_sum(nt, x & 1, 0), -ref[nt][x & 1]);
+              if (NG == 2) y = fmaf(word_min(kw[i][x >> 1][NG - 1]), row_sum(nt, x & 1, NG - 1), y);
+              l[i][nt][x] = fmaf(l[i][nt][x], row_scale(nt, x & 1), y);
             }
       }
       float vs[NS][2][NG], vm[NS][2][NG];
