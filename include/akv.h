@@ -653,8 +653,10 @@ akv_status akv_paged_read(const akv_paged_params* p, const akv_pages* pages, int
  * over the cache, their own keys and values included: query token t sees tokens
  * i < lens[b] - T + 1 + t, or with `sel` those of them that are in its kept pages.
  *     l_i = sm_scale q . k^_i,  out = sum_i softmax(l)_i v^_i,  lse = log sum_i exp(l_i)
- * (fp32 sums).  A query that sees no token has out = 0 and lse = -infinity; a request with a
- * page number outside the pool among the pages that it attends has NaN outputs.
+ * in fp32, but for the weights of the value codes, softmax numerators times scales: these are rounded
+ * to fp16, by at most 2^-11 of a weight or 2^-31 of the row's largest.  A query that sees no token
+ * has out = 0 and lse = -infinity; a request with a page number outside the pool among the pages
+ * that it attends has NaN outputs.
  * q, out: [rows][T][n_q_heads][128]; lse: fp32 [rows][T][n_q_heads] or null.  `top` of the
  * workspace size is the selection's, 0 without one. */
 akv_status akv_paged_attn_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T, int32_t top,
@@ -666,10 +668,12 @@ akv_status akv_paged_attn(const akv_paged_params* p, const akv_pages* pages, int
 /* Chooses the pages that each query token attends, from the pages' bounds.  Of the n pages that
  * it sees, the first `sink` and the last `recent` are kept, and of the others those of the
  * highest score, `top` in all (top >= sink + recent; ties to the lower page; all n where
- * n <= top).  Entries of sel->pages beyond the count are -1.  The score bounds q . k over the page from above, in
- * whole numbers of 7 bits: q^ = rne(q 2^(7 - e)) clamped to +-127, e the exponent (frexp) of the
- * largest |q| among the G rows of the query group; lo^, hi^ likewise from the page's bounds with
- * the page's own exponent e_p (clamped to +-100);
+ * n <= top).  Entries of sel->pages beyond the count are -1.  The score is the bound
+ * sum_d max(q_d lo_d, q_d hi_d) of q . k over the page in whole numbers of 7 bits, rounded to
+ * nearest (so that it may lie below the bound itself, as it does for about half of all pages):
+ * q^ = rne(q 2^(7 - e)) clamped to +-127, e the exponent (frexp) of the largest |q| among the G
+ * rows of the query group; lo^, hi^ likewise from the page's bounds with the page's own exponent
+ * e_p (both exponents clamped to +-100);
  *     score = 2^e_p max over the G rows of sum_d max(q^_d lo^_d, q^_d hi^_d),
  * whose sums are exact: the choice does not depend on an order of additions.  A page with an
  * infinite or NaN bound has the score +infinity; a page number outside the pool -infinity; with an

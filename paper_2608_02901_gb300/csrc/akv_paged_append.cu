@@ -1,7 +1,7 @@
 // Paged 4-bit cache: quantising new tokens into their pages, and reading rows back.
 //
-// Both move a row between 256 dense bytes and 64 + 4 NG held ones; what bounds them is the operations per value (about
-// 17 an element appended with rotation, 9 read back, where the bytes alone would leave room for 14), so the layout saves
+// Both move a row between 256 dense bytes and 64 + 4 NG held ones; what bounds them is the operations per value (16
+// an element appended with rotation, 10 read back, where the bytes alone would leave room for 14), so the layout saves
 // those.  Four lanes share a row: lane u of them holds dimensions 32 c + 8 u + n (c < 4, n < 8), so that
 //   - the dense side is four 16-byte accesses a lane, 64 contiguous bytes a row each time;
 //   - the key codes of a lane are the 16 contiguous bytes of its row's words 4 u .. 4 u + 3, the value codes (after an

@@ -1,17 +1,18 @@
 // Attention over the paged 4-bit cache: a persistent launch that reads each attended page once, and a launch that joins
 // the shares of units that several CTAs worked on.
 //
-// Bound by HBM in principle (144 bytes a token and head at two groups a row, 2 x 16 products of 16 x 16 x 8), by the integer
-// operations and the latency of a warp's chain in practice: 4 x 131072 tokens, 8 KV heads, 4 or 8 query heads each, take
-// 114 to 122 us (5.0 TB/s, 74 % of the measured rate), rotated 130 (half as many products again), with 16 query rows 168;
-// 8 x 131072 rotated tokens 233 us (5.2 TB/s).  A call has about 8 us that do not depend on the length: the plan, the
+// Bound by HBM in principle (144 bytes a token and head at two groups a row, 2 x 16 products of 16 x 16 x 8), in practice by a
+// warp's chain, which 16 warps an SM do not cover: no pipe is full (issue 55 %, ALU 47 %, tensor 34 %, DRAM 57 %).
+// 4 x 131072 tokens, 8 KV heads, 4 or 8 query heads each, take 120 us (5.0 TB/s, 74 % of the measured rate), rotated 133
+// (half as many products again), with 16 query rows 168, rotated 207;
+// 8 x 131072 rotated tokens 235 us (5.1 TB/s).  A call has about 8 us that do not depend on the length: the plan, the
 // first page numbers and copies, the joins (1021 tokens: 7 us, and 4 of the second launch).
 //
 // A unit is one KV head of one request (or of one query token, where each has its own pages) with up to 8 NT query
 // rows.  Units are cut into tiles of 128 tokens, and the tiles of all units into equal contiguous ranges, one per CTA,
-// so that one long request and many short ones fill the GPU alike (where CTAs have few tiles, see plan).  In a CTA one warp copies (bulk copies of whole
-// sub-blocks into a ring of stages) and the others take the sub-blocks of 16 tokens in turn, without a barrier between
-// them: each has its own running maximum, sum and output, joined at the unit's end.
+// so that one long request and many short ones fill the GPU alike (where CTAs have few tiles, see plan).  In a CTA one warp
+// copies (bulk copies of whole sub-blocks into a ring of stages) and the others take the sub-blocks of 16 tokens in turn,
+// without a barrier between them: each has its own running reference, sum and output, joined at the unit's end.
 //
 // The codes go into the tensor cores as they are.  A nibble, masked in place, is the fp16 subnormal c 2^-24 (or
 // 16 c 2^-24 for the odd ones, whose partner is scaled by 1/16), so eight values cost five integer operations and no
@@ -36,7 +37,7 @@ namespace {
 
 constexpr int kTileTokens = 128, kTileSubs = kTileTokens / kSubTokens;
 // A unit has 8 NT query rows, NT 1 or 2.  (Four were slower than two units of 16 rows that read the cache twice: 375 and
-// 357 us for 32 rows a head over 4 x 131072 tokens, 53 and 42 us over 4 x 8192: 255 registers leave an SM seven warps.)
+// 319 us for 32 rows a head over 4 x 131072 tokens, 53 and 40 us over 4 x 8192: 255 registers leave an SM seven warps.)
 // Computing warps of a CTA, next to one that copies: an SM has room for 16 warps of 128 registers or 12 of 168 (a 17th
 // and a 13th would take them down to 96 and 128, which spill).  Two CTAs per SM of 8 rows, one of 16.
 AKV_HD constexpr int warps_of(int nt) { return nt == 1 ? 7 : 11; }

@@ -5,8 +5,8 @@
 // q+ hi + q- lo, two products.  The numbers are at most 127, exact in bf16 and fp16, and the sums at most 2^22, exact in
 // fp32: the tensor cores add them up without rounding, in any order, so that the choice is the same on every machine.
 // What costs is turning the bounds into whole numbers (three operations a pair); a warp does it once for all query rows.
-// 8 x 2048 pages of 8 heads: 21 us, 3.2 TB/s.  The bytes bound it: a plain read of 512-byte pieces 9.7 KB apart reaches 3.35
-// TB/s in any order and at any number of CTAs.
+// 8 x 2048 pages of 8 heads: 20 to 22 us, 3.1 to 3.3 TB/s.  The page format bounds it: a plain read of 512-byte pieces 9.7 KB
+// apart, as bounds inside the pages' blocks are, reaches 3.35 TB/s in any order and at any number of CTAs.
 // The choice finds the key of the last page kept, 8 bits of its range a pass: 6 us for 512 pages and 8 us for 2048,
 // latency alone.
 #include "akv_paged.cuh"
