@@ -375,7 +375,7 @@ def _run_own(s):
         return {"share": s["share"], "out": s["out"], "lse": s["lse"]}
     if case["op"] == "weigh":
         old = s["old"] if case["decay"] else None
-        akv.akv_paged_weights(p, pages, s["q"], s["lse"], s["new"], old=old, decay=case["decay"], sm_scale=SM_SCALE)
+        akv.akv_paged_weights(p, pages, s["q"], s["lse"], s["new"], was=old, decay=case["decay"], sm_scale=SM_SCALE)
         return {"new": s["new"]}
     akv.akv_paged_evict(p, pages, s["src"], s["dst"], s["scores"], h["kept"], keep=s["keep"], sink=case["sink"], recent=case["recent"])
     return {"kept": s["kept"], "count": s["count"], "scores": s["scores"], "pool": s["pool"]}
