@@ -684,6 +684,87 @@ akv_status akv_paged_select(const akv_paged_params* p, const akv_pages* pages, i
                             int32_t T, int32_t sink, int32_t recent, const akv_selection* sel, void* ws,
                             size_t ws_bytes, akv_stream_t stream);
 
+/* Rows that begin with the same pages (akv_pages_fork makes such rows).  A group is all rows whose table has the same page
+ * of the pool at position 0 and that hold tokens; other rows are groups of their own.  Four device int32 [rows] arrays:
+ *   leader  the lowest row of the row's group
+ *   pages   the table positions, from the first on, at which every row of the group holds tokens of the same page; 0 where the
+ *           group is one row
+ *   size    rows of the group
+ *   order   the rows by (leader, row): a group's rows are neighbours there
+ * One level: rows that share more with some of their group than with all of it share what all have. */
+typedef struct akv_share {
+  int32_t* leader;
+  int32_t* pages;
+  int32_t* size;
+  int32_t* order;
+} akv_share;
+
+/* Fills `share` from the table and the lengths.  It stays valid until a shared page or a row's first pages change
+ * (akv_pages_fork, _free, _reserve into a shared page, _compact, _trim, a lowered length); tokens may be appended.
+ * ws: akv_pages_workspace_size. */
+akv_status akv_pages_share(const akv_paged_params* p, const akv_pages* pages, const akv_share* share, void* ws,
+                           size_t ws_bytes, akv_stream_t stream);
+
+/* akv_paged_attn of the same arguments, but for the order of its sums: the shared pages of a group are read once for all its rows'
+ * queries (as one matrix product), every row's further tokens as akv_paged_attn reads them, and both parts are joined in one
+ * softmax.  Numbers in `share` that are out of range are left out (rows outside the table) or clamped (pages).
+ *   In the shared part a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
+ * m + c a to fp16 as well (2^-11 of it; where a tile of 128 tokens has a scale above 2048, at most 2^-20).  A query that sees a token
+ * with an infinity or a NaN has NaN in all its outputs. */
+akv_status akv_paged_attn_shared_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
+                                                size_t* ws_bytes);
+akv_status akv_paged_attn_shared(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
+                                 const akv_rows* out, float* lse, int32_t T, float sm_scale, const akv_share* share,
+                                 void* ws, size_t ws_bytes, akv_stream_t stream);
+
+/* A number for each token that a request holds and each KV head: request b, head h, token i at
+ * ptr + b stride_b + h stride_h + i (elements; device fp32).  cap: numbers of a head, at least max_pages * page_tokens. */
+typedef struct akv_scores {
+  float* ptr;
+  int64_t stride_b, stride_h;
+  int32_t cap;
+} akv_scores;
+
+/* Adds up the attention weights that tokens got from the last T query tokens (1 .. AKV_PAGED_MAX_QUERY; those of akv_paged_attn,
+ * which gives their lse, fp32 [rows][T][n_q_heads]):
+ *     now[b][h][i] = decay was[b][h][i] + sum over t and the G query heads of h of exp(sm_scale q . k^_i - lse)
+ * over the queries that see token i, for the tokens i < lens[b] that request b holds; further numbers are left as they were.
+ * `was` may be null (zeros) or the same as `now`, and is not read where decay is 0.  Queries whose lse is not a finite number, and
+ * tokens whose key has an infinity or a NaN or whose page is none of the pool's, add nothing.  Sums in fp32, in a fixed order. */
+akv_status akv_paged_weights(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
+                             const float* lse, int32_t T, float sm_scale, float decay, const akv_scores* was,
+                             const akv_scores* now, akv_stream_t stream);
+
+/* The tokens that rows keep: [n][n_kv_heads][top] places in the row that they come from, ascending, -1 beyond the count, and
+ * count [n]. */
+typedef struct akv_kept {
+  int32_t* tokens;
+  int32_t* count;
+  int32_t top;
+} akv_kept;
+
+/* Row dst[i] gets the tokens that row src[i] keeps (device int32 [n]; dst[i] = src[i]: in place), in their order, at its first
+ * places; dst rows are named once and are no other pair's src.  Of the `held` tokens of row src[i] each KV head keeps
+ * count[i] = min(held, keep[i]) (device int32 [n], null = top each; clamped to 0 .. top): the first `sink`, the last `recent` (if
+ * both are more than the count, the first of these), and of the others those of the highest scores, ties to the lower place; a NaN
+ * is below all numbers.  Their scores go with them to row dst[i].  Places of dst behind the count are left as they were, in the
+ * pool and among the scores.
+ *   The pages of dst[i] at its first count[i] places must be its own (akv_pages_reserve sees to it).  Where one of them is
+ * none of the pool's or, pages->refs given, has more than one holder (in place: if a token is evicted), or a row is outside the table, or a
+ * page with tokens of src[i] is none of the pool's, the pair is left alone: count[i] = -1, its tokens -1.
+ *   lens is read, not changed, since a model's layers share it: the caller sets lens[dst[i]] to the count once every layer is done
+ * (every layer has the same counts), and gives up what is behind it (akv_pages_trim in place, akv_pages_free of src).  Pages with bounds
+ * (AKV_FLAG_BOUNDS) are not supported: theirs are of the keys before quantisation.  Order is kept because tokens are told apart by
+ * it (the last ones, and those that a draft sees), so that eviction in place moves all tokens behind the first that goes: a decode
+ * loop evicts some tens of tokens at a time, not one a step. */
+akv_status akv_paged_evict(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const int32_t* src,
+                           const int32_t* dst, int32_t n, const akv_scores* scores, const int32_t* keep, int32_t sink,
+                           int32_t recent, const akv_kept* kept, akv_stream_t stream);
+
+/* Rows rows[i] (device int32 [n]) give up the pages behind their length: one holder less each, table entries -1. */
+akv_status akv_pages_trim(const akv_paged_params* p, const akv_pages* pages, const int32_t* rows, int32_t n,
+                          akv_stream_t stream);
+
 /* Copies page src[i] to page dst[i] (device int32 [n]) in every layer.  No page may be written
  * twice or both read and written; pairs with a number outside the pool are left out. */
 akv_status akv_pages_copy(const akv_paged_params* p, const akv_pages* pages, const int32_t* src, const int32_t* dst,

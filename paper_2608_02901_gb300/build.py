@@ -28,7 +28,10 @@ SOURCES = {
     "akv_paged_api.cpp": [],
     "akv_paged_append.cu": [],
     "akv_paged_attn.cu": [],
+    "akv_paged_evict.cu": [],
     "akv_paged_select.cu": [],
+    "akv_paged_shared.cu": [],
+    "akv_paged_weights.cu": [],
     "akv_pages.cu": [],
     "akv_encode.cu": ["--fmad=false"],  # fp64 decisions: no contraction
 }

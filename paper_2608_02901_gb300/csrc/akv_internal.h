@@ -205,15 +205,40 @@ AKV_HD constexpr size_t paged_slot_floats(int rows) { return (size_t)rows * 130;
 // query rows of one attention unit: one or two 8-column operand tiles
 constexpr int paged_unit_rows(int rows) { return rows <= 8 ? 8 : 16; }
 
+// Part of a query row's softmax: 128 sums, the reference of their exponents (log2 units), the normaliser; padded.
+constexpr int kPartFloats = 132;
+// A launch over each request's own tokens, those behind the pages that it shares: [rows] first pages to leave out, and for
+// each query row [rows][T][n_q_heads] its part, or the CTAs (first, how many) whose slots hold the shares of it.
+struct PagedWhere {
+  int32_t first, n;  // first CTA, -1: the part is whole in its place
+};
+struct PagedOwn {
+  const int32_t* pages;
+  float* part;
+  PagedWhere* where;
+};
+
 int launch_paged_append(const PagedView& v, const akv_rows& K, const akv_rows& V, int32_t T, const int32_t* n_new, void* stream);
 int launch_paged_read(const PagedView& v, const int32_t* start, const akv_rows& K, const akv_rows& V, int32_t T, void* stream);
 int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
                       const akv_selection* sel, void* ws, void* stream);
 size_t paged_attn_ws_bytes(const PagedView& v, int32_t T, int32_t top);
+// The own tokens' part alone; ws of paged_attn_ws_bytes(v, T, 0), whose slots are read at paged_own_slots(ws).
+int launch_paged_own(const PagedView& v, const akv_rows& q, int32_t T, float sm_scale, const PagedOwn& own, void* ws, void* stream);
+const float* paged_own_slots(const void* ws);
 int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_t sink, int32_t recent, const akv_selection& sel,
                         void* ws, void* stream);
 size_t paged_select_ws_bytes(const PagedView& v, int32_t T);
+int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
+                        const akv_share& share, void* ws, void* stream);
+size_t paged_shared_ws_bytes(const PagedView& v, int32_t T);
+int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse, int32_t T, float sm_scale, float decay,
+                         const akv_scores* was, const akv_scores& now, void* stream);
+int launch_paged_evict(const PagedView& v, const int32_t* src, const int32_t* dst, int32_t n, const akv_scores& scores,
+                       const int32_t* keep, int32_t sink, int32_t recent, const akv_kept& kept, void* stream);
 size_t pages_ws_bytes(const PagesState& s);
+int launch_pages_share(const PagesState& s, const akv_share& share, void* ws, void* stream);
+int launch_pages_trim(const PagesState& s, const int32_t* rows, int32_t n, void* stream);
 int launch_pages_copy(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
 int launch_pages_fork(const PagesState& s, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
 int launch_pages_reserve(const PagesState& s, const int32_t* n_new, int32_t* missing, void* ws, void* stream);

@@ -154,6 +154,35 @@ akv_status check_list(const int32_t* a, const int32_t* b, int32_t n) {
   return AKV_OK;
 }
 
+akv_status check_share(const akv_share* s, const akv_pages* g) {
+  // (every row's place among the others is counted)
+  if (g->rows > (1 << 16)) return fail(AKV_ERR_UNSUPPORTED, "share: more than 2^16 rows");
+  if (!s || !s->leader || !s->pages || !s->size || !s->order) return fail(AKV_ERR_INVALID, "null share or array of it");
+  if (((uintptr_t)s->leader | (uintptr_t)s->pages | (uintptr_t)s->size | (uintptr_t)s->order) % 4)
+    return fail(AKV_ERR_INVALID, "share must be 4-byte aligned");
+  return AKV_OK;
+}
+
+akv_status check_scores(const akv_scores* s, const char* what, const akv_pages* g, const akv_paged_params* p, bool written) {
+  if (!s || !s->ptr) return fail(AKV_ERR_INVALID, "null ", what);
+  if ((uintptr_t)s->ptr % 4) return fail(AKV_ERR_INVALID, what, " must be 4-byte aligned");
+  if (s->cap < g->max_pages * p->page_tokens) return fail(AKV_ERR_TOO_SMALL, what, ": room for max_pages * page_tokens numbers a head");
+  if (s->stride_b < 0 || s->stride_h < 0) return fail(AKV_ERR_INVALID, what, ": negative stride");
+  if (!written) return AKV_OK;
+  // numbers on top of one another: the smaller stride steps over a head's, the larger over all of the smaller's axis
+  int64_t near = s->stride_h, far = s->stride_b, n = p->n_kv_heads, m = g->rows;
+  if (far < near) std::swap(near, far), std::swap(n, m);
+  int64_t extent = s->cap;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t stride = i ? far : near, count = i ? m : n;
+    if (count <= 1) continue;
+    if (stride < extent) return fail(AKV_ERR_INVALID, what, ": heads' numbers overlap");
+    if (stride > (INT64_MAX / 8 - extent) / (count - 1)) return fail(AKV_ERR_INVALID, what, ": strides out of range");
+    extent += stride * (count - 1);
+  }
+  return AKV_OK;
+}
+
 akv_status launched(int err, const char* what) {
   if (err) return fail(AKV_ERR_CUDA, what, " launch failed: ", cuda_error_string(err));
   return AKV_OK;
@@ -255,6 +284,83 @@ akv_status akv_paged_select(const akv_paged_params* p, const akv_pages* pages, i
     return fail(AKV_ERR_INVALID, "sink and recent must be >= 0 and together at most top");
   AKV_TRY(check_ws(ws, ws_bytes, paged_select_ws_bytes(c.v, T)));
   return launched(launch_paged_select(c.v, *q, T, sink, recent, *sel, ws, (void*)stream), "selection");
+}
+
+akv_status akv_pages_share(const akv_paged_params* p, const akv_pages* pages, const akv_share* share, void* ws,
+                           size_t ws_bytes, akv_stream_t stream) {
+  PagesState s;
+  AKV_TRY(check_state(p, pages, false, &s));
+  AKV_TRY(check_share(share, pages));
+  AKV_TRY(check_ws(ws, ws_bytes, pages_ws_bytes(s)));
+  return launched(launch_pages_share(s, *share, ws, (void*)stream), "share");
+}
+
+akv_status akv_paged_attn_shared_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
+                                                size_t* ws_bytes) {
+  PagedCall c;
+  AKV_TRY(check_pages(p, pages, &c));
+  AKV_TRY(check_query(T));
+  if (!ws_bytes) return fail(AKV_ERR_INVALID, "null ws_bytes");
+  *ws_bytes = paged_shared_ws_bytes(c.v, T);
+  return AKV_OK;
+}
+
+akv_status akv_paged_attn_shared(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
+                                 const akv_rows* out, float* lse, int32_t T, float sm_scale, const akv_share* share,
+                                 void* ws, size_t ws_bytes, akv_stream_t stream) {
+  PagedCall c;
+  AKV_TRY(check_layer(p, pages, layer, &c));
+  AKV_TRY(check_query(T));
+  AKV_TRY(check_rows(q, "q"));
+  AKV_TRY(check_written(out, "out", pages->rows, T, p->n_q_heads));
+  if ((uintptr_t)lse % 4) return fail(AKV_ERR_INVALID, "lse must be 4-byte aligned");
+  if (!std::isfinite(sm_scale)) return fail(AKV_ERR_INVALID, "sm_scale must be finite");
+  AKV_TRY(check_share(share, pages));
+  AKV_TRY(check_ws(ws, ws_bytes, paged_shared_ws_bytes(c.v, T)));
+  return launched(launch_paged_shared(c.v, *q, *out, lse, T, sm_scale, *share, ws, (void*)stream), "shared attention");
+}
+
+akv_status akv_paged_weights(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
+                             const float* lse, int32_t T, float sm_scale, float decay, const akv_scores* was,
+                             const akv_scores* now, akv_stream_t stream) {
+  PagedCall c;
+  AKV_TRY(check_layer(p, pages, layer, &c));
+  AKV_TRY(check_query(T));
+  AKV_TRY(check_rows(q, "q"));
+  if (!lse) return fail(AKV_ERR_INVALID, "null lse");
+  if ((uintptr_t)lse % 4) return fail(AKV_ERR_INVALID, "lse must be 4-byte aligned");
+  if (!std::isfinite(sm_scale)) return fail(AKV_ERR_INVALID, "sm_scale must be finite");
+  if (!std::isfinite(decay)) return fail(AKV_ERR_INVALID, "decay must be finite");
+  if (was) AKV_TRY(check_scores(was, "was", pages, p, false));
+  AKV_TRY(check_scores(now, "now", pages, p, true));
+  return launched(launch_paged_weights(c.v, *q, lse, T, sm_scale, decay, decay != 0.f ? was : nullptr, *now, (void*)stream), "weights");
+}
+
+akv_status akv_paged_evict(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const int32_t* src,
+                           const int32_t* dst, int32_t n, const akv_scores* scores, const int32_t* keep, int32_t sink,
+                           int32_t recent, const akv_kept* kept, akv_stream_t stream) {
+  PagedCall c;
+  AKV_TRY(check_layer(p, pages, layer, &c));
+  if (c.v.bounds) return fail(AKV_ERR_UNSUPPORTED, "a cache with bounds (AKV_FLAG_BOUNDS) cannot evict");
+  AKV_TRY(check_list(src, dst, n));
+  if ((int64_t)n * p->n_kv_heads > (1 << 22)) return fail(AKV_ERR_UNSUPPORTED, "too many rows and heads");
+  AKV_TRY(check_scores(scores, "scores", pages, p, true));
+  if ((uintptr_t)keep % 4) return fail(AKV_ERR_INVALID, "keep must be 4-byte aligned");
+  if (sink < 0 || recent < 0) return fail(AKV_ERR_INVALID, "sink and recent must be >= 0");
+  if (!kept || (n && (!kept->tokens || !kept->count))) return fail(AKV_ERR_INVALID, "null kept or array of it");
+  if (((uintptr_t)kept->tokens | (uintptr_t)kept->count) % 4) return fail(AKV_ERR_INVALID, "kept must be 4-byte aligned");
+  if (kept->top < 1 || kept->top > (1 << 30)) return fail(AKV_ERR_INVALID, "kept: top must be in 1 .. 2^30");
+  if (n == 0) return AKV_OK;
+  return launched(launch_paged_evict(c.v, src, dst, n, *scores, keep, sink, recent, *kept, (void*)stream), "eviction");
+}
+
+akv_status akv_pages_trim(const akv_paged_params* p, const akv_pages* pages, const int32_t* rows, int32_t n,
+                          akv_stream_t stream) {
+  PagesState s;
+  AKV_TRY(check_state(p, pages, true, &s));
+  AKV_TRY(check_list(rows, rows, n));
+  if (n == 0) return AKV_OK;
+  return launched(launch_pages_trim(s, rows, n, (void*)stream), "trim");
 }
 
 akv_status akv_pages_workspace_size(const akv_paged_params* p, const akv_pages* pages, size_t* ws_bytes) {

@@ -70,7 +70,12 @@ struct AttnArgs {
   int n_blocks;   // units that share them
   int groups;     // requests, or (request, query token, head) with a selection
   int per_group;  // units of a group
+  PagedOwn own;   // kOwn: where a request's own tokens begin, and where their part of the softmax goes
 };
+
+// What a launch attends: all of a request's tokens, those of its kept pages, or those behind the pages that it shares, whose
+// sums are joined with the shared pages' elsewhere.
+enum Mode { kAll, kKept, kOwn };
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -117,11 +122,13 @@ struct Group {
   int b, t, h;   // (t, h: with a selection)
   int tokens;    // positions its tiles cover: the request's, or the kept pages'
   int sees;      // tokens that may be attended at all
+  int start;     // position of the first of them
 };
-template <bool SEL>
+template <Mode M>
 __device__ __forceinline__ Group group_of(const AttnArgs& a, int gi) {
   Group g;
-  if (SEL) {
+  g.start = 0;
+  if (M == kKept) {
     g.h = gi % a.v.H;
     g.t = gi / a.v.H % a.T;
     g.b = gi / a.v.H / a.T;
@@ -131,6 +138,10 @@ __device__ __forceinline__ Group group_of(const AttnArgs& a, int gi) {
     g.b = gi;
     g.t = g.h = 0;
     g.sees = g.tokens = held_tokens(a.v, gi);
+    if (M == kOwn) {
+      g.start = min(max(a.own.pages[gi], 0), a.v.max_pages) << a.v.page_log;
+      g.tokens = max(0, g.tokens - g.start);
+    }
   }
   return g;
 }
@@ -142,12 +153,12 @@ struct Range {
   int ctas, shares;  // shares: into how many CTAs' parts the CTA's one unit is cut; 0: the CTA goes over tiles of several
 };
 // The place of a tile: unit `index` of group `gi`, tile `ti` of the unit.
-template <bool SEL>
+template <Mode M>
 struct Cursor {
   int gi, index, ti, tiles;
   Group g;
   __device__ __forceinline__ void open(const AttnArgs& a) {
-    g = group_of<SEL>(a, gi);
+    g = group_of<M>(a, gi);
     tiles = tiles_of(g);
   }
   // the first tile of the next unit
@@ -164,7 +175,7 @@ struct Cursor {
 struct PlanSmem {
   int64_t part[2][16];  // sums of the warps
   int most[16];
-  int place[10];        // the CTA's place: what the thread that finds it writes down
+  int place[11];        // the CTA's place: what the thread that finds it writes down
 };
 // Sum over the CTA's threads before this one; *total: over all.  All threads call it.
 template <int kThreads>
@@ -189,17 +200,17 @@ __device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* part, int64_t*
 }
 
 // Every thread: this CTA's range and its first tile.
-template <int kThreads, bool SEL>
-__device__ __forceinline__ Range plan(const AttnArgs& a, PlanSmem& S, Cursor<SEL>& c) {
+template <int kThreads, Mode M>
+__device__ __forceinline__ Range plan(const AttnArgs& a, PlanSmem& S, Cursor<M>& c) {
   const int tid = threadIdx.x, strip = (a.groups + kThreads - 1) / kThreads;  // groups of a thread
   const int g0 = tid * strip, g1 = min(a.groups, g0 + strip);
-  Cursor<SEL> mine;  // the thread's first group
+  Cursor<M> mine;  // the thread's first group
   mine.gi = g0;
   int64_t tiles = 0;
   if (g0 < g1) {
     mine.open(a);
     tiles = mine.tiles;
-    for (int gi = g0 + 1; gi < g1; ++gi) tiles += tiles_of(group_of<SEL>(a, gi));
+    for (int gi = g0 + 1; gi < g1; ++gi) tiles += tiles_of(group_of<M>(a, gi));
   }
   Range r;
   r.shares = 0;
@@ -239,10 +250,12 @@ __device__ __forceinline__ Range plan(const AttnArgs& a, PlanSmem& S, Cursor<SEL
     int each = r.shares ? shares_of(mine.tiles) : mine.tiles, i = (int)(rest % each);
     S.place[0] = mine.gi, S.place[1] = (int)(rest / each), S.place[2] = i, S.place[3] = mine.tiles, S.place[4] = mine.g.b;
     S.place[5] = mine.g.t, S.place[6] = mine.g.h, S.place[7] = mine.g.tokens, S.place[8] = mine.g.sees, S.place[9] = each;
+    if (M == kOwn) S.place[10] = mine.g.start;
   }
   __syncthreads();
   c.gi = S.place[0], c.index = S.place[1], c.ti = S.place[2], c.tiles = S.place[3], c.g.b = S.place[4];
   c.g.t = S.place[5], c.g.h = S.place[6], c.g.tokens = S.place[7], c.g.sees = S.place[8];
+  c.g.start = M == kOwn ? S.place[10] : 0;
   if (r.shares) {
     const int i = c.ti;
     r.shares = S.place[9];
@@ -276,8 +289,9 @@ struct Smem {
 
 constexpr int kConsumerBar = 1;
 
-template <int NG, int NT, bool HILO, bool SEL>
+template <int NG, int NT, bool HILO, Mode M>
 __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_paged_attn_kernel(const __grid_constant__ AttnArgs a) {
+  constexpr bool SEL = M == kKept;
   extern __shared__ __align__(128) uint8_t smem_raw[];
   Smem<NT>& S = *reinterpret_cast<Smem<NT>*>(smem_raw);
   constexpr uint32_t kSub = 2048 + 128 * NG;
@@ -285,7 +299,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedView& v = a.v;
 
-  launch_dependents();
+  if (M != kOwn) launch_dependents();
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&S.full[s]), 1);
@@ -296,9 +310,11 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   wait_for_stream();
-  Cursor<SEL> c;
-  const Range r = plan<kThreads, SEL>(a, S.plan, c);  // (its barriers order the initialisation too)
-  if (tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  // (the shared pages' launch runs beside this one, and reads what was written before it: every CTA has waited for that)
+  if (M == kOwn) launch_dependents();
+  Cursor<M> c;
+  const Range r = plan<kThreads, M>(a, S.plan, c);  // (its barriers order the initialisation too)
+  if (M != kOwn && tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);
   if (r.lo >= r.hi) return;
   volatile int* failed = &S.failed;
 
@@ -323,9 +339,10 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       Place p{-1, 0, 0, 0, 0};
       if (looked >= r.hi) return p;
       if (looked++ > r.lo && ++c.ti == c.tiles) c.next_unit(a);
-      const int i = c.ti * kTileTokens + lane * kSubTokens;
+      int i = c.ti * kTileTokens + lane * kSubTokens;
       p.b = c.g.b, p.h = SEL ? c.g.h : c.index / a.n_blocks, p.sees = c.g.sees;
       if (lane >= kTileSubs || i >= c.g.tokens) return p;
+      if (M == kOwn) i += c.g.start;
       p.off = i & ((1 << v.page_log) - 1);
       p.j = SEL ? a.sel[(int64_t)c.gi * a.top + (i >> v.page_log)] : i >> v.page_log;
       return p;
@@ -391,7 +408,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   // ---- the computing warps
   const int g8 = lane >> 2, t4 = lane & 3;
   const uint32_t range = (uint32_t)(r.hi - r.lo);  // tiles of the CTA
-  auto keep = [&](const Cursor<SEL>& x) {
+  auto keep = [&](const Cursor<M>& x) {
     __syncwarp();
     if (lane == 0) {
       volatile int* to = S.cursor[warp];
@@ -402,19 +419,19 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   };
   auto kept = [&]() {
     const volatile int* from = S.cursor[warp];
-    Cursor<SEL> x;
+    Cursor<M> x;
     x.gi = from[0], x.index = from[1], x.ti = from[2], x.tiles = from[3], x.g.b = from[4], x.g.t = from[5], x.g.h = from[6];
     x.g.tokens = from[7], x.g.sees = from[8];
     return x;
   };
-  auto tiles_here = [&](const Cursor<SEL>& x, uint32_t at) { return (int)min((uint32_t)(x.tiles - x.ti), range - at); };
+  auto tiles_here = [&](const Cursor<M>& x, uint32_t at) { return (int)min((uint32_t)(x.tiles - x.ti), range - at); };
   keep(c);
   if (tid == 0) S.range_lo = r.lo, S.range_total = r.total, S.range_shares = r.shares;  // (read by the same thread)
   uint32_t at = 0;  // tiles done
   while (at < range) {
     int row0, n_tiles, sees, all_see;
     {
-    const Cursor<SEL> cu = kept();
+    const Cursor<M> cu = kept();
     const int b = cu.g.b, h = SEL ? cu.g.h : cu.index / a.n_blocks;
     row0 = (SEL ? cu.index : cu.index % a.n_blocks) * kRows;
     const int n_rows = min(kRows, a.rows - row0);
@@ -807,10 +824,16 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         }
     }
     named_sync(kConsumerBar, 32 * kWarps);
-    Cursor<SEL> cu = kept();
+    Cursor<M> cu = kept();
     const int b = cu.g.b, h = SEL ? cu.g.h : cu.index / a.n_blocks, n_rows = min(kRows, a.rows - row0);
     const bool from_start = cu.ti == 0, to_end = cu.ti + n_tiles == cu.tiles, whole = from_start && to_end;
     float* slot = a.slots + (2 * (size_t)blockIdx.x + (from_start ? 1 : 0)) * paged_slot_floats(kRows);
+    int at_last = blockIdx.x;  // the CTA of the unit's last tile: (x + 1) ctas - 1 over the tiles of all
+    if (from_start && !to_end && (M == kOwn || tid == 0)) {
+      const int64_t total = S.range_total, last = S.range_lo + at + cu.tiles - 1;
+      const int64_t ctas = min((int64_t)gridDim.x, total);
+      at_last = S.range_shares ? blockIdx.x + S.range_shares - 1 : (int)(((last + 1) * ctas - 1) / total);
+    }
 #pragma unroll 1
     for (int rr = warp; rr < n_rows; rr += kWarps) {
       float m = kLow, l = 0.f;
@@ -826,6 +849,17 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
         y[1] = fmaf(f, x.y, y[1]);
         y[2] = fmaf(f, x.z, y[2]);
         y[3] = fmaf(f, x.w, y[3]);
+      }
+      if (M == kOwn) {
+        const int t = (row0 + rr) / v.G, g = (row0 + rr) % v.G;
+        const size_t row = ((size_t)b * a.T + t) * (v.H * v.G) + h * v.G + g;
+        if (from_start && lane == 0) a.own.where[row] = PagedWhere{whole ? -1 : (int)blockIdx.x, at_last - (int)blockIdx.x + 1};
+        if (whole) {
+          float* to = a.own.part + row * kPartFloats;
+          *(float4*)(to + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
+          if (lane == 0) to[kD] = m, to[kD + 1] = l;
+          continue;
+        }
       }
       if (!whole) {
         *(float4*)(slot + rr * kD + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
@@ -847,13 +881,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       if (a.lse && lane == 0)
         a.lse[((int64_t)b * a.T + t) * (v.H * v.G) + h * v.G + g] = l == 0.f ? kNegInf : (m + log2f(l)) * 0.693147180559945f;
     }
-    if (from_start && !to_end && tid == 0) {
-      // the CTA of the unit's last tile: (x + 1) ctas - 1 over the tiles of all
-      const int64_t total = S.range_total, last = S.range_lo + at + cu.tiles - 1;
-      const int64_t ctas = min((int64_t)gridDim.x, total);
-      const int at_last = S.range_shares ? blockIdx.x + S.range_shares - 1 : (int)(((last + 1) * ctas - 1) / total);
-      a.desc[blockIdx.x] = make_int4(cu.gi, cu.index, at_last, 1);
-    }
+    if (M != kOwn && from_start && !to_end && tid == 0) a.desc[blockIdx.x] = make_int4(cu.gi, cu.index, at_last, 1);
     at += (uint32_t)n_tiles;
     if (at < range) {
       cu.next_unit(a);
@@ -866,8 +894,9 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
 // take the shares in turn.  Latency alone: 4 to 6 us after the attention's last CTA by itself, about 3 as its dependent.
 // (Joined by the CTA that ends last instead, 8 shares of 8 rows took 11 us a call where this takes 8, 64 shares 27 for 10.)
 constexpr int kJoinWarps = 8;
-template <bool SEL>
+template <Mode M>
 __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_join_kernel(const __grid_constant__ AttnArgs a, int kRows) {
+  constexpr bool SEL = M == kKept;
   launch_dependents();
   wait_for_stream();
   const int4 d = a.desc[blockIdx.x];
@@ -933,7 +962,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_join_kernel(const _
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(y[e] * 0.0625f) ^ sign_flip(v, 4 * lane + e));
   }
-  const Group grp = group_of<SEL>(a, d.x);
+  const Group grp = group_of<M>(a, d.x);
   const int h = SEL ? grp.h : d.y / a.n_blocks, t = SEL ? grp.t : row / v.G, g = SEL ? row : row % v.G;
   uint16_t* o = a.out + grp.b * a.ob + t * a.ot + (int64_t)(h * v.G + g) * a.oh + 4 * lane;
 #pragma unroll
@@ -948,9 +977,9 @@ constexpr size_t kShareDescBytes = (kPagedMaxGrid * sizeof(int4) + 255) & ~(size
 static_assert(sizeof(Smem<1>) <= 115712, "two CTAs of an SM share 228 KiB, 1 KiB each of it taken");
 static_assert(sizeof(Smem<2>) <= 232448, "shared memory of a CTA");
 
-template <int NG, int NT, bool HILO, bool SEL>
+template <int NG, int NT, bool HILO, Mode M>
 int launch(const AttnArgs& a, int dev, int sms, cudaStream_t stream) {
-  auto* kernel = akv_paged_attn_kernel<NG, NT, HILO, SEL>;
+  auto* kernel = akv_paged_attn_kernel<NG, NT, HILO, M>;
   const size_t smem = sizeof(Smem<NT>);
   cudaError_t e;
   static std::atomic<uint64_t> ready{0};  // devices on which the kernel's shared memory has been set
@@ -964,17 +993,18 @@ int launch(const AttnArgs& a, int dev, int sms, cudaStream_t stream) {
   if (grid > kPagedMaxGrid) grid = kPagedMaxGrid;
   const int err = launch_after(kernel, dim3(grid), Smem<NT>::kThreads, smem, stream, a);
   // units of one tile at most are nobody's share (100 tokens: 8.7 us a call with the second launch, 6.6 without)
-  if (err || ((int64_t)(SEL ? a.top : a.v.max_pages) << a.v.page_log) <= kTileTokens) return err;
-  return launch_after(akv_paged_join_kernel<SEL>, dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT), 32 * kJoinWarps, 0, stream, a, 8 * NT);
+  if (err || M == kOwn || ((int64_t)(M == kKept ? a.top : a.v.max_pages) << a.v.page_log) <= kTileTokens) return err;
+  return launch_after(akv_paged_join_kernel<M>, dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT), 32 * kJoinWarps, 0, stream, a, 8 * NT);
 }
 
-template <int NT, bool HILO, bool SEL>
+template <int NT, bool HILO, Mode M>
 int launch_ng(const AttnArgs& a, int dev, int sms, cudaStream_t s) {
-  return a.v.ng == 2 ? launch<2, NT, HILO, SEL>(a, dev, sms, s) : launch<1, NT, HILO, SEL>(a, dev, sms, s);
+  return a.v.ng == 2 ? launch<2, NT, HILO, M>(a, dev, sms, s) : launch<1, NT, HILO, M>(a, dev, sms, s);
 }
-template <bool HILO, bool SEL>
-int launch_nt(const AttnArgs& a, int unit_rows, int dev, int sms, cudaStream_t s) {
-  return unit_rows == 8 ? launch_ng<1, HILO, SEL>(a, dev, sms, s) : launch_ng<2, HILO, SEL>(a, dev, sms, s);
+template <Mode M>
+int launch_mode(const AttnArgs& a, int unit_rows, int dev, int sms, cudaStream_t s) {
+  if (a.v.rotate) return unit_rows == 8 ? launch_ng<1, true, M>(a, dev, sms, s) : launch_ng<2, true, M>(a, dev, sms, s);
+  return unit_rows == 8 ? launch_ng<1, false, M>(a, dev, sms, s) : launch_ng<2, false, M>(a, dev, sms, s);
 }
 
 }  // namespace
@@ -984,8 +1014,9 @@ size_t paged_attn_ws_bytes(const PagedView& v, int32_t T, int32_t top) {
   return kShareDescBytes + kPagedMaxGrid * 2 * paged_slot_floats(rows) * sizeof(float);
 }
 
-int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
-                      const akv_selection* sel, void* ws, void* stream) {
+namespace {
+int attend(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale, const akv_selection* sel,
+           const PagedOwn* own, void* ws, void* stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -1012,11 +1043,24 @@ int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out
     a.groups = v.rows;
     a.per_group = v.H * a.n_blocks;
   }
+  if (own) a.own = *own;
   a.desc = (int4*)ws;
   a.slots = (float*)((uint8_t*)ws + kShareDescBytes);
   cudaStream_t s = (cudaStream_t)stream;
-  if (v.rotate) return sel ? launch_nt<true, true>(a, unit_rows, dev, sms, s) : launch_nt<true, false>(a, unit_rows, dev, sms, s);
-  return sel ? launch_nt<false, true>(a, unit_rows, dev, sms, s) : launch_nt<false, false>(a, unit_rows, dev, sms, s);
+  if (own) return launch_mode<kOwn>(a, unit_rows, dev, sms, s);
+  return sel ? launch_mode<kKept>(a, unit_rows, dev, sms, s) : launch_mode<kAll>(a, unit_rows, dev, sms, s);
 }
+}  // namespace
+
+int launch_paged_attn(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
+                      const akv_selection* sel, void* ws, void* stream) {
+  return attend(v, q, out, lse, T, sm_scale, sel, nullptr, ws, stream);
+}
+
+int launch_paged_own(const PagedView& v, const akv_rows& q, int32_t T, float sm_scale, const PagedOwn& own, void* ws, void* stream) {
+  return attend(v, q, q, nullptr, T, sm_scale, nullptr, &own, ws, stream);
+}
+
+const float* paged_own_slots(const void* ws) { return (const float*)((const uint8_t*)ws + kShareDescBytes); }
 
 }  // namespace akv

@@ -1,0 +1,822 @@
+// Attention over pages that rows share: the shared pages once for all rows of a group, as matrix products on the fifth-generation
+// tensor cores, and a launch that joins them with the rows' own tokens (akv_paged_attn.cu's part, launched before and run beside).
+//
+// A unit is a group's KV head and up to 128 of its query rows (members x query tokens x query heads); units are cut into tiles of
+// 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA, one CTA an SM.  In a CTA
+//   8 warps turn codes into operands, a sub-block of 16 tokens each: keys as c a in two fp16 halves (hi = fp16(c a), lo = the exact rest),
+//     values as fp16(m + c a),
+//   1 thread issues the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry m sum(q), so that a logit comes out
+//     whole, then O += P V with P out of tensor memory,
+//   2 x 4 warps take the tiles in turn, a thread per query row: p = 2^(S scale - reference), its sum, P as fp16 over S's columns.
+// Each of the two has its own O, reference and sum; they are put together at the unit's end.
+//   S is as exact as fp32 sums: products of fp16 numbers are, a query enters as one fp16 number (a power of two times what was given)
+// or, rotated, as a high and a low one.  The scales of tokens could not be applied behind the products instead: a thread that owns a row would
+// read four numbers a token from shared memory, 512 bytes a warp, four times what the tensor cores need for the extra products.
+//   A reference moves when a weight would pass 2^kSlack times it; a weight counts 2^kPlace in P, so that fp16 keeps 2^-11 of those
+// down to 2^-19 of the reference's.  Sub-blocks with a scale above 2048 or a minimum beyond 32768 enter as 2^-5 of themselves (their
+// columns of S count 32, their P is 32 times as large).  Tokens with a NaN enter as values of 0 and a NaN in S: rows that do not see
+// them do not feel them.
+#include <cuda_runtime.h>
+
+#include <atomic>
+
+#include "akv_device.cuh"
+#include "akv_paged.cuh"
+
+namespace akv {
+namespace {
+
+constexpr int kRows = 128, kTile = 128;
+constexpr int kSoftWarps = 8, kUnpackWarps = 8, kMmaWarp = kSoftWarps + kUnpackWarps;
+constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr uint32_t kPanel = 128 * 128;    // bytes of 64 of an operand's K for 128 of its rows
+constexpr uint32_t kExtra = 128 * 32;     // 16 of K
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLow = -3.402823466e38f;  // reference of a row that saw no token: below all others
+constexpr float kSlack = 5.f, kPlace = 5.f;
+constexpr int kMaxCtas = 256;
+constexpr uint32_t kCols = 512;           // tensor memory: S of both, O of both
+
+struct SharedArgs {
+  PagedView v;
+  const uint16_t* q;
+  int64_t qb, qt, qh;
+  akv_share share;
+  float* part;         // [rows][T][n_q_heads] parts, and where they are
+  PagedWhere* where;
+  float* slots;        // [ctas][2][kRows] parts of units that several CTAs worked on
+  float scale;         // sm_scale log2(e)
+  int T;
+};
+
+struct Smem {
+  uint8_t q[4 * kPanel];      // high, then low halves
+  uint8_t k[4 * kPanel];
+  uint8_t v[2][2 * kPanel];   // values: [dimension][token]
+  uint8_t qx[kExtra], kx[kExtra];
+  float row_scale[kRows], ref[2][kRows], sum[2][kRows];
+  int lim[kRows];             // tokens of the unit that a row sees
+  int64_t row_at[kRows];      // its number among all query rows; -1: none
+  uint8_t big[4][8];          // sub-blocks that enter as 2^-5 of themselves, by tile modulo 4
+  uint64_t k_full, k_free, v_full[2], v_free[2], s_full[2], p_full[2], q_full, o_full, drained;
+  int64_t part[kMmaWarp + 1];
+  int place[8];
+  uint32_t tmem;
+  int failed;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // -126 .. 127
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
+__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+__device__ __forceinline__ bool finite_word(uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; }
+__device__ __forceinline__ void sts128(uint32_t a, uint4 x) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 32 columns of the thread's lane of tensor memory
+__device__ __forceinline__ void tm_ld32(uint32_t at, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      " tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tm_st32(uint32_t at, const float (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t at, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// D[tmem] (+)= A[tmem] B[smem]^T
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+      ::"r"(d), "r"(a), "l"(b_desc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// Operand of 16 K without swizzle: [2][16][8 rows][16 bytes], 2048 bytes from one half of K to the other, 128 between groups of rows.
+__device__ __forceinline__ uint64_t plain_desc(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(2048u >> 4) << 16) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1u << 46);
+}
+__device__ __forceinline__ uint32_t extra_at(int row) { return (uint32_t)((row >> 3) * 128 + (row & 7) * 16); }
+
+// A unit's share of a CTA: tiles t0 .. t0 + n - 1.
+struct Segment {
+  int k0, size, lead, tokens;  // the group: its first place in the order, rows, leader, shared tokens
+  int h, block, tiles, t0, n;
+};
+
+struct Walk {
+  int64_t lo, hi, total;
+  int ctas;
+};
+__device__ __forceinline__ int row_in_order(const SharedArgs& a, int k) {
+  const int b = a.share.order[k];
+  return (uint32_t)b < (uint32_t)a.v.rows ? b : -1;
+}
+// The group that begins at place k of the order, and how many tiles its units have; 0: none begins here, or it shares nothing.
+__device__ __forceinline__ int group_at(const SharedArgs& a, int k, Segment& s) {
+  const PagedView& v = a.v;
+  const int b = row_in_order(a, k);
+  if (b < 0 || a.share.leader[b] != b) return 0;
+  s.k0 = k;
+  s.lead = b;
+  s.size = min(max(a.share.size[b], 1), v.rows - k);
+  s.tokens = min(max(a.share.pages[b], 0), v.max_pages) << v.page_log;
+  s.tiles = (s.tokens + kTile - 1) / kTile;
+  return s.tiles;
+}
+__device__ __forceinline__ int blocks_of(const SharedArgs& a, const Segment& s) {
+  return (int)(((int64_t)s.size * a.T * a.v.G + kRows - 1) / kRows);
+}
+
+// Every thread: the CTA's range of tiles, and its first segment.
+__device__ __forceinline__ Walk plan(const SharedArgs& a, Smem& S, Segment& seg) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rows = a.v.rows;
+  const int strip = (rows + kThreads - 1) / kThreads, k0 = min(rows, tid * strip), k1 = min(rows, k0 + strip);
+  int64_t mine = 0;
+  Segment s;
+  for (int k = k0; k < k1; ++k)
+    if (group_at(a, k, s)) mine += (int64_t)s.tiles * blocks_of(a, s) * a.v.H;
+  int64_t inc = mine;
+#pragma unroll
+  for (int i = 1; i < 32; i *= 2) {
+    const int64_t o = __shfl_up_sync(0xffffffffu, inc, i);
+    if (lane >= i) inc += o;
+  }
+  if (lane == 31) S.part[warp] = inc;
+  __syncthreads();
+  int64_t before = inc - mine;
+  Walk w;
+  w.total = 0;
+  for (int i = 0; i <= kMmaWarp; ++i) {
+    if (i < warp) before += S.part[i];
+    w.total += S.part[i];
+  }
+  w.ctas = (int)min((int64_t)gridDim.x, w.total);
+  w.lo = w.hi = 0;
+  if ((int)blockIdx.x >= w.ctas) return w;
+  w.lo = blockIdx.x * w.total / w.ctas;
+  w.hi = (blockIdx.x + 1) * w.total / w.ctas;
+  if (w.lo >= before && w.lo < before + mine) {
+    int64_t rest = w.lo - before;
+    for (int k = k0; k < k1; ++k) {
+      if (!group_at(a, k, s)) continue;
+      const int64_t here = (int64_t)s.tiles * blocks_of(a, s) * a.v.H;
+      if (rest < here) break;
+      rest -= here;
+    }
+    const int unit = (int)(rest / s.tiles), blocks = blocks_of(a, s);
+    S.place[0] = s.k0, S.place[1] = unit / blocks, S.place[2] = unit % blocks, S.place[3] = (int)(rest % s.tiles);
+  }
+  __syncthreads();
+  group_at(a, S.place[0], seg);
+  seg.h = S.place[1], seg.block = S.place[2], seg.t0 = S.place[3];
+  seg.n = (int)min((int64_t)(seg.tiles - seg.t0), w.hi - w.lo);
+  return w;
+}
+// The segment after s, `left` tiles of the CTA's range still to go (> 0).
+__device__ __forceinline__ void next_segment(const SharedArgs& a, Segment& s, int64_t left) {
+  s.t0 = 0;
+  if (++s.block == blocks_of(a, s)) {
+    s.block = 0;
+    if (++s.h == a.v.H) {
+      s.h = 0;
+      for (int k = s.k0 + 1; k < a.v.rows; ++k)
+        if (group_at(a, k, s)) break;
+    }
+  }
+  s.n = (int)min((int64_t)s.tiles, left);
+}
+
+template <int NG, bool HILO>
+__global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __grid_constant__ SharedArgs a) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  Smem& S = *reinterpret_cast<Smem*>(smem_raw + (1024u - (smem_u32(smem_raw) & 1023u)) % 1024u);
+  constexpr uint32_t kSub = 2048 + 128 * NG;
+  const PagedView& v = a.v;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  volatile int* failed = &S.failed;
+  // What this launch reads was written before the launch that it runs beside, whose CTAs have all waited for it.
+  launch_dependents();
+  if (tid == 0) {
+    mbar_init(smem_u32(&S.k_full), kUnpackWarps);
+    mbar_init(smem_u32(&S.k_free), 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&S.v_full[s]), kUnpackWarps);
+      mbar_init(smem_u32(&S.v_free[s]), 1);
+      mbar_init(smem_u32(&S.s_full[s]), 1);
+      mbar_init(smem_u32(&S.p_full[s]), 4);
+    }
+    mbar_init(smem_u32(&S.q_full), kSoftWarps);
+    mbar_init(smem_u32(&S.o_full), 1);
+    mbar_init(smem_u32(&S.drained), 1);
+    S.failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // the second eight of the sixteen extra dimensions are zeros
+  if (tid < 128) {
+    sts128(smem_u32(S.qx) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
+    sts128(smem_u32(S.kx) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
+    proxy_fence();
+  }
+  Segment seg;
+  const Walk w = plan(a, S, seg);
+  if (w.lo >= w.hi) {
+    wait_for_stream();
+    return;
+  }
+  if (warp == kMmaWarp) tc_alloc(smem_u32(&S.tmem), kCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = S.tmem;
+
+  if (warp == kMmaWarp) {
+    if (lane == 0) {
+      // ---- the products
+      constexpr uint32_t idesc = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);  // fp16 x fp16 -> fp32, 128 x 128
+      const uint64_t dq = sw128_desc(smem_u32(S.q)), dk = sw128_desc(smem_u32(S.k));
+      const uint64_t dqx = plain_desc(smem_u32(S.qx)), dkx = plain_desc(smem_u32(S.kx));
+      auto step = [](int kk) { return (uint64_t)(((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4); };
+      uint32_t nk = 0, np[2] = {0, 0}, nv[2] = {0, 0}, nseg = 0;
+      bool ok = true;
+      for (int64_t at = w.lo; ok && at < w.hi; ++nseg) {
+        ok = mbar_wait(smem_u32(&S.q_full), nseg & 1);
+        auto values = [&](int i) {  // O += P V of tile i
+          const int s = i & 1;
+          ok = ok && mbar_wait(smem_u32(&S.p_full[s]), np[s]++ & 1) && mbar_wait(smem_u32(&S.v_full[s]), nv[s]++ & 1);
+          if (!ok) return;
+          tc_fence_after();
+          const uint64_t dv = sw128_desc(smem_u32(S.v[s]));
+          for (int kk = 0; kk < 8; ++kk)
+            tc_mma_ts(tmem + 256 + 128 * s, tmem + 128 * s + 8 * kk, dv + step(kk), idesc, i >= 2 || kk > 0);
+          tc_commit(smem_u32(&S.v_free[s]));
+        };
+        for (int i = 0; ok && i < seg.n; ++i) {
+          const int s = i & 1;
+          ok = mbar_wait(smem_u32(&S.k_full), nk++ & 1) && !*failed;
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t d = tmem + 128 * s;
+          constexpr uint64_t low = 2 * kPanel >> 4;
+          if (HILO)
+            for (int kk = 0; kk < 8; ++kk) tc_mma(d, dq + low + step(kk), dk + step(kk), idesc, kk > 0);
+          for (int kk = 0; kk < 8; ++kk) tc_mma(d, dq + step(kk), dk + low + step(kk), idesc, HILO || kk > 0);
+          for (int kk = 0; kk < 8; ++kk) tc_mma(d, dq + step(kk), dk + step(kk), idesc, 1);
+          tc_mma(d, dqx, dkx, idesc, 1);
+          tc_commit(smem_u32(&S.k_free));
+          tc_commit(smem_u32(&S.s_full[s]));
+          if (i) values(i - 1);
+        }
+        if (ok) values(seg.n - 1);
+        if (ok) tc_commit(smem_u32(&S.o_full));
+        at += seg.n;
+        if (at < w.hi) next_segment(a, seg, w.hi - at);
+      }
+      if (!ok) *failed = 1;
+      tc_commit(smem_u32(&S.drained));
+      mbar_wait(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
+    }
+    __syncwarp();
+  } else if (warp >= kSoftWarps) {
+    // ---- operands of keys and values: a sub-block a warp
+    const int u = warp - kSoftWarps;
+    const int token = lane & 15, half = lane >> 4;                       // keys: a token's dimensions 32 j + 8 t + i, t = 2 half ..
+    const int g = lane & 7, p = lane >> 3 & 1, sd = lane >> 4;           // values: tokens 8 p .. + 7, dimensions 64 sd + 8 g ..
+    const uint32_t kx_at = smem_u32(S.kx) + extra_at(16 * u + token);
+    const uint32_t k_row = smem_u32(S.k) + (uint32_t)(16 * u + token) * 128;
+    const int v_chunk = 2 * (u & 3) + p;
+    struct Raw {
+      uint4 k[2];
+      uint2 kv[4];       // value words of tokens 2 t, 2 t + 1
+      uint32_t kw[2 * NG], vw[8];
+      bool there;        // false: behind the shared tokens; pages outside the pool have NaN parameters
+    };
+    auto page_at = [&](const Segment& s, int i) {  // page of the warp's sub-block of tile i: -1 outside the pool, -2 behind the end
+      const int tok = (s.t0 + i) * kTile + 16 * u;
+      return tok < s.tokens ? page_of(v, s.lead, tok >> v.page_log) : -2;
+    };
+    auto load = [&](const Segment& s, int i, int page) {
+      Raw r;
+      r.there = page != -2;
+      const uint32_t none = r.there ? 0x7e007e00u : 0u;
+      if (page >= 0) {
+        const int tok = (s.t0 + i) * kTile + 16 * u;
+        const uint8_t* b = block_of(v, page, s.h) + (uint64_t)((tok & ((1 << v.page_log) - 1)) >> 4) * kSub;
+        const uint4* k = (const uint4*)(b + 64 * token + 32 * half);
+        r.k[0] = k[0], r.k[1] = k[1];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) r.kv[t] = *(const uint2*)(b + 1024 + 512 * p + 16 * (4 * g + t) + 8 * sd);
+        if (NG == 2) {
+          const uint4 x = *(const uint4*)(b + 2048 + 16 * token);
+          r.kw[0] = x.x, r.kw[1] = x.y, r.kw[2 * NG - 2] = x.z, r.kw[2 * NG - 1] = x.w;
+        } else {
+          const uint2 x = *(const uint2*)(b + 2048 + 8 * token);
+          r.kw[0] = x.x, r.kw[1] = x.y;
+        }
+#pragma unroll
+        for (int k8 = 0; k8 < 8; ++k8) r.vw[k8] = *(const uint32_t*)(b + 2048 + 8 * NG * (8 * p + k8) + 4 * NG + (NG == 2 ? 4 * sd : 0));
+      } else {
+        r.k[0] = r.k[1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) r.kv[t] = make_uint2(0, 0);
+#pragma unroll
+        for (int x = 0; x < 2 * NG; ++x) r.kw[x] = none;
+#pragma unroll
+        for (int k8 = 0; k8 < 8; ++k8) r.vw[k8] = none;
+      }
+      return r;
+    };
+    const __half2 k1024 = __float2half2_rn(1024.f);
+    auto codes = [&](uint32_t x) { return __hsub2(as_half2((x & 0x000f000fu) | 0x64006400u), k1024); };
+    uint32_t nk = 0, nv[2] = {0, 0}, n_tile = 0;
+    bool ok = true;
+    Raw next = load(seg, 0, page_at(seg, 0));
+    for (int64_t at = w.lo; ok && at < w.hi;) {
+      Segment after = seg;
+      if (at + seg.n < w.hi) next_segment(a, after, w.hi - at - seg.n);
+      int page = seg.n > 1 ? page_at(seg, 1) : page_at(after, 0);
+      for (int i = 0; i < seg.n; ++i, ++n_tile) {
+        const Raw r = next;
+        const int s = i & 1;
+        // what the next tile needs is under way while this one waits for its place
+        if (i + 1 < seg.n) {
+          next = load(seg, i + 1, page);
+          page = i + 2 < seg.n ? page_at(seg, i + 2) : page_at(after, 0);
+        } else if (at + seg.n < w.hi) {
+          next = load(after, 0, page);
+        }
+        // the sub-block's size, and tokens with a NaN
+        auto large = [](uint32_t x) { return (x & 0x7fffu) > 0x6800u || (x >> 16 & 0x7fffu) > 0x7800u; };  // 2048, 32768
+        bool fine = true, is_large = false;
+#pragma unroll
+        for (int x = 0; x < 2 * NG; ++x) {
+          fine = fine && finite_word(r.kw[x]);
+          is_large = is_large || (finite_word(r.kw[x]) && large(r.kw[x]));
+        }
+        const bool big = __any_sync(0xffffffffu, is_large);
+        const __half2 down = __float2half2_rn(big ? 0.03125f : 1.f);
+        // keys
+        if (!mbar_wait_w(smem_u32(&S.k_free), (nk++ & 1) ^ 1) || warp_failed(failed)) {
+          ok = false;
+          break;
+        }
+        if (lane == 0) S.big[n_tile & 3][u] = big;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t word = fine ? r.kw[NG == 2 ? j >> 1 : 0] : 0u;
+          const __half2 sc = __hmul2(__half2half2(__ushort_as_half((unsigned short)word)), down);
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt) {
+            const uint4& q4 = r.k[tt];
+            const uint32_t x = j == 0 ? q4.x : j == 1 ? q4.y : j == 2 ? q4.z : q4.w;
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const __half2 c = codes(x >> (4 * e));
+              const __half2 y = __hmul2(c, sc);
+              hi[e] = bits(y);
+              lo[e] = bits(__hfma2(c, sc, __hneg2(y)));
+            }
+            const int t = 2 * half + tt, chunk = ((j & 1) * 4 + t) ^ (token & 7);
+            const uint32_t to = k_row + (uint32_t)(j >> 1) * kPanel + 16 * chunk;
+            sts128(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+            sts128(to + 2 * kPanel, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+          }
+        }
+        if (half == 0) {
+          const __half2 m0 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(fine ? r.kw[0] >> 16 : 0x7e00u))), down);
+          const __half2 m1 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(NG == 2 && fine ? r.kw[1] >> 16 : 0u))), down);
+          const uint32_t b0 = bits(m0), b1 = bits(m1);
+          sts128(kx_at, make_uint4(b0, (b0 & 0xffffu) | (b1 & 0xffff0000u), b1, 0));
+        }
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.k_full));
+        // values
+        if (!mbar_wait_w(smem_u32(&S.v_free[s]), (nv[s]++ & 1) ^ 1)) {
+          ok = false;
+          break;
+        }
+        // a token with a NaN anywhere is a zero
+        const uint32_t all_fine = __ballot_sync(0xffffffffu, fine);
+        __half2 sc[4], mn[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t w0 = all_fine >> (8 * p + 2 * t) & 1 ? r.vw[2 * t] : 0u, w1 = all_fine >> (8 * p + 2 * t + 1) & 1 ? r.vw[2 * t + 1] : 0u;
+          sc[t] = __hmul2(as_half2(__byte_perm(w0, w1, 0x5410)), down);
+          mn[t] = __hmul2(as_half2(__byte_perm(w0, w1, 0x7632)), down);
+        }
+#pragma unroll
+        for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            uint32_t y[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) y[t] = bits(__hfma2(codes((uu ? r.kv[t].y : r.kv[t].x) >> (4 * n)), sc[t], mn[t]));
+            // dimension 64 sd + 8 g + 4 uu + n is operand row 64 sd + 8 (4 uu + n) + g: eight lanes write eight places
+            const int row = 64 * sd + 8 * (4 * uu + n) + g;
+            sts128(smem_u32(S.v[s]) + (uint32_t)(u >> 2) * kPanel + 128 * row + 16 * (v_chunk ^ g), make_uint4(y[0], y[1], y[2], y[3]));
+          }
+        proxy_fence();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.v_full[s]));
+      }
+      at += seg.n;
+      seg = after;
+    }
+    if (!ok) *failed = 1;
+  } else {
+    // ---- softmax: a thread a query row, the tiles of parity s
+    const int s = warp >> 2, row = tid & 127;
+    const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16, tS = tmem + lane_at + 128 * s, tO = tmem + lane_at + 256;
+    const float sign = a.scale < 0.f ? -1.f : 1.f;
+    const int tg = a.T * v.G;
+    uint32_t ns = 0, nseg = 0, n_tile = 0;
+    for (int64_t at = w.lo; at < w.hi; ++nseg) {
+      // the unit's queries as operands: a warp a row
+      for (int rr = warp; rr < kRows; rr += kSoftWarps) {
+        const int64_t qi = (int64_t)seg.block * kRows + rr;
+        const int k = seg.k0 + (int)(qi / tg), t = (int)(qi % tg) / v.G, gq = (int)(qi % tg) % v.G;
+        const int b = k < seg.k0 + seg.size ? row_in_order(a, k) : -1;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        if (b >= 0) {
+          const uint16_t* from = a.q + b * a.qb + t * a.qt + (int64_t)(seg.h * v.G + gq) * a.qh + 4 * lane;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = sign * row_to_float(from[e], v.half);
+        }
+        if (HILO) {  // q' = H (s o q) / 16
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign_flip(v, 4 * lane + e));
+          wht_32x4(x, lane);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
+        }
+        float big = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = fabsf(x[e]);
+          if (y <= 3.402823466e38f) big = fmaxf(big, y);  // an infinite or NaN row spoils itself alone
+        }
+        big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
+        // a row times 2^(7 - e): below 2^7 (its sums below 2^14), exact in fp16 down to 2^-23 of that
+        const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
+        const float up = pow2(7 - e2);
+        float sum = (x[0] + x[1]) + (x[2] + x[3]);
+#pragma unroll
+        for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+        const float s0 = __shfl_sync(0xffffffffu, sum, 0) * up, s1 = __shfl_sync(0xffffffffu, sum, 16) * up;
+        uint4 f[2];
+#pragma unroll
+        for (int lo = 0; lo < 2; ++lo) {
+          uint32_t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float z = x[e] * up, hi = __half2float(__float2half_rn(z)), mine = lo ? z - hi : z;
+            const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
+            y[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
+          }
+          f[lo] = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        // lanes 2 x, 2 x + 1 hold dimensions 8 x .. of word j = x / 4, t = x % 4
+        const int j = lane >> 3, chunk = ((j & 1) * 4 + (lane >> 1 & 3)) ^ (rr & 7);
+        const uint32_t to = smem_u32(S.q) + (uint32_t)(j >> 1) * kPanel + 128 * rr + 16 * chunk;
+        if (!(lane & 1)) sts128(to, f[0]);
+        if (HILO && (lane & 1)) sts128(to + 2 * kPanel, f[1]);
+        if (lane == 0) {
+          auto parts = [](float z, float (&y)[3]) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+              y[i] = __half2float(__float2half_rn(z));
+              z -= y[i];
+            }
+          };
+          float y0[3], y1[3] = {0.f, 0.f, 0.f};
+          parts(s0, y0);
+          if (NG == 2) parts(s1, y1);
+          sts128(smem_u32(S.qx) + extra_at(rr), make_uint4(half2_bits(y0[0], y0[1]), half2_bits(y0[2], y1[0]), half2_bits(y1[1], y1[2]), 0));
+          S.row_scale[rr] = fabsf(a.scale) * pow2(e2 - 7);
+          S.lim[rr] = b >= 0 ? min(seg.tokens, held_tokens(v, b) - a.T + 1 + t) : 0;
+          S.row_at[rr] = b >= 0 ? ((int64_t)b * a.T + t) * (v.H * v.G) + seg.h * v.G + gq : -1;
+        }
+      }
+      proxy_fence();
+      __syncwarp();
+      named_sync(1, 32 * kSoftWarps);
+      if (lane == 0) mbar_arrive(smem_u32(&S.q_full));
+
+      const float row_scale = S.row_scale[row];
+      const int lim = S.lim[row] - seg.t0 * kTile;  // from the segment's first token
+      float ref = kLow, sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int i = s; i < seg.n; i += 2) {
+        if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[s]), ns++ & 1)) {
+          *failed = 1;
+          break;
+        }
+        tc_fence_after();
+        const int sees = lim - i * kTile;
+        const uint64_t big = *(const volatile uint64_t*)&S.big[(n_tile + i) & 3][0];
+        const bool whole = __all_sync(0xffffffffu, sees >= kTile);
+        // the largest logit
+        float most = kNegInf;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float x[32];
+          tm_ld32(tS + 32 * c, x);
+          float m2[2] = {kNegInf, kNegInf};
+          if (whole) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) m2[e >> 4] = max3(m2[e >> 4], x[e], x[e + 1]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) m2[e >> 4] = fmaxf(m2[e >> 4], 32 * c + e < sees ? x[e] : kNegInf);
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y) most = fmaxf(most, big >> (8 * (2 * c + y)) & 1 ? 32.f * m2[y] : m2[y]);
+        }
+        most *= row_scale;
+        const bool up = most - ref > kSlack;  // (a row that sees nothing here sees nothing later)
+        if (__any_sync(0xffffffffu, up)) {
+          const float to = up ? most : ref, f = up ? exp2_fast(ref - to) : 1.f;
+          ref = to;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] *= f;
+          if (i >= 2) {  // (S of this tile is behind O of the one before in the order of the products)
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              float x[32];
+              tm_ld32(tO + 128 * s + 32 * c, x);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[e] *= f;
+              tm_st32(tO + 128 * s + 32 * c, x);
+            }
+            tm_wait_st();
+          }
+        }
+        const float shift = kPlace - ref;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float x[32];
+          tm_ld32(tS + 32 * c, x);
+          uint32_t pk[16];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const bool b = big >> (8 * (2 * c + y)) & 1;
+            const float sc = b ? 32.f * row_scale : row_scale;
+#pragma unroll
+            for (int e = 16 * y; e < 16 * y + 16; ++e) {
+              x[e] = exp2_fast(fmaf(x[e], sc, shift));
+              if (!whole && 32 * c + e >= sees) x[e] = 0.f;
+              sum[e & 3] += x[e];
+              if (b) x[e] *= 32.f;
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) pk[e] = half2_bits(x[2 * e], x[2 * e + 1]);
+          tm_st16(tS + 16 * c, pk);
+        }
+        tm_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.p_full[s]));
+      }
+      n_tile += seg.n;
+      // ---- the segment's end: both sums together, each half of the threads takes half of the columns
+      S.ref[s][row] = ref;
+      S.sum[s][row] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      const bool done = !warp_failed(failed) && mbar_wait_w(smem_u32(&S.o_full), nseg & 1);
+      if (!done) *failed = 1;
+      named_sync(1, 32 * kSoftWarps);
+      tc_fence_after();
+      const float r0 = S.ref[0][row], r1 = S.ref[1][row], m = fmaxf(r0, r1);
+      const float f0 = exp2_fast(r0 - m), f1 = exp2_fast(r1 - m);
+      const bool whole = seg.t0 == 0 && seg.n == seg.tiles;
+      const int64_t out_row = S.row_at[row];
+      float* to = whole ? a.part + (out_row < 0 ? 0 : out_row) * kPartFloats
+                        : a.slots + ((size_t)(2 * blockIdx.x + (seg.t0 == 0)) * kRows + row) * kPartFloats;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x[32], y[32];
+        tm_ld32(tO + 64 * s + 32 * c, x);
+        if (seg.n > 1) tm_ld32(tO + 128 + 64 * s + 32 * c, y);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = seg.n > 1 ? f0 * x[e] + f1 * y[e] : x[e];
+        if (out_row >= 0) {
+          // operand column 32 (2 s + c) + 8 n + g is dimension 64 s + 8 g + 4 c + n
+#pragma unroll
+          for (int gg = 0; gg < 8; ++gg) *(float4*)(to + 64 * s + 8 * gg + 4 * c) = make_float4(x[gg], x[8 + gg], x[16 + gg], x[24 + gg]);
+        }
+      }
+      if (s == 0 && out_row >= 0) {
+        const float l = f0 * S.sum[0][row] + f1 * S.sum[1][row];
+        to[kD] = l == 0.f ? kLow : m - kPlace;
+        to[kD + 1] = done ? l : __int_as_float(0x7fffffff);
+        if (seg.t0 == 0) {
+          const int64_t last = at + seg.tiles - 1;
+          const int at_last = (int)(((last + 1) * w.ctas - 1) / w.total);
+          a.where[out_row] = PagedWhere{whole ? -1 : (int)blockIdx.x, at_last - (int)blockIdx.x + 1};
+        }
+      }
+      tc_fence_before();
+      named_sync(1, 32 * kSoftWarps);  // (what was read is the next segment's)
+      at += seg.n;
+      if (at < w.hi) next_segment(a, seg, w.hi - at);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) tc_dealloc(tmem, kCols);
+  wait_for_stream();  // (so that whoever depends on this launch has waited for the one beside it as well)
+}
+
+// The parts of every query row together: its own tokens' and the shared ones', each whole or in the slots of several CTAs.  A warp a row.
+struct JoinArgs {
+  PagedView v;
+  akv_share share;
+  const float *own_part, *own_slots, *pre_part, *pre_slots;
+  const PagedWhere *own_where, *pre_where;
+  uint16_t* out;
+  float* lse;
+  int64_t ob, ot, oh, total;  // total: query rows
+  int T, own_rows;            // own_rows: rows of an own slot
+};
+constexpr int kJoinWarps = 8;
+__global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_shared_join_kernel(const __grid_constant__ JoinArgs a) {
+  launch_dependents();
+  wait_for_stream();
+  const PagedView& v = a.v;
+  const int lane = threadIdx.x & 31, hq = v.H * v.G;
+  const int64_t row = (int64_t)blockIdx.x * kJoinWarps + (threadIdx.x >> 5);
+  if (row >= a.total) return;
+  const int64_t bt = row / hq;
+  const int head = (int)(row % hq), b = (int)(bt / a.T), t = (int)(bt % a.T), g = head % v.G;
+  float m = kLow, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](int n, auto at, auto ml) {  // n parts, four under way at a time
+    for (int i0 = 0; i0 < n; i0 += 4) {
+      float4 x[4];
+      float2 s[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        x[u] = make_float4(0.f, 0.f, 0.f, 0.f), s[u] = make_float2(kLow, 0.f);
+        if (i0 + u < n) x[u] = *(const float4*)(at(i0 + u) + 4 * lane), s[u] = *(const float2*)ml(i0 + u);
+      }
+      const float mn = fmaxf(m, fmaxf(fmaxf(s[0].x, s[1].x), fmaxf(s[2].x, s[3].x))), f = exp2_fast(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + u >= n) break;
+        const float w = exp2_fast(s[u].x - m);
+        l = fmaf(w, s[u].y, l);
+        y[0] = fmaf(w, x[u].x, y[0]);
+        y[1] = fmaf(w, x[u].y, y[1]);
+        y[2] = fmaf(w, x[u].z, y[2]);
+        y[3] = fmaf(w, x[u].w, y[3]);
+      }
+    }
+  };
+  // shared pages; the block of 128 that the row is in counts from its group's first row
+  const int lead = a.share.leader[b];
+  if ((uint32_t)lead < (uint32_t)v.rows && min(a.share.pages[lead], v.max_pages) > 0) {
+    const PagedWhere w = a.pre_where[row];
+    if (w.first < 0) {
+      const float* p = a.pre_part + row * kPartFloats;
+      add(1, [&](int) { return p; }, [&](int) { return p + kD; });
+    } else {
+      int before = 0;  // members of the group before the row: rows with its leader and a lower number
+      for (int j0 = 0; j0 < b; j0 += 32) before += __popc(__ballot_sync(0xffffffffu, j0 + lane < b && a.share.leader[j0 + lane] == lead));
+      const int rr = (int)((((int64_t)before * a.T + t) * v.G + g) % kRows), first = min(w.first, kMaxCtas - 1), n = min(w.n, kMaxCtas - first);
+      auto at = [&](int i) { return a.pre_slots + ((size_t)(2 * (first + i) + (i == 0)) * kRows + rr) * kPartFloats; };
+      add(n, at, [&](int i) { return at(i) + kD; });
+    }
+  }
+  {
+    const PagedWhere w = a.own_where[row];
+    if (w.first < 0) {
+      const float* p = a.own_part + row * kPartFloats;
+      add(1, [&](int) { return p; }, [&](int) { return p + kD; });
+    } else {
+      const int rr = (t * v.G + g) % a.own_rows, first = min(w.first, kPagedMaxGrid - 1), n = min(w.n, kPagedMaxGrid - first);
+      auto slot = [&](int i) { return a.own_slots + (2 * (size_t)(first + i) + (i == 0)) * paged_slot_floats(a.own_rows); };
+      add(n, [&](int i) { return slot(i) + rr * kD; }, [&](int i) { return slot(i) + a.own_rows * kD + 2 * rr; });
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] *= inv;
+  if (v.rotate) {
+    wht_32x4(y, lane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __uint_as_float(__float_as_uint(y[e] * 0.0625f) ^ sign_flip(v, 4 * lane + e));
+  }
+  uint16_t* o = a.out + b * a.ob + t * a.ot + (int64_t)head * a.oh + 4 * lane;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = float_to_row(y[e], v.half);
+  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? kNegInf : (m + log2f(l)) * 0.693147180559945f;
+}
+
+template <int NG, bool HILO>
+int launch(const SharedArgs& a, int dev, int sms, void* stream) {
+  auto* kernel = akv_paged_shared_kernel<NG, HILO>;
+  constexpr size_t smem = sizeof(Smem) + 1024;
+  static_assert(smem <= 232448, "shared memory of a CTA");
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel's shared memory has been set
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return (int)e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_after(kernel, dim3(sms < kMaxCtas ? sms : kMaxCtas), kThreads, smem, stream, a);
+}
+
+// Workspace: the own part's (its slots), then parts and places of both sides, then the shared part's slots.
+struct SharedWs {
+  size_t own_part, own_where, pre_part, pre_where, slots, total;
+};
+SharedWs shared_ws(const PagedView& v, int32_t T) {
+  const size_t rows = (size_t)v.rows * T * v.H * v.G;
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  SharedWs w;
+  w.own_part = up(paged_attn_ws_bytes(v, T, 0));
+  w.own_where = w.own_part + up(rows * kPartFloats * sizeof(float));
+  w.pre_part = w.own_where + up(rows * sizeof(PagedWhere));
+  w.pre_where = w.pre_part + up(rows * kPartFloats * sizeof(float));
+  w.slots = w.pre_where + up(rows * sizeof(PagedWhere));
+  w.total = w.slots + (size_t)kMaxCtas * 2 * kRows * kPartFloats * sizeof(float);
+  return w;
+}
+
+}  // namespace
+
+size_t paged_shared_ws_bytes(const PagedView& v, int32_t T) { return shared_ws(v, T).total; }
+
+int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
+                        const akv_share& share, void* ws, void* stream) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return (int)e;
+  const SharedWs w = shared_ws(v, T);
+  uint8_t* base = (uint8_t*)ws;
+  PagedOwn own;
+  own.pages = share.pages;
+  own.part = (float*)(base + w.own_part);
+  own.where = (PagedWhere*)(base + w.own_where);
+  int err = launch_paged_own(v, q, T, sm_scale, own, ws, stream);
+  if (err) return err;
+  SharedArgs a{};
+  a.v = v;
+  a.q = (const uint16_t*)q.ptr;
+  a.qb = q.stride_b, a.qt = q.stride_t, a.qh = q.stride_h;
+  a.share = share;
+  a.part = (float*)(base + w.pre_part);
+  a.where = (PagedWhere*)(base + w.pre_where);
+  a.slots = (float*)(base + w.slots);
+  a.scale = (float)((double)sm_scale * 1.4426950408889634);
+  a.T = T;
+  if (v.rotate) err = v.ng == 2 ? launch<2, true>(a, dev, sms, stream) : launch<1, true>(a, dev, sms, stream);
+  else err = v.ng == 2 ? launch<2, false>(a, dev, sms, stream) : launch<1, false>(a, dev, sms, stream);
+  if (err) return err;
+  JoinArgs j{};
+  j.v = v;
+  j.share = share;
+  j.own_part = own.part, j.own_where = own.where, j.own_slots = paged_own_slots(ws);
+  j.pre_part = a.part, j.pre_where = a.where, j.pre_slots = a.slots;
+  j.out = (uint16_t*)out.ptr;
+  j.ob = out.stride_b, j.ot = out.stride_t, j.oh = out.stride_h;
+  j.lse = lse;
+  j.total = (int64_t)v.rows * T * v.H * v.G;
+  j.T = T;
+  j.own_rows = paged_unit_rows(T * v.G);
+  return launch_after(akv_paged_shared_join_kernel, dim3((unsigned)((j.total + kJoinWarps - 1) / kJoinWarps)), 32 * kJoinWarps, 0, stream, j);
+}
+
+}  // namespace akv

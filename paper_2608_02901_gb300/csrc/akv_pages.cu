@@ -1,9 +1,13 @@
-// Page operations of the paged cache: copy, fork, reserve (with copy on write), free, compact.
+// Page operations of the paged cache: copy, fork, reserve (with copy on write), free, compact, trim, and which rows share pages.
 //
 // Their integer work is small (a table, a count per page); what costs is the pages' bytes, 2 x page bytes x layers for
 // each copied page.  The state is on the device, so a plan kernel of one CTA decides (its order is the documented
 // one: rows ascending, lowest free page first) and a copy kernel over all SMs moves what the plan lists.
+#include <cooperative_groups.h>
+
 #include "akv_paged.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace akv {
 namespace {
@@ -171,6 +175,98 @@ __global__ void __launch_bounds__(256) akv_pages_free_kernel(PagesState s, const
   if (threadIdx.x == 0) s.lens[r] = 0;
 }
 
+// The same for the pages behind a row's length.
+__global__ void __launch_bounds__(256) akv_pages_trim_kernel(PagesState s, const int32_t* rows) {
+  launch_dependents();
+  wait_for_stream();
+  const int r = rows[blockIdx.x];
+  if ((uint32_t)r >= (uint32_t)s.rows) return;
+  const int len = min(max(s.lens[r], 0), s.max_pages << s.page_log);
+  for (int j = ((len + (1 << s.page_log) - 1) >> s.page_log) + threadIdx.x; j < s.max_pages; j += blockDim.x) {
+    const int page = atomicExch(s.table + (int64_t)r * s.table_stride + j, -1);
+    if (in_pool(s, page)) atomicSub(s.refs + page, 1);
+  }
+}
+
+// Rows that begin with the same pages, in one cluster: the lowest row of each first page, the positions alike with it
+// (a warp per row and 1024 positions), then each row's rank among (leader, row) by counting.  A chain of five phases, each the
+// latency of a few dependent reads and a cluster barrier.
+constexpr int kShareCtas = 8, kShareThreads = 1024, kSharePart = 1024;
+__global__ void __cluster_dims__(kShareCtas, 1, 1) __launch_bounds__(kShareThreads)
+    akv_pages_share_kernel(PagesState s, akv_share out, int32_t* first) {
+  launch_dependents();
+  wait_for_stream();
+  cg::cluster_group cl = cg::this_cluster();
+  const int tid = blockIdx.x * kShareThreads + threadIdx.x, all = kShareCtas * kShareThreads;
+  const int lane = threadIdx.x & 31, warp = tid >> 5, warps = all / 32;
+  auto held = [&](int r) {
+    const int len = min(max(s.lens[r], 0), s.max_pages << s.page_log);
+    return (len + (1 << s.page_log) - 1) >> s.page_log;
+  };
+  auto page0 = [&](int r) {
+    const int page = held(r) > 0 ? s.table[(int64_t)r * s.table_stride] : -1;
+    return in_pool(s, page) ? page : -1;
+  };
+  for (int r = tid; r < s.rows; r += all) {
+    const int page = page0(r);
+    if (page >= 0) first[page] = INT32_MAX;
+  }
+  cl.sync();
+  for (int r = tid; r < s.rows; r += all) {
+    const int page = page0(r);
+    if (page >= 0) atomicMin(first + page, r);
+  }
+  cl.sync();
+  for (int r = tid; r < s.rows; r += all) {
+    const int page = page0(r);
+    out.leader[r] = page >= 0 ? __ldcg(first + page) : r;
+    out.pages[r] = held(r);
+  }
+  cl.sync();
+  const int parts = (s.max_pages + kSharePart - 1) / kSharePart;
+  for (int64_t k = warp; k < (int64_t)s.rows * parts; k += warps) {
+    const int r = (int)(k / parts), lead = __ldcg(out.leader + r);
+    if (lead == r) continue;
+    const int both = min(held(r), held(lead));
+    const int from = (int)(k % parts) * kSharePart, to = min(both, from + kSharePart);
+    const int32_t *a = s.table + (int64_t)r * s.table_stride, *b = s.table + (int64_t)lead * s.table_stride;
+    int differs = from == 0 ? both : INT32_MAX;  // (the first part sees to the lengths)
+    for (int j0 = from; j0 < to && differs > j0; j0 += 256) {
+      int x[8], y[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = j0 + 32 * u + lane;
+        x[u] = j < to ? a[j] : 0, y[u] = j < to ? b[j] : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = j0 + 32 * u + lane;
+        if (j < to && (x[u] != y[u] || !in_pool(s, x[u]))) differs = min(differs, j);
+      }
+      differs = __reduce_min_sync(0xffffffffu, differs);
+    }
+    if (lane == 0 && differs != INT32_MAX) atomicMin(out.pages + lead, differs);
+  }
+  cl.sync();
+  for (int r = warp; r < s.rows; r += warps) {
+    const int lead = __ldcg(out.leader + r);
+    int rank = 0, size = 0;
+    for (int j = lane; j < s.rows; j += 32) {
+      const int x = __ldcg(out.leader + j);
+      rank += x < lead || (x == lead && j < r);
+      size += x == lead;
+    }
+    rank = __reduce_add_sync(0xffffffffu, rank);
+    size = __reduce_add_sync(0xffffffffu, size);
+    if (lane == 0) {
+      // (a group's number is its leader's, which the leader writes back as it is)
+      out.pages[r] = size > 1 ? __ldcg(out.pages + lead) : 0;
+      out.size[r] = size;
+      out.order[rank] = r;
+    }
+  }
+}
+
 struct RowPlan {
   int first, need;  // table positions that the new tokens fall into
   bool cut;         // the first of them holds tokens of the row already
@@ -321,6 +417,14 @@ int launch_pages_fork(const PagesState& s, const int32_t* src, const int32_t* ds
 
 int launch_pages_free(const PagesState& s, const int32_t* rows, int32_t n, void* stream) {
   return launch_after(akv_pages_free_kernel, dim3(n), 256, 0, stream, s, rows);
+}
+
+int launch_pages_trim(const PagesState& s, const int32_t* rows, int32_t n, void* stream) {
+  return launch_after(akv_pages_trim_kernel, dim3(n), 256, 0, stream, s, rows);
+}
+
+int launch_pages_share(const PagesState& s, const akv_share& share, void* ws, void* stream) {
+  return launch_after(akv_pages_share_kernel, dim3(kShareCtas), kShareThreads, 0, stream, s, share, pages_ws(s, ws).lowest);
 }
 
 int launch_pages_reserve(const PagesState& s, const int32_t* n_new, int32_t* missing, void* ws, void* stream) {

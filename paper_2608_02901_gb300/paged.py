@@ -17,7 +17,8 @@ AKV_PAGED_MAX_QUERY = 64
 EXPORTED = (
     "akv_paged_page_bytes", "akv_paged_append", "akv_paged_read", "akv_paged_attn_workspace_size", "akv_paged_attn",
     "akv_paged_select_workspace_size", "akv_paged_select", "akv_pages_copy", "akv_pages_fork",
-    "akv_pages_workspace_size", "akv_pages_reserve", "akv_pages_free", "akv_pages_compact",
+    "akv_pages_workspace_size", "akv_pages_reserve", "akv_pages_free", "akv_pages_compact", "akv_pages_share",
+    "akv_paged_attn_shared_workspace_size", "akv_paged_attn_shared", "akv_paged_weights", "akv_paged_evict", "akv_pages_trim",
 )
 
 _vp, _i32, _i64, _sz, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
@@ -42,9 +43,21 @@ class _Selection(ctypes.Structure):
     _fields_ = [("pages", _vp), ("count", _vp), ("top", _i32)]
 
 
+class _Share(ctypes.Structure):
+    _fields_ = [("leader", _vp), ("pages", _vp), ("size", _vp), ("order", _vp)]
+
+
+class _Scores(ctypes.Structure):
+    _fields_ = [("ptr", _vp), ("stride_b", _i64), ("stride_h", _i64), ("cap", _i32)]
+
+
+class _Kept(ctypes.Structure):
+    _fields_ = [("tokens", _vp), ("count", _vp), ("top", _i32)]
+
+
 def declare(L):
     """Argument types of the entry points in a loaded libakv.so."""
-    P, G, R, S = (ctypes.POINTER(t) for t in (_PagedParams, _Pages, _Rows, _Selection))
+    P, G, R, S, H, N, K = (ctypes.POINTER(t) for t in (_PagedParams, _Pages, _Rows, _Selection, _Share, _Scores, _Kept))
     out = ctypes.POINTER(_sz)
     for name, args in (
             ("akv_paged_page_bytes", [P, out]),
@@ -59,7 +72,13 @@ def declare(L):
             ("akv_pages_workspace_size", [P, G, out]),
             ("akv_pages_reserve", [P, G, _vp, _vp, _vp, _sz, _vp]),
             ("akv_pages_free", [P, G, _vp, _i32, _vp]),
-            ("akv_pages_compact", [P, G, _vp, _vp, _sz, _vp])):
+            ("akv_pages_compact", [P, G, _vp, _vp, _sz, _vp]),
+            ("akv_pages_share", [P, G, H, _vp, _sz, _vp]),
+            ("akv_paged_attn_shared_workspace_size", [P, G, _i32, out]),
+            ("akv_paged_attn_shared", [P, G, _i32, R, R, _vp, _i32, _f32, H, _vp, _sz, _vp]),
+            ("akv_paged_weights", [P, G, _i32, R, _vp, _i32, _f32, _f32, N, N, _vp]),
+            ("akv_paged_evict", [P, G, _i32, _vp, _vp, _i32, N, _vp, _i32, _i32, K, _vp]),
+            ("akv_pages_trim", [P, G, _vp, _i32, _vp])):
         f = getattr(L, name)
         f.restype, f.argtypes = ctypes.c_int, args
 
@@ -191,6 +210,35 @@ class PageSelection:
         self.ref = ctypes.byref(self._c)
 
 
+class PageShare:
+    """Rows that begin with the same pages, as akv_pages_share finds them: a contiguous CUDA int32 tensor [4][rows] of
+    leader, pages, size and order (akv_share in include/akv.h)."""
+
+    def __init__(self, arrays):
+        if arrays.dim() != 2 or arrays.shape[0] != 4:
+            raise ValueError("share must be [4][rows]")
+        _lib()
+        self.arrays, self.rows, self.index = arrays, int(arrays.shape[1]), arrays.get_device()
+        at = _ints(arrays, "share", None, self.index)
+        if self.index < 0:
+            raise ValueError("share must be on the pool's device")
+        self._c = _Share(*(at + 4 * self.rows * i for i in range(4)))
+        self.ref = ctypes.byref(self._c)
+
+
+class KeptTokens:
+    """Tokens that rows keep: CUDA int32 tokens [n][n_kv_heads][top], count [n], both contiguous."""
+
+    def __init__(self, tokens, count):
+        if tokens.dim() != 3 or tuple(count.shape) != (tokens.shape[0],):
+            raise ValueError("kept: tokens [n][n_kv_heads][top] and count [n]")
+        self.tokens, self.count, self.top = tokens, count, int(tokens.shape[2])
+        _lib()
+        self._c = _Kept(_ints(tokens, "kept tokens", None, tokens.get_device()),
+                        _ints(count, "kept count", None, tokens.get_device()), self.top)
+        self.ref = ctypes.byref(self._c)
+
+
 def _params(p: PagedParams, pages: Pages):
     """The C parameters of p, which describes the pool's pages (its query heads may differ)."""
     if p is pages.p:
@@ -304,6 +352,100 @@ def akv_paged_select(p: PagedParams, pages: Pages, q, sel: PageSelection, sink: 
     ws, at, n = _workspace(ws, pages, stream, akv_paged_select_workspace_size, p, pages, T)
     _check(L.akv_paged_select(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads), T, sink, recent,
                               sel.ref, at, n, _stream(stream, pages)), "akv_paged_select")
+
+
+def _shared(share: PageShare, pages: Pages):
+    if share.rows != pages.rows or share.index != pages.index:
+        raise ValueError(f"share must be for {pages.rows} rows, on the pool's device")
+    return share.ref
+
+
+def akv_pages_share(p: PagedParams, pages: Pages, share: PageShare, ws=None, stream=None):
+    """Fills share: which rows begin with the same pages.  Once a step, for all layers.  ws as in akv_pages_reserve."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_share, p, pages, share, ws, stream)
+    L = _lib()
+    ref = _shared(share, pages)
+    ws, at, n = _workspace(ws, pages, stream, akv_pages_workspace_size, pages)
+    _check(L.akv_pages_share(_params(p, pages), pages.ref, ref, at, n, _stream(stream, pages)), "akv_pages_share")
+
+
+def akv_paged_attn_shared_workspace_size(p: PagedParams, pages: Pages, T: int = 1) -> int:
+    n = _sz()
+    _check(_lib().akv_paged_attn_shared_workspace_size(_params(p, pages), pages.ref, T, ctypes.byref(n)),
+           "akv_paged_attn_shared_workspace_size")
+    return n.value
+
+
+def _lse(lse, p: PagedParams, pages: Pages, T):
+    if (lse.dtype is not _torch.float32 or lse.get_device() != pages.index or not lse.is_contiguous()
+            or lse.shape != (pages.rows, T, p.n_q_heads)):
+        raise ValueError(f"lse must be a contiguous CUDA fp32 tensor [{pages.rows}][{T}][{p.n_q_heads}]")
+    return lse.data_ptr()
+
+
+def akv_paged_attn_shared(p: PagedParams, pages: Pages, q, out, share: PageShare, lse=None, sm_scale: float = 1.0,
+                          layer: int = 0, ws=None, stream=None):
+    """akv_paged_attn over rows that share pages (share of akv_pages_share): those are read once for all.
+    ws as there, of akv_paged_attn_shared_workspace_size bytes."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_attn_shared, p, pages, q, out, share, lse, sm_scale, layer, ws, stream)
+    T = _tokens(q, "q")
+    L = _lib()
+    ref = _shared(share, pages)
+    lse = None if lse is None else _lse(lse, p, pages, T)
+    ws, at, n = _workspace(ws, pages, stream, akv_paged_attn_shared_workspace_size, p, pages, T)
+    _check(L.akv_paged_attn_shared(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads),
+                                   _rows(out, "out", p, pages, T, p.n_q_heads), lse, T, sm_scale, ref, at, n,
+                                   _stream(stream, pages)), "akv_paged_attn_shared")
+
+
+def _scores(t, what, p: PagedParams, pages: Pages):
+    """The C view of an fp32 [rows][n_kv_heads][cap] tensor with adjacent numbers in its last axis."""
+    if t.dtype is not _torch.float32 or t.get_device() != pages.index:
+        raise ValueError(f"{what} must be a CUDA fp32 tensor on the pool's device")
+    if t.dim() != 3 or t.shape[:2] != (pages.rows, p.n_kv_heads):
+        raise ValueError(f"{what} must be [{pages.rows}][{p.n_kv_heads}][cap], got {list(t.shape)}")
+    sb, sh, si = t.stride()
+    if si != 1 and t.shape[2] > 1:
+        raise ValueError(f"{what} must have adjacent numbers in its last axis")
+    return _Scores(t.data_ptr(), sb, sh, min(t.shape[2], 2**31 - 1))
+
+
+def akv_paged_weights(p: PagedParams, pages: Pages, q, lse, now, was=None, decay: float = 1.0, sm_scale: float = 1.0,
+                      layer: int = 0, stream=None):
+    """now = decay was + the attention weights of the last T query tokens.  q: [rows][T][n_q_heads][128], lse of
+    akv_paged_attn; now, was: fp32 [rows][n_kv_heads][cap], was None (zeros) or now itself."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_weights, p, pages, q, lse, now, was, decay, sm_scale, layer, stream)
+    T = _tokens(q, "q")
+    L = _lib()
+    _check(L.akv_paged_weights(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads),
+                               _lse(lse, p, pages, T), T, sm_scale, decay,
+                               None if was is None else _scores(was, "was", p, pages), _scores(now, "now", p, pages),
+                               _stream(stream, pages)), "akv_paged_weights")
+
+
+def akv_paged_evict(p: PagedParams, pages: Pages, src, dst, scores, kept: KeptTokens, keep=None, sink: int = 0,
+                    recent: int = 0, layer: int = 0, stream=None):
+    """Row dst[i] gets the tokens that row src[i] keeps by their scores (CUDA int32 [n]; the same row: in place).  scores: fp32
+    [rows][n_kv_heads][cap]; keep: CUDA int32 [n] (None: kept.top each); fills kept.  lens is not changed."""
+    if _device() != pages.index:
+        return _there(pages, akv_paged_evict, p, pages, src, dst, scores, kept, keep, sink, recent, layer, stream)
+    a, b, n = _pair(src, dst, pages)
+    if tuple(kept.tokens.shape[:2]) != (n, p.n_kv_heads) or kept.tokens.device != pages.device:
+        raise ValueError(f"kept must be for [{n}][{p.n_kv_heads}], on the pool's device")
+    _check(_lib().akv_paged_evict(_params(p, pages), pages.ref, layer, a, b, n, _scores(scores, "scores", p, pages),
+                                  _ints(keep, "keep", n, pages.index), sink, recent, kept.ref, _stream(stream, pages)),
+           "akv_paged_evict")
+
+
+def akv_pages_trim(p: PagedParams, pages: Pages, rows, stream=None):
+    """Rows (CUDA int32) give up the pages behind their length."""
+    if _device() != pages.index:
+        return _there(pages, akv_pages_trim, p, pages, rows, stream)
+    _check(_lib().akv_pages_trim(_params(p, pages), pages.ref, _ints(rows, "rows", None, pages.index), rows.numel(),
+                                 _stream(stream, pages)), "akv_pages_trim")
 
 
 def _pair(src, dst, pages):
