@@ -17,8 +17,9 @@ namespace cg = cooperative_groups;
 namespace akv {
 namespace {
 
-constexpr int kCtas = 8, kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
+constexpr int kEach = 8, kBatch = kThreads * kEach;  // scores of a thread, of a CTA, that are under way at a time
 
 struct EvictArgs {
   PagedView v;
@@ -53,13 +54,28 @@ struct Moved {  // a warp's share of a sub-block on its way
   float score;
 };
 
-__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv_paged_evict_kernel(const __grid_constant__ EvictArgs a) {
-  __shared__ uint32_t hist[kBins], slice[kBins / kCtas], part[kWarps], part2[kWarps];
+// A cluster of C CTAs; one is on its own.
+template <int C>
+struct Cluster {
+  __device__ __forceinline__ int rank() const { return C == 1 ? 0 : (int)cg::this_cluster().block_rank(); }
+  __device__ __forceinline__ void sync() const {
+    if (C == 1) __syncthreads();
+    else cg::this_cluster().sync();
+  }
+  template <class T>
+  __device__ __forceinline__ T* of(T* p, int r) const {
+    return C == 1 ? p : cg::this_cluster().map_shared_rank(p, r);
+  }
+};
+
+template <int C>
+__global__ void __launch_bounds__(kThreads, 2) akv_paged_evict_kernel(const __grid_constant__ EvictArgs a) {
+  __shared__ uint32_t hist[kBins], slice[kBins / C], part[kWarps], part2[kWarps];
   __shared__ uint32_t total, flag, n_above, n_equal, first_gone;
-  cg::cluster_group cl = cg::this_cluster();
+  const Cluster<C> cl;
   const PagedView& v = a.v;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = (int)cl.block_rank(), unit = blockIdx.x / kCtas, pair = unit / v.H, h = unit % v.H;
+  const int rank = cl.rank(), unit = blockIdx.x / C, pair = unit / v.H, h = unit % v.H;
   launch_dependents();
   wait_for_stream();
 
@@ -70,9 +86,33 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
   const int m = min(held, min(max(a.keep ? a.keep[pair] : a.top, 0), a.top));
   const bool in_place = from == to, stays = in_place && m == held;
   const int P = 1 << v.page_log;
+
+  // the CTA's share of the scores: its only batch stays in registers
+  const float* mine = rows_ok ? a.scores + (int64_t)from * a.sb + (int64_t)h * a.sh : a.scores;
+  const int share = ((held + C - 1) / C + 31) & ~31, lo = min(held, rank * share), hi = min(held, lo + share);
+  uint32_t key[kEach];  // of tokens i0 + 32 (kEach warp + e) + lane, 0 behind the share
+  auto place = [&](int i0, int e) { return i0 + 32 * (kEach * warp + e) + lane; };
+  auto load = [&](int i0) {
+    float x[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) x[e] = place(i0, e) < hi ? mine[place(i0, e)] : 0.f;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = place(i0, e);
+      key[e] = i < a.sink || i >= held - a.recent ? kForced : score_key(x[e]);
+    }
+  };
+  auto each_batch = [&](auto f) {
+    for (int i0 = lo; i0 < hi; i0 += kBatch) {
+      if (hi - lo > kBatch) load(i0);
+      f(i0);
+    }
+  };
+  if (m < held && hi - lo <= kBatch) load(lo);
+
   bool bad = !rows_ok;
-  for (int j = rank * kThreads + tid; j < (held + P - 1) >> v.page_log; j += kCtas * kThreads) bad = bad || page_of(v, from, j) < 0;
-  for (int j = rank * kThreads + tid; j < (m + P - 1) >> v.page_log && rows_ok; j += kCtas * kThreads) {
+  for (int j = rank * kThreads + tid; j < (held + P - 1) >> v.page_log; j += C * kThreads) bad = bad || page_of(v, from, j) < 0;
+  for (int j = rank * kThreads + tid; j < (m + P - 1) >> v.page_log && rows_ok; j += C * kThreads) {
     const int page = page_of(v, to, j);
     bad = bad || page < 0 || (!stays && v.refs && v.refs[page] > 1);
   }
@@ -81,52 +121,62 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
   cl.sync();
   uint32_t refuse = 0;
 #pragma unroll
-  for (int r = 0; r < kCtas; ++r) refuse |= *cl.map_shared_rank(&flag, r);
+  for (int r = 0; r < C; ++r) refuse |= *cl.of(&flag, r);
   int32_t* list = a.tokens + (int64_t)unit * a.top;
   const int listed = refuse ? 0 : m;
-  for (int k = listed + rank * kThreads + tid; k < a.top; k += kCtas * kThreads) list[k] = -1;
+  for (int k = listed + rank * kThreads + tid; k < a.top; k += C * kThreads) list[k] = -1;
   if (rank == 0 && tid == 0 && h == 0) a.count[pair] = refuse ? -1 : m;
   if (refuse || m == 0) {
     cl.sync();  // (the others have read the flag)
     return;
   }
 
-  const float* mine = a.scores + (int64_t)from * a.sb + (int64_t)h * a.sh;
-  const int share = ((held + kCtas - 1) / kCtas + 31) & ~31, lo = min(held, rank * share), hi = min(held, lo + share);
-  auto key_of = [&](int i) { return i < a.sink || i >= held - a.recent ? kForced : score_key(mine[i]); };
-
   // ---- the lowest key that is kept, and how many of that key
   uint32_t cut = 0, left = (uint32_t)m;
   if (m < held) {
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048, top_shift = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048, top_shift = pass == 1 ? 21 : 10;
       for (int k = tid; k < bins; k += kThreads) hist[k] = 0;
       __syncthreads();
-      for (int i = lo + tid; i < hi; i += kThreads) {
-        const uint32_t k = key_of(i);
-        if (pass == 0 || (k ^ cut) >> top_shift == 0) atomicAdd(&hist[k >> shift & (bins - 1)], 1u);
-      }
-      cl.sync();
-      const int each = bins / kCtas;  // bins of a CTA
-      uint32_t sum = 0;
-      if (tid < each) {
+      each_batch([&](int i0) {
 #pragma unroll
-        for (int r = 0; r < kCtas; ++r) sum += cl.map_shared_rank(hist, r)[rank * each + tid];
-        slice[tid] = sum;
-      }
-      sum = smem_sum(sum, part);
-      if (tid == 0) total = sum;
+        for (int e = 0; e < kEach; ++e)
+          if (place(i0, e) < hi && (pass == 0 || (key[e] ^ cut) >> top_shift == 0)) atomicAdd(&hist[key[e] >> shift & (bins - 1)], 1u);
+      });
       cl.sync();
-      int owner = kCtas - 1;  // the CTA in whose bins the count is reached, from the top
+      const int each = bins / C;  // bins of a CTA
+      uint32_t sum = 0;
+      if (C > 1) {
+        for (int k = tid; k < each; k += kThreads) {
+          uint32_t x = 0;
+#pragma unroll
+          for (int r = 0; r < C; ++r) x += cl.of(hist, r)[rank * each + k];
+          slice[k] = x;
+          sum += x;
+        }
+        sum = smem_sum(sum, part);
+        if (tid == 0) total = sum;
+        cl.sync();
+      }
+      int owner = C - 1;  // the CTA in whose bins the count is reached, from the top
       for (; owner > 0; --owner) {
-        const uint32_t there = *cl.map_shared_rank(&total, owner);
+        const uint32_t there = *cl.of(&total, owner);
         if (there >= left) break;
         left -= there;
       }
-      // thread t: bin each - 1 - t, so that sums over the threads before are sums from the top
-      const uint32_t mine_n = tid < each ? cl.map_shared_rank(slice, owner)[each - 1 - tid] : 0;
-      uint32_t inc = mine_n;
+      // thread t: bins each - 1 - n t and the n - 1 before, so that sums over the threads before are sums from the top
+      constexpr int kMost = kBins / C > kThreads ? kBins / C / kThreads : 1;
+      const int n = each > kThreads ? each / kThreads : 1;
+      const uint32_t* bin = C > 1 ? cl.of(slice, owner) : hist;
+      uint32_t here[kMost], inc = 0;
+#pragma unroll
+      for (int k = 0; k < kMost; ++k) {
+        const int x = each - 1 - (n * tid + k);
+        here[k] = k < n && x >= 0 ? bin[x] : 0;
+        inc += here[k];
+      }
+      const uint32_t mine_n = inc;
 #pragma unroll
       for (int s = 1; s < 32; s *= 2) {
         const uint32_t o = __shfl_up_sync(0xffffffffu, inc, s);
@@ -136,7 +186,12 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
       if (lane == 31) part[warp] = inc;
       __syncthreads();
       for (int w = 0; w < warp; ++w) inc += part[w];
-      if (mine_n && inc >= left && inc - mine_n < left) part2[0] = (uint32_t)(owner * each + each - 1 - tid), part2[1] = left - (inc - mine_n);
+      inc -= mine_n;
+#pragma unroll
+      for (int k = 0; k < kMost; ++k) {
+        if (here[k] && inc < left && inc + here[k] >= left) part2[0] = (uint32_t)(owner * each + each - 1 - (n * tid + k)), part2[1] = left - inc;
+        inc += here[k];
+      }
       __syncthreads();
       cut |= part2[0] << shift;
       left = part2[1];
@@ -145,28 +200,31 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
   }
 
   // ---- the list: tokens above the cut, and the first `left` at it
-  uint32_t above = 0, equal = 0;
   if (m < held) {
-    for (int i = lo + tid; i < hi; i += kThreads) {
-      const uint32_t k = key_of(i);
-      above += k > cut, equal += k == cut;
+    uint32_t above = 0, equal = 0;
+    if (C > 1) {
+      each_batch([&](int i0) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const bool in = place(i0, e) < hi;
+          above += in && key[e] > cut, equal += in && key[e] == cut;
+        }
+      });
+      above = smem_sum(above, part);
+      equal = smem_sum(equal, part);
+      if (tid == 0) n_above = above, n_equal = equal;
+      cl.sync();
+      above = equal = 0;
+      for (int r = 0; r < rank; ++r) above += *cl.of(&n_above, r), equal += *cl.of(&n_equal, r);
     }
-    above = smem_sum(above, part);
-    equal = smem_sum(equal, part);
-    if (tid == 0) n_above = above, n_equal = equal;
-    cl.sync();
-    above = equal = 0;
-    for (int r = 0; r < rank; ++r) above += *cl.map_shared_rank(&n_above, r), equal += *cl.map_shared_rank(&n_equal, r);
-    constexpr int kEach = 8;  // tokens of a thread a turn
     uint32_t gone = (uint32_t)held;
-    for (int i0 = lo; i0 < hi; i0 += kThreads * kEach) {
+    each_batch([&](int i0) {
       uint32_t is_above[kEach], is_equal[kEach], na = 0, ne = 0;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const int i = i0 + 32 * (kEach * warp + e) + lane;
-        const uint32_t k = i < hi ? key_of(i) : 0;
-        is_above[e] = __ballot_sync(0xffffffffu, i < hi && k > cut);
-        is_equal[e] = __ballot_sync(0xffffffffu, i < hi && k == cut);
+        const bool in = place(i0, e) < hi;
+        is_above[e] = __ballot_sync(0xffffffffu, in && key[e] > cut);
+        is_equal[e] = __ballot_sync(0xffffffffu, in && key[e] == cut);
         na += __popc(is_above[e]), ne += __popc(is_equal[e]);
       }
       __syncthreads();
@@ -181,13 +239,13 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
       const uint32_t before = (1u << lane) - 1;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const int i = i0 + 32 * (kEach * warp + e) + lane;
+        const int i = place(i0, e);
         const uint32_t ea = xa + __popc(is_above[e] & before), ee = xe + __popc(is_equal[e] & before);
         if ((is_above[e] >> lane & 1) || ((is_equal[e] >> lane & 1) && ee < left)) list[ea + min(ee, left)] = i;
         else if (i < hi) gone = min(gone, (uint32_t)i);
         xa += __popc(is_above[e]), xe += __popc(is_equal[e]);
       }
-    }
+    });
     gone = __reduce_min_sync(0xffffffffu, gone);
     if (lane == 0) atomicMin(&first_gone, gone);
   } else {
@@ -198,7 +256,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
   if (in_place) {
     uint32_t first = (uint32_t)held;
 #pragma unroll
-    for (int r = 0; r < kCtas; ++r) first = min(first, *cl.map_shared_rank(&first_gone, r));
+    for (int r = 0; r < C; ++r) first = min(first, *cl.of(&first_gone, r));
     start = (int)first >> 4;
   }
   cl.sync();  // (nobody's shared memory is read from here on)
@@ -207,18 +265,29 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
   // ---- the move
   const uint32_t sub_size = sub_bytes(v.ng);
   const int subs = (m + 15) >> 4;
+  constexpr int kStep = C * kWarps;
   float* theirs = a.scores + (int64_t)to * a.sb + (int64_t)h * a.sh;
+  // Lanes 0 .. 15 look up a token each; places two rounds ahead, pages one.
+  auto token_at = [&](int s) { return s < subs ? __ldcg(list + min(16 * s + (lane & 15), m - 1)) : 0; };
+  auto source_of = [&](int tok) {
+    return block_of(v, page_of(v, from, tok >> v.page_log), h) + (uint64_t)((tok & (P - 1)) >> 4) * sub_size;
+  };
+  auto target_page = [&](int s) { return page_of(v, to, s < subs ? 16 * s >> v.page_log : 0); };
+  const int first_sub = start + rank * kWarps + warp;
+  int tok = token_at(first_sub), next_tok = token_at(first_sub + kStep);
+  const uint8_t* source = source_of(tok);
+  int page = target_page(first_sub);
 #pragma unroll 1
-  for (int s0 = start; s0 < subs; s0 += kCtas * kWarps) {
+  for (int s0 = start; s0 < subs; s0 += kStep) {
     const int s = s0 + rank * kWarps + warp, n = min(16, m - 16 * s);  // tokens of the warp's sub-block
+    const uint8_t* next_source = source_of(next_tok);
+    const int next_page = target_page(s + kStep);
+    const int after_tok = token_at(s + 2 * kStep);
     Moved x{};
     if (n > 0) {
-      // lanes 0 .. 15 look up a token each
-      const int tok = __ldcg(list + 16 * s + min(lane & 15, n - 1));
-      const uint8_t* base = block_of(v, page_of(v, from, tok >> v.page_log), h) + (uint64_t)((tok & (P - 1)) >> 4) * sub_size;
-      auto of = [&](int k, int& place) {
-        place = __shfl_sync(0xffffffffu, tok, k) & 15;
-        return (const uint8_t*)__shfl_sync(0xffffffffu, (unsigned long long)base, k);
+      auto of = [&](int k, int& at) {
+        at = __shfl_sync(0xffffffffu, tok, k) & 15;
+        return (const uint8_t*)__shfl_sync(0xffffffffu, (unsigned long long)source, k);
       };
       int i0, i1;
       {
@@ -238,7 +307,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
                                 __byte_perm(y0.w, y1.w, pick));
       }
       if (lane < n) {
-        const uint8_t* at = base + 2048 + 8 * v.ng * (tok & 15);
+        const uint8_t* at = source + 2048 + 8 * v.ng * (tok & 15);
         if (v.ng == 2) {
           x.meta = *(const uint4*)at;
         } else {
@@ -250,7 +319,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
     }
     if (in_place) cl.sync();
     if (n > 0) {
-      uint8_t* base = block_of(v, page_of(v, to, 16 * s >> v.page_log), h) + (uint64_t)((16 * s & (P - 1)) >> 4) * sub_size;
+      uint8_t* base = block_of(v, page, h) + (uint64_t)((16 * s & (P - 1)) >> 4) * sub_size;
       if (lane >> 1 < n) {
         uint4* k = (uint4*)(base + 32 * lane);
         k[0] = x.key[0], k[1] = x.key[1];
@@ -274,7 +343,24 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads, 2) akv
         theirs[16 * s + lane] = x.score;
       }
     }
+    tok = next_tok, next_tok = after_tok, source = next_source, page = next_page;
   }
+}
+
+template <int C>
+int launch(const EvictArgs& a, int units, void* stream) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = C, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)units * C);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = (cudaStream_t)stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = C > 1 ? 2 : 1;
+  return (int)cudaLaunchKernelEx(&cfg, akv_paged_evict_kernel<C>, a);
 }
 
 }  // namespace
@@ -288,7 +374,13 @@ int launch_paged_evict(const PagedView& v, const int32_t* src, const int32_t* ds
   a.sb = scores.stride_b, a.sh = scores.stride_h;
   a.sink = sink, a.recent = recent;
   a.tokens = kept.tokens, a.count = kept.count, a.top = kept.top;
-  return launch_after(akv_paged_evict_kernel, dim3((unsigned)(n * v.H * kCtas)), kThreads, 0, stream, a);
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return (int)e;
+  // two CTAs an SM
+  const int units = n * v.H, fit = 2 * sms / units;
+  return fit >= 8 ? launch<8>(a, units, stream) : fit >= 4 ? launch<4>(a, units, stream) : fit >= 2 ? launch<2>(a, units, stream) : launch<1>(a, units, stream);
 }
 
 }  // namespace akv

@@ -5,10 +5,12 @@
 // 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA, one CTA an SM.  In a CTA
 //   8 warps turn codes into operands, a sub-block of 16 tokens each: keys as c a in two fp16 halves (hi = fp16(c a), lo = the exact rest),
 //     values as fp16(m + c a),
-//   1 thread issues the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry m sum(q), so that a logit comes out
-//     whole, then O += P V with P out of tensor memory,
+//   1 warp issues the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry m sum(q), so that a logit comes out
+//     whole, then O += P V; Q and P come out of tensor memory, so that a product reads 4 KiB of shared memory and not 8.  (The warp goes
+//     through its loop as one and elects the issuing thread at each batch: descriptors then are sums in uniform registers.  Out of a
+//     loop of one thread a product took 94 to 107 cycles, where the tensor cores need 64 for 128 x 128 x 16.)
 //   2 x 4 warps take the tiles in turn, a thread per query row: p = 2^(S scale - reference), its sum, P as fp16 over S's columns.
-// Each of the two has its own O, reference and sum; they are put together at the unit's end.
+//     Both add to one O, so a row has one reference: it goes from tile to tile, and to the other thread of its row.
 //   S is as exact as fp32 sums: products of fp16 numbers are, a query enters as one fp16 number (a power of two times what was given)
 // or, rotated, as a high and a low one.  The scales of tokens could not be applied behind the products instead: a thread that owns a row would
 // read four numbers a token from shared memory, 512 bytes a warp, four times what the tensor cores need for the extra products.
@@ -16,6 +18,7 @@
 // down to 2^-19 of the reference's.  Sub-blocks with a scale above 2048 or a minimum beyond 32768 enter as 2^-5 of themselves (their
 // columns of S count 32, their P is 32 times as large).  Tokens with a NaN enter as values of 0 and a NaN in S: rows that do not see
 // them do not feel them.
+//   Loops over a row's columns are not unrolled beyond 32: a call's first tile waits for its instructions.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -28,14 +31,14 @@ namespace {
 
 constexpr int kRows = 128, kTile = 128;
 constexpr int kSoftWarps = 8, kUnpackWarps = 8, kMmaWarp = kSoftWarps + kUnpackWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kThreads = 32 * (kMmaWarp + 4);  // (whole warpgroups, which share registers out: three warps are idle)
 constexpr uint32_t kPanel = 128 * 128;    // bytes of 64 of an operand's K for 128 of its rows
 constexpr uint32_t kExtra = 128 * 32;     // 16 of K
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -3.402823466e38f;  // reference of a row that saw no token: below all others
 constexpr float kSlack = 5.f, kPlace = 5.f;
 constexpr int kMaxCtas = 256;
-constexpr uint32_t kCols = 512;           // tensor memory: S of both, O of both
+constexpr uint32_t kCols = 512, kColO = 256, kColQ = 384;  // tensor memory: S of two tiles, O, Q's high and low halves
 
 struct SharedArgs {
   PagedView v;
@@ -47,19 +50,19 @@ struct SharedArgs {
   float* slots;        // [ctas][2][kRows] parts of units that several CTAs worked on
   float scale;         // sm_scale log2(e)
   int T;
+  int aligned;         // every query row begins at a multiple of 8 bytes
 };
 
 struct Smem {
-  uint8_t q[4 * kPanel];      // high, then low halves
-  uint8_t k[4 * kPanel];
+  uint8_t k[2][4 * kPanel];   // keys: high, then low halves; the first is where a unit's queries are put together, too
   uint8_t v[2][2 * kPanel];   // values: [dimension][token]
-  uint8_t qx[kExtra], kx[kExtra];
-  float row_scale[kRows], ref[2][kRows], sum[2][kRows];
+  uint8_t qx[kExtra], kx[2][kExtra];
+  float row_scale[kRows], ref[kRows], sum[2][kRows];
   int lim[kRows];             // tokens of the unit that a row sees
   int64_t row_at[kRows];      // its number among all query rows; -1: none
   uint8_t big[4][8];          // sub-blocks that enter as 2^-5 of themselves, by tile modulo 4
-  uint64_t k_full, k_free, v_full[2], v_free[2], s_full[2], p_full[2], q_full, o_full, drained;
-  int64_t part[kMmaWarp + 1];
+  uint64_t k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], ref_at[2][4], q_full, o_full, drained;
+  int64_t part[kThreads / 32];
   int place[8];
   uint32_t tmem;
   int failed;
@@ -85,6 +88,17 @@ __device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<c
 __device__ __forceinline__ bool finite_word(uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; }
 __device__ __forceinline__ void sts128(uint32_t a, uint4 x) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+// Registers of a warpgroup's threads; a launch has 20 warps of 96: 8 x 120 + 8 x 88 + 4 x 64 are 20 x 96.
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// One lane of the warp, the same each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t on;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(on));
+  return on != 0;
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // 32 columns of the thread's lane of tensor memory
@@ -172,7 +186,7 @@ __device__ __forceinline__ Walk plan(const SharedArgs& a, Smem& S, Segment& seg)
   int64_t before = inc - mine;
   Walk w;
   w.total = 0;
-  for (int i = 0; i <= kMmaWarp; ++i) {
+  for (int i = 0; i < kThreads / 32; ++i) {
     if (i < warp) before += S.part[i];
     w.total += S.part[i];
   }
@@ -212,20 +226,120 @@ __device__ __forceinline__ void next_segment(const SharedArgs& a, Segment& s, in
   s.n = (int)min((int64_t)s.tiles, left);
 }
 
+// A unit's queries as operands, put together where the first keys will be, with what goes with its rows.  The 16 warps of both roles
+// call it at each segment's start (its barriers are theirs: the first waits for the segment before), 8 rows a warp.
+template <int NG, bool HILO>
+__device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, const Segment& seg, int warp) {
+  const PagedView& v = a.v;
+  const int lane = threadIdx.x & 31;
+  const uint32_t sign = a.scale < 0.f ? 0x80000000u : 0u;
+  named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
+  constexpr int kEach = kRows / (kSoftWarps + kUnpackWarps);
+  int64_t from = -1;
+  {
+    const int tg = a.T * v.G, qi = seg.block * kRows + warp * kEach + (lane & (kEach - 1));
+    const int k = seg.k0 + qi / tg, t = qi % tg / v.G, gq = qi % tg % v.G;
+    const int b = k < seg.k0 + seg.size ? row_in_order(a, k) : -1;
+    if (b >= 0) from = b * a.qb + t * a.qt + (int64_t)(seg.h * v.G + gq) * a.qh;
+    if (lane < kEach) {
+      S.lim[warp * kEach + lane] = b >= 0 ? min(seg.tokens, held_tokens(v, b) - a.T + 1 + t) : seg.tokens;
+      S.row_at[warp * kEach + lane] = b >= 0 ? ((int64_t)b * a.T + t) * (v.H * v.G) + seg.h * v.G + gq : -1;
+    }
+  }
+  constexpr int kAhead = 4;  // rows under way
+  auto fetch = [&](int r) {
+    const int64_t at_row = __shfl_sync(0xffffffffu, from, r & (kEach - 1));
+    uint2 x = make_uint2(0, 0);
+    if (at_row >= 0 && r < kEach) {
+      const uint16_t* q = a.q + at_row + 4 * lane;
+      if (a.aligned) x = *(const uint2*)q;
+      else x = make_uint2(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16);
+    }
+    return x;
+  };
+  uint2 raw[kAhead];
+#pragma unroll
+  for (int r = 0; r < kAhead; ++r) raw[r] = fetch(r);
+#pragma unroll 1
+  for (int r = 0; r < kEach; ++r) {
+    const int rr = warp * kEach + r;
+    const uint2 now = raw[0];
+#pragma unroll
+    for (int k = 0; k + 1 < kAhead; ++k) raw[k] = raw[k + 1];
+    raw[kAhead - 1] = fetch(r + kAhead);
+    float x[4] = {row_to_float((uint16_t)now.x, v.half), row_to_float((uint16_t)(now.x >> 16), v.half),
+                  row_to_float((uint16_t)now.y, v.half), row_to_float((uint16_t)(now.y >> 16), v.half)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign ^ (HILO ? sign_flip(v, 4 * lane + e) : 0u));
+    if (HILO) {  // q' = H (s o q) / 16
+      wht_32x4(x, lane);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
+    }
+    float big = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float y = fabsf(x[e]);
+      if (y <= 3.402823466e38f) big = fmaxf(big, y);  // an infinite or NaN row spoils itself alone
+    }
+    big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
+    // a row times 2^(7 - e): below 2^7 (its sums below 2^14), exact in fp16 down to 2^-23 of that
+    const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
+    const float up = pow2(7 - e2);
+    float sum = (x[0] + x[1]) + (x[2] + x[3]);
+#pragma unroll
+    for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+    uint4 f[HILO ? 2 : 1];
+#pragma unroll
+    for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
+      uint32_t y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = x[e] * up, hi = __half2float(__float2half_rn(z)), mine = lo ? z - hi : z;
+        const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
+        y[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
+      }
+      f[lo] = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    // lanes 2 x, 2 x + 1 hold dimensions 8 x .. of word j = x / 4, t = x % 4
+    const int j = lane >> 3, chunk = ((j & 1) * 4 + (lane >> 1 & 3)) ^ (rr & 7);
+    const uint32_t to = smem_u32(S.k[0]) + (uint32_t)(j >> 1) * kPanel + 128 * rr + 16 * chunk;
+    if (!(lane & 1)) sts128(to, f[0]);
+    if (HILO && (lane & 1)) sts128(to + 2 * kPanel, f[HILO ? 1 : 0]);
+    // the sums of each group, in three halves (lanes 0 and 16)
+    if ((lane & 15) == 0) {
+      float z = lane == 0 || NG == 2 ? sum * up : 0.f;
+      uint16_t y[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const __half p = __float2half_rn(z);
+        y[i] = __half_as_ushort(p);
+        z -= __half2float(p);
+      }
+      uint16_t* x8 = (uint16_t*)(S.qx + extra_at(rr)) + (lane ? 3 : 0);
+      x8[0] = y[0], x8[1] = y[1], x8[2] = y[2];
+      if (lane) x8[3] = x8[4] = 0;
+      else S.row_scale[rr] = fabsf(a.scale) * pow2(e2 - 7);
+    }
+  }
+  named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
+}
+
 template <int NG, bool HILO>
 __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __grid_constant__ SharedArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   Smem& S = *reinterpret_cast<Smem*>(smem_raw + (1024u - (smem_u32(smem_raw) & 1023u)) % 1024u);
   constexpr uint32_t kSub = 2048 + 128 * NG;
   const PagedView& v = a.v;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   volatile int* failed = &S.failed;
   // What this launch reads was written before the launch that it runs beside, whose CTAs have all waited for it.
   launch_dependents();
   if (tid == 0) {
-    mbar_init(smem_u32(&S.k_full), kUnpackWarps);
-    mbar_init(smem_u32(&S.k_free), 1);
     for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&S.k_full[s]), kUnpackWarps);
+      mbar_init(smem_u32(&S.k_free[s]), 1);
+      for (int q = 0; q < 4; ++q) mbar_init(smem_u32(&S.ref_at[s][q]), 1);
       mbar_init(smem_u32(&S.v_full[s]), kUnpackWarps);
       mbar_init(smem_u32(&S.v_free[s]), 1);
       mbar_init(smem_u32(&S.s_full[s]), 1);
@@ -240,7 +354,8 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
   // the second eight of the sixteen extra dimensions are zeros
   if (tid < 128) {
     sts128(smem_u32(S.qx) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
-    sts128(smem_u32(S.kx) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
+    sts128(smem_u32(S.kx[0]) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
+    sts128(smem_u32(S.kx[1]) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
     proxy_fence();
   }
   Segment seg;
@@ -253,198 +368,255 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = S.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, S.tmem, 0);
 
-  if (warp == kMmaWarp) {
-    if (lane == 0) {
+  if (warp >= kMmaWarp) {
+    fewer_registers<64>();
+    if (warp == kMmaWarp) {
       // ---- the products
       constexpr uint32_t idesc = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);  // fp16 x fp16 -> fp32, 128 x 128
-      const uint64_t dq = sw128_desc(smem_u32(S.q)), dk = sw128_desc(smem_u32(S.k));
-      const uint64_t dqx = plain_desc(smem_u32(S.qx)), dkx = plain_desc(smem_u32(S.kx));
-      auto step = [](int kk) { return (uint64_t)(((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4); };
-      uint32_t nk = 0, np[2] = {0, 0}, nv[2] = {0, 0}, nseg = 0;
+      const uint64_t dqx = plain_desc(smem_u32(S.qx));
+      // D (+)= A B^T over 128 of K, A out of tensor memory
+      auto product = [&](uint32_t d, uint32_t at, uint64_t desc, bool first) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+          tc_mma_ts(d, at + 8 * kk, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || kk > 0);
+      };
+      uint32_t n_tile = 0, nseg = 0;
       bool ok = true;
       for (int64_t at = w.lo; ok && at < w.hi; ++nseg) {
-        ok = mbar_wait(smem_u32(&S.q_full), nseg & 1);
-        auto values = [&](int i) {  // O += P V of tile i
-          const int s = i & 1;
-          ok = ok && mbar_wait(smem_u32(&S.p_full[s]), np[s]++ & 1) && mbar_wait(smem_u32(&S.v_full[s]), nv[s]++ & 1);
-          if (!ok) return;
-          tc_fence_after();
-          const uint64_t dv = sw128_desc(smem_u32(S.v[s]));
-          for (int kk = 0; kk < 8; ++kk)
-            tc_mma_ts(tmem + 256 + 128 * s, tmem + 128 * s + 8 * kk, dv + step(kk), idesc, i >= 2 || kk > 0);
-          tc_commit(smem_u32(&S.v_free[s]));
-        };
-        for (int i = 0; ok && i < seg.n; ++i) {
-          const int s = i & 1;
-          ok = mbar_wait(smem_u32(&S.k_full), nk++ & 1) && !*failed;
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t d = tmem + 128 * s;
-          constexpr uint64_t low = 2 * kPanel >> 4;
-          if (HILO)
-            for (int kk = 0; kk < 8; ++kk) tc_mma(d, dq + low + step(kk), dk + step(kk), idesc, kk > 0);
-          for (int kk = 0; kk < 8; ++kk) tc_mma(d, dq + step(kk), dk + low + step(kk), idesc, HILO || kk > 0);
-          for (int kk = 0; kk < 8; ++kk) tc_mma(d, dq + step(kk), dk + step(kk), idesc, 1);
-          tc_mma(d, dqx, dkx, idesc, 1);
-          tc_commit(smem_u32(&S.k_free));
-          tc_commit(smem_u32(&S.s_full[s]));
-          if (i) values(i - 1);
+        ok = mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
+        // S of tile i, then P V of the tile before
+#pragma unroll 1
+        for (int i = 0; ok && i <= seg.n; ++i) {
+          if (i < seg.n) {
+            const uint32_t n = n_tile + i, s = n & 1;
+            ok = mbar_wait_w(smem_u32(&S.k_full[s]), n >> 1 & 1) && !warp_failed(failed);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t d = tmem + 128 * s;
+              const uint64_t dk = sw128_desc(smem_u32(S.k[s]));
+              constexpr uint64_t low = 2 * kPanel >> 4;
+              if (HILO) product(d, tmem + kColQ + 64, dk, true);
+              product(d, tmem + kColQ, dk + low, !HILO);
+              product(d, tmem + kColQ, dk, false);
+              tc_mma(d, dqx, plain_desc(smem_u32(S.kx[s])), idesc, 1);
+              tc_commit(smem_u32(&S.k_free[s]));
+              tc_commit(smem_u32(&S.s_full[s]));
+            }
+            __syncwarp();
+          }
+          if (i) {
+            const uint32_t n = n_tile + i - 1, s = n & 1, use = n >> 1 & 1;
+            ok = mbar_wait_w(smem_u32(&S.p_full[s]), use) && mbar_wait_w(smem_u32(&S.v_full[s]), use);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              product(tmem + kColO, tmem + 128 * s, sw128_desc(smem_u32(S.v[s])), i == 1);
+              tc_commit(smem_u32(&S.v_free[s]));
+              if (i == seg.n) tc_commit(smem_u32(&S.o_full));
+            }
+            __syncwarp();
+          }
         }
-        if (ok) values(seg.n - 1);
-        if (ok) tc_commit(smem_u32(&S.o_full));
+        n_tile += seg.n;
         at += seg.n;
         if (at < w.hi) next_segment(a, seg, w.hi - at);
       }
       if (!ok) *failed = 1;
-      tc_commit(smem_u32(&S.drained));
-      mbar_wait(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
+      if (elect_one()) tc_commit(smem_u32(&S.drained));
+      __syncwarp();
+      mbar_wait_w(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
+    } else if (warp == kMmaWarp + 1) {
+      // ---- what the operands are made of, on its way into L2 some tiles ahead: a lane a sub-block
+      constexpr int kAhead = 4;
+      Segment ahead = seg;
+      int64_t to = w.lo;  // tiles asked for
+      uint32_t n_tile = 0;
+      auto ask = [&]() {
+        const int tok = ahead.t0 * kTile + 16 * lane;
+        if (lane < 8 && tok < ahead.tokens) {
+          const int page = page_of(v, ahead.lead, tok >> v.page_log);
+          if (page >= 0) {
+            const uint8_t* b = block_of(v, page, ahead.h) + (uint64_t)((tok & ((1 << v.page_log) - 1)) >> 4) * kSub;
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(b), "r"(kSub) : "memory");
+          }
+        }
+        ++to;
+        if (++ahead.t0, --ahead.n == 0 && to < w.hi) next_segment(a, ahead, w.hi - to);
+      };
+      while (to < w.hi && to < w.lo + kAhead) ask();
+      while (to < w.hi) {
+        if (!mbar_wait_w(smem_u32(&S.k_full[n_tile & 1]), n_tile >> 1 & 1) || warp_failed(failed)) break;
+        ++n_tile;
+        ask();
+      }
     }
-    __syncwarp();
   } else if (warp >= kSoftWarps) {
     // ---- operands of keys and values: a sub-block a warp
+    fewer_registers<88>();
     const int u = warp - kSoftWarps;
     const int token = lane & 15, half = lane >> 4;                       // keys: a token's dimensions 32 j + 8 t + i, t = 2 half ..
     const int g = lane & 7, p = lane >> 3 & 1, sd = lane >> 4;           // values: tokens 8 p .. + 7, dimensions 64 sd + 8 g ..
-    const uint32_t kx_at = smem_u32(S.kx) + extra_at(16 * u + token);
-    const uint32_t k_row = smem_u32(S.k) + (uint32_t)(16 * u + token) * 128;
+    const uint32_t kx_at = smem_u32(S.kx[0]) + extra_at(16 * u + token);
+    const uint32_t k_at = smem_u32(S.k[0]) + (uint32_t)(16 * u + token) * 128;
     const int v_chunk = 2 * (u & 3) + p;
-    struct Raw {
-      uint4 k[2];
-      uint2 kv[4];       // value words of tokens 2 t, 2 t + 1
-      uint32_t kw[2 * NG], vw[8];
-      bool there;        // false: behind the shared tokens; pages outside the pool have NaN parameters
-    };
+    uint4 kc[2];       // a key's codes, its parameters (and its value's)
+    uint32_t kw[2 * NG];
+    uint2 vc[4];       // value words of tokens 2 t, 2 t + 1; the parameters of eight tokens
+    uint32_t vw[8];
     auto page_at = [&](const Segment& s, int i) {  // page of the warp's sub-block of tile i: -1 outside the pool, -2 behind the end
       const int tok = (s.t0 + i) * kTile + 16 * u;
       return tok < s.tokens ? page_of(v, s.lead, tok >> v.page_log) : -2;
     };
-    auto load = [&](const Segment& s, int i, int page) {
-      Raw r;
-      r.there = page != -2;
-      const uint32_t none = r.there ? 0x7e007e00u : 0u;
+    auto place = [&](const Segment& s, int i, int page) {
+      return block_of(v, page, s.h) + (uint64_t)(((s.t0 + i) * kTile + 16 * u & ((1 << v.page_log) - 1)) >> 4) * kSub;
+    };
+    // Tokens behind the end are zeros, those of pages outside the pool have NaN parameters.
+    auto load_keys = [&](const Segment& s, int i, int page) {
       if (page >= 0) {
-        const int tok = (s.t0 + i) * kTile + 16 * u;
-        const uint8_t* b = block_of(v, page, s.h) + (uint64_t)((tok & ((1 << v.page_log) - 1)) >> 4) * kSub;
+        const uint8_t* b = place(s, i, page);
         const uint4* k = (const uint4*)(b + 64 * token + 32 * half);
-        r.k[0] = k[0], r.k[1] = k[1];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) r.kv[t] = *(const uint2*)(b + 1024 + 512 * p + 16 * (4 * g + t) + 8 * sd);
+        kc[0] = k[0], kc[1] = k[1];
         if (NG == 2) {
           const uint4 x = *(const uint4*)(b + 2048 + 16 * token);
-          r.kw[0] = x.x, r.kw[1] = x.y, r.kw[2 * NG - 2] = x.z, r.kw[2 * NG - 1] = x.w;
+          kw[0] = x.x, kw[1] = x.y, kw[2 * NG - 2] = x.z, kw[2 * NG - 1] = x.w;
         } else {
           const uint2 x = *(const uint2*)(b + 2048 + 8 * token);
-          r.kw[0] = x.x, r.kw[1] = x.y;
+          kw[0] = x.x, kw[1] = x.y;
         }
-#pragma unroll
-        for (int k8 = 0; k8 < 8; ++k8) r.vw[k8] = *(const uint32_t*)(b + 2048 + 8 * NG * (8 * p + k8) + 4 * NG + (NG == 2 ? 4 * sd : 0));
       } else {
-        r.k[0] = r.k[1] = make_uint4(0, 0, 0, 0);
+        kc[0] = kc[1] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) r.kv[t] = make_uint2(0, 0);
-#pragma unroll
-        for (int x = 0; x < 2 * NG; ++x) r.kw[x] = none;
-#pragma unroll
-        for (int k8 = 0; k8 < 8; ++k8) r.vw[k8] = none;
+        for (int x = 0; x < 2 * NG; ++x) kw[x] = page == -2 ? 0u : 0x7e007e00u;
       }
-      return r;
     };
-    const __half2 k1024 = __float2half2_rn(1024.f);
-    auto codes = [&](uint32_t x) { return __hsub2(as_half2((x & 0x000f000fu) | 0x64006400u), k1024); };
-    uint32_t nk = 0, nv[2] = {0, 0}, n_tile = 0;
+    auto load_values = [&](const Segment& s, int i, int page) {
+      if (page >= 0) {
+        const uint8_t* b = place(s, i, page);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) vc[t] = *(const uint2*)(b + 1024 + 512 * p + 16 * (4 * g + t) + 8 * sd);
+#pragma unroll
+        for (int k8 = 0; k8 < 8; ++k8) vw[k8] = *(const uint32_t*)(b + 2048 + 8 * NG * (8 * p + k8) + 4 * NG + (NG == 2 ? 4 * sd : 0));
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) vc[t] = make_uint2(0, 0);
+#pragma unroll
+        for (int k8 = 0; k8 < 8; ++k8) vw[k8] = 0;
+      }
+    };
+    // Nibbles e and e + 4 of x (e = 0 .. 3, y = x >> 8) as two fp16 numbers: 1024 + c less 1024, or (1024 + 16 c) / 16 less 64
+    const __half2 one024 = __float2half2_rn(1024.f), sixteenth = __float2half2_rn(0.0625f), minus64 = __float2half2_rn(-64.f);
+    auto codes = [&](uint32_t x, uint32_t y, int e) {
+      const uint32_t z = e < 2 ? x : y;
+      return e & 1 ? __hfma2(as_half2((z & 0x00f000f0u) | 0x64006400u), sixteenth, minus64)
+                   : __hsub2(as_half2((z & 0x000f000fu) | 0x64006400u), one024);
+    };
+    uint32_t n_tile = 0, nseg = 0;
     bool ok = true;
-    Raw next = load(seg, 0, page_at(seg, 0));
-    for (int64_t at = w.lo; ok && at < w.hi;) {
+    int page = page_at(seg, 0);
+    load_keys(seg, 0, page);
+    load_values(seg, 0, page);
+    for (int64_t at = w.lo; at < w.hi; ++nseg) {
       Segment after = seg;
-      if (at + seg.n < w.hi) next_segment(a, after, w.hi - at - seg.n);
-      int page = seg.n > 1 ? page_at(seg, 1) : page_at(after, 0);
-      for (int i = 0; i < seg.n; ++i, ++n_tile) {
-        const Raw r = next;
-        const int s = i & 1;
-        // what the next tile needs is under way while this one waits for its place
-        if (i + 1 < seg.n) {
-          next = load(seg, i + 1, page);
-          page = i + 2 < seg.n ? page_at(seg, i + 2) : page_at(after, 0);
-        } else if (at + seg.n < w.hi) {
-          next = load(after, 0, page);
-        }
+      const bool more = at + seg.n < w.hi;
+      if (more) next_segment(a, after, w.hi - at - seg.n);
+      page = seg.n > 1 ? page_at(seg, 1) : page_at(after, 0);
+      build_queries<NG, HILO>(a, S, seg, warp);
+      // (the queries were put together in a key operand's place)
+      ok = ok && mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
+#pragma unroll 1
+      for (int i = 0; ok && i < seg.n; ++i, ++n_tile) {
+        const uint32_t s = n_tile & 1, unused = (n_tile >> 1 & 1) ^ 1, k_row = k_at + s * (4 * kPanel);
         // the sub-block's size, and tokens with a NaN
         auto large = [](uint32_t x) { return (x & 0x7fffu) > 0x6800u || (x >> 16 & 0x7fffu) > 0x7800u; };  // 2048, 32768
         bool fine = true, is_large = false;
 #pragma unroll
         for (int x = 0; x < 2 * NG; ++x) {
-          fine = fine && finite_word(r.kw[x]);
-          is_large = is_large || (finite_word(r.kw[x]) && large(r.kw[x]));
+          fine = fine && finite_word(kw[x]);
+          is_large = is_large || (finite_word(kw[x]) && large(kw[x]));
         }
         const bool big = __any_sync(0xffffffffu, is_large);
+        const uint32_t all_fine = __ballot_sync(0xffffffffu, fine);
         const __half2 down = __float2half2_rn(big ? 0.03125f : 1.f);
         // keys
-        if (!mbar_wait_w(smem_u32(&S.k_free), (nk++ & 1) ^ 1) || warp_failed(failed)) {
+        if (!mbar_wait_w(smem_u32(&S.k_free[s]), unused) || warp_failed(failed)) {
           ok = false;
           break;
         }
         if (lane == 0) S.big[n_tile & 3][u] = big;
+        __half2 scale[NG];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t word = fine ? r.kw[NG == 2 ? j >> 1 : 0] : 0u;
-          const __half2 sc = __hmul2(__half2half2(__ushort_as_half((unsigned short)word)), down);
+        for (int x = 0; x < NG; ++x) scale[x] = __hmul2(__half2half2(__ushort_as_half((unsigned short)(fine ? kw[x] : 0u))), down);
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            const uint4& q4 = r.k[tt];
-            const uint32_t x = j == 0 ? q4.x : j == 1 ? q4.y : j == 2 ? q4.z : q4.w;
+        for (int tt = 0; tt < 2; ++tt) {
+          const uint32_t to_t = k_row + 16 * ((2 * half + tt) ^ (token & 7));  // (chunk 4 (j & 1) + t, its bit 2 turned by the row as well)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t x = j == 0 ? kc[tt].x : j == 1 ? kc[tt].y : j == 2 ? kc[tt].z : kc[tt].w, y = x >> 8;
+            const __half2 sc = scale[NG == 2 ? j >> 1 : 0];
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const __half2 c = codes(x >> (4 * e));
-              const __half2 y = __hmul2(c, sc);
-              hi[e] = bits(y);
-              lo[e] = bits(__hfma2(c, sc, __hneg2(y)));
+              const __half2 c = codes(x, y, e), z = __hmul2(c, sc);
+              hi[e] = bits(z);
+              lo[e] = bits(__hfma2(c, sc, __hneg2(z)));
             }
-            const int t = 2 * half + tt, chunk = ((j & 1) * 4 + t) ^ (token & 7);
-            const uint32_t to = k_row + (uint32_t)(j >> 1) * kPanel + 16 * chunk;
+            const uint32_t to = (to_t ^ (j & 1 ? 64u : 0u)) + (uint32_t)(j >> 1) * kPanel;
             sts128(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
             sts128(to + 2 * kPanel, make_uint4(lo[0], lo[1], lo[2], lo[3]));
           }
         }
         if (half == 0) {
-          const __half2 m0 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(fine ? r.kw[0] >> 16 : 0x7e00u))), down);
-          const __half2 m1 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(NG == 2 && fine ? r.kw[1] >> 16 : 0u))), down);
+          const __half2 m0 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(fine ? kw[0] >> 16 : 0x7e00u))), down);
+          const __half2 m1 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(NG == 2 && fine ? kw[1] >> 16 : 0u))), down);
           const uint32_t b0 = bits(m0), b1 = bits(m1);
-          sts128(kx_at, make_uint4(b0, (b0 & 0xffffu) | (b1 & 0xffff0000u), b1, 0));
+          sts128(kx_at + s * kExtra, make_uint4(b0, (b0 & 0xffffu) | (b1 & 0xffff0000u), b1, 0));
         }
         proxy_fence();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&S.k_full));
+        if (lane == 0) mbar_arrive(smem_u32(&S.k_full[s]));
+        // the next tile's keys are under way while the values are done, its values while its keys are
+        if (i + 1 < seg.n) load_keys(seg, i + 1, page);
+        else if (more) load_keys(after, 0, page);
         // values
-        if (!mbar_wait_w(smem_u32(&S.v_free[s]), (nv[s]++ & 1) ^ 1)) {
+        if (!mbar_wait_w(smem_u32(&S.v_free[s]), unused)) {
           ok = false;
           break;
         }
-        // a token with a NaN anywhere is a zero
-        const uint32_t all_fine = __ballot_sync(0xffffffffu, fine);
         __half2 sc[4], mn[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t w0 = all_fine >> (8 * p + 2 * t) & 1 ? r.vw[2 * t] : 0u, w1 = all_fine >> (8 * p + 2 * t + 1) & 1 ? r.vw[2 * t + 1] : 0u;
+        for (int t = 0; t < 4; ++t) {  // (a token with a NaN anywhere is a zero)
+          const uint32_t w0 = all_fine >> (8 * p + 2 * t) & 1 ? vw[2 * t] : 0u, w1 = all_fine >> (8 * p + 2 * t + 1) & 1 ? vw[2 * t + 1] : 0u;
           sc[t] = __hmul2(as_half2(__byte_perm(w0, w1, 0x5410)), down);
           mn[t] = __hmul2(as_half2(__byte_perm(w0, w1, 0x7632)), down);
         }
+        // dimension 64 sd + 8 g + 4 uu + n is operand row 64 sd + 8 (4 uu + n) + g: eight lanes write eight places
+        const uint32_t v_to = smem_u32(S.v[s]) + (uint32_t)(u >> 2) * kPanel + 128 * (64 * sd + g) + 16 * (v_chunk ^ g);
 #pragma unroll
-        for (int uu = 0; uu < 2; ++uu)
+        for (int uu = 0; uu < 2; ++uu) {
+          uint32_t x[4], y[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) x[t] = uu ? vc[t].y : vc[t].x, y[t] = x[t] >> 8;
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
-            uint32_t y[4];
+            // (nibbles n and n + 4 are the two tokens)
+            uint32_t z[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) y[t] = bits(__hfma2(codes((uu ? r.kv[t].y : r.kv[t].x) >> (4 * n)), sc[t], mn[t]));
-            // dimension 64 sd + 8 g + 4 uu + n is operand row 64 sd + 8 (4 uu + n) + g: eight lanes write eight places
-            const int row = 64 * sd + 8 * (4 * uu + n) + g;
-            sts128(smem_u32(S.v[s]) + (uint32_t)(u >> 2) * kPanel + 128 * row + 16 * (v_chunk ^ g), make_uint4(y[0], y[1], y[2], y[3]));
+            for (int t = 0; t < 4; ++t) z[t] = bits(__hfma2(codes(x[t], y[t], n), sc[t], mn[t]));
+            sts128(v_to + 1024 * (4 * uu + n), make_uint4(z[0], z[1], z[2], z[3]));
           }
+        }
         proxy_fence();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&S.v_full[s]));
+        if (i + 1 < seg.n) {
+          load_values(seg, i + 1, page);
+          page = i + 2 < seg.n ? page_at(seg, i + 2) : page_at(after, 0);
+        } else if (more) {
+          load_values(after, 0, page);
+        }
       }
       at += seg.n;
       seg = after;
@@ -452,152 +624,155 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     if (!ok) *failed = 1;
   } else {
     // ---- softmax: a thread a query row, the tiles of parity s
-    const int s = warp >> 2, row = tid & 127;
-    const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16, tS = tmem + lane_at + 128 * s, tO = tmem + lane_at + 256;
-    const float sign = a.scale < 0.f ? -1.f : 1.f;
-    const int tg = a.T * v.G;
-    uint32_t ns = 0, nseg = 0, n_tile = 0;
+    more_registers<120>();
+    const int half = warp >> 2, quarter = warp & 3, row = tid & 127;
+    const uint32_t lane_at = tmem + ((uint32_t)(quarter * 32) << 16);
+    uint32_t nseg = 0, n_tile = 0, n_ref = 0;  // n_ref: references that came from the other thread
     for (int64_t at = w.lo; at < w.hi; ++nseg) {
-      // the unit's queries as operands: a warp a row
-      for (int rr = warp; rr < kRows; rr += kSoftWarps) {
-        const int64_t qi = (int64_t)seg.block * kRows + rr;
-        const int k = seg.k0 + (int)(qi / tg), t = (int)(qi % tg) / v.G, gq = (int)(qi % tg) % v.G;
-        const int b = k < seg.k0 + seg.size ? row_in_order(a, k) : -1;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        if (b >= 0) {
-          const uint16_t* from = a.q + b * a.qb + t * a.qt + (int64_t)(seg.h * v.G + gq) * a.qh + 4 * lane;
+      if (half == 0) S.ref[row] = kLow;
+      build_queries<NG, HILO>(a, S, seg, warp);
+      // a thread takes its row's high or low halves into tensor memory
+      if (half == 0 || HILO)
+#pragma unroll 1
+        for (int p = 0; p < 2; ++p) {
+          float x[32];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = sign * row_to_float(from[e], v.half);
-        }
-        if (HILO) {  // q' = H (s o q) / 16
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign_flip(v, 4 * lane + e));
-          wht_32x4(x, lane);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
-        }
-        float big = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = fabsf(x[e]);
-          if (y <= 3.402823466e38f) big = fmaxf(big, y);  // an infinite or NaN row spoils itself alone
-        }
-        big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-        // a row times 2^(7 - e): below 2^7 (its sums below 2^14), exact in fp16 down to 2^-23 of that
-        const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
-        const float up = pow2(7 - e2);
-        float sum = (x[0] + x[1]) + (x[2] + x[3]);
-#pragma unroll
-        for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        const float s0 = __shfl_sync(0xffffffffu, sum, 0) * up, s1 = __shfl_sync(0xffffffffu, sum, 16) * up;
-        uint4 f[2];
-#pragma unroll
-        for (int lo = 0; lo < 2; ++lo) {
-          uint32_t y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float z = x[e] * up, hi = __half2float(__float2half_rn(z)), mine = lo ? z - hi : z;
-            const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
-            y[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
+          for (int c = 0; c < 8; ++c) {
+            const float4 y = *(const float4*)(S.k[0] + (2 * half + p) * kPanel + 128 * row + 16 * (c ^ (row & 7)));
+            x[4 * c] = y.x, x[4 * c + 1] = y.y, x[4 * c + 2] = y.z, x[4 * c + 3] = y.w;
           }
-          f[lo] = make_uint4(y[0], y[1], y[2], y[3]);
+          tm_st32(lane_at + kColQ + 64 * half + 32 * p, x);
         }
-        // lanes 2 x, 2 x + 1 hold dimensions 8 x .. of word j = x / 4, t = x % 4
-        const int j = lane >> 3, chunk = ((j & 1) * 4 + (lane >> 1 & 3)) ^ (rr & 7);
-        const uint32_t to = smem_u32(S.q) + (uint32_t)(j >> 1) * kPanel + 128 * rr + 16 * chunk;
-        if (!(lane & 1)) sts128(to, f[0]);
-        if (HILO && (lane & 1)) sts128(to + 2 * kPanel, f[1]);
-        if (lane == 0) {
-          auto parts = [](float z, float (&y)[3]) {
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-              y[i] = __half2float(__float2half_rn(z));
-              z -= y[i];
-            }
-          };
-          float y0[3], y1[3] = {0.f, 0.f, 0.f};
-          parts(s0, y0);
-          if (NG == 2) parts(s1, y1);
-          sts128(smem_u32(S.qx) + extra_at(rr), make_uint4(half2_bits(y0[0], y0[1]), half2_bits(y0[2], y1[0]), half2_bits(y1[1], y1[2]), 0));
-          S.row_scale[rr] = fabsf(a.scale) * pow2(e2 - 7);
-          S.lim[rr] = b >= 0 ? min(seg.tokens, held_tokens(v, b) - a.T + 1 + t) : 0;
-          S.row_at[rr] = b >= 0 ? ((int64_t)b * a.T + t) * (v.H * v.G) + seg.h * v.G + gq : -1;
-        }
-      }
+      tm_wait_st();
+      tc_fence_before();
       proxy_fence();
       __syncwarp();
-      named_sync(1, 32 * kSoftWarps);
       if (lane == 0) mbar_arrive(smem_u32(&S.q_full));
 
+
+      const bool idle = __all_sync(0xffffffffu, S.row_at[row] < 0);  // (what P holds in these rows stays in them)
       const float row_scale = S.row_scale[row];
       const int lim = S.lim[row] - seg.t0 * kTile;  // from the segment's first token
-      float ref = kLow, sum[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int i = s; i < seg.n; i += 2) {
-        if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[s]), ns++ & 1)) {
+      float ref = kLow;
+      float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+      for (int i = (n_tile ^ half) & 1; i < seg.n; i += 2) {
+        const uint32_t n = n_tile + i, s = half, tS = lane_at + 128 * s;
+        if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[s]), n >> 1 & 1)) {
           *failed = 1;
           break;
         }
+        if (idle) {
+          if (lane == 0) mbar_arrive(smem_u32(&S.p_full[s]));
+          continue;
+        }
         tc_fence_after();
         const int sees = lim - i * kTile;
-        const uint64_t big = *(const volatile uint64_t*)&S.big[(n_tile + i) & 3][0];
-        const bool whole = __all_sync(0xffffffffu, sees >= kTile);
+        const uint64_t big = *(const volatile uint64_t*)&S.big[n & 3][0];
+        // tiles that every row sees whole, without large sub-blocks, are what there is most of
+        const bool plain = __all_sync(0xffffffffu, sees >= kTile && big == 0);
         // the largest logit
         float most = kNegInf;
+        if (plain) {
+          float m4[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float x[32];
+            tm_ld32(tS + 32 * c, x);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float x[32];
-          tm_ld32(tS + 32 * c, x);
-          float m2[2] = {kNegInf, kNegInf};
-          if (whole) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) m2[e >> 4] = max3(m2[e >> 4], x[e], x[e + 1]);
-          } else {
+            for (int e = 0; e < 32; e += 2) m4[e >> 1 & 3] = max3(m4[e >> 1 & 3], x[e], x[e + 1]);
+          }
+          most = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float x[32], m2[2] = {kNegInf, kNegInf};
+            tm_ld32(tS + 32 * c, x);
 #pragma unroll
             for (int e = 0; e < 32; ++e) m2[e >> 4] = fmaxf(m2[e >> 4], 32 * c + e < sees ? x[e] : kNegInf);
-          }
 #pragma unroll
-          for (int y = 0; y < 2; ++y) most = fmaxf(most, big >> (8 * (2 * c + y)) & 1 ? 32.f * m2[y] : m2[y]);
+            for (int y = 0; y < 2; ++y) most = fmaxf(most, big >> (8 * (2 * c + y)) & 1 ? 32.f * m2[y] : m2[y]);
+          }
         }
         most *= row_scale;
+        // the reference, as the tile before left it
+        if (i) {
+          if (!mbar_wait_w(smem_u32(&S.ref_at[s][quarter]), n_ref++ & 1)) {
+            *failed = 1;
+            break;
+          }
+          const float now = *(volatile float*)&S.ref[row], f = exp2_fast(ref - now);
+          if (__any_sync(0xffffffffu, now != ref)) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) sum[e].x *= f, sum[e].y *= f;
+            ref = now;
+          }
+        }
         const bool up = most - ref > kSlack;  // (a row that sees nothing here sees nothing later)
         if (__any_sync(0xffffffffu, up)) {
           const float to = up ? most : ref, f = up ? exp2_fast(ref - to) : 1.f;
           ref = to;
+          *(volatile float*)&S.ref[row] = ref;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum[e] *= f;
-          if (i >= 2) {  // (S of this tile is behind O of the one before in the order of the products)
+          for (int e = 0; e < 2; ++e) sum[e].x *= f, sum[e].y *= f;
+          if (i) {  // O, once the tile before is in it
+            if (!mbar_wait_w(smem_u32(&S.v_free[s ^ 1]), (n - 1) >> 1 & 1)) {
+              *failed = 1;
+              break;
+            }
+            tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
               float x[32];
-              tm_ld32(tO + 128 * s + 32 * c, x);
+              tm_ld32(lane_at + kColO + 32 * c, x);
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] *= f;
-              tm_st32(tO + 128 * s + 32 * c, x);
+              tm_st32(lane_at + kColO + 32 * c, x);
             }
             tm_wait_st();
           }
         }
+        __syncwarp();
+        if (lane == 0 && i + 1 < seg.n) mbar_arrive(smem_u32(&S.ref_at[s ^ 1][quarter]));
         const float shift = kPlace - ref;
+        if (plain) {
+          const float2 sc = make_float2(row_scale, row_scale), sh = make_float2(shift, shift);
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float x[32];
+            tm_ld32(tS + 32 * c, x);
+            uint32_t pk[16];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float x[32];
-          tm_ld32(tS + 32 * c, x);
-          uint32_t pk[16];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const bool b = big >> (8 * (2 * c + y)) & 1;
-            const float sc = b ? 32.f * row_scale : row_scale;
-#pragma unroll
-            for (int e = 16 * y; e < 16 * y + 16; ++e) {
-              x[e] = exp2_fast(fmaf(x[e], sc, shift));
-              if (!whole && 32 * c + e >= sees) x[e] = 0.f;
-              sum[e & 3] += x[e];
-              if (b) x[e] *= 32.f;
+            for (int e = 0; e < 16; ++e) {
+              float2 y = __ffma2_rn(make_float2(x[2 * e], x[2 * e + 1]), sc, sh);
+              y.x = exp2_fast(y.x), y.y = exp2_fast(y.y);
+              sum[e & 1] = __fadd2_rn(sum[e & 1], y);
+              pk[e] = half2_bits(y.x, y.y);
             }
+            tm_st16(tS + 16 * c, pk);
           }
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            float x[32];
+            tm_ld32(tS + 32 * c, x);
+            uint32_t pk[16];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) pk[e] = half2_bits(x[2 * e], x[2 * e + 1]);
-          tm_st16(tS + 16 * c, pk);
+            for (int y = 0; y < 2; ++y) {
+              const bool b = big >> (8 * (2 * c + y)) & 1;
+              const float sc = b ? 32.f * row_scale : row_scale;
+#pragma unroll
+              for (int e = 16 * y; e < 16 * y + 16; ++e) {
+                x[e] = 32 * c + e < sees ? exp2_fast(fmaf(x[e], sc, shift)) : 0.f;
+                if (e & 1) sum[e >> 1 & 1].y += x[e];
+                else sum[e >> 1 & 1].x += x[e];
+                if (b) x[e] *= 32.f;
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) pk[e] = half2_bits(x[2 * e], x[2 * e + 1]);
+            tm_st16(tS + 16 * c, pk);
+          }
         }
         tm_wait_st();
         tc_fence_before();
@@ -605,34 +780,31 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
         if (lane == 0) mbar_arrive(smem_u32(&S.p_full[s]));
       }
       n_tile += seg.n;
-      // ---- the segment's end: both sums together, each half of the threads takes half of the columns
-      S.ref[s][row] = ref;
-      S.sum[s][row] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      // ---- the segment's end: each half of the threads takes half of the columns
       const bool done = !warp_failed(failed) && mbar_wait_w(smem_u32(&S.o_full), nseg & 1);
       if (!done) *failed = 1;
+      named_sync(1, 32 * kSoftWarps);  // (the last reference is there)
+      const float m = S.ref[row];
+      S.sum[half][row] = exp2_fast(ref - m) * ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
       named_sync(1, 32 * kSoftWarps);
       tc_fence_after();
-      const float r0 = S.ref[0][row], r1 = S.ref[1][row], m = fmaxf(r0, r1);
-      const float f0 = exp2_fast(r0 - m), f1 = exp2_fast(r1 - m);
       const bool whole = seg.t0 == 0 && seg.n == seg.tiles;
       const int64_t out_row = S.row_at[row];
       float* to = whole ? a.part + (out_row < 0 ? 0 : out_row) * kPartFloats
                         : a.slots + ((size_t)(2 * blockIdx.x + (seg.t0 == 0)) * kRows + row) * kPartFloats;
+      if (!idle)
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          float x[32];
+          tm_ld32(lane_at + kColO + 64 * half + 32 * c, x);
+          if (out_row >= 0) {
+            // operand column 32 (2 half + c) + 8 n + g is dimension 64 half + 8 g + 4 c + n
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float x[32], y[32];
-        tm_ld32(tO + 64 * s + 32 * c, x);
-        if (seg.n > 1) tm_ld32(tO + 128 + 64 * s + 32 * c, y);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = seg.n > 1 ? f0 * x[e] + f1 * y[e] : x[e];
-        if (out_row >= 0) {
-          // operand column 32 (2 s + c) + 8 n + g is dimension 64 s + 8 g + 4 c + n
-#pragma unroll
-          for (int gg = 0; gg < 8; ++gg) *(float4*)(to + 64 * s + 8 * gg + 4 * c) = make_float4(x[gg], x[8 + gg], x[16 + gg], x[24 + gg]);
+            for (int gg = 0; gg < 8; ++gg) *(float4*)(to + 64 * half + 8 * gg + 4 * c) = make_float4(x[gg], x[8 + gg], x[16 + gg], x[24 + gg]);
+          }
         }
-      }
-      if (s == 0 && out_row >= 0) {
-        const float l = f0 * S.sum[0][row] + f1 * S.sum[1][row];
+      if (half == 0 && out_row >= 0) {
+        const float l = S.sum[0][row] + S.sum[1][row];
         to[kD] = l == 0.f ? kLow : m - kPlace;
         to[kD + 1] = done ? l : __int_as_float(0x7fffffff);
         if (seg.t0 == 0) {
@@ -642,7 +814,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
         }
       }
       tc_fence_before();
-      named_sync(1, 32 * kSoftWarps);  // (what was read is the next segment's)
       at += seg.n;
       if (at < w.hi) next_segment(a, seg, w.hi - at);
     }
@@ -802,6 +973,7 @@ int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& o
   a.slots = (float*)(base + w.slots);
   a.scale = (float)((double)sm_scale * 1.4426950408889634);
   a.T = T;
+  a.aligned = (uintptr_t)q.ptr % 8 == 0 && q.stride_b % 4 == 0 && q.stride_t % 4 == 0 && q.stride_h % 4 == 0;
   if (v.rotate) err = v.ng == 2 ? launch<2, true>(a, dev, sms, stream) : launch<1, true>(a, dev, sms, stream);
   else err = v.ng == 2 ? launch<2, false>(a, dev, sms, stream) : launch<1, false>(a, dev, sms, stream);
   if (err) return err;
