@@ -709,7 +709,7 @@ akv_status akv_pages_share(const akv_paged_params* p, const akv_pages* pages, co
  * queries (as one matrix product), every row's further tokens as akv_paged_attn reads them, and both parts are joined in one
  * softmax.  Numbers in `share` that are out of range are left out (rows outside the table) or clamped (pages).
  *   In the shared part a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
- * m + c a to fp16 as well (2^-11 of it; where a tile of 128 tokens has a scale above 2048, at most 2^-20).  A query that sees a token
+ * m + c a to fp16 as well (2^-11 of it; where 16 tokens have a scale above 2048 or a minimum beyond 16384, 2^-20 at least).  A query that sees a token
  * with an infinity or a NaN has NaN in all its outputs. */
 akv_status akv_paged_attn_shared_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
                                                 size_t* ws_bytes);

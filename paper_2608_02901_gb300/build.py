@@ -48,7 +48,7 @@ def _compile(src: str, extra: list, verbose: bool) -> str:
     obj = os.path.join(BUILD, src + ".o")
     path = os.path.join(CSRC, src)
     deps = [path, os.path.join(ROOT, "include", "akv.h")]
-    deps += [os.path.join(CSRC, h) for h in ("akv_internal.h", "akv_device.cuh", "akv_decode.cuh", "akv_paged.cuh")]
+    deps += [os.path.join(CSRC, h) for h in ("akv_internal.h", "akv_device.cuh", "akv_decode.cuh", "akv_paged.cuh", "akv_paged_tc.cuh")]
     if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
         return obj
     cmd = [_nvcc(), *ARCH, *COMMON, *extra, "-c", path, "-o", obj]

@@ -3,10 +3,10 @@
 //
 // A unit is a group's KV head and up to 128 of its query rows (members x query tokens x query heads); units are cut into tiles of
 // 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA, one CTA an SM.  In a CTA
-//   8 warps turn codes into operands, a sub-block of 16 tokens each: keys as c a in two fp16 halves (hi = fp16(c a), lo = the exact rest),
+//   8 warps turn codes into operands, a sub-block of 16 tokens each: keys as (2 c - 15) a in two fp16 halves (the second the exact rest),
 //     values as fp16(m + c a),
-//   1 warp issues the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry m sum(q), so that a logit comes out
-//     whole, then O += P V; Q and P come out of tensor memory, so that a product reads 4 KiB of shared memory and not 8.  (The warp goes
+//   1 warp issues the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry (2 m + 15 a) sum(q), so that a logit comes out
+//     whole (doubled), then O += P V; Q and P come out of tensor memory, so that a product reads 4 KiB of shared memory and not 8.  (The warp goes
 //     through its loop as one and elects the issuing thread at each batch: descriptors then are sums in uniform registers.  Out of a
 //     loop of one thread a product took 94 to 107 cycles, where the tensor cores need 64 for 128 x 128 x 16.)
 //   2 x 4 warps take the tiles in turn, a thread per query row: p = 2^(S scale - reference), its sum, P as fp16 over S's columns.
@@ -15,7 +15,7 @@
 // or, rotated, as a high and a low one.  The scales of tokens could not be applied behind the products instead: a thread that owns a row would
 // read four numbers a token from shared memory, 512 bytes a warp, four times what the tensor cores need for the extra products.
 //   A reference moves when a weight would pass 2^kSlack times it; a weight counts 2^kPlace in P, so that fp16 keeps 2^-11 of those
-// down to 2^-19 of the reference's.  Sub-blocks with a scale above 2048 or a minimum beyond 32768 enter as 2^-5 of themselves (their
+// down to 2^-19 of the reference's.  Sub-blocks with a scale above 2048 or a minimum beyond 16384 enter as 2^-5 of themselves (their
 // columns of S count 32, their P is 32 times as large).  Tokens with a NaN enter as values of 0 and a NaN in S: rows that do not see
 // them do not feel them.
 //   Loops over a row's columns are not unrolled beyond 32: a call's first tile waits for its instructions.
@@ -25,15 +25,15 @@
 
 #include "akv_device.cuh"
 #include "akv_paged.cuh"
+#include "akv_paged_tc.cuh"
 
 namespace akv {
 namespace {
 
 constexpr int kRows = 128, kTile = 128;
 constexpr int kSoftWarps = 8, kUnpackWarps = 8, kMmaWarp = kSoftWarps + kUnpackWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 4);  // (whole warpgroups, which share registers out: three warps are idle)
-constexpr uint32_t kPanel = 128 * 128;    // bytes of 64 of an operand's K for 128 of its rows
-constexpr uint32_t kExtra = 128 * 32;     // 16 of K
+// Whole warpgroups, which share registers out (three warps are idle): 20 warps of 96 at the launch, then 8 x 120 + 8 x 88 + 4 x 64.
+constexpr int kThreads = 32 * (kMmaWarp + 4);
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -3.402823466e38f;  // reference of a row that saw no token: below all others
 constexpr float kSlack = 5.f, kPlace = 5.f;
@@ -67,75 +67,6 @@ struct Smem {
   uint32_t tmem;
   int failed;
 };
-
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // -126 .. 127
-__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<const __half2*>(&x); }
-__device__ __forceinline__ uint32_t bits(__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
-__device__ __forceinline__ bool finite_word(uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; }
-__device__ __forceinline__ void sts128(uint32_t a, uint4 x) {
-  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
-}
-// Registers of a warpgroup's threads; a launch has 20 warps of 96: 8 x 120 + 8 x 88 + 4 x 64 are 20 x 96.
-template <int N>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// One lane of the warp, the same each time.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t on;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(on));
-  return on != 0;
-}
-__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// 32 columns of the thread's lane of tensor memory
-__device__ __forceinline__ void tm_ld32(uint32_t at, float (&v)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-      " tcgen05.wait::ld.sync.aligned;"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
-      : "r"(at)
-      : "memory");
-}
-__device__ __forceinline__ void tm_st32(uint32_t at, const float (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
-      : "memory");
-}
-__device__ __forceinline__ void tm_st16(uint32_t at, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
-__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// D[tmem] (+)= A[tmem] B[smem]^T
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, uint32_t acc) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-      ::"r"(d), "r"(a), "l"(b_desc), "r"(idesc), "r"(acc)
-      : "memory");
-}
-// Operand of 16 K without swizzle: [2][16][8 rows][16 bytes], 2048 bytes from one half of K to the other, 128 between groups of rows.
-__device__ __forceinline__ uint64_t plain_desc(uint32_t saddr) {
-  return (uint64_t)((saddr >> 4) & 0x3FFFu) | ((uint64_t)(2048u >> 4) << 16) | ((uint64_t)(128u >> 4) << 32) | ((uint64_t)1u << 46);
-}
-__device__ __forceinline__ uint32_t extra_at(int row) { return (uint32_t)((row >> 3) * 128 + (row & 7) * 16); }
 
 // A unit's share of a CTA: tiles t0 .. t0 + n - 1.
 struct Segment {
@@ -276,51 +207,8 @@ __device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, cons
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
     }
-    float big = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float y = fabsf(x[e]);
-      if (y <= 3.402823466e38f) big = fmaxf(big, y);  // an infinite or NaN row spoils itself alone
-    }
-    big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-    // a row times 2^(7 - e): below 2^7 (its sums below 2^14), exact in fp16 down to 2^-23 of that
-    const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
-    const float up = pow2(7 - e2);
-    float sum = (x[0] + x[1]) + (x[2] + x[3]);
-#pragma unroll
-    for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-    uint4 f[HILO ? 2 : 1];
-#pragma unroll
-    for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
-      uint32_t y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float z = x[e] * up, hi = __half2float(__float2half_rn(z)), mine = lo ? z - hi : z;
-        const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
-        y[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
-      }
-      f[lo] = make_uint4(y[0], y[1], y[2], y[3]);
-    }
-    // lanes 2 x, 2 x + 1 hold dimensions 8 x .. of word j = x / 4, t = x % 4
-    const int j = lane >> 3, chunk = ((j & 1) * 4 + (lane >> 1 & 3)) ^ (rr & 7);
-    const uint32_t to = smem_u32(S.k[0]) + (uint32_t)(j >> 1) * kPanel + 128 * rr + 16 * chunk;
-    if (!(lane & 1)) sts128(to, f[0]);
-    if (HILO && (lane & 1)) sts128(to + 2 * kPanel, f[HILO ? 1 : 0]);
-    // the sums of each group, in three halves (lanes 0 and 16)
-    if ((lane & 15) == 0) {
-      float z = lane == 0 || NG == 2 ? sum * up : 0.f;
-      uint16_t y[3];
-#pragma unroll
-      for (int i = 0; i < 3; ++i) {
-        const __half p = __float2half_rn(z);
-        y[i] = __half_as_ushort(p);
-        z -= __half2float(p);
-      }
-      uint16_t* x8 = (uint16_t*)(S.qx + extra_at(rr)) + (lane ? 3 : 0);
-      x8[0] = y[0], x8[1] = y[1], x8[2] = y[2];
-      if (lane) x8[3] = x8[4] = 0;
-      else S.row_scale[rr] = fabsf(a.scale) * pow2(e2 - 7);
-    }
+    const int up = query_row<NG, HILO>(x, lane, rr, smem_u32(S.k[0]), S.qx);
+    if (lane == 0) S.row_scale[rr] = 0.5f * fabsf(a.scale) * pow2(-up);  // (keys enter twice as large)
   }
   named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
 }
@@ -351,11 +239,9 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // the second eight of the sixteen extra dimensions are zeros
+  // what the sixteen extra dimensions do not use is zeros
   if (tid < 128) {
     sts128(smem_u32(S.qx) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
-    sts128(smem_u32(S.kx[0]) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
-    sts128(smem_u32(S.kx[1]) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
     proxy_fence();
   }
   Segment seg;
@@ -428,30 +314,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       if (elect_one()) tc_commit(smem_u32(&S.drained));
       __syncwarp();
       mbar_wait_w(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
-    } else if (warp == kMmaWarp + 1) {
-      // ---- what the operands are made of, on its way into L2 some tiles ahead: a lane a sub-block
-      constexpr int kAhead = 4;
-      Segment ahead = seg;
-      int64_t to = w.lo;  // tiles asked for
-      uint32_t n_tile = 0;
-      auto ask = [&]() {
-        const int tok = ahead.t0 * kTile + 16 * lane;
-        if (lane < 8 && tok < ahead.tokens) {
-          const int page = page_of(v, ahead.lead, tok >> v.page_log);
-          if (page >= 0) {
-            const uint8_t* b = block_of(v, page, ahead.h) + (uint64_t)((tok & ((1 << v.page_log) - 1)) >> 4) * kSub;
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(b), "r"(kSub) : "memory");
-          }
-        }
-        ++to;
-        if (++ahead.t0, --ahead.n == 0 && to < w.hi) next_segment(a, ahead, w.hi - to);
-      };
-      while (to < w.hi && to < w.lo + kAhead) ask();
-      while (to < w.hi) {
-        if (!mbar_wait_w(smem_u32(&S.k_full[n_tile & 1]), n_tile >> 1 & 1) || warp_failed(failed)) break;
-        ++n_tile;
-        ask();
-      }
     }
   } else if (warp >= kSoftWarps) {
     // ---- operands of keys and values: a sub-block a warp
@@ -466,16 +328,16 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     uint32_t kw[2 * NG];
     uint2 vc[4];       // value words of tokens 2 t, 2 t + 1; the parameters of eight tokens
     uint32_t vw[8];
-    auto page_at = [&](const Segment& s, int i) {  // page of the warp's sub-block of tile i: -1 outside the pool, -2 behind the end
+    auto page_at = [&](const Segment& s, int i) {  // page of the warp's sub-block of tile i as the table says (looked at when it is used)
       const int tok = (s.t0 + i) * kTile + 16 * u;
-      return tok < s.tokens ? page_of(v, s.lead, tok >> v.page_log) : -2;
+      return tok < s.tokens ? v.table[(int64_t)s.lead * v.table_stride + (tok >> v.page_log)] : INT32_MIN;
     };
     auto place = [&](const Segment& s, int i, int page) {
       return block_of(v, page, s.h) + (uint64_t)(((s.t0 + i) * kTile + 16 * u & ((1 << v.page_log) - 1)) >> 4) * kSub;
     };
     // Tokens behind the end are zeros, those of pages outside the pool have NaN parameters.
     auto load_keys = [&](const Segment& s, int i, int page) {
-      if (page >= 0) {
+      if ((uint32_t)page < (uint32_t)v.n_pages) {
         const uint8_t* b = place(s, i, page);
         const uint4* k = (const uint4*)(b + 64 * token + 32 * half);
         kc[0] = k[0], kc[1] = k[1];
@@ -489,11 +351,11 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       } else {
         kc[0] = kc[1] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int x = 0; x < 2 * NG; ++x) kw[x] = page == -2 ? 0u : 0x7e007e00u;
+        for (int x = 0; x < 2 * NG; ++x) kw[x] = (s.t0 + i) * kTile + 16 * u >= s.tokens ? 0u : 0x7e007e00u;
       }
     };
     auto load_values = [&](const Segment& s, int i, int page) {
-      if (page >= 0) {
+      if ((uint32_t)page < (uint32_t)v.n_pages) {
         const uint8_t* b = place(s, i, page);
 #pragma unroll
         for (int t = 0; t < 4; ++t) vc[t] = *(const uint2*)(b + 1024 + 512 * p + 16 * (4 * g + t) + 8 * sd);
@@ -506,12 +368,15 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
         for (int k8 = 0; k8 < 8; ++k8) vw[k8] = 0;
       }
     };
-    // Nibbles e and e + 4 of x (e = 0 .. 3, y = x >> 8) as two fp16 numbers: 1024 + c less 1024, or (1024 + 16 c) / 16 less 64
-    const __half2 one024 = __float2half2_rn(1024.f), sixteenth = __float2half2_rn(0.0625f), minus64 = __float2half2_rn(-64.f);
-    auto codes = [&](uint32_t x, uint32_t y, int e) {
-      const uint32_t z = e < 2 ? x : y;
-      return e & 1 ? __hfma2(as_half2((z & 0x00f000f0u) | 0x64006400u), sixteenth, minus64)
-                   : __hsub2(as_half2((z & 0x000f000fu) | 0x64006400u), one024);
+    const KeyCodes key_codes;
+    const ValueCodes value_codes;
+    // Tiles further ahead are on their way into L2.
+    constexpr int kAhead = 4;
+    int far = INT32_MIN;  // page of the tile kAhead on
+    auto ask = [&](int i) {
+      if (lane == 0 && (uint32_t)far < (uint32_t)v.n_pages)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(place(seg, i, far)), "r"(kSub) : "memory");
+      far = i + 1 < seg.n ? page_at(seg, i + 1) : INT32_MIN;
     };
     uint32_t n_tile = 0, nseg = 0;
     bool ok = true;
@@ -526,20 +391,21 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       build_queries<NG, HILO>(a, S, seg, warp);
       // (the queries were put together in a key operand's place)
       ok = ok && mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
+      far = seg.n > 2 ? page_at(seg, 2) : INT32_MIN;
+#pragma unroll 1
+      for (int i = 2; i < kAhead; ++i) ask(i);
 #pragma unroll 1
       for (int i = 0; ok && i < seg.n; ++i, ++n_tile) {
         const uint32_t s = n_tile & 1, unused = (n_tile >> 1 & 1) ^ 1, k_row = k_at + s * (4 * kPanel);
-        // the sub-block's size, and tokens with a NaN
-        auto large = [](uint32_t x) { return (x & 0x7fffu) > 0x6800u || (x >> 16 & 0x7fffu) > 0x7800u; };  // 2048, 32768
-        bool fine = true, is_large = false;
+        // the sub-block's size (scales beyond 2048, minima beyond 16384), and tokens with an infinity or a NaN
+        uint32_t most = kw[0] & 0x7fff7fffu;
 #pragma unroll
-        for (int x = 0; x < 2 * NG; ++x) {
-          fine = fine && finite_word(kw[x]);
-          is_large = is_large || (finite_word(kw[x]) && large(kw[x]));
-        }
-        const bool big = __any_sync(0xffffffffu, is_large);
+        for (int x = 1; x < 2 * NG; ++x) most = bits(__hmax2_nan(as_half2(most), as_half2(kw[x] & 0x7fff7fffu)));
+        const bool fine = (most & 0xffffu) < 0x7c00u && most < 0x7c000000u;
+        const bool big = __any_sync(0xffffffffu, fine && ((most & 0xffffu) > 0x6800u || most > 0x7400ffffu));
         const uint32_t all_fine = __ballot_sync(0xffffffffu, fine);
-        const __half2 down = __float2half2_rn(big ? 0.03125f : 1.f);
+        const float down1 = big ? kLargeDown : 1.f;
+        const __half2 down = __float2half2_rn(down1);
         // keys
         if (!mbar_wait_w(smem_u32(&S.k_free[s]), unused) || warp_failed(failed)) {
           ok = false;
@@ -554,29 +420,26 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
           const uint32_t to_t = k_row + 16 * ((2 * half + tt) ^ (token & 7));  // (chunk 4 (j & 1) + t, its bit 2 turned by the row as well)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t x = j == 0 ? kc[tt].x : j == 1 ? kc[tt].y : j == 2 ? kc[tt].z : kc[tt].w, y = x >> 8;
-            const __half2 sc = scale[NG == 2 ? j >> 1 : 0];
             uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const __half2 c = codes(x, y, e), z = __hmul2(c, sc);
-              hi[e] = bits(z);
-              lo[e] = bits(__hfma2(c, sc, __hneg2(z)));
-            }
+            key_word(key_codes, j == 0 ? kc[tt].x : j == 1 ? kc[tt].y : j == 2 ? kc[tt].z : kc[tt].w, scale[NG == 2 ? j >> 1 : 0], hi, lo);
             const uint32_t to = (to_t ^ (j & 1 ? 64u : 0u)) + (uint32_t)(j >> 1) * kPanel;
             sts128(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
             sts128(to + 2 * kPanel, make_uint4(lo[0], lo[1], lo[2], lo[3]));
           }
         }
         if (half == 0) {
-          const __half2 m0 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(fine ? kw[0] >> 16 : 0x7e00u))), down);
-          const __half2 m1 = __hmul2(__half2half2(__ushort_as_half((unsigned short)(NG == 2 && fine ? kw[1] >> 16 : 0u))), down);
-          const uint32_t b0 = bits(m0), b1 = bits(m1);
-          sts128(kx_at + s * kExtra, make_uint4(b0, (b0 & 0xffffu) | (b1 & 0xffff0000u), b1, 0));
+          uint32_t words[NG];
+#pragma unroll
+          for (int x = 0; x < NG; ++x) words[x] = fine ? kw[x] : 0u;
+          uint4 first, second;
+          key_extra<NG>(words, down1, !fine, 0.f, first, second);
+          sts128(kx_at + s * kExtra, first);
+          sts128(kx_at + s * kExtra + 2048, second);
         }
         proxy_fence();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&S.k_full[s]));
+        ask(i + kAhead);
         // the next tile's keys are under way while the values are done, its values while its keys are
         if (i + 1 < seg.n) load_keys(seg, i + 1, page);
         else if (more) load_keys(after, 0, page);
@@ -604,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
             // (nibbles n and n + 4 are the two tokens)
             uint32_t z[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) z[t] = bits(__hfma2(codes(x[t], y[t], n), sc[t], mn[t]));
+            for (int t = 0; t < 4; ++t) z[t] = bits(__hfma2(value_codes(x[t], y[t], n), sc[t], mn[t]));
             sts128(v_to + 1024 * (4 * uu + n), make_uint4(z[0], z[1], z[2], z[3]));
           }
         }

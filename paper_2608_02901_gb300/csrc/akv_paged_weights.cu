@@ -1,19 +1,28 @@
 // Attention weights that the tokens of a paged cache got, added to their scores.
 //
 // The softmax's normaliser is known (lse), so a token's weight needs its own key alone: one pass over the key codes and their
-// parameters, no reference, no join, and every score is written by one lane.  Units (request, KV head) are cut into tiles of
-// 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA; in a CTA a warp takes sub-blocks of 16
-// tokens, straight from memory to the tensor cores' operands (nibbles as fp16 subnormals, as in the attention).
+// parameters, no reference, no join, and every score is written by one thread.  Two kernels:
+//   up to 16 query rows a unit (a decode step): warp-level products of 16 tokens and 8 rows, codes straight from memory into operands
+//     (nibbles as fp16 subnormals, as in the attention): bound by memory.
+//   more rows (a prompt's last tokens): S = K Q^T on the fifth-generation tensor cores with the tokens as rows.  A thread owns a token:
+//     it turns the codes into its lane of the operand in tensor memory, applies the token's scales to the products behind them,
+//     and adds its weights up along its lane without a shuffle; the queries are the columns.
+// In both, tiles of all units (request, KV head) go in equal contiguous ranges to the CTAs.
+//   With codes 2 c - 15 or c in the products and a's outside, a logit is
+//     k (a_0 S_0 + a_1 S_1 + (2 m_0 + 15 a_0) sum q_0 + (2 m_1 + 15 a_1) sum q_1)
+// over the groups of dimensions, and a weight 2 to that less lse, which is subtracted in such parts that it costs no rounding of its own.
 #include <cuda_runtime.h>
 
+#include <atomic>
+
+#include "akv_device.cuh"
 #include "akv_paged.cuh"
+#include "akv_paged_tc.cuh"
 
 namespace akv {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kTileTokens = 128, kTileSubs = 8;
-constexpr int kBlocks = 8;  // blocks of 8 query rows in shared memory at a time
+constexpr int kTile = 128;                           // tokens of a tile
 constexpr float kInf = __builtin_huge_valf();
 
 struct WeightArgs {
@@ -25,248 +34,650 @@ struct WeightArgs {
   int64_t qb, qt, qh, wb, wh, nb, nh;
   float scale, decay;  // scale: sm_scale log2(e)
   int T, rows;         // rows: query rows of a unit, T G
+  int aligned;         // every query row begins at a multiple of 8 bytes
 };
 
-struct Smem {
-  uint4 frag[2][kBlocks][4][32];     // query operand: high, low halves
-  float qsum[8 * kBlocks][2];        // sums of a query row over each group of dimensions, times scale
-  float qscale[8 * kBlocks];         // what its products count; 0 for rows that add nothing
-  float lse2[8 * kBlocks];           // lse in log2 units; +infinity for rows that add nothing
-  int64_t part[kWarps];
-  int64_t place[2];
+// A unit's share of a CTA: tiles t0 .. t0 + n - 1 of request b, head h.
+struct Segment {
+  int b, h, held, tiles, t0, n;
 };
+__device__ __forceinline__ int tiles_of(const WeightArgs& a, int b) { return (held_tokens(a.v, b) + kTile - 1) / kTile; }
+__device__ __forceinline__ void open(const WeightArgs& a, Segment& s) {
+  s.held = held_tokens(a.v, s.b);
+  s.tiles = (s.held + kTile - 1) / kTile;
+}
+// The segment after s, `left` tiles of the CTA's range still to go (> 0).
+__device__ __forceinline__ void next_segment(const WeightArgs& a, Segment& s, int64_t left) {
+  s.t0 = 0;
+  if (++s.h == a.v.H) {
+    s.h = 0;
+    do ++s.b;
+    while (s.b + 1 < a.v.rows && tiles_of(a, s.b) == 0);  // (rows without tokens have no tiles)
+    open(a, s);
+  }
+  s.n = (int)min((int64_t)s.tiles, left);
+}
+
+// The CTA's range lo .. hi - 1 of all units' tiles, and its first segment; false: none.  All threads call it.
+template <int kThreads>
+__device__ __forceinline__ bool plan(const WeightArgs& a, int64_t* part, int64_t* place, Segment& seg, int64_t& lo, int64_t& hi) {
+  const PagedView& v = a.v;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int strip = (v.rows + kThreads - 1) / kThreads, b0 = min(v.rows, tid * strip), b1 = min(v.rows, b0 + strip);
+  int64_t mine = 0, total = 0;
+  for (int b = b0; b < b1; ++b) mine += (int64_t)tiles_of(a, b) * v.H;
+  int64_t inc = mine;
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2) {
+    const int64_t o = __shfl_up_sync(0xffffffffu, inc, s);
+    if (lane >= s) inc += o;
+  }
+  if (lane == 31) part[warp] = inc;
+  __syncthreads();
+  int64_t before = inc - mine;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += part[w];
+    total += part[w];
+  }
+  lo = blockIdx.x * total / gridDim.x, hi = (blockIdx.x + 1) * total / gridDim.x;
+  if (lo >= hi) return false;
+  if (lo >= before && lo < before + mine) {
+    int64_t rest = lo - before;
+    int b = b0;
+    for (;; ++b) {
+      const int64_t here = (int64_t)tiles_of(a, b) * v.H;
+      if (rest < here) break;
+      rest -= here;
+    }
+    place[0] = b, place[1] = rest;
+  }
+  __syncthreads();
+  seg.b = (int)place[0];
+  open(a, seg);
+  seg.h = (int)(place[1] / seg.tiles), seg.t0 = (int)(place[1] % seg.tiles);
+  seg.n = (int)min((int64_t)(seg.tiles - seg.t0), hi - lo);
+  return true;
+}
+
+// A query row's four values a lane, rotated where the cache is, times the sign of the scale; zeros, and lse infinite, where the row adds nothing:
+// no finite lse, or an infinity or a NaN of its own.
+template <bool HILO>
+__device__ __forceinline__ void load_row(const WeightArgs& a, const Segment& seg, int row, float (&x)[4], float& lse) {
+  const PagedView& v = a.v;
+  const int lane = threadIdx.x & 31, t = row / v.G, g = row % v.G;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = 0.f;
+  lse = kInf;
+  if (row < a.rows) {
+    const uint16_t* q = a.q + seg.b * a.qb + t * a.qt + (int64_t)(seg.h * v.G + g) * a.qh + 4 * lane;
+    const uint2 raw = a.aligned ? *(const uint2*)q : make_uint2(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16);
+    x[0] = row_to_float((uint16_t)raw.x, v.half), x[1] = row_to_float((uint16_t)(raw.x >> 16), v.half);
+    x[2] = row_to_float((uint16_t)raw.y, v.half), x[3] = row_to_float((uint16_t)(raw.y >> 16), v.half);
+    lse = a.lse[((int64_t)seg.b * a.T + t) * (v.H * v.G) + seg.h * v.G + g];
+  }
+  const bool fine = fabsf(lse) < kInf && fabsf(x[0]) < kInf && fabsf(x[1]) < kInf && fabsf(x[2]) < kInf && fabsf(x[3]) < kInf;
+  if (!__all_sync(0xffffffffu, fine)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = 0.f;
+    lse = kInf;
+  }
+  const uint32_t sign = a.scale < 0.f ? 0x80000000u : 0u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign ^ (HILO ? sign_flip(v, 4 * lane + e) : 0u));
+  if (HILO) {  // q' = H (s o q) / 16
+    wht_32x4(x, lane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
+  }
+}
+// lse in log2 units as fp32 and what that leaves out.
+__device__ __forceinline__ void lse_log2(float lse, float& hi, float& lo) {
+  constexpr float c = 1.44269504f, c_rest = 1.92596299e-8f;  // log2(e) in two parts
+  hi = lse * c;
+  lo = fabsf(lse) < kInf ? fmaf(lse, c, -hi) + lse * c_rest : 0.f;
+}
+__device__ __forceinline__ bool finite_word(uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; }
+__device__ __forceinline__ float word_scale(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
+__device__ __forceinline__ float word_min(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+__device__ __forceinline__ uint32_t comp(const uint4& x, int j) { return j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w; }
+
+// ---- few query rows -----------------------------------------------------------------------------
+// A warp takes two sub-blocks of 16 tokens at a time (of 16 rows one), the next on their way meanwhile, their pages known a step earlier still, and what
+// comes a few steps later on its way into L2.
+
+constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ float word_scale(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
-__device__ __forceinline__ float word_min(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
-__device__ __forceinline__ uint32_t comp(const uint4& x, int j) { return j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w; }
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }  // -126 .. 127
-__device__ __forceinline__ bool finite_word(uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; }
 
-// Query rows row0 .. of unit (b, h) as operands, a warp per row; up to `blocks` blocks of 8.
-template <int NG, bool HILO>
-__device__ __forceinline__ void load_queries(const WeightArgs& a, Smem& S, int b, int h, int row0, int blocks) {
-  const PagedView& v = a.v;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int rr = warp; rr < 8 * blocks; rr += kWarps) {
-    float x[4] = {0.f, 0.f, 0.f, 0.f}, lse = kInf;
-    const int row = row0 + rr;
-    if (row < a.rows) {
-      const int t = row / v.G, g = row % v.G;
-      const uint16_t* at = a.q + b * a.qb + t * a.qt + (int64_t)(h * v.G + g) * a.qh + 4 * lane;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = row_to_float(at[e], v.half);
-      lse = a.lse[((int64_t)b * a.T + t) * (v.H * v.G) + h * v.G + g];
-    }
-    if (HILO) {  // q' = H (s o q) / 16
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign_flip(v, 4 * lane + e));
-      wht_32x4(x, lane);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
-    }
-    // a row with no finite lse, or with an infinity or a NaN of its own, adds nothing
-    const bool fine = fabsf(lse) < kInf && fabsf(x[0]) < kInf && fabsf(x[1]) < kInf && fabsf(x[2]) < kInf && fabsf(x[3]) < kInf;
-    const bool counts = __all_sync(0xffffffffu, fine);
-    float big = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (!counts) x[e] = 0.f;
-      big = fmaxf(big, fabsf(x[e]));
-    }
-    big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-    const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
-    const float up = pow2(14 - e2);  // below 2^14, exact in fp16 down to 2^-23 of that
-    float sum = (x[0] + x[1]) + (x[2] + x[3]);
-#pragma unroll
-    for (int s = 1; s < 32 / NG; s *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-    if (lane % (32 / NG) == 0) S.qsum[rr][lane / (32 / NG)] = sum * a.scale;
-    if (lane == 0) {
-      S.qscale[rr] = a.scale * pow2(e2 - 10) * 1048576.f;  // codes count 2^-24, queries 2^(14 - e2)
-      S.lse2[rr] = counts ? lse * 1.4426950408889634f : kInf;
-    }
-    uint4 f[HILO ? 2 : 1];
-#pragma unroll
-    for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
-      uint32_t w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {  // nibble e: odd ones stand for 16 times their value
-        const float y = x[e] * (e & 1 ? up * 0.0625f : up);
-        const float hi = __half2float(__float2half_rn(y));
-        const float mine = lo ? y - hi : y;
-        const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
-        w[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
-      }
-      f[lo] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    // lanes 2 x and 2 x + 1 hold dimensions 8 x ..: word j = x / 4, operand lane 4 row + x % 4
-    const int to = 4 * (rr & 7) + (lane >> 1 & 3);
-    if (!(lane & 1)) S.frag[0][rr >> 3][lane >> 3][to] = f[0];
-    if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][to] = f[HILO ? 1 : 0];
-  }
-}
+template <int NT>
+struct FewSmem {
+  uint4 frag[2][NT][4][32];     // query operand: high, low halves
+  // of a row, in what its products count: sums over each group, k, -lse (the part behind the products, and the one before)
+  float qsum[8 * NT][2], k[8 * NT], lse[8 * NT], lse_in[8 * NT];
+  int64_t part[kFewWarps], place[2];
+};
 
 template <int NG>
 struct Sub {  // key codes and parameters of a sub-block, a lane's part: tokens g8, g8 + 8
   uint4 c[2];
   uint32_t w[2][NG];
-  bool there;
 };
 
-template <int NG, bool HILO>
-__global__ void __launch_bounds__(kThreads, 2) akv_paged_weights_kernel(const __grid_constant__ WeightArgs a) {
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  Smem& S = *reinterpret_cast<Smem*>(smem_raw);
+template <int NG, int NT, bool HILO>
+__global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(const __grid_constant__ WeightArgs a) {
+  __shared__ FewSmem<NT> S;
   constexpr uint32_t kSub = 2048 + 128 * NG;
+  constexpr int kSubs = NT == 1 ? 2 : 1, kStep = kFewWarps * kSubs;  // (two of 16 rows spill)
   const PagedView& v = a.v;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   launch_dependents();
   wait_for_stream();
+  Segment seg;
+  int64_t lo, hi;
+  if (!plan<kFewThreads>(a, S.part, S.place, seg, lo, hi)) return;
 
-  // ---- the CTA's range of tiles: row by row, its heads in turn
-  auto tiles_of = [&](int b) { return (held_tokens(v, b) + kTileTokens - 1) / kTileTokens; };
-  const int strip = (v.rows + kThreads - 1) / kThreads, b0 = min(v.rows, tid * strip), b1 = min(v.rows, b0 + strip);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (int64_t)tiles_of(b) * v.H;
-  int64_t inc = mine, before, total = 0;
+  for (int64_t at = lo; at < hi;) {
+    const int first = seg.t0 * (kTile / 16), end = min((seg.t0 + seg.n) * (kTile / 16), (seg.held + 15) >> 4);
+    auto page_at = [&](int s) {  // as the table says (looked at when it is used)
+      return s < end ? v.table[(int64_t)seg.b * v.table_stride + (16 * s >> v.page_log)] : -1;
+    };
+    auto place = [&](int s, int page) {
+      return block_of(v, page, seg.h) + (uint64_t)((16 * s & ((1 << v.page_log) - 1)) >> 4) * kSub;
+    };
+    auto load = [&](int s, int page) {  // (no token, or a page that is none of the pool's: NaN parameters)
+      Sub<NG> x;
+      if ((uint32_t)page < (uint32_t)v.n_pages) {
+        const uint8_t* base = place(s, page);
+        x.c[0] = *(const uint4*)(base + 16 * lane);
+        x.c[1] = *(const uint4*)(base + 512 + 16 * lane);
 #pragma unroll
-  for (int s = 1; s < 32; s *= 2) {
-    const int64_t o = __shfl_up_sync(0xffffffffu, inc, s);
-    if (lane >= s) inc += o;
-  }
-  if (lane == 31) S.part[warp] = inc;
-  __syncthreads();
-  before = inc - mine;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += S.part[w];
-    total += S.part[w];
-  }
-  const int64_t lo = blockIdx.x * total / gridDim.x, hi = (blockIdx.x + 1) * total / gridDim.x;
-  if (lo >= hi) return;
-  if (lo >= before && lo < before + mine) {
-    int64_t rest = lo - before;
-    int b = b0;
-    for (;; ++b) {
-      const int64_t here = (int64_t)tiles_of(b) * v.H;
-      if (rest < here) break;
-      rest -= here;
-    }
-    S.place[0] = b, S.place[1] = rest;
-  }
-  __syncthreads();
-  int b = (int)S.place[0];
-  int64_t at = S.place[1];  // tile of the row's H x tiles
-
-  for (int64_t k = lo; k < hi;) {
-    const int held = held_tokens(v, b), tiles = tiles_of(b), h = (int)(at / tiles), t0 = (int)(at % tiles);
-    const int n = (int)min((int64_t)(tiles - t0), hi - k);  // tiles of this unit
-    const int sees0 = held - a.T + 1;                        // tokens that the first query token sees
-    const int sub1 = min((t0 + n) * kTileSubs, (held + 15) >> 4);
-    for (int row0 = 0; row0 < a.rows; row0 += 8 * kBlocks) {
-      const int blocks = min(kBlocks, (a.rows - row0 + 7) >> 3);
-      __syncthreads();
-      load_queries<NG, HILO>(a, S, b, h, row0, blocks);
-      __syncthreads();
-      auto load = [&](int s) {
-        Sub<NG> x{};
-        const int page = s < sub1 ? page_of(v, b, 16 * s >> v.page_log) : -1;
-        x.there = page >= 0;
-        if (x.there) {
-          const uint8_t* base = block_of(v, page, h) + (uint64_t)((16 * s & ((1 << v.page_log) - 1)) >> 4) * kSub;
-          x.c[0] = *(const uint4*)(base + 16 * lane);
-          x.c[1] = *(const uint4*)(base + 512 + 16 * lane);
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const uint8_t* p = base + 2048 + 8 * NG * (g8 + 8 * y);
-            if (NG == 2) {
-              const uint2 w = *(const uint2*)p;
-              x.w[y][0] = w.x, x.w[y][NG - 1] = w.y;
-            } else {
-              x.w[y][0] = *(const uint32_t*)p;
-            }
+        for (int y = 0; y < 2; ++y) {
+          const uint8_t* p = base + 2048 + 8 * NG * (g8 + 8 * y);
+          if (NG == 2) {
+            const uint2 w = *(const uint2*)p;
+            x.w[y][0] = w.x, x.w[y][NG - 1] = w.y;
+          } else {
+            x.w[y][0] = *(const uint32_t*)p;
           }
         }
-        return x;
-      };
-      Sub<NG> next = load(t0 * kTileSubs + warp);
-      for (int s = t0 * kTileSubs + warp; s < sub1; s += kWarps) {
-        const Sub<NG> x = next;
-        next = load(s + kWarps);
-        const bool edge = 16 * s + 16 > sees0;
-        float sum[2] = {0.f, 0.f};
+      } else {
+        x.c[0] = x.c[1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int g = 0; g < NG; ++g) x.w[y][g] = 0x7e007e00u;
+      }
+      return x;
+    };
+    const int mine = first + kSubs * warp;
+    int page[kSubs], far[kSubs];
+    Sub<NG> next[kSubs];
+#pragma unroll
+    for (int i = 0; i < kSubs; ++i) page[i] = page_at(mine + i);
+#pragma unroll
+    for (int i = 0; i < kSubs; ++i) {
+      next[i] = load(mine + i, page[i]);
+      page[i] = page_at(mine + kStep + i);
+      far[i] = page_at(mine + 2 * kStep + i);
+    }
+
+    // ---- queries: a warp per row, four dimensions a lane
+    __syncthreads();
 #pragma unroll 1
-        for (int nt = 0; nt < blocks; ++nt) {
-          // logits of tokens g8 and g8 + 8, query rows 2 t4 and 2 t4 + 1; sums of 64 dimensions, the low halves first
-          float l[4];
+    for (int rr = warp; rr < 8 * NT; rr += kFewWarps) {
+      float x[4], lse;
+      load_row<HILO>(a, seg, rr, x, lse);
+      float big = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+      big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
+      const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
+      const float up = pow2(14 - e2);  // below 2^14, exact in fp16 down to 2^-23 of that
+      float sum = (x[0] + x[1]) + (x[2] + x[3]);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int s = 1; s < 32 / NG; s *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+      if (lane % (32 / NG) == 0) S.qsum[rr][lane / (32 / NG)] = sum * up;
+      if (lane == 0) {
+        const float k = 0.5f * fabsf(a.scale) * pow2(e2 - 14);
+        float l, rest;
+        lse_log2(lse, l, rest);
+        const float coarse = fabsf(l) < 8192.f ? rintf(l * 256.f) * 0.00390625f : l;
+        const float in = (rest + (l - coarse)) / k;  // (rows so small that their logits hardly differ: not worth it)
+        S.k[rr] = k, S.lse[rr] = -coarse, S.lse_in[rr] = fabsf(in) < 1e30f ? -in : 0.f;
+      }
+      uint4 f[HILO ? 2 : 1];
 #pragma unroll
-            for (int part = HILO ? 1 : 0; part >= 0; --part)
+      for (int low = 0; low < (HILO ? 2 : 1); ++low) {
+        uint32_t w[4];
 #pragma unroll
-              for (int j = 2 * half; j < 2 * half + 2; ++j) {
-                const uint4 q = S.frag[part][nt][j][lane];
-                const uint32_t x0 = comp(x.c[0], j), x1 = comp(x.c[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
-                mma_16816(d, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
-                mma_16816(d, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
+        for (int e = 0; e < 4; ++e) {  // nibble e: odd ones stand for 16 times their value
+          const float y = x[e] * (e & 1 ? up * 0.0625f : up);
+          const float high = __half2float(__float2half_rn(y));
+          const float own = low ? y - high : y;
+          const float other = __shfl_xor_sync(0xffffffffu, own, 1);
+          w[e] = lane & 1 ? half2_bits(other, own) : half2_bits(own, other);
+        }
+        f[low] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      // lanes 2 x and 2 x + 1 hold dimensions 8 x ..: word j = x / 4, operand lane 4 row + x % 4
+      const int to = 4 * (rr & 7) + (lane >> 1 & 3);
+      if (!(lane & 1)) S.frag[0][rr >> 3][lane >> 3][to] = f[0];
+      if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][to] = f[HILO ? 1 : 0];
+    }
+    __syncthreads();
+
+    const float* was = a.was ? a.was + seg.b * a.wb + seg.h * a.wh : nullptr;
+    float* now = a.now + seg.b * a.nb + seg.h * a.nh;
+    const int sees0 = seg.held - a.T + 1;  // tokens that the first query token sees
+#pragma unroll 1
+    for (int s0 = mine; s0 < end; s0 += kStep) {
+      Sub<NG> x[kSubs];
+#pragma unroll
+      for (int i = 0; i < kSubs; ++i) x[i] = next[i];
+#pragma unroll
+      for (int i = 0; i < kSubs; ++i) {
+        next[i] = load(s0 + kStep + i, page[i]);
+        page[i] = far[i];
+        if (lane == 0 && (uint32_t)far[i] < (uint32_t)v.n_pages) {
+          const uint8_t* p = place(s0 + 2 * kStep + i, far[i]);
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(1024) : "memory");
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p + 2048), "r"(128 * NG) : "memory");
+        }
+        far[i] = page_at(s0 + 3 * kStep + i);
+      }
+      float old[kSubs][2], sum[kSubs][2];
+#pragma unroll
+      for (int i = 0; i < kSubs; ++i)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int tok = 16 * (s0 + i) + g8 + 8 * y;
+          old[i][y] = was && t4 == 0 && tok < seg.held && s0 + i < end ? was[tok] : 0.f;
+          sum[i][y] = 0.f;
+        }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        // products of tokens g8 and g8 + 8 with query rows 2 t4 and 2 t4 + 1 over 64 dimensions each, the low halves first; 2^-24 of codes from 0
+        float z[kSubs][4];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float d[kSubs][4];
+#pragma unroll
+          for (int i = 0; i < kSubs; ++i) d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.f;
+#pragma unroll
+          for (int part = HILO ? 1 : 0; part >= 0; --part)
+#pragma unroll
+            for (int j = 2 * half; j < 2 * half + 2; ++j) {
+              const uint4 q = S.frag[part][nt][j][lane];
+#pragma unroll
+              for (int i = 0; i < kSubs; ++i) {
+                const uint32_t x0 = comp(x[i].c[0], j), x1 = comp(x[i].c[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+                mma_16816(d[i], x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
+                mma_16816(d[i], x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
               }
+            }
+#pragma unroll
+          for (int i = 0; i < kSubs; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float unit = word_scale(x.w[e >> 1][half * (NG - 1)]);
-              l[e] = half ? fmaf(unit, d[e], l[e]) : unit * d[e];
+              // a (2 c - 15) . q + (2 m + 15 a) sum q: of one group the sums over all its dimensions in its first half
+              const int r = 8 * nt + 2 * t4 + (e & 1);
+              const uint32_t w = x[i].w[e >> 1][half * (NG - 1)];
+              const float scale = word_scale(w);
+              if (NG == 2 || half == 0) {
+                const float qsum = S.qsum[r][half * (NG - 1)], add = fmaf(scale, 15.f, 2.f * word_min(w));
+                z[i][e] = fmaf(add, qsum, half ? z[i][e] : S.lse_in[r]);
+                z[i][e] = fmaf(scale, fmaf(d[i][e], 33554432.f, -15.f * qsum), z[i][e]);
+              } else {
+                z[i][e] = fmaf(scale, d[i][e] * 33554432.f, z[i][e]);
+              }
             }
-          }
+        }
+#pragma unroll
+        for (int i = 0; i < kSubs; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 8 * nt + 2 * t4 + (e & 1);
-            float y = fmaf(word_min(x.w[e >> 1][0]), S.qsum[r][0], -S.lse2[r]);
-            if (NG == 2) y = fmaf(word_min(x.w[e >> 1][NG - 1]), S.qsum[r][NG - 1], y);
-            float p = exp2_fast(fmaf(l[e], S.qscale[r], y));
-            if (edge && 16 * s + g8 + 8 * (e >> 1) >= sees0 + (row0 + r) / v.G) p = 0.f;
-            sum[e >> 1] += p;
+            float p = exp2_fast(fmaf(z[i][e], S.k[r], S.lse[r]));
+            if (16 * (s0 + i) + 16 > sees0 && 16 * (s0 + i) + g8 + 8 * (e >> 1) >= sees0 + r / v.G) p = 0.f;
+            sum[i][e >> 1] += p;
           }
-        }
+      }
+#pragma unroll
+      for (int i = 0; i < kSubs; ++i)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
-          sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
-          const int i = 16 * s + g8 + 8 * y;
-          if (t4 == 0 && i < held) {
-            bool fine = x.there;
+          sum[i][y] += __shfl_xor_sync(0xffffffffu, sum[i][y], 1);
+          sum[i][y] += __shfl_xor_sync(0xffffffffu, sum[i][y], 2);
+          const int tok = 16 * (s0 + i) + g8 + 8 * y;
+          if (t4 == 0 && tok < seg.held && s0 + i < end) {
+            bool fine = true;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) fine = fine && finite_word(x.w[y][g]);
-            float* to = a.now + b * a.nb + h * a.nh + i;
-            const float old = row0 ? *to : a.was ? a.decay * a.was[b * a.wb + h * a.wh + i] : 0.f;
-            *to = fine ? old + sum[y] : old;
+            for (int g = 0; g < NG; ++g) fine = fine && finite_word(x[i].w[y][g]);
+            now[tok] = fine ? fmaf(a.decay, old[i][y], sum[i][y]) : a.decay * old[i][y];
           }
         }
-      }
     }
-    k += n;
-    at += n;
-    while (k < hi && at >= (int64_t)tiles_of(b) * v.H) at = 0, ++b;  // (rows without tokens have no tiles)
+    at += seg.n;
+    if (at < hi) next_segment(a, seg, hi - at);
   }
 }
 
+// ---- many query rows ----------------------------------------------------------------------------
+// Two warpgroups take the tiles in turn, a warp issues the products, 64 columns a time.  Queries of up to 256 rows lie in shared memory as
+// operands; a unit with more goes over its tiles again for each 256.
+
+constexpr int W = 2, kWorkers = 4 * W, kThreads = 128 * (W + 1);
+constexpr int kCols = 64, kBlocks = 4, kHeld = kBlocks * kCols;  // query rows of a product, and in shared memory
+// Tensor memory: the warpgroups' keys, then their sums over the first group of dimensions (or all), the second, and the rest
+constexpr uint32_t kColK = 0, kColS = 64 * W, kColsS = 3 * kCols;
+constexpr float kOnes = 16.f;  // the dimensions that carry lse count 16
+
+struct Smem {
+  uint8_t q[2][4 * kPanel];  // 128 rows each: high, then low halves
+  uint8_t qx[2][kExtra], kx[W][kExtra];
+  float k[kHeld], lse[kHeld];  // what a row's products count; the part of -lse behind them (-infinity: the row adds nothing)
+  int sees[kHeld];             // tokens that it sees
+  int behind[kBlocks];         // whether a block has rows with such a part
+  uint64_t k_full[W], s_full[W], s_free[W], q_full, drained;
+  int64_t part[4 * W + 4], place[2];
+  uint32_t tmem;
+  int failed;
+};
+
 template <int NG, bool HILO>
-int launch(const WeightArgs& a, int sms, void* stream) {
+__global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __grid_constant__ WeightArgs a) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  Smem& S = *reinterpret_cast<Smem*>(smem_raw + (1024u - (smem_u32(smem_raw) & 1023u)) % 1024u);
+  constexpr uint32_t kSub = 2048 + 128 * NG;
+  const PagedView& v = a.v;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  volatile int* failed = &S.failed;
+  launch_dependents();
+  if (tid == 0) {
+    for (int w = 0; w < W; ++w) {
+      mbar_init(smem_u32(&S.k_full[w]), 4);
+      mbar_init(smem_u32(&S.s_full[w]), 1);
+      mbar_init(smem_u32(&S.s_free[w]), 4);
+    }
+    mbar_init(smem_u32(&S.q_full), kWorkers);
+    mbar_init(smem_u32(&S.drained), 1);
+    S.failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // what the sixteen extra dimensions do not use is zeros
+  for (int k = tid; k < 256; k += kThreads) sts128(smem_u32(S.qx) + k / 128 * kExtra + 2048 + 16 * (k % 128), make_uint4(0, 0, 0, 0));
+  wait_for_stream();
+  Segment seg;
+  int64_t lo, hi;
+  if (!plan<kThreads>(a, S.part, S.place, seg, lo, hi)) return;
+  if (warp == kWorkers) tc_alloc(smem_u32(&S.tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, S.tmem, 0);
+  const int passes = (a.rows + kHeld - 1) / kHeld;
+  auto rows_of = [&](int pass) { return min(kHeld, a.rows - pass * kHeld); };
+  auto columns = [](int rows, int block) { return min(kCols, (rows - block * kCols + 15) & ~15); };
+
+  if (warp == kWorkers) {
+    // ---- the products: the warpgroups' tiles side by side, their blocks of columns in turn
+    uint32_t nk[W], ns[W], nq = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) nk[w] = ns[w] = 0;
+    bool ok = true;
+    for (int64_t at = lo; ok && at < hi;) {
+      for (int pass = 0; ok && pass < passes; ++pass) {
+        const int rows = rows_of(pass), blocks = (rows + kCols - 1) / kCols;
+        ok = mbar_wait_w(smem_u32(&S.q_full), nq++ & 1);
+#pragma unroll 1
+        for (int i0 = 0; ok && i0 < seg.n; i0 += W)
+#pragma unroll 1
+          for (int block = 0; ok && block < blocks; ++block) {
+            const uint32_t n = (uint32_t)columns(rows, block), idesc = (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+            const uint32_t rows_at = (uint32_t)(block & 1) * (kCols * 128);  // of a panel
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+              if (!ok || i0 + w >= seg.n) break;
+              if (block == 0) ok = mbar_wait_w(smem_u32(&S.k_full[w]), nk[w]++ & 1);
+              ok = ok && mbar_wait_w(smem_u32(&S.s_free[w]), (ns[w]++ & 1) ^ 1) && !warp_failed(failed);
+              if (!ok) break;
+              tc_fence_after();
+              if (elect_one()) {
+                const uint32_t d = tmem + kColS + kColsS * w, k = tmem + kColK + 64 * w;
+                const uint64_t dq = sw128_desc(smem_u32(S.q[block >> 1]) + rows_at);
+                auto product = [&](uint32_t to, int first_step, int steps, uint64_t desc, bool first) {
+#pragma unroll
+                  for (int i = 0; i < steps; ++i) {
+                    const int kk = first_step + i;
+                    tc_mma_ts(to, k + 8 * kk, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || i > 0);
+                  }
+                };
+                constexpr uint64_t low = 2 * kPanel >> 4;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                  if (HILO) product(d + kCols * g, 8 / NG * g, 8 / NG, dq + low, true);
+                  product(d + kCols * g, 8 / NG * g, 8 / NG, dq, !HILO);
+                }
+                tc_mma(d + 2 * kCols, plain_desc(smem_u32(S.kx[w])), plain_desc(smem_u32(S.qx[block >> 1]) + extra_at(kCols * (block & 1))), idesc, 0);
+                tc_commit(smem_u32(&S.s_full[w]));
+              }
+              __syncwarp();
+            }
+          }
+      }
+      at += seg.n;
+      if (at < hi) next_segment(a, seg, hi - at);
+    }
+    if (!ok) *failed = 1;
+    if (elect_one()) tc_commit(smem_u32(&S.drained));
+    __syncwarp();
+    mbar_wait_w(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
+  } else if (warp < kWorkers) {
+    // ---- a warpgroup, a thread a token
+    const int w = warp >> 2, token = tid & 127;
+    const uint32_t lane_at = tmem + ((uint32_t)((warp & 3) * 32) << 16), tK = lane_at + kColK + 64 * w, tS = lane_at + kColS + kColsS * w;
+    const uint32_t kx_at = smem_u32(S.kx[w]) + extra_at(token);
+    const KeyCodes codes;
+    uint32_t n_s = 0;
+    uint4 kc[4];
+    uint32_t kw[NG];
+    int page;
+    auto page_at = [&](const Segment& s, int i) {  // as the table says (looked at when it is used)
+      const int tok = (s.t0 + i) * kTile + token;
+      return i < s.n && tok < s.held ? v.table[(int64_t)s.b * v.table_stride + (tok >> v.page_log)] : -1;
+    };
+    auto load = [&](const Segment& s, int i, int pg) {
+      if ((uint32_t)pg < (uint32_t)v.n_pages) {
+        const int tok = (s.t0 + i) * kTile + token;
+        const uint8_t* p = block_of(v, pg, s.h) + (uint64_t)((tok & ((1 << v.page_log) - 1)) >> 4) * kSub;
+        const uint4* k = (const uint4*)(p + 64 * (tok & 15));
+#pragma unroll
+        for (int t = 0; t < 4; ++t) kc[t] = k[t];
+        if (NG == 2) {
+          const uint2 x = *(const uint2*)(p + 2048 + 16 * (tok & 15));
+          kw[0] = x.x, kw[NG - 1] = x.y;
+        } else {
+          kw[0] = *(const uint32_t*)(p + 2048 + 8 * (tok & 15));
+        }
+      } else {  // no token, or a page that is none of the pool's: adds nothing
+#pragma unroll
+        for (int t = 0; t < 4; ++t) kc[t] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) kw[g] = 0x7e007e00u;
+      }
+    };
+    load(seg, w, page_at(seg, w));
+    page = page_at(seg, w + W);
+    for (int64_t at = lo; at < hi;) {
+      Segment after = seg;
+      const bool more = at + seg.n < hi;
+      if (more) next_segment(a, after, hi - at - seg.n);
+      const float* was = a.was ? a.was + seg.b * a.wb + seg.h * a.wh : nullptr;
+      float* now = a.now + seg.b * a.nb + seg.h * a.nh;
+      for (int pass = 0; pass < passes; ++pass) {
+        const int rows = rows_of(pass), blocks = (rows + kCols - 1) / kCols;
+        // queries as operands, a warp a row (the products of the pass before have been waited for by every warpgroup)
+        named_sync(1, 32 * kWorkers);
+        if (tid < kBlocks) S.behind[tid] = 0;
+        named_sync(1, 32 * kWorkers);
+        const int padded = (blocks - 1) * kCols + columns(rows, blocks - 1);
+#pragma unroll 1
+        for (int rr = warp; rr < padded; rr += kWorkers) {
+          float x[4], lse;
+          load_row<HILO>(a, seg, rr < rows ? pass * kHeld + rr : a.rows, x, lse);
+          const int up = query_row<NG, HILO>(x, lane, rr & 127, smem_u32(S.q[rr >> 7]), S.qx[rr >> 7]);
+          if (lane == 0) {
+            // -lse goes with the products in three parts where it fits them (rows so small that it does not: behind them)
+            const float k = 0.5f * fabsf(a.scale) * pow2(-up);  // (keys enter twice as large)
+            float l, rest;
+            lse_log2(lse, l, rest);
+            float in = -l / k * (1.f / kOnes), in_rest = fmaf(-in * kOnes, k, -l) / k * (1.f / kOnes) - rest / k * (1.f / kOnes);
+            const bool fits = fabsf(in) < 32768.f;
+            if (!fits) in = in_rest = 0.f, S.behind[rr / kCols] = 1;
+            uint16_t* to = (uint16_t*)(S.qx[rr >> 7] + extra_at(rr & 127) + 2048) + 2;
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+              const __half p = __float2half_rn(in);
+              to[i] = __half_as_ushort(p);
+              in = in - __half2float(p) + (i == 0 ? in_rest : 0.f);
+            }
+            S.k[rr] = k, S.lse[rr] = fits ? 0.f : -l;
+            S.sees[rr] = min(seg.held, seg.held - a.T + 1 + (pass * kHeld + rr) / v.G);
+          }
+        }
+        proxy_fence();
+        __syncwarp();
+        named_sync(1, 32 * kWorkers);
+        if (lane == 0) mbar_arrive(smem_u32(&S.q_full));
+
+        bool ok = true;
+#pragma unroll 1
+        for (int i = w; i < seg.n; i += W) {
+          // ---- the token's codes into tensor memory
+          bool fine = true;
+          float scale[NG];
+#pragma unroll
+          for (int g = 0; g < NG; ++g) fine = fine && finite_word(kw[g]);
+          uint32_t words[NG];
+#pragma unroll
+          for (int g = 0; g < NG; ++g) words[g] = fine ? kw[g] : 0u, scale[g] = word_scale(words[g]);
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            float x[32];
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                const uint32_t word = comp(kc[t], 2 * p + jj), x2 = word << 1, y2 = word >> 7;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[16 * jj + 4 * t + e] = __uint_as_float(bits(codes(x2, y2, e)));
+              }
+            tm_st32(tK + 32 * p, x);
+          }
+          // (2 m + 15 a beyond fp16's range: 2^-5 of it, and of lse)
+          bool big = false;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) big = big || scale[g] > 2048.f || fabsf(word_min(words[g])) > 16384.f;
+          const float down = big ? kLargeDown : 1.f, back = big ? 32.f : 1.f;
+          uint4 first, second;
+          key_extra<NG>(words, down, false, kOnes * down, first, second);
+          sts128(kx_at, first);
+          sts128(kx_at + 2048, second);
+          tm_wait_st();
+          tc_fence_before();
+          proxy_fence();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&S.k_full[w]));
+          // the warpgroup's next tile is under way meanwhile
+          if (i + W < seg.n) {
+            load(seg, i + W, page);
+            page = page_at(seg, i + 2 * W);
+          }
+          const int tok = (seg.t0 + i) * kTile + token;
+          const bool held = tok < seg.held;
+          float old = 0.f;
+          if (held) old = pass ? now[tok] : was ? a.decay * was[tok] : 0.f;
+          const bool edge = (seg.t0 + i + 1) * kTile > seg.held - a.T + 1;  // some row may not see some token
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          const float2 s0 = make_float2(scale[0], scale[0]), s1 = make_float2(scale[NG - 1], scale[NG - 1]), b2 = make_float2(back, back);
+#pragma unroll 1
+          for (int block = 0; block < blocks; ++block) {
+            if (!ok || warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[w]), n_s++ & 1)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const int n = columns(rows, block);
+            const bool behind = edge || *(volatile int*)&S.behind[block];
+#pragma unroll 1
+            for (int c = 0; c < n; c += 16) {
+              float x[16], y[16], z[16];
+              tm_ld16(tS + c, x);
+              if (NG == 2) tm_ld16(tS + kCols + c, y);
+              tm_ld16(tS + 2 * kCols + c, z);
+              const float2* k2 = (const float2*)&S.k[block * kCols + c];
+#pragma unroll
+              for (int e = 0; e < 16; e += 2) {
+                float2 l = make_float2(z[e], z[e + 1]);
+                if (NG == 2) l = __ffma2_rn(s1, make_float2(y[e], y[e + 1]), big ? __fmul2_rn(l, b2) : l);
+                else if (big) l = __fmul2_rn(l, b2);
+                l = __ffma2_rn(s0, make_float2(x[e], x[e + 1]), l);
+                l = __fmul2_rn(l, k2[e >> 1]);
+                if (behind) {
+                  const float2 lse = *(const float2*)&S.lse[block * kCols + c + e];
+                  const int2 sees = *(const int2*)&S.sees[block * kCols + c + e];
+                  l.x = tok < sees.x ? l.x + lse.x : -kInf;
+                  l.y = tok < sees.y ? l.y + lse.y : -kInf;
+                }
+                l.x = exp2_fast(l.x), l.y = exp2_fast(l.y);
+                sum[e >> 1 & 1] = __fadd2_rn(sum[e >> 1 & 1], l);
+              }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&S.s_free[w]));
+          }
+          if (held) now[tok] = ok ? (fine ? old + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y)) : old) : __int_as_float(0x7fffffff);
+        }
+        if (!ok) *failed = 1;
+        // the first tile of what comes next
+        if (pass + 1 < passes) {
+          load(seg, w, page_at(seg, w));
+          page = page_at(seg, w + W);
+        } else if (more) {
+          load(after, w, page_at(after, w));
+          page = page_at(after, w + W);
+        }
+      }
+      at += seg.n;
+      seg = after;
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kWorkers) tc_dealloc(tmem, 512);
+}
+
+template <int NG, bool HILO>
+int launch(const WeightArgs& a, int dev, int sms, void* stream) {
+  // (16 rows and fewer: see the top)
+  if (a.rows <= 8) return launch_after(akv_paged_weights_few_kernel<NG, 1, HILO>, dim3(2 * sms), kFewThreads, 0, stream, a);
+  if (a.rows <= 16) return launch_after(akv_paged_weights_few_kernel<NG, 2, HILO>, dim3(2 * sms), kFewThreads, 0, stream, a);
   auto* kernel = akv_paged_weights_kernel<NG, HILO>;
-  static_assert(sizeof(Smem) <= 48 * 1024, "shared memory without an attribute");
-  return launch_after(kernel, dim3(2 * sms), kThreads, sizeof(Smem), stream, a);
+  constexpr size_t smem = sizeof(Smem) + 1024;
+  static_assert(smem <= 232448, "shared memory of a CTA");
+  static std::atomic<uint64_t> ready{0};  // devices on which the kernel's shared memory has been set
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return (int)e;
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  return launch_after(kernel, dim3(sms), kThreads, smem, stream, a);
 }
 
 }  // namespace
@@ -281,6 +692,7 @@ int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse
   a.v = v;
   a.q = (const uint16_t*)q.ptr;
   a.qb = q.stride_b, a.qt = q.stride_t, a.qh = q.stride_h;
+  a.aligned = (uintptr_t)q.ptr % 8 == 0 && q.stride_b % 4 == 0 && q.stride_t % 4 == 0 && q.stride_h % 4 == 0;
   a.lse = lse;
   if (was) a.was = was->ptr, a.wb = was->stride_b, a.wh = was->stride_h;
   a.now = now.ptr, a.nb = now.stride_b, a.nh = now.stride_h;
@@ -288,8 +700,8 @@ int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse
   a.decay = decay;
   a.T = T;
   a.rows = T * v.G;
-  if (v.rotate) return v.ng == 2 ? launch<2, true>(a, sms, stream) : launch<1, true>(a, sms, stream);
-  return v.ng == 2 ? launch<2, false>(a, sms, stream) : launch<1, false>(a, sms, stream);
+  if (v.rotate) return v.ng == 2 ? launch<2, true>(a, dev, sms, stream) : launch<1, true>(a, dev, sms, stream);
+  return v.ng == 2 ? launch<2, false>(a, dev, sms, stream) : launch<1, false>(a, dev, sms, stream);
 }
 
 }  // namespace akv

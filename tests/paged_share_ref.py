@@ -75,7 +75,7 @@ def attend_shared(E, q, sm_scale):
       weights  a share of a weight is rounded to fp16: 2^-11 of what it brings (either w a with the codes, or w with the whole value, which
                bounds both), and 2^-29 of the row's largest for each token
       values   fp16(m + c a): 2^-11 of each, 2^-25 below the normal range; where a sub-block has a scale above 2048 or a minimum
-               beyond 32768, 2^-20
+               beyond 16384, 2^-20
       sums     of at most 2^13 tiles' steps a thread, four at a time, over parts of at most 2^9 steps here: 2^9 u of sum w |v|
                and of the normaliser; 2^-14 of sum w |v| on tensor cores
       output   half an ulp of its type"""
@@ -91,7 +91,7 @@ def attend_shared(E, q, sm_scale):
             continue
         for h in range(p.n_kv_heads):
             r = Rows(E, b, h, n)
-            coarse = bool((r.va > 2048).any() or (r.vm.abs() > 32768).any())
+            coarse = bool((r.va > 2048).any() or (r.vm.abs() > 16384).any())
             for t in range(T):
                 sees = n - T + 1 + t
                 if sees <= 0:
