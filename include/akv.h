@@ -731,9 +731,11 @@ typedef struct akv_scores {
  * over the queries that see token i, for the tokens i < lens[b] that request b holds; further numbers are left as they were.
  * `was` may be null (zeros) or the same as `now`, and is not read where decay is 0.  Queries whose lse is not a finite number, and
  * tokens whose key has an infinity or a NaN or whose page is none of the pool's, add nothing.  Sums in fp32, in a fixed order. */
+akv_status akv_paged_weights_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
+                                            size_t* ws_bytes);
 akv_status akv_paged_weights(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
                              const float* lse, int32_t T, float sm_scale, float decay, const akv_scores* was,
-                             const akv_scores* now, akv_stream_t stream);
+                             const akv_scores* now, void* ws, size_t ws_bytes, akv_stream_t stream);
 
 /* The tokens that rows keep: [n][n_kv_heads][top] places in the row that they come from, ascending, -1 beyond the count, and
  * count [n]. */

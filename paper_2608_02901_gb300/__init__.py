@@ -19,7 +19,7 @@ from .paged import (  # noqa: F401 - the paged 4-bit cache
     AKV_DTYPE_BF16, AKV_DTYPE_FP16, AKV_FLAG_BOUNDS, AKV_PAGED_MAX_QUERY, KeptTokens, PagedParams, Pages, PageSelection,
     PageShare, akv_paged_append, akv_paged_attn, akv_paged_attn_shared, akv_paged_attn_shared_workspace_size,
     akv_paged_attn_workspace_size, akv_paged_evict, akv_paged_page_bytes, akv_paged_read, akv_paged_select,
-    akv_paged_select_workspace_size, akv_paged_weights, akv_pages_compact, akv_pages_copy, akv_pages_fork,
+    akv_paged_select_workspace_size, akv_paged_weights, akv_paged_weights_workspace_size, akv_pages_compact, akv_pages_copy, akv_pages_fork,
     akv_pages_free, akv_pages_reserve, akv_pages_share, akv_pages_trim, akv_pages_workspace_size)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))

@@ -29,6 +29,7 @@ SOURCES = {
     "akv_paged_append.cu": [],
     "akv_paged_attn.cu": [],
     "akv_paged_evict.cu": [],
+    "akv_paged_query.cu": [],
     "akv_paged_select.cu": [],
     "akv_paged_shared.cu": [],
     "akv_paged_weights.cu": [],

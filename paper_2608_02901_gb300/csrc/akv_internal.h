@@ -229,11 +229,16 @@ const float* paged_own_slots(const void* ws);
 int launch_paged_select(const PagedView& v, const akv_rows& q, int32_t T, int32_t sink, int32_t recent, const akv_selection& sel,
                         void* ws, void* stream);
 size_t paged_select_ws_bytes(const PagedView& v, int32_t T);
+// Query rows [rows][T][n_q_heads] as operands of the tensor-core kernels: a record each of 16 chunks of high and 16 of low halves, 16 more
+// dimensions, and two numbers: what the row's values were divided by, and whether it counts (1 or 0).
+constexpr size_t kQueryRecord = 576;
+int launch_paged_queries(const PagedView& v, const akv_rows& q, int32_t T, bool negative, const float* lse, void* records, void* stream);
 int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
                         const akv_share& share, void* ws, void* stream);
 size_t paged_shared_ws_bytes(const PagedView& v, int32_t T);
 int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse, int32_t T, float sm_scale, float decay,
-                         const akv_scores* was, const akv_scores& now, void* stream);
+                         const akv_scores* was, const akv_scores& now, void* ws, void* stream);
+size_t paged_weights_ws_bytes(const PagedView& v, int32_t T);
 int launch_paged_evict(const PagedView& v, const int32_t* src, const int32_t* dst, int32_t n, const akv_scores& scores,
                        const int32_t* keep, int32_t sink, int32_t recent, const akv_kept& kept, void* stream);
 size_t pages_ws_bytes(const PagesState& s);

@@ -320,9 +320,18 @@ akv_status akv_paged_attn_shared(const akv_paged_params* p, const akv_pages* pag
   return launched(launch_paged_shared(c.v, *q, *out, lse, T, sm_scale, *share, ws, (void*)stream), "shared attention");
 }
 
+akv_status akv_paged_weights_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T, size_t* ws_bytes) {
+  PagedCall c;
+  AKV_TRY(check_pages(p, pages, &c));
+  AKV_TRY(check_query(T));
+  if (!ws_bytes) return fail(AKV_ERR_INVALID, "null ws_bytes");
+  *ws_bytes = paged_weights_ws_bytes(c.v, T);
+  return AKV_OK;
+}
+
 akv_status akv_paged_weights(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
                              const float* lse, int32_t T, float sm_scale, float decay, const akv_scores* was,
-                             const akv_scores* now, akv_stream_t stream) {
+                             const akv_scores* now, void* ws, size_t ws_bytes, akv_stream_t stream) {
   PagedCall c;
   AKV_TRY(check_layer(p, pages, layer, &c));
   AKV_TRY(check_query(T));
@@ -333,7 +342,8 @@ akv_status akv_paged_weights(const akv_paged_params* p, const akv_pages* pages, 
   if (!std::isfinite(decay)) return fail(AKV_ERR_INVALID, "decay must be finite");
   if (was) AKV_TRY(check_scores(was, "was", pages, p, false));
   AKV_TRY(check_scores(now, "now", pages, p, true));
-  return launched(launch_paged_weights(c.v, *q, lse, T, sm_scale, decay, decay != 0.f ? was : nullptr, *now, (void*)stream), "weights");
+  AKV_TRY(check_ws(ws, ws_bytes, paged_weights_ws_bytes(c.v, T)));
+  return launched(launch_paged_weights(c.v, *q, lse, T, sm_scale, decay, decay != 0.f ? was : nullptr, *now, ws, (void*)stream), "weights");
 }
 
 akv_status akv_paged_evict(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const int32_t* src,

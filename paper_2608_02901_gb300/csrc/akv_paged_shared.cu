@@ -42,15 +42,13 @@ constexpr uint32_t kCols = 512, kColO = 256, kColQ = 384;  // tensor memory: S o
 
 struct SharedArgs {
   PagedView v;
-  const uint16_t* q;
-  int64_t qb, qt, qh;
+  const uint8_t* queries;  // the query rows' records
   akv_share share;
   float* part;         // [rows][T][n_q_heads] parts, and where they are
   PagedWhere* where;
   float* slots;        // [ctas][2][kRows] parts of units that several CTAs worked on
   float scale;         // sm_scale log2(e)
   int T;
-  int aligned;         // every query row begins at a multiple of 8 bytes
 };
 
 struct Smem {
@@ -159,57 +157,28 @@ __device__ __forceinline__ void next_segment(const SharedArgs& a, Segment& s, in
 
 // A unit's queries as operands, put together where the first keys will be, with what goes with its rows.  The 16 warps of both roles
 // call it at each segment's start (its barriers are theirs: the first waits for the segment before), 8 rows a warp.
-template <int NG, bool HILO>
+template <bool HILO>
 __device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, const Segment& seg, int warp) {
   const PagedView& v = a.v;
   const int lane = threadIdx.x & 31;
-  const uint32_t sign = a.scale < 0.f ? 0x80000000u : 0u;
-  named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
   constexpr int kEach = kRows / (kSoftWarps + kUnpackWarps);
-  int64_t from = -1;
-  {
-    const int tg = a.T * v.G, qi = seg.block * kRows + warp * kEach + (lane & (kEach - 1));
-    const int k = seg.k0 + qi / tg, t = qi % tg / v.G, gq = qi % tg % v.G;
-    const int b = k < seg.k0 + seg.size ? row_in_order(a, k) : -1;
-    if (b >= 0) from = b * a.qb + t * a.qt + (int64_t)(seg.h * v.G + gq) * a.qh;
-    if (lane < kEach) {
-      S.lim[warp * kEach + lane] = b >= 0 ? min(seg.tokens, held_tokens(v, b) - a.T + 1 + t) : seg.tokens;
-      S.row_at[warp * kEach + lane] = b >= 0 ? ((int64_t)b * a.T + t) * (v.H * v.G) + seg.h * v.G + gq : -1;
-    }
-  }
-  constexpr int kAhead = 4;  // rows under way
-  auto fetch = [&](int r) {
-    const int64_t at_row = __shfl_sync(0xffffffffu, from, r & (kEach - 1));
-    uint2 x = make_uint2(0, 0);
-    if (at_row >= 0 && r < kEach) {
-      const uint16_t* q = a.q + at_row + 4 * lane;
-      if (a.aligned) x = *(const uint2*)q;
-      else x = make_uint2(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16);
-    }
-    return x;
-  };
-  uint2 raw[kAhead];
-#pragma unroll
-  for (int r = 0; r < kAhead; ++r) raw[r] = fetch(r);
-#pragma unroll 1
-  for (int r = 0; r < kEach; ++r) {
-    const int rr = warp * kEach + r;
-    const uint2 now = raw[0];
-#pragma unroll
-    for (int k = 0; k + 1 < kAhead; ++k) raw[k] = raw[k + 1];
-    raw[kAhead - 1] = fetch(r + kAhead);
-    float x[4] = {row_to_float((uint16_t)now.x, v.half), row_to_float((uint16_t)(now.x >> 16), v.half),
-                  row_to_float((uint16_t)now.y, v.half), row_to_float((uint16_t)(now.y >> 16), v.half)};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign ^ (HILO ? sign_flip(v, 4 * lane + e) : 0u));
-    if (HILO) {  // q' = H (s o q) / 16
-      wht_32x4(x, lane);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
-    }
-    const int up = query_row<NG, HILO>(x, lane, rr, smem_u32(S.k[0]), S.qx);
-    if (lane == 0) S.row_scale[rr] = 0.5f * fabsf(a.scale) * pow2(-up);  // (keys enter twice as large)
-  }
+  static_assert(kEach == 8, "rows of place_queries");
+  const int tg = a.T * v.G, rr = warp * kEach + (lane & (kEach - 1)), qi = seg.block * kRows + rr;
+  const int k = seg.k0 + qi / tg, t = qi % tg / v.G, gq = qi % tg % v.G;
+  const int b = k < seg.k0 + seg.size ? row_in_order(a, k) : -1;
+  const int64_t row = b >= 0 ? ((int64_t)b * a.T + t) * (v.H * v.G) + seg.h * v.G + gq : -1;
+  const int lim = b >= 0 ? min(seg.tokens, held_tokens(v, b) - a.T + 1 + t) : seg.tokens;
+  const float down = b >= 0 ? *(const float*)(a.queries + row * kQueryRecord + 544) : 0.f;
+  named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
+  if (lane < kEach) S.lim[rr] = lim, S.row_at[rr] = row, S.row_scale[rr] = 0.5f * fabsf(a.scale) * down;  // (keys enter twice as large)
+  place_queries<HILO>(
+      lane,
+      [&](int r) {
+        const int64_t at = __shfl_sync(0xffffffffu, row, r);
+        return at < 0 ? nullptr : a.queries + at * kQueryRecord;
+      },
+      [&](int r, int& to, uint32_t& panels, uint32_t& extra) { to = warp * kEach + r, panels = smem_u32(S.k[0]), extra = smem_u32(S.qx); });
+  proxy_fence();
   named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
 }
 
@@ -238,11 +207,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     mbar_init(smem_u32(&S.drained), 1);
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  // what the sixteen extra dimensions do not use is zeros
-  if (tid < 128) {
-    sts128(smem_u32(S.qx) + 2048 + 16 * tid, make_uint4(0, 0, 0, 0));
-    proxy_fence();
   }
   Segment seg;
   const Walk w = plan(a, S, seg);
@@ -388,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       const bool more = at + seg.n < w.hi;
       if (more) next_segment(a, after, w.hi - at - seg.n);
       page = seg.n > 1 ? page_at(seg, 1) : page_at(after, 0);
-      build_queries<NG, HILO>(a, S, seg, warp);
+      build_queries<HILO>(a, S, seg, warp);
       // (the queries were put together in a key operand's place)
       ok = ok && mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
       far = seg.n > 2 ? page_at(seg, 2) : INT32_MIN;
@@ -493,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     uint32_t nseg = 0, n_tile = 0, n_ref = 0;  // n_ref: references that came from the other thread
     for (int64_t at = w.lo; at < w.hi; ++nseg) {
       if (half == 0) S.ref[row] = kLow;
-      build_queries<NG, HILO>(a, S, seg, warp);
+      build_queries<HILO>(a, S, seg, warp);
       // a thread takes its row's high or low halves into tensor memory
       if (half == 0 || HILO)
 #pragma unroll 1
@@ -508,7 +472,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
         }
       tm_wait_st();
       tc_fence_before();
-      proxy_fence();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&S.q_full));
 
@@ -791,9 +754,9 @@ int launch(const SharedArgs& a, int dev, int sms, void* stream) {
   return launch_after(kernel, dim3(sms < kMaxCtas ? sms : kMaxCtas), kThreads, smem, stream, a);
 }
 
-// Workspace: the own part's (its slots), then parts and places of both sides, then the shared part's slots.
+// Workspace: the own part's (its slots), then parts and places of both sides, the query rows' records, the shared part's slots.
 struct SharedWs {
-  size_t own_part, own_where, pre_part, pre_where, slots, total;
+  size_t own_part, own_where, pre_part, pre_where, queries, slots, total;
 };
 SharedWs shared_ws(const PagedView& v, int32_t T) {
   const size_t rows = (size_t)v.rows * T * v.H * v.G;
@@ -803,7 +766,8 @@ SharedWs shared_ws(const PagedView& v, int32_t T) {
   w.own_where = w.own_part + up(rows * kPartFloats * sizeof(float));
   w.pre_part = w.own_where + up(rows * sizeof(PagedWhere));
   w.pre_where = w.pre_part + up(rows * kPartFloats * sizeof(float));
-  w.slots = w.pre_where + up(rows * sizeof(PagedWhere));
+  w.queries = w.pre_where + up(rows * sizeof(PagedWhere));
+  w.slots = w.queries + up(rows * kQueryRecord);
   w.total = w.slots + (size_t)kMaxCtas * 2 * kRows * kPartFloats * sizeof(float);
   return w;
 }
@@ -824,19 +788,18 @@ int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& o
   own.pages = share.pages;
   own.part = (float*)(base + w.own_part);
   own.where = (PagedWhere*)(base + w.own_where);
-  int err = launch_paged_own(v, q, T, sm_scale, own, ws, stream);
+  int err = launch_paged_queries(v, q, T, sm_scale < 0.f, nullptr, base + w.queries, stream);
+  if (!err) err = launch_paged_own(v, q, T, sm_scale, own, ws, stream);
   if (err) return err;
   SharedArgs a{};
   a.v = v;
-  a.q = (const uint16_t*)q.ptr;
-  a.qb = q.stride_b, a.qt = q.stride_t, a.qh = q.stride_h;
+  a.queries = base + w.queries;
   a.share = share;
   a.part = (float*)(base + w.pre_part);
   a.where = (PagedWhere*)(base + w.pre_where);
   a.slots = (float*)(base + w.slots);
   a.scale = (float)((double)sm_scale * 1.4426950408889634);
   a.T = T;
-  a.aligned = (uintptr_t)q.ptr % 8 == 0 && q.stride_b % 4 == 0 && q.stride_t % 4 == 0 && q.stride_h % 4 == 0;
   if (v.rotate) err = v.ng == 2 ? launch<2, true>(a, dev, sms, stream) : launch<1, true>(a, dev, sms, stream);
   else err = v.ng == 2 ? launch<2, false>(a, dev, sms, stream) : launch<1, false>(a, dev, sms, stream);
   if (err) return err;

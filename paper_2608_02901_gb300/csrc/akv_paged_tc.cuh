@@ -65,6 +65,19 @@ __device__ __forceinline__ void tm_ld16(uint32_t at, float (&v)[16]) {
       : "r"(at)
       : "memory");
 }
+// The same of three places, waited for together.
+__device__ __forceinline__ void tm_ld16x3(uint32_t at0, uint32_t at1, uint32_t at2, float (&u)[16], float (&v)[16], float (&w)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%48];\n"
+      " tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%49];\n"
+      " tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47}, [%50];\n"
+      " tcgen05.wait::ld.sync.aligned;"
+      : "=f"(u[0]), "=f"(u[1]), "=f"(u[2]), "=f"(u[3]), "=f"(u[4]), "=f"(u[5]), "=f"(u[6]), "=f"(u[7]), "=f"(u[8]), "=f"(u[9]), "=f"(u[10]), "=f"(u[11]), "=f"(u[12]), "=f"(u[13]), "=f"(u[14]), "=f"(u[15]),
+        "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]), "=f"(w[4]), "=f"(w[5]), "=f"(w[6]), "=f"(w[7]), "=f"(w[8]), "=f"(w[9]), "=f"(w[10]), "=f"(w[11]), "=f"(w[12]), "=f"(w[13]), "=f"(w[14]), "=f"(w[15])
+      : "r"(at0), "r"(at1), "r"(at2)
+      : "memory");
+}
 __device__ __forceinline__ void tm_st32(uint32_t at, const float (&v)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
@@ -137,57 +150,46 @@ __device__ __forceinline__ void key_extra(const uint32_t (&words)[NG], float dow
   const uint32_t one = __half_as_ushort(__float2half_rn(ones));
   second = make_uint4(l[1] * 0x10001u, one * 0x10001u, one, 0);
 }
-// A query row, four dimensions a lane, as an operand's row: times 2^(7 - e), which is returned, so below 2^7 (its sums below 2^14) and exact in
-// fp16 down to 2^-23 of that; with HILO (rows of fp32 numbers) a low half beside, two panels on.  An infinite or NaN row spoils itself alone.
-template <int NG, bool HILO>
-__device__ __forceinline__ int query_row(const float (&x)[4], int lane, int row, uint32_t panels, uint8_t* extra) {
-  float big = 0.f;
+// Butterfly of R rows side by side (a row by itself waits for each of its exchanges).
+template <int R>
+__device__ __forceinline__ void wht_rows(float (&x)[R][4], int lane) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float y = fabsf(x[e]);
-    if (y <= 3.402823466e38f) big = fmaxf(big, y);
+  for (int r = 0; r < R; ++r) {
+    const float a = x[r][0] + x[r][1], b = x[r][0] - x[r][1], c = x[r][2] + x[r][3], d = x[r][2] - x[r][3];
+    x[r][0] = a + c, x[r][1] = b + d, x[r][2] = a - c, x[r][3] = b - d;
   }
-  big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-  const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
-  const float up = pow2(7 - e2);
-  float sum = (x[0] + x[1]) + (x[2] + x[3]);
 #pragma unroll
-  for (int m = 1; m < 32 / NG; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-  uint4 f[HILO ? 2 : 1];
+  for (int h = 1; h < 32; h *= 2)
 #pragma unroll
-  for (int lo = 0; lo < (HILO ? 2 : 1); ++lo) {
-    uint32_t y[4];
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float z = x[e] * up, hi = __half2float(__float2half_rn(z)), mine = lo ? z - hi : z;
-      const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
-      y[e] = lane & 1 ? half2_bits(other, mine) : half2_bits(mine, other);
-    }
-    f[lo] = make_uint4(y[0], y[1], y[2], y[3]);
+      for (int e = 0; e < 4; ++e) {
+        const float o = __shfl_xor_sync(0xffffffffu, x[r][e], h);
+        x[r][e] = lane & h ? o - x[r][e] : x[r][e] + o;
+      }
+}
+// Eight query rows of akv_paged_query.cu by a warp: from their records (null: zeros) into operand panels (hi, with HILO low halves two panels on) and
+// the 16 more dimensions; record(r), then place(r, row, panels, extra).  All loads come first: each would wait for the store before it.
+template <bool HILO, class Record, class Place>
+__device__ __forceinline__ void place_queries(int lane, Record record, Place place) {
+  uint4 x[8], y[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const uint8_t* from = record(r);
+    x[r] = y[r] = make_uint4(0, 0, 0, 0);
+    if (from && (HILO || lane < 16)) x[r] = *(const uint4*)(from + 16 * lane);
+    if (from && lane < 2) y[r] = *(const uint4*)(from + 512 + 16 * lane);
   }
-  // lanes 2 x, 2 x + 1 hold dimensions 8 x .. of word j = x / 4, t = x % 4
-  const int j = lane >> 3, chunk = ((j & 1) * 4 + (lane >> 1 & 3)) ^ (row & 7);
-  const uint32_t to = panels + (uint32_t)(j >> 1) * kPanel + 128 * row + 16 * chunk;
-  if (!(lane & 1)) sts128(to, f[0]);
-  if (HILO && (lane & 1)) sts128(to + 2 * kPanel, f[HILO ? 1 : 0]);
-  // a group's sum in three parts (lanes 0 and 16)
-  if ((lane & 15) == 0) {
-    float z = lane == 0 || NG == 2 ? sum * up : 0.f;
-    uint16_t y[3];
+  const int c = lane & 15;  // chunk 4 j + t: panel j / 2, chunk 4 (j & 1) + t of it
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const __half p = __float2half_rn(z);
-      y[i] = __half_as_ushort(p);
-      z -= __half2float(p);
-    }
-    const int first = lane ? 5 : 0;
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      const int at = first + i;
-      *(uint16_t*)(extra + extra_at(row) + (at >> 3) * 2048 + 2 * (at & 7)) = y[i < 3 ? i : i - 3];
-    }
+  for (int r = 0; r < 8; ++r) {
+    int row;
+    uint32_t panels, extra;
+    place(r, row, panels, extra);
+    if (HILO || lane < 16)
+      sts128(panels + (uint32_t)(lane >> 4) * (2 * kPanel) + (uint32_t)(c >> 3) * kPanel + 128 * row + 16 * ((c & 7) ^ (row & 7)), x[r]);
+    if (lane < 2) sts128(extra + extra_at(row) + 2048 * lane, y[r]);
   }
-  return 7 - e2;
 }
 // Operand of 16 K without swizzle: [2][16][8 rows][16 bytes], 2048 bytes from one half of K to the other, 128 between groups of rows.
 __device__ __forceinline__ uint64_t plain_desc(uint32_t saddr) {

@@ -28,6 +28,7 @@ constexpr float kInf = __builtin_huge_valf();
 struct WeightArgs {
   PagedView v;
   const uint16_t* q;
+  const uint8_t* queries;  // many rows: their records
   const float* lse;
   const float* was;
   float* now;
@@ -100,35 +101,50 @@ __device__ __forceinline__ bool plan(const WeightArgs& a, int64_t* part, int64_t
   return true;
 }
 
-// A query row's four values a lane, rotated where the cache is, times the sign of the scale; zeros, and lse infinite, where the row adds nothing:
-// no finite lse, or an infinity or a NaN of its own.
-template <bool HILO>
-__device__ __forceinline__ void load_row(const WeightArgs& a, const Segment& seg, int row, float (&x)[4], float& lse) {
-  const PagedView& v = a.v;
-  const int lane = threadIdx.x & 31, t = row / v.G, g = row % v.G;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = 0.f;
-  lse = kInf;
+// A query row as it lies in memory, four values a lane.
+struct RowRaw {
+  uint2 x;
+  float lse;
+};
+__device__ __forceinline__ RowRaw fetch_row(const WeightArgs& a, const Segment& seg, int row) {
+  RowRaw r{make_uint2(0, 0), kInf};
   if (row < a.rows) {
+    const PagedView& v = a.v;
+    const int lane = threadIdx.x & 31, t = row / v.G, g = row % v.G;
     const uint16_t* q = a.q + seg.b * a.qb + t * a.qt + (int64_t)(seg.h * v.G + g) * a.qh + 4 * lane;
-    const uint2 raw = a.aligned ? *(const uint2*)q : make_uint2(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16);
-    x[0] = row_to_float((uint16_t)raw.x, v.half), x[1] = row_to_float((uint16_t)(raw.x >> 16), v.half);
-    x[2] = row_to_float((uint16_t)raw.y, v.half), x[3] = row_to_float((uint16_t)(raw.y >> 16), v.half);
-    lse = a.lse[((int64_t)seg.b * a.T + t) * (v.H * v.G) + seg.h * v.G + g];
+    r.x = a.aligned ? *(const uint2*)q : make_uint2(q[0] | (uint32_t)q[1] << 16, q[2] | (uint32_t)q[3] << 16);
+    r.lse = a.lse[((int64_t)seg.b * a.T + t) * (v.H * v.G) + seg.h * v.G + g];
   }
-  const bool fine = fabsf(lse) < kInf && fabsf(x[0]) < kInf && fabsf(x[1]) < kInf && fabsf(x[2]) < kInf && fabsf(x[3]) < kInf;
-  if (!__all_sync(0xffffffffu, fine)) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = 0.f;
-    lse = kInf;
-  }
+  return r;
+}
+// R rows' values, rotated where the cache is, times the sign of the scale; zeros, and lse infinite, where a row adds nothing: no finite lse, or an
+// infinity or a NaN of its own.
+template <bool HILO, int R>
+__device__ __forceinline__ void open_rows(const WeightArgs& a, const RowRaw (&raw)[R], float (&x)[R][4], float (&lse)[R]) {
+  const PagedView& v = a.v;
+  const int lane = threadIdx.x & 31;
   const uint32_t sign = a.scale < 0.f ? 0x80000000u : 0u;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(__float_as_uint(x[e]) ^ sign ^ (HILO ? sign_flip(v, 4 * lane + e) : 0u));
-  if (HILO) {  // q' = H (s o q) / 16
-    wht_32x4(x, lane);
+  for (int r = 0; r < R; ++r) {
+    lse[r] = raw[r].lse;
+    bool fine = fabsf(lse[r]) < kInf;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] *= 0.0625f;
+    for (int e = 0; e < 4; ++e) {
+      x[r][e] = row_to_float((uint16_t)((e < 2 ? raw[r].x.x : raw[r].x.y) >> (16 * (e & 1))), v.half);
+      fine = fine && fabsf(x[r][e]) < kInf;
+    }
+    const bool counts = __all_sync(0xffffffffu, fine);
+    if (!counts) lse[r] = kInf;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[r][e] = counts ? __uint_as_float(__float_as_uint(x[r][e]) ^ sign ^ (HILO ? sign_flip(v, 4 * lane + e) : 0u)) : 0.f;
+  }
+  if (HILO) {  // q' = H (s o q) / 16
+    wht_rows(x, lane);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[r][e] *= 0.0625f;
   }
 }
 // lse in log2 units as fp32 and what that leaves out.
@@ -230,8 +246,11 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
     __syncthreads();
 #pragma unroll 1
     for (int rr = warp; rr < 8 * NT; rr += kFewWarps) {
-      float x[4], lse;
-      load_row<HILO>(a, seg, rr, x, lse);
+      const RowRaw raw[1] = {fetch_row(a, seg, rr)};
+      float x1[1][4], lse1[1];
+      open_rows<HILO>(a, raw, x1, lse1);
+      const float(&x)[4] = x1[0];
+      const float lse = lse1[0];
       float big = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
       big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
       const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
@@ -366,12 +385,12 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
 }
 
 // ---- many query rows ----------------------------------------------------------------------------
-// Two warpgroups take the tiles in turn, a warp issues the products, 64 columns a time.  Queries of up to 256 rows lie in shared memory as
+// Two warpgroups take the tiles in turn, a warp for each issues its products, 32 columns a time into two buffers.  Queries of up to 256 rows lie in shared memory as
 // operands; a unit with more goes over its tiles again for each 256.
 
 constexpr int W = 2, kWorkers = 4 * W, kThreads = 128 * (W + 1);
-constexpr int kCols = 64, kBlocks = 4, kHeld = kBlocks * kCols;  // query rows of a product, and in shared memory
-// Tensor memory: the warpgroups' keys, then their sums over the first group of dimensions (or all), the second, and the rest
+constexpr int kCols = 32, kBlocks = 8, kHeld = kBlocks * kCols;  // query rows of a product, and in shared memory
+// Tensor memory: the warpgroups' keys, then of each two buffers of sums over the first group of dimensions (or all), the second, and the rest
 constexpr uint32_t kColK = 0, kColS = 64 * W, kColsS = 3 * kCols;
 constexpr float kOnes = 16.f;  // the dimensions that carry lse count 16
 
@@ -381,7 +400,7 @@ struct Smem {
   float k[kHeld], lse[kHeld];  // what a row's products count; the part of -lse behind them (-infinity: the row adds nothing)
   int sees[kHeld];             // tokens that it sees
   int behind[kBlocks];         // whether a block has rows with such a part
-  uint64_t k_full[W], s_full[W], s_free[W], q_full, drained;
+  uint64_t k_full[W], s_full[W][2], s_free[W][2], q_full, drained[W];
   int64_t part[4 * W + 4], place[2];
   uint32_t tmem;
   int failed;
@@ -399,16 +418,16 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
   if (tid == 0) {
     for (int w = 0; w < W; ++w) {
       mbar_init(smem_u32(&S.k_full[w]), 4);
-      mbar_init(smem_u32(&S.s_full[w]), 1);
-      mbar_init(smem_u32(&S.s_free[w]), 4);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(smem_u32(&S.s_full[w][b]), 1);
+        mbar_init(smem_u32(&S.s_free[w][b]), 4);
+      }
     }
     mbar_init(smem_u32(&S.q_full), kWorkers);
-    mbar_init(smem_u32(&S.drained), 1);
+    for (int w = 0; w < W; ++w) mbar_init(smem_u32(&S.drained[w]), 1);
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // what the sixteen extra dimensions do not use is zeros
-  for (int k = tid; k < 256; k += kThreads) sts128(smem_u32(S.qx) + k / 128 * kExtra + 2048 + 16 * (k % 128), make_uint4(0, 0, 0, 0));
   wait_for_stream();
   Segment seg;
   int64_t lo, hi;
@@ -422,63 +441,62 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
   auto rows_of = [&](int pass) { return min(kHeld, a.rows - pass * kHeld); };
   auto columns = [](int rows, int block) { return min(kCols, (rows - block * kCols + 15) & ~15); };
 
-  if (warp == kWorkers) {
-    // ---- the products: the warpgroups' tiles side by side, their blocks of columns in turn
-    uint32_t nk[W], ns[W], nq = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) nk[w] = ns[w] = 0;
+  if (warp >= kWorkers && warp < kWorkers + W) {
+    // ---- the products of a warpgroup's tiles, a block of columns after the other
+    const int w = warp - kWorkers;
+    uint32_t n_k = 0, n_s = 0, n_q = 0;
     bool ok = true;
+    const uint32_t k = tmem + kColK + 64 * w, d0 = tmem + kColS + 2 * kColsS * w;
+    const uint64_t dkx = plain_desc(smem_u32(S.kx[w]));
     for (int64_t at = lo; ok && at < hi;) {
       for (int pass = 0; ok && pass < passes; ++pass) {
         const int rows = rows_of(pass), blocks = (rows + kCols - 1) / kCols;
-        ok = mbar_wait_w(smem_u32(&S.q_full), nq++ & 1);
+        ok = mbar_wait_w(smem_u32(&S.q_full), n_q++ & 1);
 #pragma unroll 1
-        for (int i0 = 0; ok && i0 < seg.n; i0 += W)
+        for (int i = w; ok && i < seg.n; i += W) {
+          ok = mbar_wait_w(smem_u32(&S.k_full[w]), n_k++ & 1) && !warp_failed(failed);
 #pragma unroll 1
-          for (int block = 0; ok && block < blocks; ++block) {
+          for (int block = 0; ok && block < blocks; ++block, ++n_s) {
             const uint32_t n = (uint32_t)columns(rows, block), idesc = (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24);
-            const uint32_t rows_at = (uint32_t)(block & 1) * (kCols * 128);  // of a panel
+            const int held_at = block * kCols / 128, row_at = block * kCols % 128;  // the block's rows
+            const uint32_t b = n_s & 1;
+            ok = mbar_wait_w(smem_u32(&S.s_free[w][b]), (n_s >> 1 & 1) ^ 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t d = d0 + kColsS * b;
+              const uint64_t dq = sw128_desc(smem_u32(S.q[held_at]) + 128 * row_at);
+              auto product = [&](uint32_t to, int first_step, int steps, uint64_t desc, bool first) {
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-              if (!ok || i0 + w >= seg.n) break;
-              if (block == 0) ok = mbar_wait_w(smem_u32(&S.k_full[w]), nk[w]++ & 1);
-              ok = ok && mbar_wait_w(smem_u32(&S.s_free[w]), (ns[w]++ & 1) ^ 1) && !warp_failed(failed);
-              if (!ok) break;
-              tc_fence_after();
-              if (elect_one()) {
-                const uint32_t d = tmem + kColS + kColsS * w, k = tmem + kColK + 64 * w;
-                const uint64_t dq = sw128_desc(smem_u32(S.q[block >> 1]) + rows_at);
-                auto product = [&](uint32_t to, int first_step, int steps, uint64_t desc, bool first) {
-#pragma unroll
-                  for (int i = 0; i < steps; ++i) {
-                    const int kk = first_step + i;
-                    tc_mma_ts(to, k + 8 * kk, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || i > 0);
-                  }
-                };
-                constexpr uint64_t low = 2 * kPanel >> 4;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                  if (HILO) product(d + kCols * g, 8 / NG * g, 8 / NG, dq + low, true);
-                  product(d + kCols * g, 8 / NG * g, 8 / NG, dq, !HILO);
+                for (int i = 0; i < steps; ++i) {
+                  const int kk = first_step + i;
+                  tc_mma_ts(to, k + 8 * kk, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || i > 0);
                 }
-                tc_mma(d + 2 * kCols, plain_desc(smem_u32(S.kx[w])), plain_desc(smem_u32(S.qx[block >> 1]) + extra_at(kCols * (block & 1))), idesc, 0);
-                tc_commit(smem_u32(&S.s_full[w]));
+              };
+              constexpr uint64_t low = 2 * kPanel >> 4;
+#pragma unroll
+              for (int g = 0; g < NG; ++g) {
+                if (HILO) product(d + kCols * g, 8 / NG * g, 8 / NG, dq + low, true);
+                product(d + kCols * g, 8 / NG * g, 8 / NG, dq, !HILO);
               }
-              __syncwarp();
+              tc_mma(d + 2 * kCols, dkx, plain_desc(smem_u32(S.qx[held_at]) + extra_at(row_at)), idesc, 0);
+              tc_commit(smem_u32(&S.s_full[w][b]));
             }
+            __syncwarp();
           }
+        }
       }
       at += seg.n;
       if (at < hi) next_segment(a, seg, hi - at);
     }
     if (!ok) *failed = 1;
-    if (elect_one()) tc_commit(smem_u32(&S.drained));
+    if (elect_one()) tc_commit(smem_u32(&S.drained[w]));
     __syncwarp();
-    mbar_wait_w(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
+    mbar_wait_w(smem_u32(&S.drained[w]), 0);  // nothing is under way when tensor memory is given back
   } else if (warp < kWorkers) {
     // ---- a warpgroup, a thread a token
     const int w = warp >> 2, token = tid & 127;
-    const uint32_t lane_at = tmem + ((uint32_t)((warp & 3) * 32) << 16), tK = lane_at + kColK + 64 * w, tS = lane_at + kColS + kColsS * w;
+    const uint32_t lane_at = tmem + ((uint32_t)((warp & 3) * 32) << 16), tK = lane_at + kColK + 64 * w, tS0 = lane_at + kColS + 2 * kColsS * w;
     const uint32_t kx_at = smem_u32(S.kx[w]) + extra_at(token);
     const KeyCodes codes;
     uint32_t n_s = 0;
@@ -519,34 +537,48 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
       float* now = a.now + seg.b * a.nb + seg.h * a.nh;
       for (int pass = 0; pass < passes; ++pass) {
         const int rows = rows_of(pass), blocks = (rows + kCols - 1) / kCols;
-        // queries as operands, a warp a row (the products of the pass before have been waited for by every warpgroup)
+        // queries as operands (the products of the pass before have been waited for by every warpgroup)
         named_sync(1, 32 * kWorkers);
         if (tid < kBlocks) S.behind[tid] = 0;
         named_sync(1, 32 * kWorkers);
         const int padded = (blocks - 1) * kCols + columns(rows, blocks - 1);
+        auto record_of = [&](int rr) {
+          const int row = pass * kHeld + rr, t = row / v.G, g = row % v.G;
+          return rr < rows ? a.queries + (((int64_t)seg.b * a.T + t) * (v.H * v.G) + seg.h * v.G + g) * kQueryRecord : nullptr;
+        };
+        float2 own = make_float2(1.f, 0.f);
+        float lse = kInf;
+        if (tid < rows) {
+          const int row = pass * kHeld + tid;
+          own = *(const float2*)(record_of(tid) + 544);
+          lse = a.lse[((int64_t)seg.b * a.T + row / v.G) * (v.H * v.G) + seg.h * v.G + row % v.G];
+        }
 #pragma unroll 1
-        for (int rr = warp; rr < padded; rr += kWorkers) {
-          float x[4], lse;
-          load_row<HILO>(a, seg, rr < rows ? pass * kHeld + rr : a.rows, x, lse);
-          const int up = query_row<NG, HILO>(x, lane, rr & 127, smem_u32(S.q[rr >> 7]), S.qx[rr >> 7]);
-          if (lane == 0) {
-            // -lse goes with the products in three parts where it fits them (rows so small that it does not: behind them)
-            const float k = 0.5f * fabsf(a.scale) * pow2(-up);  // (keys enter twice as large)
-            float l, rest;
-            lse_log2(lse, l, rest);
-            float in = -l / k * (1.f / kOnes), in_rest = fmaf(-in * kOnes, k, -l) / k * (1.f / kOnes) - rest / k * (1.f / kOnes);
-            const bool fits = fabsf(in) < 32768.f;
-            if (!fits) in = in_rest = 0.f, S.behind[rr / kCols] = 1;
-            uint16_t* to = (uint16_t*)(S.qx[rr >> 7] + extra_at(rr & 127) + 2048) + 2;
+        for (int r0 = 8 * warp; r0 < padded; r0 += 8 * kWorkers)  // (padded is a multiple of 16)
+          place_queries<HILO>(
+              lane, [&](int r) { return record_of(r0 + r); },
+              [&](int r, int& row, uint32_t& panels, uint32_t& extra) {
+                row = (r0 + r) & 127, panels = smem_u32(S.q[r0 >> 7]), extra = smem_u32(S.qx[r0 >> 7]);
+              });
+        named_sync(1, 32 * kWorkers);
+        // -lse goes with the products in three parts where it fits them (rows so small that it does not: behind them); a thread a row
+        if (tid < padded) {
+          if (own.y == 0.f) lse = kInf;
+          const float k = 0.5f * fabsf(a.scale) * own.x, inv = 1.f / (k * kOnes);  // (keys enter twice as large)
+          float l, rest;
+          lse_log2(lse, l, rest);
+          float in = -l * inv, in_rest = (fmaf(-in * kOnes, k, -l) - rest) * inv;
+          const bool fits = fabsf(in) < 32768.f;
+          if (!fits) in = in_rest = 0.f, S.behind[tid / kCols] = 1;
+          uint16_t* to = (uint16_t*)(S.qx[tid >> 7] + extra_at(tid & 127) + 2048) + 2;
 #pragma unroll
-            for (int i = 0; i < 3; ++i) {
-              const __half p = __float2half_rn(in);
-              to[i] = __half_as_ushort(p);
-              in = in - __half2float(p) + (i == 0 ? in_rest : 0.f);
-            }
-            S.k[rr] = k, S.lse[rr] = fits ? 0.f : -l;
-            S.sees[rr] = min(seg.held, seg.held - a.T + 1 + (pass * kHeld + rr) / v.G);
+          for (int i = 0; i < 3; ++i) {
+            const __half p = __float2half_rn(in);
+            to[i] = __half_as_ushort(p);
+            in = in - __half2float(p) + (i == 0 ? in_rest : 0.f);
           }
+          S.k[tid] = k, S.lse[tid] = fits ? 0.f : -l;
+          S.sees[tid] = min(seg.held, seg.held - a.T + 1 + (pass * kHeld + tid) / v.G);
         }
         proxy_fence();
         __syncwarp();
@@ -605,7 +637,9 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
           const float2 s0 = make_float2(scale[0], scale[0]), s1 = make_float2(scale[NG - 1], scale[NG - 1]), b2 = make_float2(back, back);
 #pragma unroll 1
           for (int block = 0; block < blocks; ++block) {
-            if (!ok || warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[w]), n_s++ & 1)) {
+            const uint32_t b = n_s & 1, use = n_s >> 1 & 1, tS = tS0 + kColsS * b;
+            ++n_s;
+            if (!ok || warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[w][b]), use)) {
               ok = false;
               break;
             }
@@ -615,9 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
 #pragma unroll 1
             for (int c = 0; c < n; c += 16) {
               float x[16], y[16], z[16];
-              tm_ld16(tS + c, x);
-              if (NG == 2) tm_ld16(tS + kCols + c, y);
-              tm_ld16(tS + 2 * kCols + c, z);
+              tm_ld16x3(tS + c, tS + (NG - 1) * kCols + c, tS + 2 * kCols + c, x, y, z);
               const float2* k2 = (const float2*)&S.k[block * kCols + c];
 #pragma unroll
               for (int e = 0; e < 16; e += 2) {
@@ -638,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&S.s_free[w]));
+            if (lane == 0) mbar_arrive(smem_u32(&S.s_free[w][b]));
           }
           if (held) now[tok] = ok ? (fine ? old + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y)) : old) : __int_as_float(0x7fffffff);
         }
@@ -662,11 +694,12 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
   if (warp == kWorkers) tc_dealloc(tmem, 512);
 }
 
+constexpr int kFew = 16;  // query rows up to which the first kernel is the faster one
+
 template <int NG, bool HILO>
 int launch(const WeightArgs& a, int dev, int sms, void* stream) {
-  // (16 rows and fewer: see the top)
   if (a.rows <= 8) return launch_after(akv_paged_weights_few_kernel<NG, 1, HILO>, dim3(2 * sms), kFewThreads, 0, stream, a);
-  if (a.rows <= 16) return launch_after(akv_paged_weights_few_kernel<NG, 2, HILO>, dim3(2 * sms), kFewThreads, 0, stream, a);
+  if (a.rows <= kFew) return launch_after(akv_paged_weights_few_kernel<NG, 2, HILO>, dim3(2 * sms), kFewThreads, 0, stream, a);
   auto* kernel = akv_paged_weights_kernel<NG, HILO>;
   constexpr size_t smem = sizeof(Smem) + 1024;
   static_assert(smem <= 232448, "shared memory of a CTA");
@@ -682,8 +715,12 @@ int launch(const WeightArgs& a, int dev, int sms, void* stream) {
 
 }  // namespace
 
+size_t paged_weights_ws_bytes(const PagedView& v, int32_t T) {
+  return T * v.G <= kFew ? 256 : ((size_t)v.rows * T * v.H * v.G * kQueryRecord + 255) & ~(size_t)255;
+}
+
 int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse, int32_t T, float sm_scale, float decay,
-                         const akv_scores* was, const akv_scores& now, void* stream) {
+                         const akv_scores* was, const akv_scores& now, void* ws, void* stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -700,6 +737,11 @@ int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse
   a.decay = decay;
   a.T = T;
   a.rows = T * v.G;
+  if (a.rows > kFew) {
+    a.queries = (const uint8_t*)ws;
+    const int err = launch_paged_queries(v, q, T, sm_scale < 0.f, lse, ws, stream);
+    if (err) return err;
+  }
   if (v.rotate) return v.ng == 2 ? launch<2, true>(a, dev, sms, stream) : launch<1, true>(a, dev, sms, stream);
   return v.ng == 2 ? launch<2, false>(a, dev, sms, stream) : launch<1, false>(a, dev, sms, stream);
 }

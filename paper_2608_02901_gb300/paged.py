@@ -18,7 +18,8 @@ EXPORTED = (
     "akv_paged_page_bytes", "akv_paged_append", "akv_paged_read", "akv_paged_attn_workspace_size", "akv_paged_attn",
     "akv_paged_select_workspace_size", "akv_paged_select", "akv_pages_copy", "akv_pages_fork",
     "akv_pages_workspace_size", "akv_pages_reserve", "akv_pages_free", "akv_pages_compact", "akv_pages_share",
-    "akv_paged_attn_shared_workspace_size", "akv_paged_attn_shared", "akv_paged_weights", "akv_paged_evict", "akv_pages_trim",
+    "akv_paged_attn_shared_workspace_size", "akv_paged_attn_shared", "akv_paged_weights_workspace_size", "akv_paged_weights",
+    "akv_paged_evict", "akv_pages_trim",
 )
 
 _vp, _i32, _i64, _sz, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
@@ -76,7 +77,8 @@ def declare(L):
             ("akv_pages_share", [P, G, H, _vp, _sz, _vp]),
             ("akv_paged_attn_shared_workspace_size", [P, G, _i32, out]),
             ("akv_paged_attn_shared", [P, G, _i32, R, R, _vp, _i32, _f32, H, _vp, _sz, _vp]),
-            ("akv_paged_weights", [P, G, _i32, R, _vp, _i32, _f32, _f32, N, N, _vp]),
+            ("akv_paged_weights_workspace_size", [P, G, _i32, out]),
+            ("akv_paged_weights", [P, G, _i32, R, _vp, _i32, _f32, _f32, N, N, _vp, _sz, _vp]),
             ("akv_paged_evict", [P, G, _i32, _vp, _vp, _i32, N, _vp, _i32, _i32, K, _vp]),
             ("akv_pages_trim", [P, G, _vp, _i32, _vp])):
         f = getattr(L, name)
@@ -412,18 +414,27 @@ def _scores(t, what, p: PagedParams, pages: Pages):
     return _Scores(t.data_ptr(), sb, sh, min(t.shape[2], 2**31 - 1))
 
 
+def akv_paged_weights_workspace_size(p: PagedParams, pages: Pages, T: int = 1) -> int:
+    n = _sz()
+    _check(_lib().akv_paged_weights_workspace_size(_params(p, pages), pages.ref, T, ctypes.byref(n)),
+           "akv_paged_weights_workspace_size")
+    return n.value
+
+
 def akv_paged_weights(p: PagedParams, pages: Pages, q, lse, now, was=None, decay: float = 1.0, sm_scale: float = 1.0,
-                      layer: int = 0, stream=None):
+                      layer: int = 0, ws=None, stream=None):
     """now = decay was + the attention weights of the last T query tokens.  q: [rows][T][n_q_heads][128], lse of
-    akv_paged_attn; now, was: fp32 [rows][n_kv_heads][cap], was None (zeros) or now itself."""
+    akv_paged_attn; now, was: fp32 [rows][n_kv_heads][cap], was None (zeros) or now itself.  ws as there, of
+    akv_paged_weights_workspace_size bytes."""
     if _device() != pages.index:
-        return _there(pages, akv_paged_weights, p, pages, q, lse, now, was, decay, sm_scale, layer, stream)
+        return _there(pages, akv_paged_weights, p, pages, q, lse, now, was, decay, sm_scale, layer, ws, stream)
     T = _tokens(q, "q")
     L = _lib()
+    ws, at, n = _workspace(ws, pages, stream, akv_paged_weights_workspace_size, p, pages, T)
     _check(L.akv_paged_weights(_params(p, pages), pages.ref, layer, _rows(q, "q", p, pages, T, p.n_q_heads),
                                _lse(lse, p, pages, T), T, sm_scale, decay,
                                None if was is None else _scores(was, "was", p, pages), _scores(now, "now", p, pages),
-                               _stream(stream, pages)), "akv_paged_weights")
+                               at, n, _stream(stream, pages)), "akv_paged_weights")
 
 
 def akv_paged_evict(p: PagedParams, pages: Pages, src, dst, scores, kept: KeptTokens, keep=None, sink: int = 0,

@@ -50,8 +50,9 @@ def attn(p=None, g=None, layer=0, q=None, out=None, lse=None, T=1, sm=1.0, sh=sh
     return ("akv_paged_attn_shared", p or params(), g or pages(), layer, q or rows(), out or rows(), lse, T, sm, sh() if sh else None, ws, n, None)
 
 
-def weights(p=None, g=None, layer=0, q=None, lse=AT, T=1, sm=1.0, decay=1.0, was=None, now=scores):
-    return ("akv_paged_weights", p or params(), g or pages(), layer, q or rows(), lse, T, sm, decay, was() if was else None, now() if now else None, None)
+def weights(p=None, g=None, layer=0, q=None, lse=AT, T=1, sm=1.0, decay=1.0, was=None, now=scores, ws=AT, n=WS):
+    return ("akv_paged_weights", p or params(), g or pages(), layer, q or rows(), lse, T, sm, decay, was() if was else None, now() if now else None,
+            ws, n, None)
 
 
 def evict(p=None, g=None, layer=0, src=AT, dst=AT, n=2, sc=scores, keep=None, sink=1, recent=1, k=kept):
@@ -133,6 +134,14 @@ def test_weights():
     for kw in (dict(stride_h=159), dict(stride_b=319), dict(stride_b=0), dict(stride_h=0)):
         refused(INVALID, "now: heads' numbers overlap", *weights(now=lambda: scores(**kw)))
     refused(INVALID, "out of range", *weights(now=lambda: scores(stride_b=2**61)))
+    size = ctypes.c_size_t()
+    for T in (1, 9):
+        assert call("akv_paged_weights_workspace_size", params(), pages(), T, ctypes.byref(size)) == OK
+        refused(TOO_SMALL, "workspace", *weights(T=T, n=size.value - 1))
+    for ws in (None, AT + 8):
+        refused(INVALID, "workspace", *weights(ws=ws))
+    refused(UNSUPPORTED, "query tokens", "akv_paged_weights_workspace_size", params(), pages(), 0, ctypes.byref(size))
+    refused(INVALID, "null ws_bytes", "akv_paged_weights_workspace_size", params(), pages(), 1, None)
 
 
 def test_evict():
