@@ -8,9 +8,9 @@
 //     it turns the codes into its lane of the operand in tensor memory, applies the token's scales to the products behind them,
 //     and adds its weights up along its lane without a shuffle; the queries are the columns.
 // In both, tiles of all units (request, KV head) go in equal contiguous ranges to the CTAs.
-//   With codes 2 c - 15 or c in the products and a's outside, a logit is
-//     k (a_0 S_0 + a_1 S_1 + (2 m_0 + 15 a_0) sum q_0 + (2 m_1 + 15 a_1) sum q_1)
-// over the groups of dimensions, and a weight 2 to that less lse, which is subtracted in such parts that it costs no rounding of its own.
+//   With codes in the products and scales outside, a logit is k (a_0 S_0 + a_1 S_1 + m_0 sum q_0 + m_1 sum q_1) over the groups of dimensions (of many
+// rows with 2 c - 15 for c and 2 m + 15 a for m), and a weight 2 to that less lse, which is subtracted in such parts that it costs no
+// rounding of its own.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -159,8 +159,7 @@ __device__ __forceinline__ float word_min(uint32_t w) { return __half2float(__us
 __device__ __forceinline__ uint32_t comp(const uint4& x, int j) { return j == 0 ? x.x : j == 1 ? x.y : j == 2 ? x.z : x.w; }
 
 // ---- few query rows -----------------------------------------------------------------------------
-// A warp takes two sub-blocks of 16 tokens at a time (of 16 rows one), the next on their way meanwhile, their pages known a step earlier still, and what
-// comes a few steps later on its way into L2.
+// A warp takes two sub-blocks of 16 tokens at a time (of 16 rows one), the next on their way meanwhile, their pages known a step earlier still.
 
 constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps;
 
@@ -173,8 +172,9 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
 template <int NT>
 struct FewSmem {
   uint4 frag[2][NT][4][32];     // query operand: high, low halves
-  // of a row, in what its products count: sums over each group, k, -lse (the part behind the products, and the one before)
-  float qsum[8 * NT][2], k[8 * NT], lse[8 * NT], lse_in[8 * NT];
+  // of a row, in what its products count: sums over each group, the part of -lse that goes with them; what they count, the rest of -lse
+  float2 qsum[8 * NT], k[8 * NT];
+  float lse_in[8 * NT];
   int64_t part[kFewWarps], place[2];
 };
 
@@ -258,14 +258,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
       float sum = (x[0] + x[1]) + (x[2] + x[3]);
 #pragma unroll
       for (int s = 1; s < 32 / NG; s *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-      if (lane % (32 / NG) == 0) S.qsum[rr][lane / (32 / NG)] = sum * up;
+      // (codes count 2^-24 in the products, and so does what is added to them)
+      if (lane % (32 / NG) == 0) ((float*)&S.qsum[rr])[lane / (32 / NG)] = sum * up * 5.9604644775390625e-8f;
       if (lane == 0) {
-        const float k = 0.5f * fabsf(a.scale) * pow2(e2 - 14);
+        const float k = fabsf(a.scale) * pow2(e2 - 10) * 1048576.f;
         float l, rest;
         lse_log2(lse, l, rest);
         const float coarse = fabsf(l) < 8192.f ? rintf(l * 256.f) * 0.00390625f : l;
         const float in = (rest + (l - coarse)) / k;  // (rows so small that their logits hardly differ: not worth it)
-        S.k[rr] = k, S.lse[rr] = -coarse, S.lse_in[rr] = fabsf(in) < 1e30f ? -in : 0.f;
+        S.k[rr] = make_float2(k, -coarse), S.lse_in[rr] = fabsf(in) < 1e30f ? -in : 0.f;
       }
       uint4 f[HILO ? 2 : 1];
 #pragma unroll
@@ -300,11 +301,6 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
       for (int i = 0; i < kSubs; ++i) {
         next[i] = load(s0 + kStep + i, page[i]);
         page[i] = far[i];
-        if (lane == 0 && (uint32_t)far[i] < (uint32_t)v.n_pages) {
-          const uint8_t* p = place(s0 + 2 * kStep + i, far[i]);
-          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(1024) : "memory");
-          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p + 2048), "r"(128 * NG) : "memory");
-        }
         far[i] = page_at(s0 + 3 * kStep + i);
       }
       float old[kSubs][2], sum[kSubs][2];
@@ -316,53 +312,69 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
           old[i][y] = was && t4 == 0 && tok < seg.held && s0 + i < end ? was[tok] : 0.f;
           sum[i][y] = 0.f;
         }
+      const bool edge = 16 * (s0 + kSubs) > sees0;  // some row may not see some token
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        // products of tokens g8 and g8 + 8 with query rows 2 t4 and 2 t4 + 1 over 64 dimensions each, the low halves first; 2^-24 of codes from 0
+        // products of tokens g8 and g8 + 8 with query rows 2 t4 and 2 t4 + 1 over 64 dimensions each, the low halves first
         float z[kSubs][4];
+        float2 qsum[2], k[2];
+        float lse_in[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) qsum[r] = S.qsum[8 * nt + 2 * t4 + r], k[r] = S.k[8 * nt + 2 * t4 + r], lse_in[r] = S.lse_in[8 * nt + 2 * t4 + r];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           float d[kSubs][4];
 #pragma unroll
           for (int i = 0; i < kSubs; ++i) d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.f;
 #pragma unroll
-          for (int part = HILO ? 1 : 0; part >= 0; --part)
+          for (int j = 2 * half; j < 2 * half + 2; ++j) {
+            uint4 q[HILO ? 2 : 1];
 #pragma unroll
-            for (int j = 2 * half; j < 2 * half + 2; ++j) {
-              const uint4 q = S.frag[part][nt][j][lane];
+            for (int part = 0; part < (HILO ? 2 : 1); ++part) q[part] = S.frag[part][nt][j][lane];
 #pragma unroll
-              for (int i = 0; i < kSubs; ++i) {
-                const uint32_t x0 = comp(x[i].c[0], j), x1 = comp(x[i].c[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
-                mma_16816(d[i], x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, q.x, q.z);
-                mma_16816(d[i], x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, q.y, q.w);
+            for (int i = 0; i < kSubs; ++i) {
+              const uint32_t x0 = comp(x[i].c[0], j), x1 = comp(x[i].c[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+              const uint32_t e0 = x0 & 0x000f000fu, e1 = x1 & 0x000f000fu, e2 = y0 & 0x000f000fu, e3 = y1 & 0x000f000fu;
+              const uint32_t o0 = x0 & 0x00f000f0u, o1 = x1 & 0x00f000f0u, o2 = y0 & 0x00f000f0u, o3 = y1 & 0x00f000f0u;
+              if (HILO) {
+                mma_16816(d[i], e0, e1, e2, e3, q[HILO ? 1 : 0].x, q[HILO ? 1 : 0].z);
+                mma_16816(d[i], o0, o1, o2, o3, q[HILO ? 1 : 0].y, q[HILO ? 1 : 0].w);
               }
+              mma_16816(d[i], e0, e1, e2, e3, q[0].x, q[0].z);
+              mma_16816(d[i], o0, o1, o2, o3, q[0].y, q[0].w);
             }
+          }
+          // a c . q + m sum q: of one group of dimensions the sum over all of them in its first half
 #pragma unroll
           for (int i = 0; i < kSubs; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              // a (2 c - 15) . q + (2 m + 15 a) sum q: of one group the sums over all its dimensions in its first half
-              const int r = 8 * nt + 2 * t4 + (e & 1);
-              const uint32_t w = x[i].w[e >> 1][half * (NG - 1)];
-              const float scale = word_scale(w);
-              if (NG == 2 || half == 0) {
-                const float qsum = S.qsum[r][half * (NG - 1)], add = fmaf(scale, 15.f, 2.f * word_min(w));
-                z[i][e] = fmaf(add, qsum, half ? z[i][e] : S.lse_in[r]);
-                z[i][e] = fmaf(scale, fmaf(d[i][e], 33554432.f, -15.f * qsum), z[i][e]);
-              } else {
-                z[i][e] = fmaf(scale, d[i][e] * 33554432.f, z[i][e]);
+            for (int y = 0; y < 2; ++y) {
+              const uint32_t w = x[i].w[y][half * (NG - 1)];
+              const float scale = word_scale(w), low = word_min(w);
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                float& to = z[i][2 * y + r];
+                if (half == 0) to = fmaf(low, qsum[r].x, lse_in[r]);
+                else if (NG == 2) to = fmaf(low, qsum[r].y, to);
+                to = fmaf(scale, d[i][2 * y + r], to);
               }
             }
         }
 #pragma unroll
         for (int i = 0; i < kSubs; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 8 * nt + 2 * t4 + (e & 1);
-            float p = exp2_fast(fmaf(z[i][e], S.k[r], S.lse[r]));
-            if (16 * (s0 + i) + 16 > sees0 && 16 * (s0 + i) + g8 + 8 * (e >> 1) >= sees0 + r / v.G) p = 0.f;
-            sum[i][e >> 1] += p;
-          }
+          for (int e = 0; e < 4; ++e) z[i][e] = fmaf(z[i][e], k[e & 1].x, k[e & 1].y);
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < kSubs; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (16 * (s0 + i) + g8 + 8 * (e >> 1) >= sees0 + (8 * nt + 2 * t4 + (e & 1)) / v.G) z[i][e] = -kInf;
+        }
+#pragma unroll
+        for (int i = 0; i < kSubs; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[i][e >> 1] += exp2_fast(z[i][e]);
       }
 #pragma unroll
       for (int i = 0; i < kSubs; ++i)
