@@ -3,10 +3,10 @@
 //
 // A unit is a group's KV head and up to 128 of its query rows (members x query tokens x query heads); units are cut into tiles of
 // 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA, one CTA an SM.  In a CTA
-//   8 warps turn codes into operands, a sub-block of 16 tokens each: keys as (2 c - 15) a in two fp16 halves (the second the exact rest),
+//   2 x 8 warps turn codes into operands, a sub-block of 16 tokens each: keys as (2 c - 15) a in two fp16 halves (the second the exact rest),
 //     values as fp16(m + c a),
-//   1 warp issues the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry (2 m + 15 a) sum(q), so that a logit comes out
-//     whole (doubled), then O += P V; Q and P come out of tensor memory, so that a product reads 4 KiB of shared memory and not 8.  (The warp goes
+//   2 warps issue the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry (2 m + 15 a) sum(q), so that a logit comes out
+//     whole (doubled), then O += P V; Q and P come out of tensor memory, so that a product reads 4 KiB of shared memory and not 8.  (A warp goes
 //     through its loop as one and elects the issuing thread at each batch: descriptors then are sums in uniform registers.  Out of a
 //     loop of one thread a product took 94 to 107 cycles, where the tensor cores need 64 for 128 x 128 x 16.)
 //   2 x 4 warps take the tiles in turn, a thread per query row: p = 2^(S scale - reference), its sum, P as fp16 over S's columns.
@@ -31,13 +31,15 @@ namespace akv {
 namespace {
 
 constexpr int kRows = 128, kTile = 128;
-constexpr int kSoftWarps = 8, kUnpackWarps = 8, kMmaWarp = kSoftWarps + kUnpackWarps;
-// Whole warpgroups, which share registers out (three warps are idle): 20 warps of 96 at the launch, then 8 x 120 + 8 x 88 + 4 x 64.
+constexpr int kSoftWarps = 8, kKeyWarps = 8, kValueWarps = 8, kMmaWarp = kSoftWarps + kKeyWarps + kValueWarps;
+// Whole warpgroups, which share registers out: 28 warps of 72 at the launch, then 8 x 96 + 8 x 64 + 8 x 56 + 4 x 72.
 constexpr int kThreads = 32 * (kMmaWarp + 4);
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -3.402823466e38f;  // reference of a row that saw no token: below all others
 constexpr float kSlack = 5.f, kPlace = 5.f;
 constexpr int kMaxCtas = 256;
+constexpr int kRawSub = 1024 + 256;       // codes of a sub-block's one side, and all its parameters
+enum State : int8_t { kThere, kBehind, kOutside };
 constexpr uint32_t kCols = 512, kColO = 256, kColQ = 384;  // tensor memory: S of two tiles, O, Q's high and low halves
 
 struct SharedArgs {
@@ -52,14 +54,18 @@ struct SharedArgs {
 };
 
 struct Smem {
-  uint8_t k[2][4 * kPanel];   // keys: high, then low halves; the first is where a unit's queries are put together, too
-  uint8_t v[2][2 * kPanel];   // values: [dimension][token]
+  uint8_t k_hi[2][2 * kPanel];  // keys' high halves, which is also where a unit's queries are put together; the low ones, needed first, are
+  uint8_t k_lo[2 * kPanel];     // written again while the products go on with the high ones
+  uint8_t v[2][2 * kPanel];     // values: [dimension][token]
   uint8_t qx[kExtra], kx[2][kExtra];
+  uint8_t raw[2][2][8 * kRawSub];  // codes and parameters as they come: keys, values; by tile modulo 2
   float row_scale[kRows], ref[kRows], sum[2][kRows];
   int lim[kRows];             // tokens of the unit that a row sees
   int64_t row_at[kRows];      // its number among all query rows; -1: none
   uint8_t big[4][8];          // sub-blocks that enter as 2^-5 of themselves, by tile modulo 4
-  uint64_t k_full[2], k_free[2], v_full[2], v_free[2], s_full[2], p_full[2], ref_at[2][4], q_full, o_full, drained;
+  int8_t state[2][2][8];      // of a raw sub-block: kThere, kBehind the shared tokens, kOutside the pool
+  uint64_t raw_full[2][2], raw_free[2][2];
+  uint64_t k_full[2], k_free[2], lo_free, v_full[2], v_free[2], s_full[2], p_full[2], p_free[2], ref_at[2][4], q_full, o_full, drained[2];
   int64_t part[kThreads / 32];
   int place[8];
   uint32_t tmem;
@@ -161,7 +167,7 @@ template <bool HILO>
 __device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, const Segment& seg, int warp) {
   const PagedView& v = a.v;
   const int lane = threadIdx.x & 31;
-  constexpr int kEach = kRows / (kSoftWarps + kUnpackWarps);
+  constexpr int kEach = kRows / (kSoftWarps + kKeyWarps);
   static_assert(kEach == 8, "rows of place_queries");
   const int tg = a.T * v.G, rr = warp * kEach + (lane & (kEach - 1)), qi = seg.block * kRows + rr;
   const int k = seg.k0 + qi / tg, t = qi % tg / v.G, gq = qi % tg % v.G;
@@ -169,7 +175,7 @@ __device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, cons
   const int64_t row = b >= 0 ? ((int64_t)b * a.T + t) * (v.H * v.G) + seg.h * v.G + gq : -1;
   const int lim = b >= 0 ? min(seg.tokens, held_tokens(v, b) - a.T + 1 + t) : seg.tokens;
   const float down = b >= 0 ? *(const float*)(a.queries + row * kQueryRecord + 544) : 0.f;
-  named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
+  named_sync(2, 32 * (kSoftWarps + kKeyWarps));
   if (lane < kEach) S.lim[rr] = lim, S.row_at[rr] = row, S.row_scale[rr] = 0.5f * fabsf(a.scale) * down;  // (keys enter twice as large)
   place_queries<HILO>(
       lane,
@@ -177,9 +183,9 @@ __device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, cons
         const int64_t at = __shfl_sync(0xffffffffu, row, r);
         return at < 0 ? nullptr : a.queries + at * kQueryRecord;
       },
-      [&](int r, int& to, uint32_t& panels, uint32_t& extra) { to = warp * kEach + r, panels = smem_u32(S.k[0]), extra = smem_u32(S.qx); });
+      [&](int r, int& to, uint32_t& panels, uint32_t& extra) { to = warp * kEach + r, panels = smem_u32(S.k_hi[0]), extra = smem_u32(S.qx); });
   proxy_fence();
-  named_sync(2, 32 * (kSoftWarps + kUnpackWarps));
+  named_sync(2, 32 * (kSoftWarps + kKeyWarps));
 }
 
 template <int NG, bool HILO>
@@ -194,17 +200,23 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
   launch_dependents();
   if (tid == 0) {
     for (int s = 0; s < 2; ++s) {
-      mbar_init(smem_u32(&S.k_full[s]), kUnpackWarps);
+      mbar_init(smem_u32(&S.k_full[s]), kKeyWarps);
       mbar_init(smem_u32(&S.k_free[s]), 1);
       for (int q = 0; q < 4; ++q) mbar_init(smem_u32(&S.ref_at[s][q]), 1);
-      mbar_init(smem_u32(&S.v_full[s]), kUnpackWarps);
+      for (int side = 0; side < 2; ++side) {
+        mbar_init(smem_u32(&S.raw_full[side][s]), 1);
+        mbar_init(smem_u32(&S.raw_free[side][s]), 8);
+      }
+      mbar_init(smem_u32(&S.v_full[s]), kValueWarps);
       mbar_init(smem_u32(&S.v_free[s]), 1);
       mbar_init(smem_u32(&S.s_full[s]), 1);
       mbar_init(smem_u32(&S.p_full[s]), 4);
+      mbar_init(smem_u32(&S.p_free[s]), 1);
+      mbar_init(smem_u32(&S.drained[s]), 1);
     }
+    mbar_init(smem_u32(&S.lo_free), 1);
     mbar_init(smem_u32(&S.q_full), kSoftWarps);
     mbar_init(smem_u32(&S.o_full), 1);
-    mbar_init(smem_u32(&S.drained), 1);
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -221,35 +233,35 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
   const uint32_t tmem = __shfl_sync(0xffffffffu, S.tmem, 0);
 
   if (warp >= kMmaWarp) {
-    fewer_registers<64>();
-    if (warp == kMmaWarp) {
-      // ---- the products
+    // (72 registers, as launched)
+    if (warp < kMmaWarp + 2) {
+      // ---- the products: S = Q K^T by one warp, O += P V by another, so that neither waits while the other's could run
       constexpr uint32_t idesc = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);  // fp16 x fp16 -> fp32, 128 x 128
-      const uint64_t dqx = plain_desc(smem_u32(S.qx));
       // D (+)= A B^T over 128 of K, A out of tensor memory
       auto product = [&](uint32_t d, uint32_t at, uint64_t desc, bool first) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
           tc_mma_ts(d, at + 8 * kk, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || kk > 0);
       };
-      uint32_t n_tile = 0, nseg = 0;
+      uint32_t n = 0, nseg = 0;
       bool ok = true;
-      for (int64_t at = w.lo; ok && at < w.hi; ++nseg) {
-        ok = mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
-        // S of tile i, then P V of the tile before
+      if (warp == kMmaWarp) {
+        const uint64_t dqx = plain_desc(smem_u32(S.qx));
+        for (int64_t at = w.lo; ok && at < w.hi; ++nseg) {
+          ok = mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
 #pragma unroll 1
-        for (int i = 0; ok && i <= seg.n; ++i) {
-          if (i < seg.n) {
-            const uint32_t n = n_tile + i, s = n & 1;
-            ok = mbar_wait_w(smem_u32(&S.k_full[s]), n >> 1 & 1) && !warp_failed(failed);
+          for (int i = 0; ok && i < seg.n; ++i, ++n) {
+            // (P of the tile two before lies over this one's S)
+            const uint32_t s = n & 1;
+            ok = mbar_wait_w(smem_u32(&S.k_full[s]), n >> 1 & 1) && (n < 2 || mbar_wait_w(smem_u32(&S.p_free[s]), (n - 2) >> 1 & 1)) && !warp_failed(failed);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
               const uint32_t d = tmem + 128 * s;
-              const uint64_t dk = sw128_desc(smem_u32(S.k[s]));
-              constexpr uint64_t low = 2 * kPanel >> 4;
-              if (HILO) product(d, tmem + kColQ + 64, dk, true);
-              product(d, tmem + kColQ, dk + low, !HILO);
+              const uint64_t dk = sw128_desc(smem_u32(S.k_hi[s]));
+              product(d, tmem + kColQ, sw128_desc(smem_u32(S.k_lo)), true);
+              tc_commit(smem_u32(&S.lo_free));
+              if (HILO) product(d, tmem + kColQ + 64, dk, false);
               product(d, tmem + kColQ, dk, false);
               tc_mma(d, dqx, plain_desc(smem_u32(S.kx[s])), idesc, 1);
               tc_commit(smem_u32(&S.k_free[s]));
@@ -257,201 +269,226 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
             }
             __syncwarp();
           }
-          if (i) {
-            const uint32_t n = n_tile + i - 1, s = n & 1, use = n >> 1 & 1;
-            ok = mbar_wait_w(smem_u32(&S.p_full[s]), use) && mbar_wait_w(smem_u32(&S.v_full[s]), use);
+          at += seg.n;
+          if (at < w.hi) next_segment(a, seg, w.hi - at);
+        }
+      } else {
+        for (int64_t at = w.lo; ok && at < w.hi; ++nseg) {
+#pragma unroll 1
+          for (int i = 0; ok && i < seg.n; ++i, ++n) {
+            const uint32_t s = n & 1;
+            ok = mbar_wait_w(smem_u32(&S.v_full[s]), n >> 1 & 1) && mbar_wait_w(smem_u32(&S.p_full[s]), n >> 1 & 1) && !warp_failed(failed);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              product(tmem + kColO, tmem + 128 * s, sw128_desc(smem_u32(S.v[s])), i == 1);
+              product(tmem + kColO, tmem + 128 * s, sw128_desc(smem_u32(S.v[s])), i == 0);
               tc_commit(smem_u32(&S.v_free[s]));
-              if (i == seg.n) tc_commit(smem_u32(&S.o_full));
+              tc_commit(smem_u32(&S.p_free[s]));
+              if (i + 1 == seg.n) tc_commit(smem_u32(&S.o_full));
             }
             __syncwarp();
           }
+          at += seg.n;
+          if (at < w.hi) next_segment(a, seg, w.hi - at);
         }
-        n_tile += seg.n;
+      }
+      if (!ok) *failed = 1;
+      const uint32_t drained = smem_u32(&S.drained[warp - kMmaWarp]);
+      if (elect_one()) tc_commit(drained);
+      __syncwarp();
+      mbar_wait_w(drained, 0);  // nothing is under way when tensor memory is given back
+    } else {
+      // ---- copies of keys, and of values: a warp each, a lane a sub-block; the table's page numbers are looked up two tiles before
+      const int side = warp - kMmaWarp - 2;
+      asm volatile("fence.proxy.async.global;" ::: "memory");  // (what launches before this one wrote with ordinary stores)
+      uint32_t n = 0;
+      auto look = [&](int t) {  // page of the lane's sub-block of the unit's tile t: as the table says, behind the shared tokens INT32_MIN
+        const int tok = t * kTile + 16 * lane;
+        return lane < 8 && tok < seg.tokens ? v.table[(int64_t)seg.lead * v.table_stride + (tok >> v.page_log)] : INT32_MIN;
+      };
+      bool ok = true;
+      for (int64_t at = w.lo; ok && at < w.hi;) {
+        int page = look(seg.t0), next = look(seg.t0 + 1);
+#pragma unroll 1
+        for (int i = 0; i < seg.n; ++i, ++n) {
+          const int t = seg.t0 + i, tok = t * kTile + 16 * lane, after = look(t + 2);
+          const uint32_t st = n & 1;
+          const bool there = (uint32_t)page < (uint32_t)v.n_pages;
+          const uint32_t copies = __popc(__ballot_sync(0xffffffffu, there));
+          ok = mbar_wait_w(smem_u32(&S.raw_free[side][st]), (n >> 1 & 1) ^ 1) && !warp_failed(failed);
+          if (!ok) break;
+          if (lane < 8) S.state[side][st][lane] = there ? kThere : page == INT32_MIN ? kBehind : kOutside;
+          __syncwarp();
+          const uint32_t bar = smem_u32(&S.raw_full[side][st]), to = smem_u32(&S.raw[side][st][lane * kRawSub]);
+          if (lane == 0) mbar_expect_tx(bar, copies * (1024 + 128 * NG));
+          __syncwarp();
+          if (there) {
+            const uint8_t* from = block_of(v, page, seg.h) + (uint64_t)((tok & ((1 << v.page_log) - 1)) >> 4) * kSub;
+            bulk_g2s(to, from + 1024 * side, 1024, bar);
+            bulk_g2s(to + 1024, from + 2048, 128 * NG, bar);
+          }
+          page = next, next = after;
+        }
         at += seg.n;
         if (at < w.hi) next_segment(a, seg, w.hi - at);
       }
       if (!ok) *failed = 1;
-      if (elect_one()) tc_commit(smem_u32(&S.drained));
-      __syncwarp();
-      mbar_wait_w(smem_u32(&S.drained), 0);  // nothing is under way when tensor memory is given back
+      // shared memory is the copies' until the last have landed, also where somebody has given up
+      for (uint32_t k = n > 2 ? n - 2 : 0; k < n; ++k) mbar_wait_w(smem_u32(&S.raw_full[side][k & 1]), k >> 1 & 1);
     }
   } else if (warp >= kSoftWarps) {
-    // ---- operands of keys and values: a sub-block a warp
-    fewer_registers<88>();
-    const int u = warp - kSoftWarps;
-    const int token = lane & 15, half = lane >> 4;                       // keys: a token's dimensions 32 j + 8 t + i, t = 2 half ..
-    const int g = lane & 7, p = lane >> 3 & 1, sd = lane >> 4;           // values: tokens 8 p .. + 7, dimensions 64 sd + 8 g ..
-    const uint32_t kx_at = smem_u32(S.kx[0]) + extra_at(16 * u + token);
-    const uint32_t k_at = smem_u32(S.k[0]) + (uint32_t)(16 * u + token) * 128;
-    const int v_chunk = 2 * (u & 3) + p;
-    uint4 kc[2];       // a key's codes, its parameters (and its value's)
-    uint32_t kw[2 * NG];
-    uint2 vc[4];       // value words of tokens 2 t, 2 t + 1; the parameters of eight tokens
-    uint32_t vw[8];
-    auto page_at = [&](const Segment& s, int i) {  // page of the warp's sub-block of tile i as the table says (looked at when it is used)
-      const int tok = (s.t0 + i) * kTile + 16 * u;
-      return tok < s.tokens ? v.table[(int64_t)s.lead * v.table_stride + (tok >> v.page_log)] : INT32_MIN;
-    };
-    auto place = [&](const Segment& s, int i, int page) {
-      return block_of(v, page, s.h) + (uint64_t)(((s.t0 + i) * kTile + 16 * u & ((1 << v.page_log) - 1)) >> 4) * kSub;
-    };
+    // ---- operands of keys, and of values: a sub-block a warp of each
+    const bool keys = warp < kSoftWarps + kKeyWarps;
+    const int side = keys ? 0 : 1, u = (warp - kSoftWarps) & 7, quad = lane >> 2, t4 = lane & 3;
+    uint4 c[2];            // codes
+    uint32_t pw[2 * NG];   // all words of token lane % 16
     // Tokens behind the end are zeros, those of pages outside the pool have NaN parameters.
-    auto load_keys = [&](const Segment& s, int i, int page) {
-      if ((uint32_t)page < (uint32_t)v.n_pages) {
-        const uint8_t* b = place(s, i, page);
-        const uint4* k = (const uint4*)(b + 64 * token + 32 * half);
-        kc[0] = k[0], kc[1] = k[1];
-        if (NG == 2) {
-          const uint4 x = *(const uint4*)(b + 2048 + 16 * token);
-          kw[0] = x.x, kw[1] = x.y, kw[2 * NG - 2] = x.z, kw[2 * NG - 1] = x.w;
-        } else {
-          const uint2 x = *(const uint2*)(b + 2048 + 8 * token);
-          kw[0] = x.x, kw[1] = x.y;
-        }
+    auto load = [&](uint32_t n) {
+      const uint32_t st = n & 1;
+      if (!mbar_wait_w(smem_u32(&S.raw_full[side][st]), n >> 1 & 1) || warp_failed(failed)) return false;
+      const int state = *(volatile int8_t*)&S.state[side][st][u];
+      const uint8_t* b = &S.raw[side][st][u * kRawSub];
+      c[0] = *(const uint4*)(b + 16 * lane), c[1] = *(const uint4*)(b + 512 + 16 * lane);
+      if (NG == 2) {
+        const uint4 x = *(const uint4*)(b + 1024 + 16 * (lane & 15));
+        pw[0] = x.x, pw[1] = x.y, pw[2 * NG - 2] = x.z, pw[2 * NG - 1] = x.w;
       } else {
-        kc[0] = kc[1] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int x = 0; x < 2 * NG; ++x) kw[x] = (s.t0 + i) * kTile + 16 * u >= s.tokens ? 0u : 0x7e007e00u;
+        const uint2 x = *(const uint2*)(b + 1024 + 8 * (lane & 15));
+        pw[0] = x.x, pw[1] = x.y;
       }
-    };
-    auto load_values = [&](const Segment& s, int i, int page) {
-      if ((uint32_t)page < (uint32_t)v.n_pages) {
-        const uint8_t* b = place(s, i, page);
+      if (state != kThere) {
+        c[0] = c[1] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) vc[t] = *(const uint2*)(b + 1024 + 512 * p + 16 * (4 * g + t) + 8 * sd);
-#pragma unroll
-        for (int k8 = 0; k8 < 8; ++k8) vw[k8] = *(const uint32_t*)(b + 2048 + 8 * NG * (8 * p + k8) + 4 * NG + (NG == 2 ? 4 * sd : 0));
-      } else {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) vc[t] = make_uint2(0, 0);
-#pragma unroll
-        for (int k8 = 0; k8 < 8; ++k8) vw[k8] = 0;
+        for (int x = 0; x < 2 * NG; ++x) pw[x] = state == kBehind ? 0u : 0x7e007e00u;
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&S.raw_free[side][st]));
+      return true;
     };
-    const KeyCodes key_codes;
-    const ValueCodes value_codes;
-    // Tiles further ahead are on their way into L2.
-    constexpr int kAhead = 4;
-    int far = INT32_MIN;  // page of the tile kAhead on
-    auto ask = [&](int i) {
-      if (lane == 0 && (uint32_t)far < (uint32_t)v.n_pages)
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(place(seg, i, far)), "r"(kSub) : "memory");
-      far = i + 1 < seg.n ? page_at(seg, i + 1) : INT32_MIN;
+    // The sub-block's size (scales beyond 2048, minima beyond 16384), and whether the token is without an infinity or a NaN
+    auto look = [&](bool& fine) {
+      uint32_t most = pw[0] & 0x7fff7fffu;
+#pragma unroll
+      for (int x = 1; x < 2 * NG; ++x) most = bits(__hmax2_nan(as_half2(most), as_half2(pw[x] & 0x7fff7fffu)));
+      fine = (most & 0xffffu) < 0x7c00u && most < 0x7c000000u;
+      return (bool)__any_sync(0xffffffffu, fine && ((most & 0xffffu) > 0x6800u || most > 0x7400ffffu));
     };
     uint32_t n_tile = 0, nseg = 0;
     bool ok = true;
-    int page = page_at(seg, 0);
-    load_keys(seg, 0, page);
-    load_values(seg, 0, page);
-    for (int64_t at = w.lo; at < w.hi; ++nseg) {
-      Segment after = seg;
-      const bool more = at + seg.n < w.hi;
-      if (more) next_segment(a, after, w.hi - at - seg.n);
-      page = seg.n > 1 ? page_at(seg, 1) : page_at(after, 0);
-      build_queries<HILO>(a, S, seg, warp);
-      // (the queries were put together in a key operand's place)
-      ok = ok && mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
-      far = seg.n > 2 ? page_at(seg, 2) : INT32_MIN;
+    if (keys) {
+      fewer_registers<64>();
+      // tokens lane / 4 and 8 more, dimensions 32 j + 8 t + i with t = lane % 4
+      const uint32_t kx_at = smem_u32(S.kx[0]) + extra_at(16 * u + (lane & 15));
+      const uint32_t k_at = (uint32_t)(16 * u + quad) * 128;
+      const KeyCodes codes;
+      for (int64_t at = w.lo; at < w.hi; ++nseg) {
+        build_queries<HILO>(a, S, seg, warp);
+        // (the queries were put together in a key operand's place)
+        ok = ok && mbar_wait_w(smem_u32(&S.q_full), nseg & 1);
 #pragma unroll 1
-      for (int i = 2; i < kAhead; ++i) ask(i);
-#pragma unroll 1
-      for (int i = 0; ok && i < seg.n; ++i, ++n_tile) {
-        const uint32_t s = n_tile & 1, unused = (n_tile >> 1 & 1) ^ 1, k_row = k_at + s * (4 * kPanel);
-        // the sub-block's size (scales beyond 2048, minima beyond 16384), and tokens with an infinity or a NaN
-        uint32_t most = kw[0] & 0x7fff7fffu;
+        for (int i = 0; ok && i < seg.n; ++i, ++n_tile) {
+          const uint32_t s = n_tile & 1, unused = (n_tile >> 1 & 1) ^ 1, hi_row = smem_u32(S.k_hi[s]) + k_at, lo_up = smem_u32(S.k_lo) - smem_u32(S.k_hi[s]);
+          ok = load(n_tile);
+          if (!ok) break;
+          bool fine;
+          const bool big = look(fine);
+          const float down = big ? kLargeDown : 1.f;
+          uint32_t words[NG], both[2][NG];  // of token lane % 16; of tokens lane / 4 and 8 more
 #pragma unroll
-        for (int x = 1; x < 2 * NG; ++x) most = bits(__hmax2_nan(as_half2(most), as_half2(kw[x] & 0x7fff7fffu)));
-        const bool fine = (most & 0xffffu) < 0x7c00u && most < 0x7c000000u;
-        const bool big = __any_sync(0xffffffffu, fine && ((most & 0xffffu) > 0x6800u || most > 0x7400ffffu));
-        const uint32_t all_fine = __ballot_sync(0xffffffffu, fine);
-        const float down1 = big ? kLargeDown : 1.f;
-        const __half2 down = __float2half2_rn(down1);
-        // keys
-        if (!mbar_wait_w(smem_u32(&S.k_free[s]), unused) || warp_failed(failed)) {
-          ok = false;
-          break;
-        }
-        if (lane == 0) S.big[n_tile & 3][u] = big;
-        __half2 scale[NG];
+          for (int x = 0; x < NG; ++x) {
+            words[x] = fine ? pw[x] : 0u;
 #pragma unroll
-        for (int x = 0; x < NG; ++x) scale[x] = __hmul2(__half2half2(__ushort_as_half((unsigned short)(fine ? kw[x] : 0u))), down);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          const uint32_t to_t = k_row + 16 * ((2 * half + tt) ^ (token & 7));  // (chunk 4 (j & 1) + t, its bit 2 turned by the row as well)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t hi[4], lo[4];
-            key_word(key_codes, j == 0 ? kc[tt].x : j == 1 ? kc[tt].y : j == 2 ? kc[tt].z : kc[tt].w, scale[NG == 2 ? j >> 1 : 0], hi, lo);
-            const uint32_t to = (to_t ^ (j & 1 ? 64u : 0u)) + (uint32_t)(j >> 1) * kPanel;
-            sts128(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-            sts128(to + 2 * kPanel, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+            for (int r = 0; r < 2; ++r) both[r][x] = __shfl_sync(0xffffffffu, words[x], quad + 8 * r);
           }
-        }
-        if (half == 0) {
-          uint32_t words[NG];
+          ok = mbar_wait_w(smem_u32(&S.k_free[s]), unused) && mbar_wait_w(smem_u32(&S.lo_free), (n_tile & 1) ^ 1);
+          if (!ok) break;
+          if (lane == 0) S.big[n_tile & 3][u] = big;
 #pragma unroll
-          for (int x = 0; x < NG; ++x) words[x] = fine ? kw[x] : 0u;
-          uint4 first, second;
-          key_extra<NG>(words, down1, !fine, 0.f, first, second);
-          sts128(kx_at + s * kExtra, first);
-          sts128(kx_at + s * kExtra + 2048, second);
-        }
-        proxy_fence();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&S.k_full[s]));
-        ask(i + kAhead);
-        // the next tile's keys are under way while the values are done, its values while its keys are
-        if (i + 1 < seg.n) load_keys(seg, i + 1, page);
-        else if (more) load_keys(after, 0, page);
-        // values
-        if (!mbar_wait_w(smem_u32(&S.v_free[s]), unused)) {
-          ok = false;
-          break;
-        }
-        __half2 sc[4], mn[4];
+          for (int r = 0; r < 2; ++r) {
+            __half2 scale[NG];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {  // (a token with a NaN anywhere is a zero)
-          const uint32_t w0 = all_fine >> (8 * p + 2 * t) & 1 ? vw[2 * t] : 0u, w1 = all_fine >> (8 * p + 2 * t + 1) & 1 ? vw[2 * t + 1] : 0u;
-          sc[t] = __hmul2(as_half2(__byte_perm(w0, w1, 0x5410)), down);
-          mn[t] = __hmul2(as_half2(__byte_perm(w0, w1, 0x7632)), down);
+            for (int x = 0; x < NG; ++x) scale[x] = __hmul2(__half2half2(__ushort_as_half((unsigned short)both[r][x])), __float2half2_rn(down));
+            // (odd tokens take their words in another order: then eight lanes write eight places)
+            const bool odd = quad & 1;
+            const uint32_t to_r = hi_row + 1024 * r + 16 * ((odd ? 4 + t4 : t4) ^ (quad & 7));
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj) {
+              const uint32_t even_word = jj == 0 ? c[r].x : jj == 1 ? c[r].y : jj == 2 ? c[r].z : c[r].w;
+              const uint32_t odd_word = jj == 0 ? c[r].y : jj == 1 ? c[r].x : jj == 2 ? c[r].w : c[r].z;
+              uint32_t hi[4], lo[4];
+              key_word(codes, odd ? odd_word : even_word, scale[NG == 2 ? jj >> 1 : 0], hi, lo);
+              const uint32_t to = (to_r ^ (jj & 1 ? 64u : 0u)) + (uint32_t)(jj >> 1) * kPanel;
+              sts128(to, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+              sts128(to + lo_up, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+            }
+          }
+          if (lane < 16) {
+            uint4 first, second;
+            key_extra<NG>(words, down, !fine, 0.f, first, second);
+            sts128(kx_at + s * kExtra, first);
+            sts128(kx_at + s * kExtra + 2048, second);
+          }
+          proxy_fence();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&S.k_full[s]));
         }
-        // dimension 64 sd + 8 g + 4 uu + n is operand row 64 sd + 8 (4 uu + n) + g: eight lanes write eight places
-        const uint32_t v_to = smem_u32(S.v[s]) + (uint32_t)(u >> 2) * kPanel + 128 * (64 * sd + g) + 16 * (v_chunk ^ g);
+        at += seg.n;
+        if (at < w.hi) next_segment(a, seg, w.hi - at);
+      }
+    } else {
+      // tokens 2 t, 2 t + 1 of each 8 with t = lane % 4 and, after an exchange among four lanes, all 8 of dimensions 64 s + 8 g + 4 u + n with
+      // g = lane / 4, 2 s + u = lane % 4
+      fewer_registers<56>();
+      const ValueCodes codes;
+      const uint32_t tiles = (uint32_t)(w.hi - w.lo);
+#pragma unroll 1
+      for (; n_tile < tiles; ++n_tile) {
+        ok = load(n_tile);
+        if (!ok) break;
+        bool fine;
+        const __half2 down = __float2half2_rn(look(fine) ? kLargeDown : 1.f);
+        // scales and minima in pairs of tokens: lanes 16 g + 2 x have tokens 2 x, 2 x + 1 and group g (of one group all have it)
+        const uint32_t mine = fine ? NG == 2 && lane >= 16 ? pw[2 * NG - 1] : pw[NG] : 0u, next = __shfl_xor_sync(0xffffffffu, mine, 1);
+        const uint32_t pair_a = bits(__hmul2(as_half2(__byte_perm(mine, next, 0x5410)), down));
+        const uint32_t pair_m = bits(__hmul2(as_half2(__byte_perm(mine, next, 0x7632)), down));
+        ok = mbar_wait_w(smem_u32(&S.v_free[n_tile & 1]), (n_tile >> 1 & 1) ^ 1);
+        if (!ok) break;
+        // dimension 64 s + 8 g + 4 u + n is operand row 32 n + 4 g + 2 s + u: eight lanes write eight places
+        const uint32_t v_to = smem_u32(S.v[n_tile & 1]) + (uint32_t)(u >> 2) * kPanel + 128 * lane;
+        const bool odd = t4 & 1, high = t4 & 2;
 #pragma unroll
-        for (int uu = 0; uu < 2; ++uu) {
-          uint32_t x[4], y[4];
+        for (int p = 0; p < 2; ++p) {
+          // word lane % 4 of tokens 2 t, 2 t + 1, t = 0 .. 3
+          const uint32_t r0 = __shfl_xor_sync(0xffffffffu, odd ? c[p].x : c[p].y, 1), r1 = __shfl_xor_sync(0xffffffffu, odd ? c[p].z : c[p].w, 1);
+          const uint32_t a0 = odd ? r0 : c[p].x, a1 = odd ? c[p].y : r0, b0 = odd ? r1 : c[p].z, b1 = odd ? c[p].w : r1;
+          const uint32_t r2 = __shfl_xor_sync(0xffffffffu, high ? a0 : b0, 2), r3 = __shfl_xor_sync(0xffffffffu, high ? a1 : b1, 2);
+          const uint32_t x[4] = {high ? r2 : a0, high ? r3 : a1, high ? b0 : r2, high ? b1 : r3};
+          __half2 sc[4], mn[4];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) x[t] = uu ? vc[t].y : vc[t].x, y[t] = x[t] >> 8;
+          for (int t = 0; t < 4; ++t) {
+            const int from = 8 * p + 2 * t + (high ? 16 : 0);  // (dimensions 64 s .. are group s of two)
+            sc[t] = as_half2(__shfl_sync(0xffffffffu, pair_a, from));
+            mn[t] = as_half2(__shfl_sync(0xffffffffu, pair_m, from));
+          }
+          const uint32_t to = v_to + 16 * ((2 * (u & 3) + p) ^ (lane & 7));
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
             // (nibbles n and n + 4 are the two tokens)
             uint32_t z[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) z[t] = bits(__hfma2(value_codes(x[t], y[t], n), sc[t], mn[t]));
-            sts128(v_to + 1024 * (4 * uu + n), make_uint4(z[0], z[1], z[2], z[3]));
+            for (int t = 0; t < 4; ++t) z[t] = bits(__hfma2(codes(x[t], x[t] >> 8, n), sc[t], mn[t]));
+            sts128(to + 4096 * n, make_uint4(z[0], z[1], z[2], z[3]));
           }
         }
         proxy_fence();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&S.v_full[s]));
-        if (i + 1 < seg.n) {
-          load_values(seg, i + 1, page);
-          page = i + 2 < seg.n ? page_at(seg, i + 2) : page_at(after, 0);
-        } else if (more) {
-          load_values(after, 0, page);
-        }
+        if (lane == 0) mbar_arrive(smem_u32(&S.v_full[n_tile & 1]));
       }
-      at += seg.n;
-      seg = after;
     }
     if (!ok) *failed = 1;
   } else {
     // ---- softmax: a thread a query row, the tiles of parity s
-    more_registers<120>();
+    more_registers<96>();
     const int half = warp >> 2, quarter = warp & 3, row = tid & 127;
     const uint32_t lane_at = tmem + ((uint32_t)(quarter * 32) << 16);
     uint32_t nseg = 0, n_tile = 0, n_ref = 0;  // n_ref: references that came from the other thread
@@ -465,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
           float x[32];
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
-            const float4 y = *(const float4*)(S.k[0] + (2 * half + p) * kPanel + 128 * row + 16 * (c ^ (row & 7)));
+            const float4 y = *(const float4*)(S.k_hi[0] + (2 * half + p) * kPanel + 128 * row + 16 * (c ^ (row & 7)));
             x[4 * c] = y.x, x[4 * c + 1] = y.y, x[4 * c + 2] = y.z, x[4 * c + 3] = y.w;
           }
           tm_st32(lane_at + kColQ + 64 * half + 32 * p, x);
@@ -624,9 +661,9 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
           float x[32];
           tm_ld32(lane_at + kColO + 64 * half + 32 * c, x);
           if (out_row >= 0) {
-            // operand column 32 (2 half + c) + 8 n + g is dimension 64 half + 8 g + 4 c + n
+            // (in the operand's order: the join puts it right)
 #pragma unroll
-            for (int gg = 0; gg < 8; ++gg) *(float4*)(to + 64 * half + 8 * gg + 4 * c) = make_float4(x[gg], x[8 + gg], x[16 + gg], x[24 + gg]);
+            for (int e = 0; e < 32; e += 4) *(float4*)(to + 64 * half + 32 * c + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
           }
         }
       if (half == 0 && out_row >= 0) {
@@ -673,14 +710,20 @@ __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_shared_join_kernel(
   const int64_t bt = row / hq;
   const int head = (int)(row % hq), b = (int)(bt / a.T), t = (int)(bt % a.T), g = head % v.G;
   float m = kLow, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  auto add = [&](int n, auto at, auto ml) {  // n parts, four under way at a time
+  // dimensions 4 lane + n = 64 s + 8 g + 4 u + n lie at 32 n + 4 g + 2 s + u of shared parts
+  const int place = 4 * (lane >> 1 & 7) + 2 * (lane >> 4) + (lane & 1);
+  auto add = [&](int n, auto at, auto ml, bool shared) {  // n parts, four under way at a time
     for (int i0 = 0; i0 < n; i0 += 4) {
       float4 x[4];
       float2 s[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         x[u] = make_float4(0.f, 0.f, 0.f, 0.f), s[u] = make_float2(kLow, 0.f);
-        if (i0 + u < n) x[u] = *(const float4*)(at(i0 + u) + 4 * lane), s[u] = *(const float2*)ml(i0 + u);
+        if (i0 + u < n) {
+          const float* p = at(i0 + u);
+          x[u] = shared ? make_float4(p[place], p[32 + place], p[64 + place], p[96 + place]) : *(const float4*)(p + 4 * lane);
+          s[u] = *(const float2*)ml(i0 + u);
+        }
       }
       const float mn = fmaxf(m, fmaxf(fmaxf(s[0].x, s[1].x), fmaxf(s[2].x, s[3].x))), f = exp2_fast(m - mn);
       m = mn;
@@ -705,24 +748,24 @@ __global__ void __launch_bounds__(32 * kJoinWarps) akv_paged_shared_join_kernel(
     const PagedWhere w = a.pre_where[row];
     if (w.first < 0) {
       const float* p = a.pre_part + row * kPartFloats;
-      add(1, [&](int) { return p; }, [&](int) { return p + kD; });
+      add(1, [&](int) { return p; }, [&](int) { return p + kD; }, true);
     } else {
       int before = 0;  // members of the group before the row: rows with its leader and a lower number
       for (int j0 = 0; j0 < b; j0 += 32) before += __popc(__ballot_sync(0xffffffffu, j0 + lane < b && a.share.leader[j0 + lane] == lead));
       const int rr = (int)((((int64_t)before * a.T + t) * v.G + g) % kRows), first = min(w.first, kMaxCtas - 1), n = min(w.n, kMaxCtas - first);
       auto at = [&](int i) { return a.pre_slots + ((size_t)(2 * (first + i) + (i == 0)) * kRows + rr) * kPartFloats; };
-      add(n, at, [&](int i) { return at(i) + kD; });
+      add(n, at, [&](int i) { return at(i) + kD; }, true);
     }
   }
   {
     const PagedWhere w = a.own_where[row];
     if (w.first < 0) {
       const float* p = a.own_part + row * kPartFloats;
-      add(1, [&](int) { return p; }, [&](int) { return p + kD; });
+      add(1, [&](int) { return p; }, [&](int) { return p + kD; }, false);
     } else {
       const int rr = (t * v.G + g) % a.own_rows, first = min(w.first, kPagedMaxGrid - 1), n = min(w.n, kPagedMaxGrid - first);
       auto slot = [&](int i) { return a.own_slots + (2 * (size_t)(first + i) + (i == 0)) * paged_slot_floats(a.own_rows); };
-      add(n, [&](int i) { return slot(i) + rr * kD; }, [&](int i) { return slot(i) + a.own_rows * kD + 2 * rr; });
+      add(n, [&](int i) { return slot(i) + rr * kD; }, [&](int i) { return slot(i) + a.own_rows * kD + 2 * rr; }, false);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
