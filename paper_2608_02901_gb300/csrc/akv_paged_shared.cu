@@ -59,13 +59,14 @@ struct Smem {
   uint8_t v[2][2 * kPanel];     // values: [dimension][token]
   uint8_t qx[kExtra], kx[2][kExtra];
   uint8_t raw[2][2][8 * kRawSub];  // codes and parameters as they come: keys, values; by tile modulo 2
-  float row_scale[kRows], ref[kRows], sum[2][kRows];
+  float row_scale[kRows], sum[2][kRows];
+  float most[2][2][kRows];    // by tile modulo 2: the largest logit of each half of a row
   int lim[kRows];             // tokens of the unit that a row sees
   int64_t row_at[kRows];      // its number among all query rows; -1: none
   uint8_t big[4][8];          // sub-blocks that enter as 2^-5 of themselves, by tile modulo 4
   int8_t state[2][2][8];      // of a raw sub-block: kThere, kBehind the shared tokens, kOutside the pool
   uint64_t raw_full[2][2], raw_free[2][2];
-  uint64_t k_full[2], k_free[2], lo_free, v_full[2], v_free[2], s_full[2], p_full[2], p_free[2], ref_at[2][4], q_full, o_full, drained[2];
+  uint64_t k_full[2], k_free[2], lo_free, v_full[2], v_free[2], s_full[2], p_full[2], p_free[2], q_full, o_full, drained[2];
   int64_t part[kThreads / 32];
   int place[8];
   uint32_t tmem;
@@ -202,7 +203,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&S.k_full[s]), kKeyWarps);
       mbar_init(smem_u32(&S.k_free[s]), 1);
-      for (int q = 0; q < 4; ++q) mbar_init(smem_u32(&S.ref_at[s][q]), 1);
       for (int side = 0; side < 2; ++side) {
         mbar_init(smem_u32(&S.raw_full[side][s]), 1);
         mbar_init(smem_u32(&S.raw_free[side][s]), 8);
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       mbar_init(smem_u32(&S.v_full[s]), kValueWarps);
       mbar_init(smem_u32(&S.v_free[s]), 1);
       mbar_init(smem_u32(&S.s_full[s]), 1);
-      mbar_init(smem_u32(&S.p_full[s]), 4);
+      mbar_init(smem_u32(&S.p_full[s]), kSoftWarps);
       mbar_init(smem_u32(&S.p_free[s]), 1);
       mbar_init(smem_u32(&S.drained[s]), 1);
     }
@@ -237,11 +237,11 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     if (warp < kMmaWarp + 2) {
       // ---- the products: S = Q K^T by one warp, O += P V by another, so that neither waits while the other's could run
       constexpr uint32_t idesc = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);  // fp16 x fp16 -> fp32, 128 x 128
-      // D (+)= A B^T over 128 of K, A out of tensor memory
-      auto product = [&](uint32_t d, uint32_t at, uint64_t desc, bool first) {
+      // D (+)= A B^T over 128 of K, A out of tensor memory, its second half `gap` columns further on
+      auto product = [&](uint32_t d, uint32_t at, uint32_t gap, uint64_t desc, bool first) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          tc_mma_ts(d, at + 8 * kk, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || kk > 0);
+          tc_mma_ts(d, at + 8 * kk + (kk >> 2) * gap, desc + (((uint32_t)(kk >> 2) * kPanel + (uint32_t)(kk & 3) * 32) >> 4), idesc, !first || kk > 0);
       };
       uint32_t n = 0, nseg = 0;
       bool ok = true;
@@ -259,10 +259,10 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
             if (elect_one()) {
               const uint32_t d = tmem + 128 * s;
               const uint64_t dk = sw128_desc(smem_u32(S.k_hi[s]));
-              product(d, tmem + kColQ, sw128_desc(smem_u32(S.k_lo)), true);
+              product(d, tmem + kColQ, 0, sw128_desc(smem_u32(S.k_lo)), true);
               tc_commit(smem_u32(&S.lo_free));
-              if (HILO) product(d, tmem + kColQ + 64, dk, false);
-              product(d, tmem + kColQ, dk, false);
+              if (HILO) product(d, tmem + kColQ + 64, 0, dk, false);
+              product(d, tmem + kColQ, 0, dk, false);
               tc_mma(d, dqx, plain_desc(smem_u32(S.kx[s])), idesc, 1);
               tc_commit(smem_u32(&S.k_free[s]));
               tc_commit(smem_u32(&S.s_full[s]));
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              product(tmem + kColO, tmem + 128 * s, sw128_desc(smem_u32(S.v[s])), i == 0);
+              product(tmem + kColO, tmem + 128 * s, 32, sw128_desc(smem_u32(S.v[s])), i == 0);
               tc_commit(smem_u32(&S.v_free[s]));
               tc_commit(smem_u32(&S.p_free[s]));
               if (i + 1 == seg.n) tc_commit(smem_u32(&S.o_full));
@@ -487,13 +487,12 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     }
     if (!ok) *failed = 1;
   } else {
-    // ---- softmax: a thread a query row, the tiles of parity s
+    // ---- softmax: two threads a query row, half of a tile's columns each
     more_registers<96>();
     const int half = warp >> 2, quarter = warp & 3, row = tid & 127;
     const uint32_t lane_at = tmem + ((uint32_t)(quarter * 32) << 16);
-    uint32_t nseg = 0, n_tile = 0, n_ref = 0;  // n_ref: references that came from the other thread
+    uint32_t nseg = 0, n_tile = 0;
     for (int64_t at = w.lo; at < w.hi; ++nseg) {
-      if (half == 0) S.ref[row] = kLow;
       build_queries<HILO>(a, S, seg, warp);
       // a thread takes its row's high or low halves into tensor memory
       if (half == 0 || HILO)
@@ -519,27 +518,25 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       float ref = kLow;
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll 1
-      for (int i = (n_tile ^ half) & 1; i < seg.n; i += 2) {
-        const uint32_t n = n_tile + i, s = half, tS = lane_at + 128 * s;
-        if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[s]), n >> 1 & 1)) {
-          *failed = 1;
-          break;
-        }
+      for (int i = 0; i < seg.n; ++i) {
+        const uint32_t n = n_tile + i, s = n & 1, tS = lane_at + 128 * s + 64 * half;
+        // (after a failure the loop goes on without waiting: two warps meet in it)
+        if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.s_full[s]), n >> 1 & 1)) *failed = 1;
         if (idle) {
           if (lane == 0) mbar_arrive(smem_u32(&S.p_full[s]));
           continue;
         }
         tc_fence_after();
-        const int sees = lim - i * kTile;
-        const uint64_t big = *(const volatile uint64_t*)&S.big[n & 3][0];
+        const int sees = lim - i * kTile - 64 * half;
+        const uint32_t big = *(const volatile uint32_t*)&S.big[n & 3][4 * half];
         // tiles that every row sees whole, without large sub-blocks, are what there is most of
-        const bool plain = __all_sync(0xffffffffu, sees >= kTile && big == 0);
+        const bool plain = __all_sync(0xffffffffu, sees >= 64 && big == 0);
         // the largest logit
         float most = kNegInf;
         if (plain) {
           float m4[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             float x[32];
             tm_ld32(tS + 32 * c, x);
 #pragma unroll
@@ -548,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
           most = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
         } else {
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             float x[32], m2[2] = {kNegInf, kNegInf};
             tm_ld32(tS + 32 * c, x);
 #pragma unroll
@@ -558,50 +555,34 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
           }
         }
         most *= row_scale;
-        // the reference, as the tile before left it
-        if (i) {
-          if (!mbar_wait_w(smem_u32(&S.ref_at[s][quarter]), n_ref++ & 1)) {
-            *failed = 1;
-            break;
-          }
-          const float now = *(volatile float*)&S.ref[row], f = exp2_fast(ref - now);
-          if (__any_sync(0xffffffffu, now != ref)) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) sum[e].x *= f, sum[e].y *= f;
-            ref = now;
-          }
-        }
+        *(volatile float*)&S.most[s][half][row] = most;
+        named_sync(3 + quarter, 64);  // (1 and 2 are the barriers of all softmax warps, and of those with the key warps)
+        most = fmaxf(most, *(volatile float*)&S.most[s][half ^ 1][row]);
         const bool up = most - ref > kSlack;  // (a row that sees nothing here sees nothing later)
         if (__any_sync(0xffffffffu, up)) {
           const float to = up ? most : ref, f = up ? exp2_fast(ref - to) : 1.f;
           ref = to;
-          *(volatile float*)&S.ref[row] = ref;
 #pragma unroll
           for (int e = 0; e < 2; ++e) sum[e].x *= f, sum[e].y *= f;
           if (i) {  // O, once the tile before is in it
-            if (!mbar_wait_w(smem_u32(&S.v_free[s ^ 1]), (n - 1) >> 1 & 1)) {
-              *failed = 1;
-              break;
-            }
+            if (warp_failed(failed) || !mbar_wait_w(smem_u32(&S.v_free[s ^ 1]), (n - 1) >> 1 & 1)) *failed = 1;
             tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
               float x[32];
-              tm_ld32(lane_at + kColO + 32 * c, x);
+              tm_ld32(lane_at + kColO + 64 * half + 32 * c, x);
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] *= f;
-              tm_st32(lane_at + kColO + 32 * c, x);
+              tm_st32(lane_at + kColO + 64 * half + 32 * c, x);
             }
             tm_wait_st();
           }
         }
-        __syncwarp();
-        if (lane == 0 && i + 1 < seg.n) mbar_arrive(smem_u32(&S.ref_at[s ^ 1][quarter]));
         const float shift = kPlace - ref;
         if (plain) {
           const float2 sc = make_float2(row_scale, row_scale), sh = make_float2(shift, shift);
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             float x[32];
             tm_ld32(tS + 32 * c, x);
             uint32_t pk[16];
@@ -616,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
           }
         } else {
 #pragma unroll 1
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             float x[32];
             tm_ld32(tS + 32 * c, x);
             uint32_t pk[16];
@@ -646,9 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
       // ---- the segment's end: each half of the threads takes half of the columns
       const bool done = !warp_failed(failed) && mbar_wait_w(smem_u32(&S.o_full), nseg & 1);
       if (!done) *failed = 1;
-      named_sync(1, 32 * kSoftWarps);  // (the last reference is there)
-      const float m = S.ref[row];
-      S.sum[half][row] = exp2_fast(ref - m) * ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+      S.sum[half][row] = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       named_sync(1, 32 * kSoftWarps);
       tc_fence_after();
       const bool whole = seg.t0 == 0 && seg.n == seg.tiles;
@@ -668,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
         }
       if (half == 0 && out_row >= 0) {
         const float l = S.sum[0][row] + S.sum[1][row];
-        to[kD] = l == 0.f ? kLow : m - kPlace;
+        to[kD] = l == 0.f ? kLow : ref - kPlace;
         to[kD + 1] = done ? l : __int_as_float(0x7fffffff);
         if (seg.t0 == 0) {
           const int64_t last = at + seg.tiles - 1;
