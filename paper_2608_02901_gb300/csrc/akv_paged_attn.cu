@@ -828,12 +828,12 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     const int b = cu.g.b, h = SEL ? cu.g.h : cu.index / a.n_blocks, n_rows = min(kRows, a.rows - row0);
     const bool from_start = cu.ti == 0, to_end = cu.ti + n_tiles == cu.tiles, whole = from_start && to_end;
     float* slot = a.slots + (2 * (size_t)blockIdx.x + (from_start ? 1 : 0)) * paged_slot_floats(kRows);
-    int at_last = blockIdx.x;  // the CTA of the unit's last tile: (x + 1) ctas - 1 over the tiles of all
-    if (from_start && !to_end && (M == kOwn || tid == 0)) {
+    auto last_cta = [&]() {  // the CTA of the unit's last tile: (x + 1) ctas - 1 over the tiles of all
       const int64_t total = S.range_total, last = S.range_lo + at + cu.tiles - 1;
       const int64_t ctas = min((int64_t)gridDim.x, total);
-      at_last = S.range_shares ? blockIdx.x + S.range_shares - 1 : (int)(((last + 1) * ctas - 1) / total);
-    }
+      return S.range_shares ? (int)blockIdx.x + S.range_shares - 1 : (int)(((last + 1) * ctas - 1) / total);
+    };
+    const int parts = M == kOwn && from_start && !to_end ? last_cta() - (int)blockIdx.x + 1 : 1;
 #pragma unroll 1
     for (int rr = warp; rr < n_rows; rr += kWarps) {
       float m = kLow, l = 0.f;
@@ -853,7 +853,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       if (M == kOwn) {
         const int t = (row0 + rr) / v.G, g = (row0 + rr) % v.G;
         const size_t row = ((size_t)b * a.T + t) * (v.H * v.G) + h * v.G + g;
-        if (from_start && lane == 0) a.own.where[row] = PagedWhere{whole ? -1 : (int)blockIdx.x, at_last - (int)blockIdx.x + 1};
+        if (from_start && lane == 0) a.own.where[row] = PagedWhere{whole ? -1 : (int)blockIdx.x, parts};
         if (whole) {
           float* to = a.own.part + row * kPartFloats;
           *(float4*)(to + 4 * lane) = make_float4(y[0], y[1], y[2], y[3]);
@@ -881,7 +881,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
       if (a.lse && lane == 0)
         a.lse[((int64_t)b * a.T + t) * (v.H * v.G) + h * v.G + g] = l == 0.f ? kNegInf : (m + log2f(l)) * 0.693147180559945f;
     }
-    if (M != kOwn && from_start && !to_end && tid == 0) a.desc[blockIdx.x] = make_int4(cu.gi, cu.index, at_last, 1);
+    if (M != kOwn && from_start && !to_end && tid == 0) a.desc[blockIdx.x] = make_int4(cu.gi, cu.index, last_cta(), 1);
     at += (uint32_t)n_tiles;
     if (at < range) {
       cu.next_unit(a);
@@ -993,8 +993,11 @@ int launch(const AttnArgs& a, int dev, int sms, cudaStream_t stream) {
   if (grid > kPagedMaxGrid) grid = kPagedMaxGrid;
   const int err = launch_after(kernel, dim3(grid), Smem<NT>::kThreads, smem, stream, a);
   // units of one tile at most are nobody's share (100 tokens: 8.7 us a call with the second launch, 6.6 without)
-  if (err || M == kOwn || ((int64_t)(M == kKept ? a.top : a.v.max_pages) << a.v.page_log) <= kTileTokens) return err;
-  return launch_after(akv_paged_join_kernel<M>, dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT), 32 * kJoinWarps, 0, stream, a, 8 * NT);
+  if constexpr (M != kOwn) {
+    if (!err && ((int64_t)(M == kKept ? a.top : a.v.max_pages) << a.v.page_log) > kTileTokens)
+      return launch_after(akv_paged_join_kernel<M>, dim3(grid, a.rows < 8 * NT ? a.rows : 8 * NT), 32 * kJoinWarps, 0, stream, a, 8 * NT);
+  }
+  return err;
 }
 
 template <int NT, bool HILO, Mode M>
