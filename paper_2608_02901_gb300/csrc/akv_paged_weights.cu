@@ -8,9 +8,13 @@
 //     it turns the codes into its lane of the operand in tensor memory, applies the token's scales to the products behind them,
 //     and adds its weights up along its lane without a shuffle; the queries are the columns.
 // In both, tiles of all units (request, KV head) go in equal contiguous ranges to the CTAs.
-//   With codes in the products and scales outside, a logit is k (a_0 S_0 + a_1 S_1 + m_0 sum q_0 + m_1 sum q_1) over the groups of dimensions (of many
-// rows with 2 c - 15 for c and 2 m + 15 a for m), and a weight 2 to that less lse, which is subtracted in such parts that it costs no
-// rounding of its own.
+//   With codes in the products and scales outside, a logit is k (a_0 S_0 + a_1 S_1 + m_0 sum q_0 + m_1 sum q_1) over the groups of dimensions, with
+// c - 7.5 for c and m + 7.5 a for m (of many rows twice that), and a weight 2 to that less lse, which is subtracted in such parts that it
+// costs no rounding of its own.  Codes from 0 up would make sums that are larger than what they leave.
+//   Warp-level products cut their sums off at 24 bits of the largest term.  So of few rows the high halves of the queries are whole numbers of
+// 11 bits times a power of two of the row: their sums with codes are exact, and begin at -7.5 times the row's sum, which centres the codes;
+// the low halves (of rows that are not rotated too) have sums of their own.  With both halves' products in one sum, and codes from 0 up, a
+// weight was off by 1e-6 to 5e-6 of its size, now by 1e-7 to 5e-7, for 4 to 7 % of the time of up to 8 rows and 20 % of 16 rows that are not rotated.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -172,8 +176,9 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
 template <int NT>
 struct FewSmem {
   uint4 frag[2][NT][4][32];     // query operand: high, low halves
-  // of a row, in what its products count: sums over each group, the part of -lse that goes with them; what they count, the rest of -lse
-  float2 qsum[8 * NT], k[8 * NT];
+  // of a row, in what its products count: sums over each group, what its two sums of products begin at, the part of -lse that goes with them;
+  // what they count, the rest of -lse
+  float2 qsum[8 * NT], start[2][8 * NT], k[8 * NT];
   float lse_in[8 * NT];
   int64_t part[kFewWarps], place[2];
 };
@@ -255,11 +260,25 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
       big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
       const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
       const float up = pow2(14 - e2);  // below 2^14, exact in fp16 down to 2^-23 of that
-      float sum = (x[0] + x[1]) + (x[2] + x[3]);
+      // the high half is a multiple of 2^-11 of the largest's power of two: sums of its products with codes are exact in 24 bits
+      float high[4], sum[2];
 #pragma unroll
-      for (int s = 1; s < 32 / NG; s *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+      for (int e = 0; e < 4; ++e) high[e] = 8.f * rintf(x[e] * (0.125f * up));
+      sum[0] = (high[0] + high[1]) + (high[2] + high[3]);
+      sum[1] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[1] += fmaf(x[e], up, -high[e]);
+#pragma unroll
+      for (int s = 1; s < 32 / NG; s *= 2)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], s);
       // (codes count 2^-24 in the products, and so does what is added to them)
-      if (lane % (32 / NG) == 0) ((float*)&S.qsum[rr])[lane / (32 / NG)] = sum * up * 5.9604644775390625e-8f;
+      if (lane % (32 / NG) == 0) {
+        const int g = lane / (32 / NG);
+        constexpr float c = 5.9604644775390625e-8f;
+        ((float*)&S.qsum[rr])[g] = (sum[0] + sum[1]) * c;
+        S.start[g][rr] = make_float2(-7.5f * c * sum[0], -7.5f * c * sum[1]);
+      }
       if (lane == 0) {
         const float k = fabsf(a.scale) * pow2(e2 - 10) * 1048576.f;
         float l, rest;
@@ -268,15 +287,13 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
         const float in = (rest + (l - coarse)) / k;  // (rows so small that their logits hardly differ: not worth it)
         S.k[rr] = make_float2(k, -coarse), S.lse_in[rr] = fabsf(in) < 1e30f ? -in : 0.f;
       }
-      uint4 f[HILO ? 2 : 1];
+      uint4 f[2];
 #pragma unroll
-      for (int low = 0; low < (HILO ? 2 : 1); ++low) {
+      for (int low = 0; low < 2; ++low) {
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {  // nibble e: odd ones stand for 16 times their value
-          const float y = x[e] * (e & 1 ? up * 0.0625f : up);
-          const float high = __half2float(__float2half_rn(y));
-          const float own = low ? y - high : y;
+          const float own = (low ? fmaf(x[e], up, -high[e]) : high[e]) * (e & 1 ? 0.0625f : 1.f);
           const float other = __shfl_xor_sync(0xffffffffu, own, 1);
           w[e] = lane & 1 ? half2_bits(other, own) : half2_bits(own, other);
         }
@@ -285,7 +302,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
       // lanes 2 x and 2 x + 1 hold dimensions 8 x ..: word j = x / 4, operand lane 4 row + x % 4
       const int to = 4 * (rr & 7) + (lane >> 1 & 3);
       if (!(lane & 1)) S.frag[0][rr >> 3][lane >> 3][to] = f[0];
-      if (HILO && (lane & 1)) S.frag[1][rr >> 3][lane >> 3][to] = f[HILO ? 1 : 0];
+      if (lane & 1) S.frag[1][rr >> 3][lane >> 3][to] = f[1];
     }
     __syncthreads();
 
@@ -315,50 +332,51 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
       const bool edge = 16 * (s0 + kSubs) > sees0;  // some row may not see some token
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        // products of tokens g8 and g8 + 8 with query rows 2 t4 and 2 t4 + 1 over 64 dimensions each, the low halves first
-        float z[kSubs][4];
-        float2 qsum[2], k[2];
-        float lse_in[2];
+        // products of tokens g8 and g8 + 8 with query rows 2 t4 and 2 t4 + 1 over a group of dimensions, the high halves' and the low ones'
+        // apart: the first are whole numbers of 22 bits, the second's cut does not count
+        float z[kSubs][4], d[kSubs][4], rest[kSubs][4];
+        float2 k[2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) qsum[r] = S.qsum[8 * nt + 2 * t4 + r], k[r] = S.k[8 * nt + 2 * t4 + r], lse_in[r] = S.lse_in[8 * nt + 2 * t4 + r];
+        for (int r = 0; r < 2; ++r) k[r] = S.k[8 * nt + 2 * t4 + r];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float d[kSubs][4];
+        for (int j = 0; j < 4; ++j) {
+          const int g = NG == 2 ? j >> 1 : 0;
+          if (j == 0 || (NG == 2 && j == 2)) {
 #pragma unroll
-          for (int i = 0; i < kSubs; ++i) d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.f;
+            for (int e = 0; e < 4; ++e) {
+              const float2 y = S.start[g][8 * nt + 2 * t4 + (e & 1)];
 #pragma unroll
-          for (int j = 2 * half; j < 2 * half + 2; ++j) {
-            uint4 q[HILO ? 2 : 1];
-#pragma unroll
-            for (int part = 0; part < (HILO ? 2 : 1); ++part) q[part] = S.frag[part][nt][j][lane];
-#pragma unroll
-            for (int i = 0; i < kSubs; ++i) {
-              const uint32_t x0 = comp(x[i].c[0], j), x1 = comp(x[i].c[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
-              const uint32_t e0 = x0 & 0x000f000fu, e1 = x1 & 0x000f000fu, e2 = y0 & 0x000f000fu, e3 = y1 & 0x000f000fu;
-              const uint32_t o0 = x0 & 0x00f000f0u, o1 = x1 & 0x00f000f0u, o2 = y0 & 0x00f000f0u, o3 = y1 & 0x00f000f0u;
-              if (HILO) {
-                mma_16816(d[i], e0, e1, e2, e3, q[HILO ? 1 : 0].x, q[HILO ? 1 : 0].z);
-                mma_16816(d[i], o0, o1, o2, o3, q[HILO ? 1 : 0].y, q[HILO ? 1 : 0].w);
-              }
-              mma_16816(d[i], e0, e1, e2, e3, q[0].x, q[0].z);
-              mma_16816(d[i], o0, o1, o2, o3, q[0].y, q[0].w);
+              for (int i = 0; i < kSubs; ++i) d[i][e] = y.x, rest[i][e] = y.y;
             }
           }
-          // a c . q + m sum q: of one group of dimensions the sum over all of them in its first half
+          const uint4 q0 = S.frag[0][nt][j][lane], q1 = S.frag[1][nt][j][lane];
 #pragma unroll
-          for (int i = 0; i < kSubs; ++i)
+          for (int i = 0; i < kSubs; ++i) {
+            const uint32_t x0 = comp(x[i].c[0], j), x1 = comp(x[i].c[1], j), y0 = x0 >> 8, y1 = x1 >> 8;
+            const uint32_t e0 = x0 & 0x000f000fu, e1 = x1 & 0x000f000fu, e2 = y0 & 0x000f000fu, e3 = y1 & 0x000f000fu;
+            const uint32_t o0 = x0 & 0x00f000f0u, o1 = x1 & 0x00f000f0u, o2 = y0 & 0x00f000f0u, o3 = y1 & 0x00f000f0u;
+            mma_16816(d[i], e0, e1, e2, e3, q0.x, q0.z);
+            mma_16816(rest[i], e0, e1, e2, e3, q1.x, q1.z);
+            mma_16816(d[i], o0, o1, o2, o3, q0.y, q0.w);
+            mma_16816(rest[i], o0, o1, o2, o3, q1.y, q1.w);
+          }
+          // a (c - 7.5) . q + (m + 7.5 a) sum q
+          if (j == 3 || (NG == 2 && j == 1)) {
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const uint32_t w = x[i].w[y][half * (NG - 1)];
-              const float scale = word_scale(w), low = word_min(w);
+            for (int r = 0; r < 2; ++r) {
+              const int row = 8 * nt + 2 * t4 + r;
+              const float qsum = g ? S.qsum[row].y : S.qsum[row].x, lse_in = S.lse_in[row];
 #pragma unroll
-              for (int r = 0; r < 2; ++r) {
-                float& to = z[i][2 * y + r];
-                if (half == 0) to = fmaf(low, qsum[r].x, lse_in[r]);
-                else if (NG == 2) to = fmaf(low, qsum[r].y, to);
-                to = fmaf(scale, d[i][2 * y + r], to);
-              }
+              for (int i = 0; i < kSubs; ++i)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                  const float scale = word_scale(x[i].w[y][g]), mid = fmaf(7.5f, scale, word_min(x[i].w[y][g]));
+                  float& to = z[i][2 * y + r];
+                  to = fmaf(mid, qsum, g ? to : lse_in);
+                  to = fmaf(scale, d[i][2 * y + r] + rest[i][2 * y + r], to);
+                }
             }
+          }
         }
 #pragma unroll
         for (int i = 0; i < kSubs; ++i)
