@@ -1,16 +1,19 @@
 """A serving loop on the paged 4-bit cache: one layer, several requests, some of them with more than one answer.
 
-    python examples/paged_decode.py [--heads 8] [--group 4] [--steps 32] [--top 16]
+    python examples/paged_decode.py [--heads 8] [--group 4] [--steps 32] [--top 16] [--budget 512]
 
 What a model would give (queries, keys and values of each token) is random here.  The loop
   1. reserves pages for the prompts and appends them in chunks,
   2. forks every prompt into a few answers, which share its pages until they write,
-  3. generates: reserve (copy on write), append, then attention over all pages or over the few that akv_paged_select
-     keeps for each query; the last step checks a draft of several tokens in one pass,
+  3. generates: reserve (copy on write), append, then attention over all pages, those that answers share read once, or over the
+     few that akv_paged_select keeps for each query; the last step checks a draft of several tokens in one pass,
   4. frees the answers that are done and compacts the pool,
   5. hands the longest request over to the anchor-residual cache: akv_paged_read gives its rows, akv_encode compresses
      them, akv_decode_attn attends.
 Step 3's integer state stays on the device: no step waits for the GPU.
+
+A second loop (within_budget) keeps a bounded number of tokens a row: the weights that a prompt's last queries gave its tokens choose
+those that stay, the answers share them, and their own weights choose again when they have grown.
 """
 from __future__ import annotations
 
@@ -55,7 +58,8 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
     pages = akv.Pages(p, pool, table, lens, refs)
     sel = akv.PageSelection(torch.empty((rows, 1, heads, top), **int32), torch.empty((rows, 1, heads), **int32))
     draft = 4
-    ws = torch.empty(max(akv.akv_pages_workspace_size(pages), akv.akv_paged_attn_workspace_size(p, pages, 1),
+    sharing = akv.PageShare(torch.empty((4, rows), **int32))
+    ws = torch.empty(max(akv.akv_pages_workspace_size(pages), akv.akv_paged_attn_shared_workspace_size(p, pages, 1),
                          akv.akv_paged_attn_workspace_size(p, pages, 1, top), akv.akv_paged_attn_workspace_size(p, pages, draft),
                          akv.akv_paged_select_workspace_size(p, pages, 1)), dtype=torch.uint8, device="cuda")
     ck, cv = torch.randn((2, 32, heads, D), generator=gen, device="cuda")
@@ -99,7 +103,8 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
         at = torch.randint(0, 32, (rows,), generator=gen, device="cuda")
         q = ck[at].repeat_interleave(group, 1)[:, None] + 0.7 * torch.randn((rows, 1, heads * group, D), generator=gen, device="cuda")
         q = q.to(torch.bfloat16)
-        akv.akv_paged_attn(p, pages, q, out, lse=lse, sm_scale=1 / math.sqrt(D), ws=ws)
+        akv.akv_pages_share(p, pages, sharing, ws=ws)  # (once a step: it holds for every layer)
+        akv.akv_paged_attn_shared(p, pages, q, out, sharing, lse=lse, sm_scale=1 / math.sqrt(D), ws=ws)
         akv.akv_paged_select(p, pages, q, sel, sink=1, recent=2, ws=ws)
         akv.akv_paged_attn(p, pages, q, kept, lse=kept_lse, sel=sel, sm_scale=1 / math.sqrt(D), ws=ws)
         share += (kept_lse - lse)[answering].exp().mean() / steps
@@ -147,8 +152,101 @@ def main(heads=8, group=4, steps=32, top=16, prompts=(3000, 1777, 940), answers=
     return dict(share=share, cosine=cosine, unmoved=unmoved, agree=agree, live=int(n_live), lacked=int(lacked), table=table, lens=lens, refs=refs)
 
 
+def within_budget(heads=8, group=4, steps=32, budget=512, window=32, sink=4, prompts=(3000, 1777, 940), answers=3, page=64, seed=0, verbose=True):
+    """Rows of at most `budget` tokens, but for those of the steps since they were last cut."""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    say = print if verbose else (lambda *a: None)
+    B, n = len(prompts), len(prompts) * answers
+    rows = B + 2 * n  # the prompts, the answers, and the rows that they go to when they are cut
+    most = max(max(prompts), budget) + steps
+    max_pages = -(-most // page)
+    n_pages = sum(-(-x // page) for x in prompts) + 2 * n * (2 + (budget + steps) // page)
+    p = akv.PagedParams(n_kv_heads=heads, n_q_heads=heads * group, page_tokens=page, rotate=True)
+    int32 = dict(dtype=torch.int32, device="cuda")
+    pool = torch.zeros((1, n_pages, akv.akv_paged_page_bytes(p)), dtype=torch.uint8, device="cuda")
+    table = torch.full((rows, max_pages), -1, **int32)
+    lens, refs, missing, lacked = torch.zeros(rows, **int32), torch.zeros(n_pages, **int32), torch.zeros(1, **int32), torch.zeros(1, **int32)
+    pages = akv.Pages(p, pool, table, lens, refs)
+    sharing = akv.PageShare(torch.empty((4, rows), **int32))
+    scores = torch.zeros((rows, heads, max_pages * page), device="cuda")
+    ws = torch.empty(max(akv.akv_pages_workspace_size(pages), *(f(p, pages, T) for T in (1, window) for f in (
+        akv.akv_paged_attn_shared_workspace_size, akv.akv_paged_weights_workspace_size))), dtype=torch.uint8, device="cuda")
+    ck, cv = torch.randn((2, 32, heads, D), generator=gen, device="cuda")
+    ids = torch.arange(rows, **int32)
+
+    def reserve(n_new):
+        akv.akv_pages_reserve(p, pages, n_new, missing, ws=ws)
+        torch.maximum(lacked, missing, out=lacked)
+
+    def put(n_new, T):
+        reserve(n_new)
+        n_new = n_new * (missing == 0)
+        akv.akv_paged_append(p, pages, clustered(gen, ck, (rows, T, heads), True), clustered(gen, cv, (rows, T, heads), False), n_new=n_new)
+        lens.add_(n_new)
+
+    def queries(T):
+        at = torch.randint(0, 32, (rows, T), generator=gen, device="cuda")
+        return (ck[at].repeat_interleave(group, 2) + 0.7 * torch.randn((rows, T, heads * group, D), generator=gen, device="cuda")).to(torch.bfloat16)
+
+    def attend(q, decay):
+        """Attention of the rows that hold tokens, and what it adds to the scores (none: not added up)."""
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+        akv.akv_pages_share(p, pages, sharing, ws=ws)
+        akv.akv_paged_attn_shared(p, pages, q, out, sharing, lse=lse, sm_scale=1 / math.sqrt(D), ws=ws)
+        if decay is not None:
+            akv.akv_paged_weights(p, pages, q, lse, scores, was=scores, decay=decay, sm_scale=1 / math.sqrt(D), ws=ws)
+        return out, lse
+
+    def cut(src, dst):
+        kept = akv.KeptTokens(torch.empty((len(src), heads, budget), **int32), torch.empty(len(src), **int32))
+        akv.akv_paged_evict(p, pages, src, dst, scores, kept, sink=sink, recent=window)
+        lens[dst.long()] = kept.count.clamp(min=0)  # (every layer of a model has the same counts)
+
+    # 1. the prompts; their last tokens' queries say which of their tokens stay
+    chunk = 1024
+    want = torch.tensor(list(prompts) + [0] * (rows - B), **int32)
+    for _ in range(0, max(prompts), chunk):
+        put((want - lens).clamp(0, chunk), chunk)
+    whole = int((refs > 0).sum())
+    attend(queries(window), 0.0)
+    q = queries(1)
+    before, all_lse = attend(q, None)
+    cut(ids[:B], ids[:B])
+    akv.akv_pages_trim(p, pages, ids[:B])
+    after, lse = attend(q, None)
+    mass = float((lse - all_lse)[:B].exp().mean())
+    cosine = float(torch.cosine_similarity(before[:B].float(), after[:B].float(), dim=-1).mean())
+    say(f"prompts of {sum(prompts)} tokens cut to {int(lens.sum())}: {whole} pages before, {int((refs > 0).sum())} now; what stays holds {mass:.3f} of the "
+        f"softmax, outputs' cosine {cosine:.4f}")
+
+    # 2. the answers share what is left, and grow
+    akv.akv_pages_fork(p, pages, ids[:B].repeat_interleave(answers), ids[B : B + n])
+    scores[B : B + n] = scores[:B].repeat_interleave(answers, 0)
+    now, spare = ids[B : B + n], ids[B + n :]
+    for step in range(steps):
+        new = torch.zeros(rows, **int32)
+        new[now.long()] = 1
+        put(new, 1)
+        attend(queries(1), 0.95)
+        if step == steps // 2:
+            # 3. they are cut into rows of their own: pages that others hold are not written
+            room = torch.zeros(rows, **int32)
+            room[spare.long()] = torch.minimum(lens[now.long()], torch.full_like(now, budget))
+            reserve(room)
+            cut(now, spare)
+            akv.akv_pages_free(p, pages, now)
+            now, spare = spare, now
+    say(f"{n} answers of {int(lens[now.long()].min())} to {int(lens[now.long()].max())} tokens: {int((refs > 0).sum())} pages")
+    return dict(mass=mass, cosine=cosine, lens=lens[now.long()], lacked=int(lacked), table=table, refs=refs, scores=scores)
+
+
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, value in (("heads", 8), ("group", 4), ("steps", 32), ("top", 16), ("answers", 3), ("page", 64), ("seed", 0)):
         ap.add_argument("--" + name, type=int, default=value)
-    main(**vars(ap.parse_args()))
+    ap.add_argument("--budget", type=int, default=512)
+    args = vars(ap.parse_args())
+    budget = args.pop("budget")
+    main(**args)
+    args.pop("top")
+    within_budget(budget=budget, **args)
