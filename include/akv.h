@@ -691,12 +691,16 @@ akv_status akv_paged_select(const akv_paged_params* p, const akv_pages* pages, i
  *           group is one row
  *   size    rows of the group
  *   order   the rows by (leader, row): a group's rows are neighbours there
- * One level: rows that share more with some of their group than with all of it share what all have. */
+ * One level: rows that share more with some of their group than with all of it share what all have.
+ *   flags (not written) says how akv_paged_attn_shared uses them: 0, where it is the faster way, by the sizes of all groups; AKV_SHARE_ALWAYS, the
+ * shared pages of every group are read once. */
+#define AKV_SHARE_ALWAYS 1u
 typedef struct akv_share {
   int32_t* leader;
   int32_t* pages;
   int32_t* size;
   int32_t* order;
+  uint32_t flags;
 } akv_share;
 
 /* Fills `share` from the table and the lengths.  It stays valid until a shared page or a row's first pages change
@@ -707,7 +711,7 @@ akv_status akv_pages_share(const akv_paged_params* p, const akv_pages* pages, co
 
 /* akv_paged_attn of the same arguments, but for the order of its sums: the shared pages of a group are read once for all its rows'
  * queries (as one matrix product), every row's further tokens as akv_paged_attn reads them, and both parts are joined in one
- * softmax.  Numbers in `share` that are out of range are left out (rows outside the table) or clamped (pages).
+ * softmax.  Groups of few query rows, and batches whose groups are short, are attended row by row (share->flags).  Numbers in `share` that are out of range are left out (rows outside the table) or clamped (pages).
  *   In the shared part a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
  * m + c a to fp16 as well (2^-11 of it; where 16 tokens have a scale above 2048 or a minimum beyond 16384, 2^-20 at least).  A query that sees a token
  * with an infinity or a NaN has NaN in all its outputs. */

@@ -16,7 +16,7 @@ import numpy as np
 
 from . import paged as _paged
 from .paged import (  # noqa: F401 - the paged 4-bit cache
-    AKV_DTYPE_BF16, AKV_DTYPE_FP16, AKV_FLAG_BOUNDS, AKV_PAGED_MAX_QUERY, KeptTokens, PagedParams, Pages, PageSelection,
+    AKV_DTYPE_BF16, AKV_DTYPE_FP16, AKV_FLAG_BOUNDS, AKV_PAGED_MAX_QUERY, AKV_SHARE_ALWAYS, KeptTokens, PagedParams, Pages, PageSelection,
     PageShare, akv_paged_append, akv_paged_attn, akv_paged_attn_shared, akv_paged_attn_shared_workspace_size,
     akv_paged_attn_workspace_size, akv_paged_evict, akv_paged_page_bytes, akv_paged_read, akv_paged_select,
     akv_paged_select_workspace_size, akv_paged_weights, akv_paged_weights_workspace_size, akv_pages_compact, akv_pages_copy, akv_pages_fork,

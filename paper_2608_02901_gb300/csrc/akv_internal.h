@@ -232,7 +232,9 @@ size_t paged_select_ws_bytes(const PagedView& v, int32_t T);
 // Query rows [rows][T][n_q_heads] as operands of the tensor-core kernels: a record each of 16 chunks of high and 16 of low halves, 16 more
 // dimensions, and two numbers: what the row's values were divided by, and whether it counts (1 or 0).
 constexpr size_t kQueryRecord = 576;
-int launch_paged_queries(const PagedView& v, const akv_rows& q, int32_t T, bool negative, const float* lse, void* records, void* stream);
+// `share` (with `shared`, [rows]): also how many of each row's first pages are read once for its group.
+int launch_paged_queries(const PagedView& v, const akv_rows& q, int32_t T, bool negative, const float* lse, const akv_share* share, int32_t* shared,
+                         void* records, void* stream);
 int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
                         const akv_share& share, void* ws, void* stream);
 size_t paged_shared_ws_bytes(const PagedView& v, int32_t T);

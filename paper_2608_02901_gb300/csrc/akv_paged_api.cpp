@@ -160,6 +160,7 @@ akv_status check_share(const akv_share* s, const akv_pages* g) {
   if (!s || !s->leader || !s->pages || !s->size || !s->order) return fail(AKV_ERR_INVALID, "null share or array of it");
   if (((uintptr_t)s->leader | (uintptr_t)s->pages | (uintptr_t)s->size | (uintptr_t)s->order) % 4)
     return fail(AKV_ERR_INVALID, "share must be 4-byte aligned");
+  if (s->flags & ~AKV_SHARE_ALWAYS) return fail(AKV_ERR_INVALID, "share: unknown flags");
   return AKV_OK;
 }
 

@@ -1,7 +1,7 @@
 // Query rows as operands of the paged cache's products on the fifth-generation tensor cores, once for all CTAs that multiply with them.
 //
 // A warp a row: its rotation, its power of two, its halves and its sums are some 300 instructions, which every CTA of a unit would
-// repeat (256 rows of 8 heads for 152 CTAs: 18 us of 60).  A row's record lies as akv_paged_tc.cuh's operands have it, without their swizzle.
+// repeat (256 rows of 8 heads for 152 CTAs: 18 us of 60).  Beside it, in a CTA of its own, what the plan of shared pages is worth.  A row's record lies as akv_paged_tc.cuh's operands have it, without their swizzle.
 #include "akv_paged.cuh"
 #include "akv_paged_tc.cuh"
 
@@ -17,14 +17,53 @@ struct QueryArgs {
   uint8_t* records;
   int64_t qb, qt, qh, total;
   uint32_t sign;
-  int T, aligned;
+  int T, aligned, sms;
+  akv_share share;
+  int32_t* shared;  // null: no share
 };
+
+// Whether reading a group's pages once pays.  Its time row by row goes by each member's units of 8 or 16 query rows (the second 1.5 times the first),
+// shared by blocks of 128 rows of the whole group, at 3.5 times a unit of 8.  Microseconds row by row and shared of groups over 32 k tokens each, 8 KV
+// heads: 12 pairs of 8 query rows 171 and 266, 8 of three 171 and 190, 6 of four 163 and 153, 3 of eight 160 and 96; of 16 query rows 12 pairs 255
+// and 274 (rotated 306 and 282), 8 of three 256 and 200.
+//   The launch of the shared part takes some 15 us until it has ended by itself where its caches are cold, as what it reads then is: all groups together have
+// to save as much (4 query heads; a group of 32 rows over 4 k tokens 45 shared, 51 not; of 8 rows 39 and 32; 4 rows over 16 k tokens 45 and 39).
+constexpr int kUnit8 = 2, kUnit16 = 3, kBlock = 7;  // of a tile of 128 tokens and a KV head, in half units of 8
+constexpr int kWorth = 43;                          // what an SM saves at least, in those
+__device__ __forceinline__ int64_t saved(const PagedView& v, int T, int tokens, int size) {
+  const int rows = T * v.G;
+  const int64_t alone = (int64_t)size * (rows <= 8 ? kUnit8 : (rows + 15) / 16 * kUnit16), together = ((int64_t)size * rows + 127) / 128 * kBlock;
+  return max((int64_t)0, alone - together) * ((tokens + 127) / 128) * v.H;
+}
+__device__ __forceinline__ void choose(const QueryArgs& a) {
+  __shared__ int64_t part[kWarps];
+  const PagedView& v = a.v;
+  const bool always = a.share.flags & AKV_SHARE_ALWAYS;
+  auto pages = [&](int b) { return min(max(a.share.pages[b], 0), v.max_pages); };
+  auto saves = [&](int b) { return saved(v, a.T, pages(b) << v.page_log, min(max(a.share.size[b], 0), v.rows)); };
+  int64_t sum = 0;
+  if (!always)
+    for (int b = threadIdx.x; b < v.rows; b += 32 * kWarps)
+      if (a.share.leader[b] == b) sum += saves(b);
+#pragma unroll
+  for (int m = 1; m < 32; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = sum;
+  __syncthreads();
+  sum = 0;
+  for (int w = 0; w < kWarps; ++w) sum += part[w];
+  const bool worth = sum >= (int64_t)kWorth * a.sms;
+  for (int b = threadIdx.x; b < v.rows; b += 32 * kWarps) a.shared[b] = always || (worth && saves(b) > 0) ? pages(b) : 0;
+}
 
 template <int NG, bool HILO>
 __global__ void __launch_bounds__(32 * kWarps) akv_paged_queries_kernel(const __grid_constant__ QueryArgs a) {
   launch_dependents();
   wait_for_stream();
   const PagedView& v = a.v;
+  if (a.shared && blockIdx.x == gridDim.x - 1) {
+    choose(a);
+    return;
+  }
   const int lane = threadIdx.x & 31, hq = v.H * v.G;
   const int64_t row0 = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kSide;
   float x[kSide][4];
@@ -121,8 +160,17 @@ __global__ void __launch_bounds__(32 * kWarps) akv_paged_queries_kernel(const __
 
 }  // namespace
 
-int launch_paged_queries(const PagedView& v, const akv_rows& q, int32_t T, bool negative, const float* lse, void* records, void* stream) {
+int launch_paged_queries(const PagedView& v, const akv_rows& q, int32_t T, bool negative, const float* lse, const akv_share* share, int32_t* shared,
+                         void* records, void* stream) {
   QueryArgs a{};
+  if (share) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&a.sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return (int)e;
+    a.share = *share;
+    a.shared = shared;
+  }
   a.v = v;
   a.q = (const uint16_t*)q.ptr;
   a.qb = q.stride_b, a.qt = q.stride_t, a.qh = q.stride_h;
@@ -132,7 +180,7 @@ int launch_paged_queries(const PagedView& v, const akv_rows& q, int32_t T, bool 
   a.sign = negative ? 0x80000000u : 0u;
   a.T = T;
   a.aligned = (uintptr_t)q.ptr % 8 == 0 && q.stride_b % 4 == 0 && q.stride_t % 4 == 0 && q.stride_h % 4 == 0;
-  const dim3 grid((unsigned)((a.total + kWarps * kSide - 1) / (kWarps * kSide)));
+  const dim3 grid((unsigned)((a.total + kWarps * kSide - 1) / (kWarps * kSide)) + (share ? 1 : 0));
   auto* kernel = v.rotate ? (v.ng == 2 ? akv_paged_queries_kernel<2, true> : akv_paged_queries_kernel<1, true>)
                           : (v.ng == 2 ? akv_paged_queries_kernel<2, false> : akv_paged_queries_kernel<1, false>);
   return launch_after(kernel, grid, 32 * kWarps, 0, stream, a);

@@ -3,14 +3,20 @@
 //
 // A unit is a group's KV head and up to 128 of its query rows (members x query tokens x query heads); units are cut into tiles of
 // 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA, one CTA an SM.  In a CTA
-//   2 x 8 warps turn codes into operands, a sub-block of 16 tokens each: keys as (2 c - 15) a in two fp16 halves (the second the exact rest),
+//   2 warps copy codes and parameters into rings of two tiles,
+//   2 x 8 warps turn them into operands, a sub-block of 16 tokens each: keys as (2 c - 15) a in two fp16 halves (the second the exact rest),
 //     values as fp16(m + c a),
 //   2 warps issue the products: S = Q K^T over 128 dimensions of (hi, lo) and 16 more that carry (2 m + 15 a) sum(q), so that a logit comes out
 //     whole (doubled), then O += P V; Q and P come out of tensor memory, so that a product reads 4 KiB of shared memory and not 8.  (A warp goes
 //     through its loop as one and elects the issuing thread at each batch: descriptors then are sums in uniform registers.  Out of a
 //     loop of one thread a product took 94 to 107 cycles, where the tensor cores need 64 for 128 x 128 x 16.)
-//   2 x 4 warps take the tiles in turn, a thread per query row: p = 2^(S scale - reference), its sum, P as fp16 over S's columns.
-//     Both add to one O, so a row has one reference: it goes from tile to tile, and to the other thread of its row.
+//   8 warps are the softmax: two threads a query row, half of a tile's columns each, which tell each other their largest logit:
+//     p = 2^(S scale - reference), its sum, P as fp16 over S's columns.  (A thread a row, the two warpgroups' tiles in turn and the reference
+//     handed from one to the other, took 243 us for 256 beams of 32 k tokens where this takes 221, 249 for 236 of 32 answers over 128 k.)
+// What bounds it (32 answers, 8 x 8 heads, 128 k shared tokens, rotated: 200 us of 236, in all 583 TFLOP/s of the products that the formula
+// has, 1420 of those that are made in the 200 us): the tensor cores work 65 % of the cycles, a warp instruction is issued in 70 %; of a
+// tile's 3500 cycles the products need 2260, and the rest is the chain from S through P to the next use of its columns.  S of three tiles
+// would not fit into tensor memory.  Of few rows the products cost the same.
 //   S is as exact as fp32 sums: products of fp16 numbers are, a query enters as one fp16 number (a power of two times what was given)
 // or, rotated, as a high and a low one.  The scales of tokens could not be applied behind the products instead: a thread that owns a row would
 // read four numbers a token from shared memory, 512 bytes a warp, four times what the tensor cores need for the extra products.
@@ -87,7 +93,7 @@ __device__ __forceinline__ int row_in_order(const SharedArgs& a, int k) {
   const int b = a.share.order[k];
   return (uint32_t)b < (uint32_t)a.v.rows ? b : -1;
 }
-// The group that begins at place k of the order, and how many tiles its units have; 0: none begins here, or it shares nothing.
+// The group that begins at place k of the order, and how many tiles its units have; 0: none begins here, or it is attended row by row.
 __device__ __forceinline__ int group_at(const SharedArgs& a, int k, Segment& s) {
   const PagedView& v = a.v;
   const int b = row_in_order(a, k);
@@ -776,9 +782,9 @@ int launch(const SharedArgs& a, int dev, int sms, void* stream) {
   return launch_after(kernel, dim3(sms < kMaxCtas ? sms : kMaxCtas), kThreads, smem, stream, a);
 }
 
-// Workspace: the own part's (its slots), then parts and places of both sides, the query rows' records, the shared part's slots.
+// Workspace: the own part's (its slots), then parts and places of both sides, shared pages of rows, the query rows' records, the shared part's slots.
 struct SharedWs {
-  size_t own_part, own_where, pre_part, pre_where, queries, slots, total;
+  size_t own_part, own_where, pre_part, pre_where, shared, queries, slots, total;
 };
 SharedWs shared_ws(const PagedView& v, int32_t T) {
   const size_t rows = (size_t)v.rows * T * v.H * v.G;
@@ -788,7 +794,8 @@ SharedWs shared_ws(const PagedView& v, int32_t T) {
   w.own_where = w.own_part + up(rows * kPartFloats * sizeof(float));
   w.pre_part = w.own_where + up(rows * sizeof(PagedWhere));
   w.pre_where = w.pre_part + up(rows * kPartFloats * sizeof(float));
-  w.queries = w.pre_where + up(rows * sizeof(PagedWhere));
+  w.shared = w.pre_where + up(rows * sizeof(PagedWhere));
+  w.queries = w.shared + up((size_t)v.rows * sizeof(int32_t));
   w.slots = w.queries + up(rows * kQueryRecord);
   w.total = w.slots + (size_t)kMaxCtas * 2 * kRows * kPartFloats * sizeof(float);
   return w;
@@ -799,18 +806,20 @@ SharedWs shared_ws(const PagedView& v, int32_t T) {
 size_t paged_shared_ws_bytes(const PagedView& v, int32_t T) { return shared_ws(v, T).total; }
 
 int launch_paged_shared(const PagedView& v, const akv_rows& q, const akv_rows& out, float* lse, int32_t T, float sm_scale,
-                        const akv_share& share, void* ws, void* stream) {
+                        const akv_share& given, void* ws, void* stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return (int)e;
   const SharedWs w = shared_ws(v, T);
   uint8_t* base = (uint8_t*)ws;
+  akv_share share = given;
+  share.pages = (int32_t*)(base + w.shared);  // what of each row's pages is read once for its group
   PagedOwn own;
   own.pages = share.pages;
   own.part = (float*)(base + w.own_part);
   own.where = (PagedWhere*)(base + w.own_where);
-  int err = launch_paged_queries(v, q, T, sm_scale < 0.f, nullptr, base + w.queries, stream);
+  int err = launch_paged_queries(v, q, T, sm_scale < 0.f, nullptr, &given, share.pages, base + w.queries, stream);
   if (!err) err = launch_paged_own(v, q, T, sm_scale, own, ws, stream);
   if (err) return err;
   SharedArgs a{};

@@ -769,7 +769,7 @@ int launch_paged_weights(const PagedView& v, const akv_rows& q, const float* lse
   a.rows = T * v.G;
   if (a.rows > kFew) {
     a.queries = (const uint8_t*)ws;
-    const int err = launch_paged_queries(v, q, T, sm_scale < 0.f, lse, ws, stream);
+    const int err = launch_paged_queries(v, q, T, sm_scale < 0.f, lse, nullptr, nullptr, ws, stream);
     if (err) return err;
   }
   if (v.rotate) return v.ng == 2 ? launch<2, true>(a, dev, sms, stream) : launch<1, true>(a, dev, sms, stream);

@@ -12,6 +12,7 @@ from dataclasses import dataclass, replace
 
 AKV_FLAG_BOUNDS = 8
 AKV_DTYPE_BF16, AKV_DTYPE_FP16 = 0, 1
+AKV_SHARE_ALWAYS = 1
 AKV_PAGED_MAX_QUERY = 64
 
 EXPORTED = (
@@ -45,7 +46,7 @@ class _Selection(ctypes.Structure):
 
 
 class _Share(ctypes.Structure):
-    _fields_ = [("leader", _vp), ("pages", _vp), ("size", _vp), ("order", _vp)]
+    _fields_ = [("leader", _vp), ("pages", _vp), ("size", _vp), ("order", _vp), ("flags", ctypes.c_uint32)]
 
 
 class _Scores(ctypes.Structure):
@@ -214,9 +215,10 @@ class PageSelection:
 
 class PageShare:
     """Rows that begin with the same pages, as akv_pages_share finds them: a contiguous CUDA int32 tensor [4][rows] of
-    leader, pages, size and order (akv_share in include/akv.h)."""
+    leader, pages, size and order (akv_share in include/akv.h).  always: akv_paged_attn_shared reads every group's pages once, also where
+    row by row is faster."""
 
-    def __init__(self, arrays):
+    def __init__(self, arrays, always: bool = False):
         if arrays.dim() != 2 or arrays.shape[0] != 4:
             raise ValueError("share must be [4][rows]")
         _lib()
@@ -224,7 +226,7 @@ class PageShare:
         at = _ints(arrays, "share", None, self.index)
         if self.index < 0:
             raise ValueError("share must be on the pool's device")
-        self._c = _Share(*(at + 4 * self.rows * i for i in range(4)))
+        self._c = _Share(*(at + 4 * self.rows * i for i in range(4)), AKV_SHARE_ALWAYS if always else 0)
         self.ref = ctypes.byref(self._c)
 
 

@@ -188,3 +188,9 @@ def test_binding_refuses():
             akv.KeptTokens(tokens, count)
     with pytest.raises(ValueError, match="contiguous"):
         akv.KeptTokens(i32(2, 4, 3).transpose(1, 2), i32(2))
+
+
+def test_share_flags():
+    for flags in (2, 1 << 31, 3):
+        refused(INVALID, "flags", "akv_pages_share", params(), pages(), share(flags=flags), AT, WS, None)
+        refused(INVALID, "flags", *attn(sh=lambda: share(flags=flags)))

@@ -20,8 +20,8 @@ def cuda():
         pytest.skip("no CUDA device")
 
 
-def share_of(c):
-    share = akv.PageShare(torch.full((4, len(c.lens_h)), -7, dtype=torch.int32, device="cuda"))
+def share_of(c, always=True):
+    share = akv.PageShare(torch.full((4, len(c.lens_h)), -7, dtype=torch.int32, device="cuda"), always)
     akv.akv_pages_share(c.p, c.pages, share)
     return share
 
@@ -220,7 +220,7 @@ def test_numbers_out_of_range_in_share():
                 arrays[row, b] = value
         if row == 3:
             arrays[3] = torch.where(good.arrays[3] == alone, good.arrays[3], value)
-        out, lse = run(c, q, akv.PageShare(arrays))
+        out, lse = run(c, q, akv.PageShare(arrays, always=True))
         if row < 2:
             assert torch.equal(out[alone], want[alone])
 
@@ -238,7 +238,7 @@ def test_graph_follows_the_cache():
     q = queries(c, 1, 1.0)
     one, missing = (c.lens > 0).int(), torch.zeros(1, dtype=torch.int32, device="cuda")
     arrays = torch.zeros((4, 3), dtype=torch.int32, device="cuda")
-    share = akv.PageShare(arrays)
+    share = akv.PageShare(arrays, always=True)
     out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
     ws = torch.empty(max(akv.akv_pages_workspace_size(pages), akv.akv_paged_attn_shared_workspace_size(p, pages)), dtype=torch.uint8, device="cuda")
 
@@ -297,3 +297,16 @@ def test_layers_and_strides():
     lse = torch.empty(q.shape[:3], device="cuda")
     akv.akv_paged_attn_shared(p, c.pages, wide, out, share_of(c), lse=lse, sm_scale=SM, layer=1)
     plain.check_shared(p, c, q, out, lse, SM, layer=1)
+
+
+@pytest.mark.parametrize("groups,H,G,T", [
+    ([(16000, [40] * 40), (900, [3, 7]), (5000, [1, 2, 3])], 4, 8, 1),  # one group is worth it, the others are row by row
+    ([(16000, [40] * 24), (9000, [5, 9]), (300, [1] * 3)], 4, 4, 4),    # pairs too, of 16 query rows
+    ([(2000, [40] * 10), (900, [3, 7])], 2, 4, 1),                      # all groups are row by row
+])
+def test_where_it_pays(groups, H, G, T):
+    p = params(H, G, 64, 64, False, True)
+    c = grouped(p, groups, seed=13)
+    q = queries(c, T, 1.0)
+    out, lse = run(c, q, share_of(c, always=False))
+    plain.check_shared(p, c, q, out, lse, SM)

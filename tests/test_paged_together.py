@@ -31,14 +31,14 @@ def int32(x):
 class Loop:
     """Two prompts, four answers, four spare rows; every page is the pool's, handed out by the page operations."""
 
-    def __init__(self, H, G, page, group, half, rotate, prompts=(700, 333), room=40, seed=0):
+    def __init__(self, H, G, page, group, half, rotate, prompts=(700, 333), room=40, seed=0, always=True):
         self.p = params(H, G, page, group, half, rotate)
         self.c = c = Cache(self.p, [0] * 10, room=max(prompts) + room, seed=seed)
         c.table.fill_(-1)
         self.refs = torch.zeros(c.pool.shape[1], dtype=torch.int32, device="cuda")
         self.pages = c.pages = akv.Pages(self.p, c.pool, c.table, c.lens, self.refs)
         self.missing = torch.zeros(1, dtype=torch.int32, device="cuda")
-        self.share = akv.PageShare(torch.zeros((4, 10), dtype=torch.int32, device="cuda"))
+        self.share = akv.PageShare(torch.zeros((4, 10), dtype=torch.int32, device="cuda"), always)
         self.scores = scores(c)
         self.prompts = list(prompts)
 
@@ -167,7 +167,7 @@ def test_graphs_that_share_a_workspace():
     graphs = []
     for c, q in cases:
         out, lse, now = torch.zeros_like(q), torch.zeros(q.shape[:3], device="cuda"), scores(c)
-        share = akv.PageShare(torch.zeros((4, len(c.lens_h)), dtype=torch.int32, device="cuda"))
+        share = akv.PageShare(torch.zeros((4, len(c.lens_h)), dtype=torch.int32, device="cuda"), always=not graphs)
 
         def step():
             akv.akv_pages_share(c.p, c.pages, share, ws=ws)
