@@ -3,10 +3,12 @@
 // The softmax's normaliser is known (lse), so a token's weight needs its own key alone: one pass over the key codes and their
 // parameters, no reference, no join, and every score is written by one thread.  Two kernels:
 //   up to 16 query rows a unit (a decode step): warp-level products of 16 tokens and 8 rows, codes straight from memory into operands
-//     (nibbles as fp16 subnormals, as in the attention): bound by memory.
+//     (nibbles as fp16 subnormals, as in the attention).  8 requests of 128 k tokens, 8 x 8 heads, rotated: 197 us, 671 MB (3.4 TB/s); an instruction is
+//     issued in 67 % of the cycles, ALU 45 %, FMA 31 %, tensor 29 %: the unpacking, the sums' way into logits and the two halves' products.
 //   more rows (a prompt's last tokens): S = K Q^T on the fifth-generation tensor cores with the tokens as rows.  A thread owns a token:
 //     it turns the codes into its lane of the operand in tensor memory, applies the token's scales to the products behind them,
-//     and adds its weights up along its lane without a shuffle; the queries are the columns.
+//     and adds its weights up along its lane without a shuffle; the queries are the columns.  64 query tokens, 8 x 4 heads, over 32 k tokens:
+//     54 us; the tensor cores work 33 % of the cycles, a warp waits for barriers 1.5, memory 1.3 and fixed latencies 1.7 cycles an instruction.
 // In both, tiles of all units (request, KV head) go in equal contiguous ranges to the CTAs.
 //   With codes in the products and scales outside, a logit is k (a_0 S_0 + a_1 S_1 + m_0 sum q_0 + m_1 sum q_1) over the groups of dimensions, with
 // c - 7.5 for c and m + 7.5 a for m (of many rows twice that), and a weight 2 to that less lse, which is subtracted in such parts that it
@@ -724,7 +726,9 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
   if (warp == kWorkers) tc_dealloc(tmem, 512);
 }
 
-constexpr int kFew = 16;  // query rows up to which the first kernel is the faster one
+// Query rows up to which the first kernel is the faster one: 16 rows over 325 k tokens of 8 heads 86 us there, 118 in the second; the first has no
+// registers for more.
+constexpr int kFew = 16;
 
 template <int NG, bool HILO>
 int launch(const WeightArgs& a, int dev, int sms, void* stream) {
