@@ -3,6 +3,10 @@
 Argument marshalling only, like the rest of the package, which re-exports every name here.  A program makes
 PagedParams and Pages once and calls with them; Pages keeps the C structures, so that a call of a decode loop
 converts only what changes.
+
+A serving loop: akv_pages_reserve, akv_paged_append, akv_pages_share (where rows are forks of others), then akv_paged_attn or
+akv_paged_attn_shared, or akv_paged_select and akv_paged_attn over what it keeps.  For rows of bounded length: akv_paged_weights after the attention, and now
+and then akv_paged_evict and akv_pages_trim.
 """
 from __future__ import annotations
 
