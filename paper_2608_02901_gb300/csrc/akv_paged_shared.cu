@@ -184,12 +184,8 @@ __device__ __forceinline__ void build_queries(const SharedArgs& a, Smem& S, cons
   const float down = b >= 0 ? *(const float*)(a.queries + row * kQueryRecord + 544) : 0.f;
   named_sync(2, 32 * (kSoftWarps + kKeyWarps));
   if (lane < kEach) S.lim[rr] = lim, S.row_at[rr] = row, S.row_scale[rr] = 0.5f * fabsf(a.scale) * down;  // (keys enter twice as large)
-  place_queries<HILO>(
-      lane,
-      [&](int r) {
-        const int64_t at = __shfl_sync(0xffffffffu, row, r);
-        return at < 0 ? nullptr : a.queries + at * kQueryRecord;
-      },
+  place_queries<HILO, kEach>(
+      lane, row < 0 ? nullptr : a.queries + row * kQueryRecord,
       [&](int r, int& to, uint32_t& panels, uint32_t& extra) { to = warp * kEach + r, panels = smem_u32(S.k_hi[0]), extra = smem_u32(S.qx); });
   proxy_fence();
   named_sync(2, 32 * (kSoftWarps + kKeyWarps));

@@ -168,28 +168,31 @@ __device__ __forceinline__ void wht_rows(float (&x)[R][4], int lane) {
         x[r][e] = lane & h ? o - x[r][e] : x[r][e] + o;
       }
 }
-// Eight query rows of akv_paged_query.cu by a warp: from their records (null: zeros) into operand panels (hi, with HILO low halves two panels on) and
-// the 16 more dimensions; record(r), then place(r, row, panels, extra).  All loads come first: each would wait for the store before it.
-template <bool HILO, class Record, class Place>
-__device__ __forceinline__ void place_queries(int lane, Record record, Place place) {
-  uint4 x[8], y[8];
+// R query rows of akv_paged_query.cu by a warp, 8 or 16: from their records (lane r has row r's; null: zeros) into operand panels (hi, with HILO low
+// halves two panels on) and the 16 more dimensions; place(r, row, panels, extra).  All loads come first: each would wait for the store before it.
+template <bool HILO, int R, class Place>
+__device__ __forceinline__ void place_queries(int lane, const uint8_t* record, Place place) {
+  auto from = [&](int r) { return (const uint8_t*)__shfl_sync(0xffffffffu, (unsigned long long)record, r); };
+  uint4 x[R], y = make_uint4(0, 0, 0, 0);
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    const uint8_t* from = record(r);
-    x[r] = y[r] = make_uint4(0, 0, 0, 0);
-    if (from && (HILO || lane < 16)) x[r] = *(const uint4*)(from + 16 * lane);
-    if (from && lane < 2) y[r] = *(const uint4*)(from + 512 + 16 * lane);
+  for (int r = 0; r < R; ++r) {
+    const uint8_t* at = from(r);
+    x[r] = make_uint4(0, 0, 0, 0);
+    if (at && (HILO || lane < 16)) x[r] = *(const uint4*)(at + 16 * lane);
   }
+  const uint8_t* at = from(lane >> 1 & (R - 1));
+  if (at) y = *(const uint4*)(at + 512 + 16 * (lane & 1));
   const int c = lane & 15;  // chunk 4 j + t: panel j / 2, chunk 4 (j & 1) + t of it
+  int row;
+  uint32_t panels, extra;
 #pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    int row;
-    uint32_t panels, extra;
+  for (int r = 0; r < R; ++r) {
     place(r, row, panels, extra);
     if (HILO || lane < 16)
       sts128(panels + (uint32_t)(lane >> 4) * (2 * kPanel) + (uint32_t)(c >> 3) * kPanel + 128 * row + 16 * ((c & 7) ^ (row & 7)), x[r]);
-    if (lane < 2) sts128(extra + extra_at(row) + 2048 * lane, y[r]);
   }
+  place(lane >> 1 & (R - 1), row, panels, extra);
+  if (lane < 2 * R) sts128(extra + extra_at(row) + 2048 * (lane & 1), y);
 }
 // Operand of 16 K without swizzle: [2][16][8 rows][16 bytes], 2048 bytes from one half of K to the other, 128 between groups of rows.
 __device__ __forceinline__ uint64_t plain_desc(uint32_t saddr) {

@@ -586,9 +586,9 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
           lse = a.lse[((int64_t)seg.b * a.T + row / v.G) * (v.H * v.G) + seg.h * v.G + row % v.G];
         }
 #pragma unroll 1
-        for (int r0 = 8 * warp; r0 < padded; r0 += 8 * kWorkers)  // (padded is a multiple of 16)
-          place_queries<HILO>(
-              lane, [&](int r) { return record_of(r0 + r); },
+        for (int r0 = 16 * warp; r0 < padded; r0 += 16 * kWorkers)  // (padded is a multiple of 16)
+          place_queries<HILO, 16>(
+              lane, record_of(r0 + (lane & 15)),
               [&](int r, int& row, uint32_t& panels, uint32_t& extra) {
                 row = (r0 + r) & 127, panels = smem_u32(S.q[r0 >> 7]), extra = smem_u32(S.qx[r0 >> 7]);
               });
