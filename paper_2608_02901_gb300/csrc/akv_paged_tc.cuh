@@ -78,6 +78,29 @@ __device__ __forceinline__ void tm_ld16x3(uint32_t at0, uint32_t at1, uint32_t a
       : "r"(at0), "r"(at1), "r"(at2)
       : "memory");
 }
+// 32 columns at 0 and 64, or at 0, 32 and 64, waited for together.
+__device__ __forceinline__ void tm_ld32xn(uint32_t at, float (&v)[2][32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n"
+      " tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0][0]), "=f"(v[0][1]), "=f"(v[0][2]), "=f"(v[0][3]), "=f"(v[0][4]), "=f"(v[0][5]), "=f"(v[0][6]), "=f"(v[0][7]), "=f"(v[0][8]), "=f"(v[0][9]), "=f"(v[0][10]), "=f"(v[0][11]), "=f"(v[0][12]), "=f"(v[0][13]), "=f"(v[0][14]), "=f"(v[0][15]), "=f"(v[0][16]), "=f"(v[0][17]), "=f"(v[0][18]), "=f"(v[0][19]), "=f"(v[0][20]), "=f"(v[0][21]), "=f"(v[0][22]), "=f"(v[0][23]), "=f"(v[0][24]), "=f"(v[0][25]), "=f"(v[0][26]), "=f"(v[0][27]), "=f"(v[0][28]), "=f"(v[0][29]), "=f"(v[0][30]), "=f"(v[0][31]),
+        "=f"(v[1][0]), "=f"(v[1][1]), "=f"(v[1][2]), "=f"(v[1][3]), "=f"(v[1][4]), "=f"(v[1][5]), "=f"(v[1][6]), "=f"(v[1][7]), "=f"(v[1][8]), "=f"(v[1][9]), "=f"(v[1][10]), "=f"(v[1][11]), "=f"(v[1][12]), "=f"(v[1][13]), "=f"(v[1][14]), "=f"(v[1][15]), "=f"(v[1][16]), "=f"(v[1][17]), "=f"(v[1][18]), "=f"(v[1][19]), "=f"(v[1][20]), "=f"(v[1][21]), "=f"(v[1][22]), "=f"(v[1][23]), "=f"(v[1][24]), "=f"(v[1][25]), "=f"(v[1][26]), "=f"(v[1][27]), "=f"(v[1][28]), "=f"(v[1][29]), "=f"(v[1][30]), "=f"(v[1][31])
+      : "r"(at), "r"(at + 64)
+      : "memory");
+}
+__device__ __forceinline__ void tm_ld32xn(uint32_t at, float (&v)[3][32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%96];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%97];\n"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, %80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95}, [%98];\n"
+      " tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0][0]), "=f"(v[0][1]), "=f"(v[0][2]), "=f"(v[0][3]), "=f"(v[0][4]), "=f"(v[0][5]), "=f"(v[0][6]), "=f"(v[0][7]), "=f"(v[0][8]), "=f"(v[0][9]), "=f"(v[0][10]), "=f"(v[0][11]), "=f"(v[0][12]), "=f"(v[0][13]), "=f"(v[0][14]), "=f"(v[0][15]), "=f"(v[0][16]), "=f"(v[0][17]), "=f"(v[0][18]), "=f"(v[0][19]), "=f"(v[0][20]), "=f"(v[0][21]), "=f"(v[0][22]), "=f"(v[0][23]), "=f"(v[0][24]), "=f"(v[0][25]), "=f"(v[0][26]), "=f"(v[0][27]), "=f"(v[0][28]), "=f"(v[0][29]), "=f"(v[0][30]), "=f"(v[0][31]),
+        "=f"(v[1][0]), "=f"(v[1][1]), "=f"(v[1][2]), "=f"(v[1][3]), "=f"(v[1][4]), "=f"(v[1][5]), "=f"(v[1][6]), "=f"(v[1][7]), "=f"(v[1][8]), "=f"(v[1][9]), "=f"(v[1][10]), "=f"(v[1][11]), "=f"(v[1][12]), "=f"(v[1][13]), "=f"(v[1][14]), "=f"(v[1][15]), "=f"(v[1][16]), "=f"(v[1][17]), "=f"(v[1][18]), "=f"(v[1][19]), "=f"(v[1][20]), "=f"(v[1][21]), "=f"(v[1][22]), "=f"(v[1][23]), "=f"(v[1][24]), "=f"(v[1][25]), "=f"(v[1][26]), "=f"(v[1][27]), "=f"(v[1][28]), "=f"(v[1][29]), "=f"(v[1][30]), "=f"(v[1][31]),
+        "=f"(v[2][0]), "=f"(v[2][1]), "=f"(v[2][2]), "=f"(v[2][3]), "=f"(v[2][4]), "=f"(v[2][5]), "=f"(v[2][6]), "=f"(v[2][7]), "=f"(v[2][8]), "=f"(v[2][9]), "=f"(v[2][10]), "=f"(v[2][11]), "=f"(v[2][12]), "=f"(v[2][13]), "=f"(v[2][14]), "=f"(v[2][15]), "=f"(v[2][16]), "=f"(v[2][17]), "=f"(v[2][18]), "=f"(v[2][19]), "=f"(v[2][20]), "=f"(v[2][21]), "=f"(v[2][22]), "=f"(v[2][23]), "=f"(v[2][24]), "=f"(v[2][25]), "=f"(v[2][26]), "=f"(v[2][27]), "=f"(v[2][28]), "=f"(v[2][29]), "=f"(v[2][30]), "=f"(v[2][31])
+      : "r"(at), "r"(at + 32), "r"(at + 64)
+      : "memory");
+}
 __device__ __forceinline__ void tm_st32(uint32_t at, const float (&v)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"

@@ -8,7 +8,7 @@
 //   more rows (a prompt's last tokens): S = K Q^T on the fifth-generation tensor cores with the tokens as rows.  A thread owns a token:
 //     it turns the codes into its lane of the operand in tensor memory, applies the token's scales to the products behind them,
 //     and adds its weights up along its lane without a shuffle; the queries are the columns.  64 query tokens, 8 x 4 heads, over 32 k tokens:
-//     54 us; the tensor cores work 33 % of the cycles, a warp waits for barriers 1.5, memory 1.3 and fixed latencies 1.7 cycles an instruction.
+//     48.5 us (53 with 16 columns a load), 8 of them until the first product; then a block's 17 products take 550 cycles to issue, its weights 700.
 // In both, tiles of all units (request, KV head) go in equal contiguous ranges to the CTAs.
 //   With codes in the products and scales outside, a logit is k (a_0 S_0 + a_1 S_1 + m_0 sum q_0 + m_1 sum q_1) over the groups of dimensions, with
 // c - 7.5 for c and m + 7.5 a for m (of many rows twice that), and a weight 2 to that less lse, which is subtracted in such parts that it
@@ -429,7 +429,7 @@ constexpr float kOnes = 16.f;  // the dimensions that carry lse count 16
 struct Smem {
   uint8_t q[2][4 * kPanel];  // 128 rows each: high, then low halves
   uint8_t qx[2][kExtra], kx[W][kExtra];
-  float k[kHeld], lse[kHeld];  // what a row's products count; the part of -lse behind them (-infinity: the row adds nothing)
+  alignas(16) float k[kHeld], lse[kHeld];  // what a row's products count; the part of -lse behind them (-infinity: the row adds nothing)
   int sees[kHeld];             // tokens that it sees
   int behind[kBlocks];         // whether a block has rows with such a part
   uint64_t k_full[W], s_full[W][2], s_free[W][2], q_full, drained[W];
@@ -678,26 +678,45 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
             tc_fence_after();
             const int n = columns(rows, block);
             const bool behind = edge || *(volatile int*)&S.behind[block];
-#pragma unroll 1
-            for (int c = 0; c < n; c += 16) {
-              float x[16], y[16], z[16];
-              tm_ld16x3(tS + c, tS + (NG - 1) * kCols + c, tS + 2 * kCols + c, x, y, z);
-              const float2* k2 = (const float2*)&S.k[block * kCols + c];
+            const float* ks = &S.k[block * kCols];
+            // the logits, in log2 units less lse, of two columns
+            auto logit = [&](float x0, float x1, float y0, float y1, float z0, float z1, float2 k) {
+              float2 l = __fmul2_rn(make_float2(z0, z1), b2);  // (by a power of two)
+              if (NG == 2) l = __ffma2_rn(s1, make_float2(y0, y1), l);
+              return __fmul2_rn(__ffma2_rn(s0, make_float2(x0, x1), l), k);
+            };
+            if (n == kCols && !behind) {
+              float x[NG == 2 ? 3 : 2][32];
+              tm_ld32xn(tS, x);
 #pragma unroll
-              for (int e = 0; e < 16; e += 2) {
-                float2 l = make_float2(z[e], z[e + 1]);
-                if (NG == 2) l = __ffma2_rn(s1, make_float2(y[e], y[e + 1]), big ? __fmul2_rn(l, b2) : l);
-                else if (big) l = __fmul2_rn(l, b2);
-                l = __ffma2_rn(s0, make_float2(x[e], x[e + 1]), l);
-                l = __fmul2_rn(l, k2[e >> 1]);
-                if (behind) {
-                  const float2 lse = *(const float2*)&S.lse[block * kCols + c + e];
-                  const int2 sees = *(const int2*)&S.sees[block * kCols + c + e];
-                  l.x = tok < sees.x ? l.x + lse.x : -kInf;
-                  l.y = tok < sees.y ? l.y + lse.y : -kInf;
+              for (int e = 0; e < 32; e += 4) {
+                const float4 k = *(const float4*)(ks + e);
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                  float2 l = logit(x[0][e + i], x[0][e + i + 1], x[NG - 1][e + i], x[NG - 1][e + i + 1], x[NG][e + i], x[NG][e + i + 1],
+                                   i ? make_float2(k.z, k.w) : make_float2(k.x, k.y));
+                  l.x = exp2_fast(l.x), l.y = exp2_fast(l.y);
+                  sum[i >> 1] = __fadd2_rn(sum[i >> 1], l);
                 }
-                l.x = exp2_fast(l.x), l.y = exp2_fast(l.y);
-                sum[e >> 1 & 1] = __fadd2_rn(sum[e >> 1 & 1], l);
+              }
+            } else {
+#pragma unroll 1
+              for (int c = 0; c < n; c += 16) {
+                float x[16], y[16], z[16];
+                tm_ld16x3(tS + c, tS + (NG - 1) * kCols + c, tS + 2 * kCols + c, x, y, z);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                  const int at = block * kCols + c + e;
+                  float2 l = logit(x[e], x[e + 1], y[e], y[e + 1], z[e], z[e + 1], *(const float2*)(ks + c + e));
+                  if (behind) {
+                    const float2 lse = *(const float2*)&S.lse[at];
+                    const int2 sees = *(const int2*)&S.sees[at];
+                    l.x = tok < sees.x ? l.x + lse.x : -kInf;
+                    l.y = tok < sees.y ? l.y + lse.y : -kInf;
+                  }
+                  l.x = exp2_fast(l.x), l.y = exp2_fast(l.y);
+                  sum[e >> 1 & 1] = __fadd2_rn(sum[e >> 1 & 1], l);
+                }
               }
             }
             tc_fence_before();
