@@ -712,9 +712,9 @@ akv_status akv_pages_share(const akv_paged_params* p, const akv_pages* pages, co
 /* akv_paged_attn of the same arguments, but for the order of its sums: the shared pages of a group are read once for all its rows'
  * queries (as one matrix product), every row's further tokens as akv_paged_attn reads them, and both parts are joined in one
  * softmax.  Groups of few query rows, and batches whose groups are short, are attended row by row (share->flags).  Numbers in `share` that are out of range are left out (rows outside the table) or clamped (pages).
- *   In the shared part a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
- * m + c a to fp16 as well (2^-11 of it; where 16 tokens have a scale above 2048 or a minimum beyond 16384, 2^-20 at least).  A query that sees a token
- * with an infinity or a NaN has NaN in all its outputs. */
+ *   Of pages that are read once a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
+ * m + c a to fp16 as well (2^-11 of it; where 16 tokens have a scale above 2048 or a minimum beyond 16384, 2^-20 at least).  A query that sees
+ * such a token with an infinity or a NaN has NaN in all its outputs. */
 akv_status akv_paged_attn_shared_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
                                                 size_t* ws_bytes);
 akv_status akv_paged_attn_shared(const akv_paged_params* p, const akv_pages* pages, int32_t layer, const akv_rows* q,
@@ -733,7 +733,7 @@ typedef struct akv_scores {
  * which gives their lse, fp32 [rows][T][n_q_heads]):
  *     now[b][h][i] = decay was[b][h][i] + sum over t and the G query heads of h of exp(sm_scale q . k^_i - lse)
  * over the queries that see token i, for the tokens i < lens[b] that request b holds; further numbers are left as they were.
- * `was` may be null (zeros) or the same as `now`, and is not read where decay is 0.  Queries whose lse is not a finite number, and
+ * `was` may be null (zeros), the same as `now`, or apart from it; it is not read where decay is 0.  Queries whose lse is not a finite number, and
  * tokens whose key has an infinity or a NaN or whose page is none of the pool's, add nothing.  Sums in fp32, in a fixed order. */
 akv_status akv_paged_weights_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
                                             size_t* ws_bytes);

@@ -191,7 +191,9 @@ __global__ void __launch_bounds__(256) akv_pages_trim_kernel(PagesState s, const
 // Rows that begin with the same pages, in one cluster: the lowest row of each first page, the positions alike with it
 // (a warp per row and 1024 positions), then each row's rank among (leader, row) by counting.  A chain of five phases, each the
 // latency of a few dependent reads and a cluster barrier.
-constexpr int kShareCtas = 8, kShareThreads = 1024, kSharePart = 1024;
+// Of few rows every CTA finds the leaders by itself in shared memory, and only the positions go through the cluster: three phases.  Microseconds,
+// caches cold, of 64, 256, 512 rows with 64 positions 8.9, 12.9, 23.2; with the other way 12.9, 13.0, 19.1.
+constexpr int kShareCtas = 8, kShareThreads = 1024, kSharePart = 1024, kShareFew = 256;
 __global__ void __cluster_dims__(kShareCtas, 1, 1) __launch_bounds__(kShareThreads)
     akv_pages_share_kernel(PagesState s, akv_share out, int32_t* first) {
   launch_dependents();
@@ -207,28 +209,10 @@ __global__ void __cluster_dims__(kShareCtas, 1, 1) __launch_bounds__(kShareThrea
     const int page = held(r) > 0 ? s.table[(int64_t)r * s.table_stride] : -1;
     return in_pool(s, page) ? page : -1;
   };
-  for (int r = tid; r < s.rows; r += all) {
-    const int page = page0(r);
-    if (page >= 0) first[page] = INT32_MAX;
-  }
-  cl.sync();
-  for (int r = tid; r < s.rows; r += all) {
-    const int page = page0(r);
-    if (page >= 0) atomicMin(first + page, r);
-  }
-  cl.sync();
-  for (int r = tid; r < s.rows; r += all) {
-    const int page = page0(r);
-    out.leader[r] = page >= 0 ? __ldcg(first + page) : r;
-    out.pages[r] = held(r);
-  }
-  cl.sync();
   const int parts = (s.max_pages + kSharePart - 1) / kSharePart;
-  for (int64_t k = warp; k < (int64_t)s.rows * parts; k += warps) {
-    const int r = (int)(k / parts), lead = __ldcg(out.leader + r);
-    if (lead == r) continue;
-    const int both = min(held(r), held(lead));
-    const int from = (int)(k % parts) * kSharePart, to = min(both, from + kSharePart);
+  // where row r and its leader part, of positions of part i: a warp each
+  auto compare = [&](int r, int lead, int both, int i) {
+    const int from = i * kSharePart, to = min(both, from + kSharePart);
     const int32_t *a = s.table + (int64_t)r * s.table_stride, *b = s.table + (int64_t)lead * s.table_stride;
     int differs = from == 0 ? both : INT32_MAX;  // (the first part sees to the lengths)
     for (int j0 = from; j0 < to && differs > j0; j0 += 256) {
@@ -246,6 +230,60 @@ __global__ void __cluster_dims__(kShareCtas, 1, 1) __launch_bounds__(kShareThrea
       differs = __reduce_min_sync(0xffffffffu, differs);
     }
     if (lane == 0 && differs != INT32_MAX) atomicMin(out.pages + lead, differs);
+  };
+  if (s.rows <= kShareFew) {
+    __shared__ int pages[kShareFew], holds[kShareFew], leads[kShareFew];
+    const int r = threadIdx.x;
+    int lead = r;
+    if (r < s.rows) {
+      const int n = holds[r] = held(r);
+      pages[r] = page0(r);
+      if (blockIdx.x == 0) out.pages[r] = n;
+    }
+    __syncthreads();
+    if (r < s.rows && pages[r] >= 0)
+      for (int j = r - 1; j >= 0; --j) lead = pages[j] == pages[r] ? j : lead;
+    if (r < s.rows) leads[r] = lead;
+    cl.sync();
+    for (int k = warp; k < s.rows * parts; k += warps) {
+      const int row = k / parts, of = leads[row];
+      if (of != row) compare(row, of, min(holds[row], holds[of]), k % parts);
+    }
+    int rank = 0, size = 0;
+    if (blockIdx.x == 0 && r < s.rows)
+      for (int j = 0; j < s.rows; ++j) {
+        const int x = leads[j];
+        rank += x < lead || (x == lead && j < r);
+        size += x == lead;
+      }
+    cl.sync();
+    if (blockIdx.x == 0 && r < s.rows) {
+      out.leader[r] = lead;
+      out.pages[r] = size > 1 ? __ldcg(out.pages + lead) : 0;  // (the leader writes its number back as it is)
+      out.size[r] = size;
+      out.order[rank] = r;
+    }
+    return;
+  }
+  for (int r = tid; r < s.rows; r += all) {
+    const int page = page0(r);
+    if (page >= 0) first[page] = INT32_MAX;
+  }
+  cl.sync();
+  for (int r = tid; r < s.rows; r += all) {
+    const int page = page0(r);
+    if (page >= 0) atomicMin(first + page, r);
+  }
+  cl.sync();
+  for (int r = tid; r < s.rows; r += all) {
+    const int page = page0(r);
+    out.leader[r] = page >= 0 ? __ldcg(first + page) : r;
+    out.pages[r] = held(r);
+  }
+  cl.sync();
+  for (int64_t k = warp; k < (int64_t)s.rows * parts; k += warps) {
+    const int r = (int)(k / parts), lead = __ldcg(out.leader + r);
+    if (lead != r) compare(r, lead, min(held(r), held(lead)), (int)(k % parts));
   }
   cl.sync();
   for (int r = warp; r < s.rows; r += warps) {

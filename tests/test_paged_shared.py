@@ -88,6 +88,23 @@ def test_many_rows_and_pages():
     check_share(c, share_of(c))
 
 
+@pytest.mark.parametrize("rows", [1, 2, 255, 256, 257, 300])
+def test_numbers_of_rows(rows):
+    """Rows without tokens, of one page, of the same first pages, and pages outside the pool among them."""
+    p = params(1, 1, 16)
+    rng = np.random.default_rng(rows)
+    c = Cache(p, [int(n) for n in rng.integers(0, 80, rows)], seed=rows)
+    some = rng.integers(0, rows, rows)
+    for b in range(rows):
+        if rng.random() < 0.7:
+            n = int(rng.integers(1, 6))
+            c.table[b, :n] = c.table[int(some[b]), :n]
+    c.table[rows // 2, 0] = -1
+    c.table[rows // 3, 1] = 10**6
+    c.lens.copy_(torch.tensor(c.lens_h, dtype=torch.int32))
+    check_share(c, share_of(c))
+
+
 GROUPS = [(300, [1, 5, 100, 0]), (0, [40]), (1000, [3, 140]), (64, [1]), (129, [7] * 3)]
 
 
