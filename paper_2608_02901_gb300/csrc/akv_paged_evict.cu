@@ -1,15 +1,16 @@
 // Eviction from the paged cache by scores: which tokens a row keeps, and their move to the first places of a row.
 //
 // A cluster per row and KV head does all of it in one launch.  The lowest score that is kept comes from a radix select over
-// (forced, score) as 32-bit keys, 11, 11 and 10 bits a pass, counts joined through distributed shared memory; the kept tokens'
+// (forced, score) as 32-bit keys, 11, 11 and 10 bits a pass, counts joined through distributed shared memory (where the first pass leaves few keys
+// open, one CTA takes them and finds the rest: a pass through the cluster is 3.5 us, 27.5 to 24.6 us of 32 k tokens cut to 4 k); the kept tokens'
 // places are counted off in order, each CTA over its share of the row; then the tokens move, a sub-block of 16 a warp.
 // A token's 64 bytes of key codes and its parameters are contiguous, its value codes are 32 pieces of two bytes, next to those of
 // its neighbour: a warp loads the sixteen-byte units that hold them and puts two tokens' halves together (PRMT).
 // In place: a kept token goes to a place at or before its own, so the places that a round of sub-blocks writes hold no token
 // that a later round reads; a round is read by the whole cluster, then (cluster barrier) written.
-// What bounds it: of long rows the kept tokens' bytes, read and written (4 rows of 128 k tokens, 8 heads, half of them kept, in place: 182 us; 640 MB
-// asked for, 858 MB moved, since a 32-byte sector holds values of four tokens: 4.7 TB/s), a round's reads waiting for its barrier and its writes; of short ones
-// the chain of some twelve dependent reads and barriers (32 rows of 1.1 k tokens 25.6 us, 32 k tokens cut to 4 k 27.5).
+// What bounds it: of long rows the kept tokens' bytes, read and written (4 rows of 128 k tokens, 8 heads, half of them kept, in place: 175 us; 640 MB
+// asked for, 858 MB moved, since a 32-byte sector holds values of four tokens: 4.9 TB/s), a round's reads waiting for its barrier and its writes; of short ones
+// the chain of some twelve dependent reads and barriers (32 rows of 1.1 k tokens 25.6 us, 32 k tokens cut to 4 k 24.6).
 #include <cooperative_groups.h>
 
 #include "akv_paged.cuh"
@@ -21,6 +22,7 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
+constexpr int kCand = 6144;  // keys that one CTA of a cluster takes
 constexpr int kEach = 8, kBatch = kThreads * kEach;  // scores of a thread, of a CTA, that are under way at a time
 
 struct EvictArgs {
@@ -73,7 +75,8 @@ struct Cluster {
 template <int C>
 __global__ void __launch_bounds__(kThreads, 2) akv_paged_evict_kernel(const __grid_constant__ EvictArgs a) {
   __shared__ uint32_t hist[kBins], slice[kBins / C], part[kWarps], part2[kWarps];
-  __shared__ uint32_t total, flag, n_above, n_equal, first_gone;
+  __shared__ uint32_t total, flag, n_above, n_equal, first_gone, n_cand;
+  __shared__ uint32_t cand[C > 1 ? kCand : 1];
   const Cluster<C> cl;
   const PagedView& v = a.v;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 2) akv_paged_evict_kernel(const __gr
     bad = bad || page < 0 || (!stays && v.refs && v.refs[page] > 1);
   }
   const int any_bad = __syncthreads_or(bad);
-  if (tid == 0) flag = (uint32_t)any_bad, first_gone = (uint32_t)held;
+  if (tid == 0) flag = (uint32_t)any_bad, first_gone = (uint32_t)held, n_cand = 0;
   cl.sync();
   uint32_t refuse = 0;
 #pragma unroll
@@ -191,13 +194,69 @@ __global__ void __launch_bounds__(kThreads, 2) akv_paged_evict_kernel(const __gr
       inc -= mine_n;
 #pragma unroll
       for (int k = 0; k < kMost; ++k) {
-        if (here[k] && inc < left && inc + here[k] >= left) part2[0] = (uint32_t)(owner * each + each - 1 - (n * tid + k)), part2[1] = left - inc;
+        if (here[k] && inc < left && inc + here[k] >= left) part2[0] = (uint32_t)(owner * each + each - 1 - (n * tid + k)), part2[1] = left - inc, part2[2] = here[k];
         inc += here[k];
       }
       __syncthreads();
       cut |= part2[0] << shift;
       left = part2[1];
       cl.sync();  // (slices and histograms have been read)
+      if constexpr (C > 1) {
+        // the keys that the first bits leave open go to one CTA, which finds the rest by itself
+        if (pass == 0 && part2[2] <= (uint32_t)kCand) {
+          uint32_t* const all = cl.of(cand, 0);
+          each_batch([&](int i0) {
+            uint32_t open[kEach], n = 0, at = 0;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+              open[e] = __ballot_sync(0xffffffffu, place(i0, e) < hi && key[e] >> 21 == cut >> 21);
+              n += __popc(open[e]);
+            }
+            if (!n) return;
+            if (lane == 0) at = atomicAdd(cl.of(&n_cand, 0), n);
+            at = __shfl_sync(0xffffffffu, at, 0);
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+              if (open[e] >> lane & 1) all[at + __popc(open[e] & ((1u << lane) - 1))] = key[e];
+              at += __popc(open[e]);
+            }
+          });
+          cl.sync();
+          if (rank == 0) {
+            const int n = (int)part2[2];
+#pragma unroll 1
+            for (int low = 14; low >= 0; low -= 7) {
+              if (tid < 128) hist[tid] = 0;
+              __syncthreads();
+              for (int k = tid; k < n; k += kThreads)
+                if ((cand[k] ^ cut) >> (low + 7) == 0) atomicAdd(&hist[cand[k] >> low & 127], 1u);
+              __syncthreads();
+              uint32_t there[4], sum4 = 0;  // every warp: lane t bins 127 - 4 t and the three before
+#pragma unroll
+              for (int k = 0; k < 4; ++k) there[k] = hist[127 - 4 * lane - k], sum4 += there[k];
+              uint32_t from_top = sum4;
+#pragma unroll
+              for (int s = 1; s < 32; s *= 2) {
+                const uint32_t o = __shfl_up_sync(0xffffffffu, from_top, s);
+                if (lane >= s) from_top += o;
+              }
+              from_top -= sum4;
+              uint32_t found = 0, rest = 0;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                if (there[k] && from_top < left && from_top + there[k] >= left) found = 127 - 4 * lane - k, rest = left - from_top;
+                from_top += there[k];
+              }
+              cut |= __reduce_max_sync(0xffffffffu, found) << low, left = __reduce_max_sync(0xffffffffu, rest);
+              __syncthreads();
+            }
+            if (tid == 0) part2[0] = cut, part2[1] = left;
+          }
+          cl.sync();
+          cut = *cl.of(&part2[0], 0), left = *cl.of(&part2[1], 0);
+          break;
+        }
+      }
     }
   }
 

@@ -128,6 +128,18 @@ def test_many_of_one_score_at_the_cut():
     s.check([0], [0], [2500], 0, 0)
 
 
+@pytest.mark.parametrize("near", [1.0, 0.3, 0.05])
+@pytest.mark.parametrize("n,H", [(20000, 1), (40000, 3), (7000, 100)])
+def test_scores_close_together(near, n, H):
+    """All, some or few of the scores alike in their first bits, some of them the same; clusters of all sizes."""
+    s = State([n, 0], [0, n // 3], H=H, page=128, seed=n)
+    far = s.rng.random(s.scores.shape) > near
+    s.scores = (1 + s.rng.random(s.scores.shape) / 16).astype(np.float32)
+    s.scores[s.rng.random(s.scores.shape) < 0.2] = 1.03125
+    s.scores[far] = np.exp(4 * s.rng.standard_normal(int(far.sum()))).astype(np.float32)
+    s.check([0], [1], [n // 3], 4, 32)
+
+
 def test_pairs_left_alone():
     s = State([100, 100, 100, 100, 0, 0], [0, 0, 0, 0, 50, 50], seed=5)
     s.refs[s.table[1, 1]] = 2      # a page that would be written has another holder
