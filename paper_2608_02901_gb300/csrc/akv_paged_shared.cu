@@ -14,7 +14,7 @@
 //     p = 2^(S scale - reference), its sum, P as fp16 over S's columns.  (A thread a row, the two warpgroups' tiles in turn and the reference
 //     handed from one to the other, took 243 us for 8 prompts of 32 k tokens with 8 answers each where this
 //     takes 219, 249 for 235 of 32 answers over 128 k.)
-// What bounds it (32 answers, 8 x 8 heads, 128 k shared tokens, rotated: 200 us of 235, in all 585 TFLOP/s of the products that the formula
+// What bounds it (32 answers, 8 x 8 heads, 128 k shared tokens, rotated: 200 us of 230, in all 598 TFLOP/s of the products that the formula
 // has, 1420 of those that are made in the 200 us): the tensor cores work 65 % of the cycles, a warp instruction is issued in 70 %; of a
 // tile's 3500 cycles the products need 2260, and the rest is the chain from S through P to the next use of its columns.  S of three tiles
 // would not fit into tensor memory.  Of few rows the products cost the same.
