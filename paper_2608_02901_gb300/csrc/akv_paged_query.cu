@@ -1,7 +1,8 @@
 // Query rows as operands of the paged cache's products on the fifth-generation tensor cores, once for all CTAs that multiply with them.
 //
 // A warp a row: its rotation, its power of two, its halves and its sums are some 300 instructions, which every CTA of a unit would
-// repeat (256 rows of 8 heads for 152 CTAs: 18 us of 60).  Beside it, in a CTA of its own, what the plan of shared pages is worth.  A row's record lies as akv_paged_tc.cuh's operands have it, without their swizzle.
+// repeat (256 rows of 8 heads for 152 CTAs: 18 us of 60).  A row's record lies as akv_paged_tc.cuh's operands have it, without their swizzle.
+// Beside it, in a CTA of its own: for which groups the plan of shared pages is worth following.
 #include "akv_paged.cuh"
 #include "akv_paged_tc.cuh"
 
