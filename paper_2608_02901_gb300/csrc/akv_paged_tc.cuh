@@ -57,15 +57,7 @@ __device__ __forceinline__ void tm_ld32(uint32_t at, float (&v)[32]) {
       : "r"(at)
       : "memory");
 }
-__device__ __forceinline__ void tm_ld16(uint32_t at, float (&v)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-      " tcgen05.wait::ld.sync.aligned;"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
-      : "r"(at)
-      : "memory");
-}
-// The same of three places, waited for together.
+// 16 columns of three places, waited for together.
 __device__ __forceinline__ void tm_ld16x3(uint32_t at0, uint32_t at1, uint32_t at2, float (&u)[16], float (&v)[16], float (&w)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%48];\n"
