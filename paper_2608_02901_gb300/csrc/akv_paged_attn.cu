@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const PagedView& v = a.v;
 
-  if (M != kOwn) launch_dependents();
+  launch_dependents();
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&S.full[s]), 1);
@@ -310,8 +310,6 @@ __global__ void __launch_bounds__(32 * (warps_of(NT) + 1), ctas_of(NT)) akv_page
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   wait_for_stream();
-  // (the shared pages' launch runs beside this one, and reads what was written before it: every CTA has waited for that)
-  if (M == kOwn) launch_dependents();
   Cursor<M> c;
   const Range r = plan<kThreads, M>(a, S.plan, c);  // (its barriers order the initialisation too)
   if (M != kOwn && tid == 0) a.desc[blockIdx.x] = make_int4(-1, 0, 0, 0);

@@ -1,5 +1,5 @@
 // Attention over pages that rows share: the shared pages once for all rows of a group, as matrix products on the fifth-generation
-// tensor cores, and a launch that joins them with the rows' own tokens (akv_paged_attn.cu's part, launched before and run beside).
+// tensor cores, and a launch that joins them with the rows' own tokens (akv_paged_attn.cu's part, launched before).
 //
 // A unit is a group's KV head and up to 128 of its query rows (members x query tokens x query heads); units are cut into tiles of
 // 128 tokens, the tiles of all units into equal contiguous ranges, one per CTA, one CTA an SM.  In a CTA
@@ -200,7 +200,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
   const PagedView& v = a.v;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   volatile int* failed = &S.failed;
-  // What this launch reads was written before the launch that it runs beside, whose CTAs have all waited for it.
   launch_dependents();
   if (tid == 0) {
     for (int s = 0; s < 2; ++s) {
@@ -223,12 +222,12 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // (also for the own tokens' launch, which writes nothing that is read here: what the launch before that one wrote is
+  // only sure to be seen behind a wait)
+  wait_for_stream();
   Segment seg;
   const Walk w = plan(a, S, seg);
-  if (w.lo >= w.hi) {
-    wait_for_stream();
-    return;
-  }
+  if (w.lo >= w.hi) return;
   if (warp == kMmaWarp) tc_alloc(smem_u32(&S.tmem), kCols);
   tc_fence_before();
   __syncthreads();
@@ -667,7 +666,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) tc_dealloc(tmem, kCols);
-  wait_for_stream();  // (so that whoever depends on this launch has waited for the one beside it as well)
 }
 
 // The parts of every query row together: its own tokens' and the shared ones', each whole or in the slots of several CTAs.  A warp a row.
