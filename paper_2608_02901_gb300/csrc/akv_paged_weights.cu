@@ -432,7 +432,7 @@ struct Smem {
   alignas(16) float k[kHeld], lse[kHeld];  // what a row's products count; the part of -lse behind them (-infinity: the row adds nothing)
   int sees[kHeld];             // tokens that it sees
   int behind[kBlocks];         // whether a block has rows with such a part
-  uint64_t k_full[W], s_full[W][2], s_free[W][2], q_full, drained[W];
+  uint64_t k_full[W], s_full[W][2], s_free[W][2], drained[W];
   int64_t part[4 * W + 4], place[2];
   uint32_t tmem;
   int failed;
@@ -455,7 +455,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
         mbar_init(smem_u32(&S.s_free[w][b]), 4);
       }
     }
-    mbar_init(smem_u32(&S.q_full), kWorkers);
     for (int w = 0; w < W; ++w) mbar_init(smem_u32(&S.drained[w]), 1);
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -474,16 +473,17 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
   auto columns = [](int rows, int block) { return min(kCols, (rows - block * kCols + 15) & ~15); };
 
   if (warp >= kWorkers && warp < kWorkers + W) {
-    // ---- the products of a warpgroup's tiles, a block of columns after the other
+    // ---- the products of a warpgroup's tiles, a block of columns after the other.  Keys of a tile tell that the queries are there
+    // too: every warp of the warpgroup has passed the barrier behind them.  (A barrier for queries alone would go on without the
+    // warp where its warpgroup has no tile, and two phases of it look alike.)
     const int w = warp - kWorkers;
-    uint32_t n_k = 0, n_s = 0, n_q = 0;
+    uint32_t n_k = 0, n_s = 0;
     bool ok = true;
     const uint32_t k = tmem + kColK + 64 * w, d0 = tmem + kColS + 2 * kColsS * w;
     const uint64_t dkx = plain_desc(smem_u32(S.kx[w]));
     for (int64_t at = lo; ok && at < hi;) {
       for (int pass = 0; ok && pass < passes; ++pass) {
         const int rows = rows_of(pass), blocks = (rows + kCols - 1) / kCols;
-        ok = mbar_wait_w(smem_u32(&S.q_full), n_q++ & 1);
 #pragma unroll 1
         for (int i = w; ok && i < seg.n; i += W) {
           ok = mbar_wait_w(smem_u32(&S.k_full[w]), n_k++ & 1) && !warp_failed(failed);
@@ -615,7 +615,6 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_weights_kernel(const __
         proxy_fence();
         __syncwarp();
         named_sync(1, 32 * kWorkers);
-        if (lane == 0) mbar_arrive(smem_u32(&S.q_full));
 
         bool ok = true;
 #pragma unroll 1

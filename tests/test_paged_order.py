@@ -72,3 +72,11 @@ def test_calls_back_to_back():
     for _ in range(5):
         for (out, lse), (o, l) in zip(run(lambda: None), want):
             assert torch.equal(out, o) and torch.equal(lse, l)
+
+
+def test_barriers_of_the_weights_belong_to_a_warpgroup():
+    """A phase is told by its parity, so whoever waits must not fall two phases behind: a product warp has tiles only where its
+    warpgroup has, and may wait only for barriers on which that warpgroup waits for it in turn."""
+    (body,) = [body for name, body in kernels("akv_paged_weights.cu") if name == "akv_paged_weights_kernel"]
+    waits = re.findall(r"mbar_wait_w\(smem_u32\(&S\.(\w+(?:\[\w+\])?)", body)
+    assert waits and all(re.fullmatch(r"\w+\[w\]", x) for x in waits), waits
