@@ -256,12 +256,20 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
       const RowRaw raw[1] = {fetch_row(a, seg, rr)};
       float x1[1][4], lse1[1];
       open_rows<HILO>(a, raw, x1, lse1);
-      const float(&x)[4] = x1[0];
+      float(&x)[4] = x1[0];
       const float lse = lse1[0];
       float big = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
       big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
       const int e2 = min(max((int)(__float_as_uint(big) >> 23) - 126, -100), 128);
       const float up = pow2(14 - e2);  // below 2^14, exact in fp16 down to 2^-23 of that
+      // What the products count.  Rows of zeros, and scales of (nearly) zero, have logits below 1e-27, and what -lse has below 2^-8 would not
+      // go with their products: such rows are zeros, whose products count 1.
+      float k = fabsf(a.scale) * pow2(e2 - 10) * 1048576.f;
+      if (!(k > 2e-33f)) {
+        k = 1.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = 0.f;
+      }
       // the high half is a multiple of 2^-11 of the largest's power of two: sums of its products with codes are exact in 24 bits
       float high[4], sum[2];
 #pragma unroll
@@ -282,11 +290,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) akv_paged_weights_few_kernel(c
         S.start[g][rr] = make_float2(-7.5f * c * sum[0], -7.5f * c * sum[1]);
       }
       if (lane == 0) {
-        const float k = fabsf(a.scale) * pow2(e2 - 10) * 1048576.f;
         float l, rest;
         lse_log2(lse, l, rest);
         const float coarse = fabsf(l) < 8192.f ? rintf(l * 256.f) * 0.00390625f : l;
-        const float in = (rest + (l - coarse)) / k;  // (rows so small that their logits hardly differ: not worth it)
+        const float in = (rest + (l - coarse)) / k;  // (below 1e30 but for an lse beyond 8192, or a row that adds nothing)
         S.k[rr] = make_float2(k, -coarse), S.lse_in[rr] = fabsf(in) < 1e30f ? -in : 0.f;
       }
       uint4 f[2];
