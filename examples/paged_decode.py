@@ -202,6 +202,10 @@ def within_budget(heads=8, group=4, steps=32, budget=512, window=32, sink=4, pro
         akv.akv_paged_evict(p, pages, src, dst, scores, kept, sink=sink, recent=window)
         lens[dst.long()] = kept.count.clamp(min=0)  # (every layer of a model has the same counts)
 
+    def forget():
+        """A new token's weights are added to what stands at its place: behind what rows hold, that is of tokens that are gone."""
+        scores.masked_fill_((torch.arange(scores.shape[2], device="cuda") >= lens[:, None])[:, None], 0)
+
     # 1. the prompts; their last tokens' queries say which of their tokens stay
     chunk = 1024
     want = torch.tensor(list(prompts) + [0] * (rows - B), **int32)
@@ -213,6 +217,7 @@ def within_budget(heads=8, group=4, steps=32, budget=512, window=32, sink=4, pro
     before, all_lse = attend(q, None)
     cut(ids[:B], ids[:B])
     akv.akv_pages_trim(p, pages, ids[:B])
+    forget()
     after, lse = attend(q, None)
     mass = float((lse - all_lse)[:B].exp().mean())
     cosine = float(torch.cosine_similarity(before[:B].float(), after[:B].float(), dim=-1).mean())
@@ -235,6 +240,7 @@ def within_budget(heads=8, group=4, steps=32, budget=512, window=32, sink=4, pro
             reserve(room)
             cut(now, spare)
             akv.akv_pages_free(p, pages, now)
+            forget()
             now, spare = spare, now
     say(f"{n} answers of {int(lens[now.long()].min())} to {int(lens[now.long()].max())} tokens: {int((refs > 0).sum())} pages")
     return dict(mass=mass, cosine=cosine, lens=lens[now.long()], lacked=int(lacked), table=table, refs=refs, scores=scores)

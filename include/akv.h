@@ -733,7 +733,9 @@ typedef struct akv_scores {
  * which gives their lse, fp32 [rows][T][n_q_heads]):
  *     now[b][h][i] = decay was[b][h][i] + sum over t and the G query heads of h of exp(sm_scale q . k^_i - lse)
  * over the queries that see token i, for the tokens i < lens[b] that request b holds; further numbers are left as they were.
- * `was` may be null (zeros), the same as `now`, or apart from it; it is not read where decay is 0.  Queries whose lse is not a finite number, and
+ * `was` may be null (zeros), the same as `now`, or apart from it; it is not read where decay is 0.  Every token's number counts, also that of a token
+ * that is weighed for the first time: it begins with what stands at its place, which the caller sets (to 0) beforehand, in a fresh array and wherever a
+ * place is used again (behind the count of an eviction, in a row that was freed, behind a length that was lowered, in a row forked from such).  Queries whose lse is not a finite number, and
  * tokens whose key has an infinity or a NaN or whose page is none of the pool's, add nothing.  Sums in fp32, in a fixed order. */
 akv_status akv_paged_weights_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,
                                             size_t* ws_bytes);
@@ -754,7 +756,7 @@ typedef struct akv_kept {
  * count[i] = min(held, keep[i]) (device int32 [n], null = top each; clamped to 0 .. top): the first `sink`, the last `recent` (if
  * both are more than the count, the first of these), and of the others those of the highest scores, ties to the lower place; a NaN
  * is below all numbers.  Their scores go with them to row dst[i].  Places of dst behind the count are left as they were, in the
- * pool and among the scores.
+ * pool and among the scores: those scores are of tokens that are gone, and akv_paged_weights would add to them (see there).
  *   The pages of dst[i] at its first count[i] places must be its own (akv_pages_reserve sees to it).  Where one of them is
  * none of the pool's or, pages->refs given, has more than one holder (in place: if a token is evicted), or a row is outside the table, or a
  * page with tokens of src[i] is none of the pool's, the pair is left alone: count[i] = -1, its tokens -1.
