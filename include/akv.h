@@ -733,7 +733,7 @@ typedef struct akv_scores {
  * which gives their lse, fp32 [rows][T][n_q_heads]):
  *     now[b][h][i] = decay was[b][h][i] + sum over t and the G query heads of h of exp(sm_scale q . k^_i - lse)
  * over the queries that see token i, for the tokens i < lens[b] that request b holds; further numbers are left as they were.
- * `was` may be null (zeros), the same as `now`, or apart from it; it is not read where decay is 0.  Every token's number counts, also that of a token
+ * `was` may be null (zeros), the same as `now`, or apart from it (a number of it on another one of `now` is refused); it is not read where decay is 0.  Every token's number counts, also that of a token
  * that is weighed for the first time: it begins with what stands at its place, which the caller sets (to 0) beforehand, in a fresh array and wherever a
  * place is used again (behind the count of an eviction, in a row that was freed, behind a length that was lowered, in a row forked from such).  Queries whose lse is not a finite number, and
  * tokens whose key has an infinity or a NaN or whose page is none of the pool's, add nothing.  Sums in fp32, in a fixed order. */

@@ -1,4 +1,5 @@
 // Host side of the paged cache's entry points: validation, and the views the kernels get.
+#include <algorithm>
 #include <cmath>
 #include <utility>
 
@@ -169,7 +170,12 @@ akv_status check_scores(const akv_scores* s, const char* what, const akv_pages* 
   if ((uintptr_t)s->ptr % 4) return fail(AKV_ERR_INVALID, what, " must be 4-byte aligned");
   if (s->cap < g->max_pages * p->page_tokens) return fail(AKV_ERR_TOO_SMALL, what, ": room for max_pages * page_tokens numbers a head");
   if (s->stride_b < 0 || s->stride_h < 0) return fail(AKV_ERR_INVALID, what, ": negative stride");
-  if (!written) return AKV_OK;
+  if (!written) {
+    const int64_t most = INT64_MAX / 16;
+    if ((g->rows > 1 && s->stride_b > most / (g->rows - 1)) || (p->n_kv_heads > 1 && s->stride_h > most / (p->n_kv_heads - 1)))
+      return fail(AKV_ERR_INVALID, what, ": strides out of range");
+    return AKV_OK;
+  }
   // numbers on top of one another: the smaller stride steps over a head's, the larger over all of the smaller's axis
   int64_t near = s->stride_h, far = s->stride_b, n = p->n_kv_heads, m = g->rows;
   if (far < near) std::swap(near, far), std::swap(n, m);
@@ -182,6 +188,34 @@ akv_status check_scores(const akv_scores* s, const char* what, const akv_pages* 
     extent += stride * (count - 1);
   }
   return AKV_OK;
+}
+
+// Numbers of `was` are read while those of `now` are written: each head's n of them have to be that head's of `now`, or on none of
+// its.  Both have been checked, so that heads of `now` do not overlap, those of the smaller stride within a step of the larger.
+bool apart(const akv_scores& was, const akv_scores& now, int64_t rows, int64_t heads, int64_t n) {
+  const int64_t d = (int64_t)((uintptr_t)was.ptr - (uintptr_t)now.ptr) / 4;
+  if (d == 0 && (rows == 1 || was.stride_b == now.stride_b) && (heads == 1 || was.stride_h == now.stride_h)) return true;
+  auto extent = [&](const akv_scores& s) { return (rows - 1) * s.stride_b + (heads - 1) * s.stride_h + n; };
+  if (d >= extent(now) || -d >= extent(was)) return true;
+  struct Axis {
+    int64_t stride, count;
+    // the steps in which places x .. x + n - 1 may lie (n is no longer than one)
+    int64_t step(int64_t x) const { return count == 1 ? 0 : x < 0 ? -1 : x / stride; }
+  } b_axis{now.stride_b, rows}, h_axis{now.stride_h, heads};
+  const bool b_far = heads == 1 || (rows > 1 && b_axis.stride >= h_axis.stride);
+  const Axis &far = b_far ? b_axis : h_axis, &near = b_far ? h_axis : b_axis;
+  for (int64_t b = 0; b < rows; ++b)
+    for (int64_t h = 0; h < heads; ++h) {
+      const int64_t x = d + b * was.stride_b + h * was.stride_h;
+      for (int64_t f = std::max<int64_t>(0, far.step(x)); f <= std::min(far.count - 1, far.step(x + n - 1)); ++f) {
+        const int64_t y = far.count == 1 ? x : x - f * far.stride;
+        for (int64_t k = std::max<int64_t>(0, near.step(y)); k <= std::min(near.count - 1, near.step(y + n - 1)); ++k) {
+          const int64_t off = near.count == 1 ? y : y - k * near.stride;
+          if (off > -n && off < n && (off != 0 || (b_far ? f : k) != b || (b_far ? k : f) != h)) return false;
+        }
+      }
+    }
+  return true;
 }
 
 akv_status launched(int err, const char* what) {
@@ -343,6 +377,8 @@ akv_status akv_paged_weights(const akv_paged_params* p, const akv_pages* pages, 
   if (!std::isfinite(decay)) return fail(AKV_ERR_INVALID, "decay must be finite");
   if (was) AKV_TRY(check_scores(was, "was", pages, p, false));
   AKV_TRY(check_scores(now, "now", pages, p, true));
+  if (was && decay != 0.f && !apart(*was, *now, pages->rows, p->n_kv_heads, (int64_t)pages->max_pages * p->page_tokens))
+    return fail(AKV_ERR_INVALID, "was lies on other numbers of now");
   AKV_TRY(check_ws(ws, ws_bytes, paged_weights_ws_bytes(c.v, T)));
   return launched(launch_paged_weights(c.v, *q, lse, T, sm_scale, decay, decay != 0.f ? was : nullptr, *now, ws, (void*)stream), "weights");
 }
