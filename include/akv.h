@@ -709,10 +709,13 @@ typedef struct akv_share {
 akv_status akv_pages_share(const akv_paged_params* p, const akv_pages* pages, const akv_share* share, void* ws,
                            size_t ws_bytes, akv_stream_t stream);
 
-/* akv_paged_attn of the same arguments, but for the order of its sums: the shared pages of a group are read once for all its rows'
- * queries (as one matrix product), every row's further tokens as akv_paged_attn reads them, and both parts are joined in one
- * softmax.  Groups of few query rows, and batches whose groups are short, are attended row by row (share->flags).  Numbers in `share` that are out of range are left out (rows outside the table) or clamped (pages).
- *   Of pages that are read once a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
+/* The attention of akv_paged_attn with the same arguments: the shared pages of a group are read once for all its rows' queries (as one matrix
+ * product), every row's further tokens as akv_paged_attn reads them, and both parts are joined in one softmax.  Groups of few
+ * query rows, and batches whose groups are short, are attended row by row (share->flags).  Even then the call makes two launches more than
+ * akv_paged_attn (5 to 8 us, and the plan 2 to 3): batches without forked rows call that one.  Numbers in `share` that are out of range are left out (rows
+ * outside the table) or clamped (pages).
+ *   Results differ from akv_paged_attn's by the order of their sums and, where pages are read once, by two roundings, so that a row's last bits can
+ * depend on the rows that it is in a batch with (AKV_SHARE_ALWAYS: on those of its group alone): a weight is rounded to fp16 (by at most 2^-11 of it, or 2^-29 of the row's largest) and a value
  * m + c a to fp16 as well (2^-11 of it; where 16 tokens have a scale above 2048 or a minimum beyond 16384, 2^-20 at least).  A query that sees
  * such a token with an infinity or a NaN has NaN in all its outputs. */
 akv_status akv_paged_attn_shared_workspace_size(const akv_paged_params* p, const akv_pages* pages, int32_t T,

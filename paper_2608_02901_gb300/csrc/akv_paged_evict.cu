@@ -8,9 +8,10 @@
 // its neighbour: a warp loads the sixteen-byte units that hold them and puts two tokens' halves together (PRMT).
 // In place: a kept token goes to a place at or before its own, so the places that a round of sub-blocks writes hold no token
 // that a later round reads; a round is read by the whole cluster, then (cluster barrier) written.
-// What bounds it: of long rows the kept tokens' bytes, read and written (4 rows of 128 k tokens, 8 heads, half of them kept, in place: 175 us; 640 MB
-// asked for, 858 MB moved, since a 32-byte sector holds values of four tokens: 4.9 TB/s), a round's reads waiting for its barrier and its writes; of short ones
-// the chain of some twelve dependent reads and barriers (32 rows of 1.1 k tokens 25.6 us, 32 k tokens cut to 4 k 24.6).
+// What bounds it: of long rows the kept tokens' bytes, read and written (4 rows of 128 k tokens, 8 heads, half of them kept, into other rows: 175 us; 640 MB
+// asked for, 858 MB moved, since a 32-byte sector holds values of four tokens: 4.9 TB/s), of which a warp has one round under way at a time; in place
+// each round's barrier of the cluster as well, between its reads and its writes (241 us); of short rows the chain of some twelve dependent reads and
+// barriers (32 rows of 1.1 k tokens 25.9 us, in place 24.6; 32 k tokens cut to 4 k 24.8, in place 24.5).
 #include <cooperative_groups.h>
 
 #include "akv_paged.cuh"

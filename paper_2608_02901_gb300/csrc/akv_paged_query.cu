@@ -25,10 +25,10 @@ struct QueryArgs {
 
 // Whether reading a group's pages once pays.  Its time row by row goes by each member's units of 8 or 16 query rows (the second 1.5 times the first),
 // shared by blocks of 128 rows of the whole group, at 3.5 times a unit of 8.  Microseconds row by row and shared of groups over 32 k tokens each, 8 KV
-// heads: 12 pairs of 8 query rows 171 and 266, 8 of three 171 and 190, 6 of four 163 and 153, 3 of eight 160 and 96; of 16 query rows 12 pairs 255
-// and 274 (rotated 306 and 282), 8 of three 256 and 200.
+// heads: 12 pairs of 8 query rows 181 and 263, 8 of three 179 and 188, 6 of four 171 and 151, 3 of eight 169 and 97; of 16 query rows 12 pairs 262
+// and 269 (rotated 308 and 280), 8 of three 261 and 198.
 //   The launch of the shared part takes some 15 us until it has ended by itself where its caches are cold, as what it reads then is: all groups together have
-// to save as much (4 query heads; a group of 32 rows over 4 k tokens 45 shared, 51 not; of 8 rows 39 and 32; 4 rows over 16 k tokens 45 and 39).
+// to save as much (4 query heads; a group of 32 rows over 4 k tokens 44 shared, 50 not; of 8 rows 38 and 32; 4 rows over 16 k tokens 44 and 38).
 constexpr int kUnit8 = 2, kUnit16 = 3, kBlock = 7;  // of a tile of 128 tokens and a KV head, in half units of 8
 constexpr int kWorth = 43;                          // what an SM saves at least, in those
 __device__ __forceinline__ int64_t saved(const PagedView& v, int T, int tokens, int size) {

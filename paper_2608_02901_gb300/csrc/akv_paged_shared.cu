@@ -13,8 +13,8 @@
 //   8 warps are the softmax: two threads a query row, half of a tile's columns each, which tell each other their largest logit:
 //     p = 2^(S scale - reference), its sum, P as fp16 over S's columns.  (A thread a row, the two warpgroups' tiles in turn and the reference
 //     handed from one to the other, took 243 us for 8 prompts of 32 k tokens with 8 answers each where this
-//     takes 219, 249 for 235 of 32 answers over 128 k.)
-// What bounds it (32 answers, 8 x 8 heads, 128 k shared tokens, rotated: 200 us of 230, in all 598 TFLOP/s of the products that the formula
+//     took 219, 249 for 235 of 32 answers over 128 k.)
+// What bounds it (32 answers, 8 x 8 heads, 128 k shared tokens, rotated: 200 us of 232, in all 593 TFLOP/s of the products that the formula
 // has, 1420 of those that are made in the 200 us): the tensor cores work 65 % of the cycles, a warp instruction is issued in 70 %; of a
 // tile's 3500 cycles the products need 2260, and the rest is the chain from S through P to the next use of its columns.  S of three tiles
 // would not fit into tensor memory.  Of few rows the products cost the same.
@@ -222,8 +222,8 @@ __global__ void __launch_bounds__(kThreads, 1) akv_paged_shared_kernel(const __g
     S.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // (also for the own tokens' launch, which writes nothing that is read here: what the launch before that one wrote is
-  // only sure to be seen behind a wait)
+  // (also for the own tokens' launch, which writes nothing that is read here: what the launch before that one wrote is only sure to be seen
+  // behind a wait.  Its CTAs leave no room for this one's beside them in any case; waiting takes 0 to 2 us a call.)
   wait_for_stream();
   Segment seg;
   const Walk w = plan(a, S, seg);
