@@ -394,7 +394,8 @@ def _lse(lse, p: PagedParams, pages: Pages, T):
 
 def akv_paged_attn_shared(p: PagedParams, pages: Pages, q, out, share: PageShare, lse=None, sm_scale: float = 1.0,
                           layer: int = 0, ws=None, stream=None):
-    """akv_paged_attn over rows that share pages (share of akv_pages_share): those are read once for all.
+    """akv_paged_attn over rows that share pages (share of akv_pages_share): those are read once for all, where that pays.
+    Without forked rows akv_paged_attn is the faster call.
     ws as there, of akv_paged_attn_shared_workspace_size bytes."""
     if _device() != pages.index:
         return _there(pages, akv_paged_attn_shared, p, pages, q, out, share, lse, sm_scale, layer, ws, stream)
@@ -430,7 +431,8 @@ def akv_paged_weights_workspace_size(p: PagedParams, pages: Pages, T: int = 1) -
 def akv_paged_weights(p: PagedParams, pages: Pages, q, lse, now, was=None, decay: float = 1.0, sm_scale: float = 1.0,
                       layer: int = 0, ws=None, stream=None):
     """now = decay was + the attention weights of the last T query tokens.  q: [rows][T][n_q_heads][128], lse of
-    akv_paged_attn; now, was: fp32 [rows][n_kv_heads][cap], was None (zeros) or now itself.  ws as there, of
+    akv_paged_attn; now, was: fp32 [rows][n_kv_heads][cap], was None (zeros), now itself or apart from it.  A new token begins
+    with what stands at its place: set that to 0, also where a place is used again.  ws as there, of
     akv_paged_weights_workspace_size bytes."""
     if _device() != pages.index:
         return _there(pages, akv_paged_weights, p, pages, q, lse, now, was, decay, sm_scale, layer, ws, stream)
@@ -446,7 +448,8 @@ def akv_paged_weights(p: PagedParams, pages: Pages, q, lse, now, was=None, decay
 def akv_paged_evict(p: PagedParams, pages: Pages, src, dst, scores, kept: KeptTokens, keep=None, sink: int = 0,
                     recent: int = 0, layer: int = 0, stream=None):
     """Row dst[i] gets the tokens that row src[i] keeps by their scores (CUDA int32 [n]; the same row: in place).  scores: fp32
-    [rows][n_kv_heads][cap]; keep: CUDA int32 [n] (None: kept.top each); fills kept.  lens is not changed."""
+    [rows][n_kv_heads][cap]; keep: CUDA int32 [n] (None: kept.top each); fills kept.  lens is not changed, nor are
+    the scores behind what is kept."""
     if _device() != pages.index:
         return _there(pages, akv_paged_evict, p, pages, src, dst, scores, kept, keep, sink, recent, layer, stream)
     a, b, n = _pair(src, dst, pages)
